@@ -6,7 +6,7 @@ Three operators ("op"), each for n workers that are batched buffers on one GPU, 
           gradients per worker; otherwise the forward pass alone.
   xent    the output layer and its softmax cross entropy, mean over a worker's labelled tokens; "train": the loss and
           the gradients of the hidden states and, per worker, of the weight; otherwise the loss alone.  Labels of -100
-          mark tokens that take no part.
+          mark tokens that take no part (their row of "lse" is 0).
   ortho   an update orthogonalised by five Newton-Schulz steps; "workers" > 0: the whole momentum update of weight
           matrices from that many workers' gradients; 0: the orthogonalisation by itself.
 
@@ -269,6 +269,7 @@ def _plain_xent(case, s):
     shifted = torch.exp(z - top)
     total = shifted.sum(1, keepdim=True)
     lse = (top + torch.log(total)).squeeze(1)
+    lse = torch.where(used, lse, 0.0)
     per_token = torch.where(used, lse - z.gather(1, safe[:, None]).squeeze(1), 0.0).reshape(n, t)
     count = used.reshape(n, t).sum(1).clamp(min=1).float()
     loss = per_token.sum(1) / count
@@ -330,7 +331,7 @@ def _exact_xent(case, s):
     n, t, dim = s["h"].shape
     vocab, w = case["vocab"], s["w"].double()
     loss = torch.zeros(n, dtype=torch.float64, device="cuda")
-    lse = torch.empty((n, t), dtype=torch.float64, device="cuda")
+    lse = torch.zeros((n, t), dtype=torch.float64, device="cuda")
     dh = torch.empty((n, t, dim), dtype=torch.float64, device="cuda") if case["train"] else None
     dw = torch.empty((n, vocab, dim), dtype=torch.float64, device="cuda") if case["train"] else None
     for i in range(n):
@@ -338,7 +339,7 @@ def _exact_xent(case, s):
         used = (labels != IGNORED).nonzero().squeeze(1)
         count = max(1, used.numel())
         logp = torch.log_softmax(h @ w.t(), dim=1)
-        lse[i] = h[:, 0] * w[0, 0] - logp[:, 0] + (h[:, 1:] @ w[0, 1:])
+        lse[i, used] = (h @ w[0] - logp[:, 0])[used]
         loss[i] = -logp[used, labels[used]].sum() / count
         if case["train"]:
             p = torch.zeros((t, vocab), dtype=torch.float64, device="cuda")
