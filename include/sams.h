@@ -341,6 +341,106 @@ int amsgrad_ef_update_pa(sams_ctx *ctx, const float *g_next, float *m, float *e_
                          float *vhat_workers, float *x, const int32_t *idx, const float *delta, int64_t k_sel,
                          float beta1, float beta2, float lr, float ef_ratio);
 
+/*
+ * Training operators.  A step starts from the n workers' gradients; these operators make them, for the output end of a
+ * language model, and update weight matrices by the other rule that such models are trained with.  Each has a context of its
+ * own that is created for the largest size, holds the scratch and enqueues on the stream given; the conventions above hold
+ * (error codes, no synchronisation, one host thread at a time, nothing retained), except that
+ *   - activations and weights are of the context's `type`, and pointers need the alignment of their type only (16-byte
+ *     aligned tensors whose rows are multiples of 16 bytes are read faster);
+ *   - tensors [n][t][dim] are given with the distance from worker to worker and from row to row, in elements; the last axis is
+ *     contiguous.  So parts of the flat vectors x [d] and g [n][d] can be passed as they lie (worker distance d).  Inputs may
+ *     overlap themselves (distance 0), outputs not;
+ *   - t may be anything from 0 to the t_max of the context (0: no tokens; sums over tokens are 0).
+ * Sums, means, norms and softmax statistics are held in 32 bits or more and made in a fixed order: equal inputs give equal
+ * results, bit for bit.
+ */
+#define SAMS_F32 0
+#define SAMS_BF16 1
+#define SAMS_F16 2
+
+#define SAMS_MAX_TOKENS 268435456       /* n * t_max */
+#define SAMS_MAX_DIM 131072
+#define SAMS_MAX_VOCAB 16777216
+#define SAMS_MAX_BATCH 65535
+#define SAMS_MAX_ORTHO_STEPS 100
+
+typedef struct sams_norm sams_norm;
+typedef struct sams_xent sams_xent;
+typedef struct sams_ortho sams_ortho;
+
+/*
+ * Layer norm over the last axis:
+ *     y = (x - mean) * rstd * weight + bias,   rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ *   x, y [n][t][dim] of `type`     weight [dim], bias [dim] or NULL: fp32     mean, rstd [n][t] fp32 out, contiguous
+ * and its backward pass, with z = (x - mean) * rstd and a = dy * weight:
+ *     dx = rstd * (a - mean(a) - z * mean(a * z)),   dweight[i] = sum over worker i's rows of dy * z,   dbias[i] = sum of dy
+ *   dy, x, dx [n][t][dim]     mean, rstd: the forward pass's     dweight [n][dim], dbias [n][dim] or NULL: fp32, with the distance
+ *   from worker to worker; accumulate != 0 adds to what they hold.  y may be x, and dx may be dy or x (same distances).
+ * Ranges: 1 <= n <= 1024, n * t_max <= SAMS_MAX_TOKENS, 1 <= dim <= SAMS_MAX_DIM, eps >= 0 (with 0, a row of equal numbers gives NaN).
+ */
+int sams_norm_create(sams_norm **out, int32_t n, int64_t t_max, int64_t dim, int32_t type, void *hip_stream);
+int sams_norm_destroy(sams_norm *ctx);
+int64_t sams_norm_scratch_bytes(const sams_norm *ctx);
+int layer_norm_forward(sams_norm *ctx, int64_t t, const void *x, int64_t x_worker, int64_t x_row, const float *weight,
+                       const float *bias, float eps, void *y, int64_t y_worker, int64_t y_row, float *mean, float *rstd);
+int layer_norm_backward(sams_norm *ctx, int64_t t, const void *dy, int64_t dy_worker, int64_t dy_row, const void *x,
+                        int64_t x_worker, int64_t x_row, const float *weight, const float *mean, const float *rstd, void *dx,
+                        int64_t dx_worker, int64_t dx_row, float *dweight, int64_t dweight_worker, float *dbias,
+                        int64_t dbias_worker, int32_t accumulate);
+
+/*
+ * Output layer and softmax cross entropy, without the logits in memory:
+ *     z = h w',  lse = log sum_v exp(z_v),   loss[i] = mean over worker i's tokens that take part of (lse - z_label)
+ *   h [n][t][dim], w [vocab][dim] of `type` (w with the distance from row to row)     labels [n][t] int64, contiguous
+ *   loss [n] fp32 out     lse [n][t] fp32 out, contiguous
+ * A token whose label lies outside [0, vocab) (-100, say) takes no part: its lse is 0, its row of h may hold anything (NaN
+ * included) and changes nothing.  A worker without a token that takes part has loss 0 and gradients 0.
+ * Backward, of sum_i grad_loss[i] * loss[i] (grad_loss NULL: all 1), from the lse of the forward pass:
+ *     dh = dz w,   dw[i] = sum over worker i's tokens of dz' h,   dz = (exp(z - lse) - onehot(label)) * grad_loss / count
+ *   dh [n][t][dim] of `type`     dw [n][vocab][dim] of dw_type (`type` or SAMS_F32), with the distances from worker to worker and from
+ *   row to row; accumulate != 0 adds to what dw holds.  The logits are computed again, in pieces of the vocabulary.
+ * 16-bit tensors are multiplied as they are, and dz is held as numbers of their type between the products (so dw and dh carry
+ * its rounding whatever dw_type); 32-bit ones to 22 bits of mantissa, of numbers below 2^-17 of the tensor's largest fewer.
+ * train == 0 at creation: the forward pass only, and less scratch (backward then returns SAMS_EINVAL).
+ * Scratch: copies of h and w; 8 bytes per token and 128 words of the vocabulary; for training the dz of one piece of the vocabulary
+ * (about 256 MiB, or the whole of a smaller one; at least 1024 words per token) and up to 64 MiB, or 4*dim bytes per token, of partial sums of dh.
+ */
+int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int64_t vocab, int32_t type, int32_t train,
+                     void *hip_stream);
+int sams_xent_destroy(sams_xent *ctx);
+int64_t sams_xent_scratch_bytes(const sams_xent *ctx);
+int linear_xent_forward(sams_xent *ctx, int64_t t, const void *h, int64_t h_worker, int64_t h_row, const void *w, int64_t w_row,
+                        const int64_t *labels, float *loss, float *lse);
+int linear_xent_backward(sams_xent *ctx, int64_t t, const void *h, int64_t h_worker, int64_t h_row, const void *w, int64_t w_row,
+                         const int64_t *labels, const float *lse, const float *grad_loss, void *dh, int64_t dh_worker,
+                         int64_t dh_row, void *dw, int64_t dw_worker, int64_t dw_row, int32_t dw_type, int32_t accumulate);
+
+/*
+ * An update orthogonalised by Newton-Schulz steps (batch matrices of one shape):
+ *     X_0 = G / (|G|_F + eps),   X <- a X + b (X X') X + c (X X')^2 X   `steps` times,   (a, b, c) = coef_host[0..2]
+ *   g, out [batch][rows][cols] of `type`, with the distances from matrix to matrix and from row to row; out may be g
+ *   coef_host  HOST pointer, three finite numbers, read during the call      1 <= steps <= SAMS_MAX_ORTHO_STEPS
+ * Between the products, matrices are held to 11 bits of mantissa where `type` has 16 bits and to 22 where it has 32.
+ *
+ * muon_update is the momentum update of weight matrices that uses it (type SAMS_F32), from the n workers' gradients:
+ *     mean = (g[0] + g[1] + ...) / n  (workers in ascending order),   m_out = beta * m + (1 - beta) * mean
+ *     G = m_out, or, with nesterov != 0, beta * m_out + (1 - beta) * mean
+ *     x_out = (1 - lr * weight_decay) * x - lr * scale * orthogonalised(G)
+ *   g [n][batch][rows][cols] with distances from worker to worker and from matrix to matrix; m, x, m_out, x_out
+ *   [batch][rows][cols] with the distance from matrix to matrix; a matrix itself is contiguous.  m_out may be m, x_out may be x.
+ * Ranges: 1 <= batch <= SAMS_MAX_BATCH at creation (a call may pass fewer, or 0), 1 <= rows, cols <= SAMS_MAX_DIM, eps >= 0.
+ */
+int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t cols, int32_t type, void *hip_stream);
+int sams_ortho_destroy(sams_ortho *ctx);
+int64_t sams_ortho_scratch_bytes(const sams_ortho *ctx);
+int orthogonalize(sams_ortho *ctx, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, int32_t steps,
+                  const float *coef_host, float eps, void *out, int64_t out_mat, int64_t out_row);
+int muon_update(sams_ortho *ctx, int32_t n, int64_t batch, const float *g, int64_t g_worker, int64_t g_mat, const float *m,
+                int64_t m_mat, const float *x, int64_t x_mat, float *m_out, int64_t m_out_mat, float *x_out,
+                int64_t x_out_mat, float beta, int32_t nesterov, float lr, float scale, float weight_decay, int32_t steps,
+                const float *coef_host, float eps);
+
 #ifdef __cplusplus
 }
 #endif

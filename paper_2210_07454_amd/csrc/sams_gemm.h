@@ -1,0 +1,265 @@
+// Products of 16-bit matrices on the matrix cores: C[m][n] = sum_k A(m, k) B(n, k) for one tile of C per workgroup, with
+// 32-bit accumulators that stay in registers for whatever the kernel does with its tile.
+#pragma once
+#include "sams_ctx.h"
+
+namespace sams {
+namespace gemm {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// What the words of the operands are.  SPLIT: a 32-bit number as the sum of two 16-bit floats, the first rounded to nearest,
+// the second what that left: 22 bits of mantissa.  A row of such numbers lies in blocks of 32: 32 first parts, then 32 second
+// parts; a product of two numbers takes three of words (the fourth, of both second parts, is below the 22 bits).
+enum Kind { BF16 = 0, F16 = 1, SPLIT = 2 };
+
+// One operand.  K_ROWS false: row m (or n) has its k's next to each other; true: a row holds one k of all m (or n).
+struct Operand {
+    const uint16_t *p;
+    int64_t ld;         // words from row to row, a multiple of 8
+    int64_t size;       // extent along m (or n), in numbers
+};
+
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_>
+struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, STAGES = STAGES_;
+    static constexpr int THREADS = 64 * WAVES_M * WAVES_N;
+    static constexpr int MI = BM / WAVES_M / 32, NI = BN / WAVES_N / 32;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128;
+    static constexpr int LDS_BYTES = STAGES * (A_BYTES + B_BYTES);
+};
+
+template <int KIND>
+__device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (KIND == BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+// Where a 16-byte piece of a tile lies in LDS.  A tile whose rows are 128 bytes: piece c of row r at c ^ swizzle(r), so that the
+// fragments of 8 or 16 rows next to each other fall on different banks.  A tile whose rows are k's: piece c of row k at
+// c ^ swizzle_k(k), so that the four k's of a transposing read do.
+__device__ __forceinline__ int swizzle(int row) { return ((row ^ (row >> 3)) & 1) | (row & 6); }
+__device__ __forceinline__ int swizzle_k(int k) { return ((k & 3) << 2) | (k & 2); }
+
+template <int KIND> __host__ __device__ constexpr int tile_k() { return KIND == SPLIT ? 32 : 64; }      // numbers of k in a stage
+
+// Loads of one operand's tile straight into LDS, 64 words of k (32 numbers of k where they are split) a stage.
+template <int ROWS, int THREADS, int KIND, bool K_ROWS>
+struct Loader {
+    static constexpr int N = ROWS * 8 / THREADS;                    // 16-byte pieces a thread brings
+    static constexpr int PIECES = K_ROWS ? (KIND == SPLIT ? ROWS / 4 : ROWS / 8) : 8;       // of a row of the tile
+    const uint16_t *p[N];
+    int kpos[N];                                                    // where a piece starts, in k
+    int64_t step;
+
+    __device__ __forceinline__ void init(const Operand &op, int64_t first, int64_t k_first, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int slot = i * THREADS + tid;
+            const int row = slot / PIECES;
+            if constexpr (K_ROWS) {
+                const int c = (slot % PIECES) ^ (swizzle_k(row) & (PIECES - 1));
+                const int64_t words = KIND == SPLIT ? (op.size + 31) / 32 * 64 : (op.size + 7) / 8 * 8;
+                int64_t w = (KIND == SPLIT ? 2 * first : first) + c * 8;
+                if (w >= words) w = 0;                              // columns that no output asks for
+                p[i] = op.p + (k_first + row) * op.ld + w;
+                kpos[i] = row;
+            } else {
+                const int c = (slot % PIECES) ^ swizzle(row);
+                int64_t r = first + row;
+                if (r >= op.size) r = op.size - 1;                  // rows that no output asks for
+                p[i] = op.p + r * op.ld + (KIND == SPLIT ? 2 * k_first : k_first) + c * 8;
+                kpos[i] = KIND == SPLIT ? (c & 3) * 8 : c * 8;
+            }
+        }
+        step = K_ROWS ? tile_k<KIND>() * op.ld : 64;
+    }
+
+    // left: k's from the start of this stage on; a piece past them is read from the zeros
+    __device__ __forceinline__ void load(char *lds, int wave, const uint16_t *zeros, int64_t left)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint16_t *src = kpos[i] < left ? p[i] : zeros;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)src,
+                                             (__attribute__((address_space(3))) uint32_t *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+            p[i] += step;
+        }
+    }
+};
+
+// A lane's 8 k's of its row (lane % 32) for one matrix instruction: k = kbase + 8 * (lane / 32) .. + 7, of part `half` where split.
+// Rows that are k's are read through the transposing load: of every 16 lanes, four give the address of one k's 16 columns, and each
+// gets one column's four k's.
+template <int ROWS, int KIND, bool K_ROWS>
+__device__ __forceinline__ u32x4 fragment(const char *tile, int row0, int kbase, int half, int lane)
+{
+    if constexpr (K_ROWS) {
+        constexpr int PIECES = KIND == SPLIT ? ROWS / 4 : ROWS / 8;
+        const int g = lane >> 4, q = lane & 15;
+        const int k = kbase + 8 * (g >> 1) + (q >> 2);
+        const int w = (KIND == SPLIT ? row0 * 2 + half * 32 : row0) + (g & 1) * 16 + (q & 3) * 4;
+        const char *at = tile + k * (PIECES * 16) + (((w >> 3) ^ (swizzle_k(k) & (PIECES - 1))) << 4) + (w & 7) * 2;
+        typedef __attribute__((address_space(3))) short4v *lds_ptr;
+        const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
+        const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * (PIECES * 16)));
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+        return u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+        const int row = row0 + (lane & 31), c = (kbase >> 3) + half * 4 + (lane >> 5);
+        return *(const u32x4 *)(tile + row * 128 + ((c ^ swizzle(row)) << 4));
+    }
+}
+
+// All but the N youngest loads of this thread have landed, its reads of LDS are done, and so are those of the workgroup's others.
+template <int N>
+__device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// acc += the tile's product over k numbers from k_first on.  `lds`: S::LDS_BYTES, 16-byte aligned; every thread of the workgroup
+// calls it, and LDS is free again when it returns.  Pieces past k come from `zeros` (16 bytes of them).
+template <class S, int KIND, bool A_K_ROWS, bool B_K_ROWS>
+__device__ __forceinline__ void tile_product(f32x16 (&acc)[S::MI][S::NI], const Operand &A, int64_t m0, const Operand &B, int64_t n0, int64_t k_first,
+                                             int64_t k, const uint16_t *zeros, char *lds)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
+    constexpr int BK = tile_k<KIND>(), STAGE = S::A_BYTES + S::B_BYTES;
+    typedef Loader<S::BM, S::THREADS, KIND, A_K_ROWS> LA;
+    typedef Loader<S::BN, S::THREADS, KIND, B_K_ROWS> LB;
+    LA la;
+    LB lb;
+    la.init(A, m0, k_first, tid);
+    lb.init(B, n0, k_first, tid);
+    const int64_t steps = (k + BK - 1) / BK;
+    int64_t left = k;
+#pragma unroll
+    for (int s = 0; s < S::STAGES - 1; ++s) {
+        la.load(lds + s * STAGE, wave, zeros, left);
+        lb.load(lds + s * STAGE + S::A_BYTES, wave, zeros, left);
+        left -= BK;
+    }
+    int cur = 0, nxt = S::STAGES - 1;
+    for (int64_t s = 0; s < steps; ++s) {
+        wait_and_meet<(S::STAGES - 2) * (LA::N + LB::N)>();
+        la.load(lds + nxt * STAGE, wave, zeros, left);
+        lb.load(lds + nxt * STAGE + S::A_BYTES, wave, zeros, left);
+        left -= BK;
+        const char *ta = lds + cur * STAGE, *tb = ta + S::A_BYTES;
+        if constexpr (KIND != SPLIT) {
+#pragma unroll
+            for (int ks = 0; ks < 64; ks += 16) {
+                u32x4 a[S::MI], b[S::NI];
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i) a[i] = fragment<S::BM, KIND, A_K_ROWS>(ta, wm + i * 32, ks, 0, lane);
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) b[j] = fragment<S::BN, KIND, B_K_ROWS>(tb, wn + j * 32, ks, 0, lane);
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(a[i], b[j], acc[i][j]);
+            }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 32; ks += 16) {
+                u32x4 a[2][S::MI], b[2][S::NI];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < S::MI; ++i) a[h][i] = fragment<S::BM, KIND, A_K_ROWS>(ta, wm + i * 32, ks, h, lane);
+#pragma unroll
+                    for (int j = 0; j < S::NI; ++j) b[h][j] = fragment<S::BN, KIND, B_K_ROWS>(tb, wn + j * 32, ks, h, lane);
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q)
+#pragma unroll
+                    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(a[q == 2][i], b[q == 1][j], acc[i][j]);
+            }
+        }
+        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
+        nxt = nxt + 1 == S::STAGES ? 0 : nxt + 1;
+    }
+    wait_and_meet<0>();
+}
+
+template <class S>
+__device__ __forceinline__ void clear(f32x16 (&acc)[S::MI][S::NI])
+{
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+}
+
+// f(m, n, value) for every number of the workgroup's tile that this thread holds, m and n counted from the tile's corner; four in
+// a row are m, m + 1, m + 2, m + 3 of one n, and 32 lanes hold 32 n's next to each other.
+template <class S, typename F>
+__device__ __forceinline__ void for_each(const f32x16 (&acc)[S::MI][S::NI], F f)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) f(wm + i * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3), wn + j * 32 + (lane & 31), acc[i][j][q]);
+}
+
+// one number as the words of an operand whose row starts at `row`; its place among the row's numbers is i
+template <int KIND>
+__device__ __forceinline__ void put(uint16_t *row, int64_t i, float v)
+{
+    if constexpr (KIND == SPLIT) {
+        const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
+        uint16_t *p = row + (i >> 5) * 64 + (i & 31);
+        p[0] = __builtin_bit_cast(uint16_t, hi);
+        p[32] = __builtin_bit_cast(uint16_t, lo);
+    } else if constexpr (KIND == F16) {
+        row[i] = __builtin_bit_cast(uint16_t, (_Float16)v);
+    } else {
+        row[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ float get(const uint16_t *row, int64_t i)
+{
+    if constexpr (KIND == SPLIT) {
+        const uint16_t *p = row + (i >> 5) * 64 + (i & 31);
+        return (float)__builtin_bit_cast(_Float16, p[0]) + (float)__builtin_bit_cast(_Float16, p[32]);
+    } else if constexpr (KIND == F16) {
+        return (float)__builtin_bit_cast(_Float16, row[i]);
+    } else {
+        return (float)__builtin_bit_cast(__bf16, row[i]);
+    }
+}
+
+// words of a row of `numbers` numbers: whole 128-byte lines
+template <int KIND> __host__ __device__ constexpr int64_t row_words(int64_t numbers)
+{
+    return KIND == SPLIT ? (numbers + 31) / 32 * 64 : (numbers + 63) / 64 * 64;
+}
+// numbers of such a row, with those that only fill it up
+template <int KIND> __host__ __device__ constexpr int64_t row_numbers(int64_t numbers)
+{
+    return KIND == SPLIT ? (numbers + 31) / 32 * 32 : (numbers + 63) / 64 * 64;
+}
+
+}  // namespace gemm
+}  // namespace sams

@@ -1,0 +1,362 @@
+// Updates orthogonalised by Newton-Schulz steps, alone or within a momentum update of weight matrices.
+//
+//   X_0 = G / (|G|_F + eps);   X_{j+1} = p(X_j) = a X + b (X X') X + c (X X')^2 X = (a I + b A + c A^2) X,  A = X X'
+//
+// p acts on the singular values s of X: s -> a s + b s^3 + c s^5, with X's directions left alone.  A is formed on the shorter side
+// (for a tall matrix A = X' X, and X multiplies from the left), so that a step is three products: X X' (or X' X), A A, and P X
+// (or X P).  A and P are symmetric: half of their tiles are computed, each written twice.
+//
+// Numbers.  Every matrix of the iteration has a bound that the coefficients give on the host: |x_ij| <= the largest singular value,
+// which p keeps below max |p| over the range before.  So they are held as fixed-point-like words: 16-bit floats (11 bits) after
+// scaling by a power of two that puts the bound near the top of their range, one word where the caller's tensors have 16 bits, two
+// (22 bits) where they have 32.  bfloat16 would have 8 bits for the same cost, and nothing here needs its range.  G itself is only
+// scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the first step's products.
+#include <math.h>
+#include <new>
+
+#include "sams_gemm.h"
+#include "sams_train.h"
+
+struct sams_ortho {
+    int64_t batch, rows, cols;
+    int32_t type;
+    hipStream_t stream;
+    sams::Scratch scratch;
+    int64_t x[2], gram, poly, scale, part, update, zeros;       // offsets in the scratch
+};
+
+namespace sams {
+
+using namespace gemm;
+
+constexpr int kNormSlices = 64;         // of a matrix, for the sum of its squares
+
+struct OrthoScale {
+    float sigma, sigma2;                // what the words of G still have to be multiplied by, and its square
+    int32_t exponent;                   // words of G = G * 2^exponent
+};
+
+// sums of squares in 64 bits: no norm is too large or too small for its square
+template <int T>
+__global__ void __launch_bounds__(256) k_ortho_squares(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int64_t rows, int64_t cols, double *part)
+{
+    __shared__ double sums[4];
+    const int64_t elems = rows * cols, lo = elems * blockIdx.x / kNormSlices, hi = elems * (blockIdx.x + 1) / kNormSlices;
+    const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat;
+    double s = 0;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
+        const int64_t r = i / cols;
+        const double v = (double)(float)p[r * g_row + (i - r * cols)];
+        s += v * v;
+    }
+    s = wave_sum(s);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.y * kNormSlices + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// m' = beta m + (1 - beta) mean_i g_i (workers in ascending order); the matrix to orthogonalise is m', or beta m' + (1 - beta) mean g
+__global__ void __launch_bounds__(256) k_muon_head(const float *g, int64_t g_worker, int64_t g_mat, int32_t n, const float *m, int64_t m_mat, float *m_out, int64_t m_out_mat,
+                                                   float beta, int nesterov, float *update, int64_t elems)
+{
+    const float rest = 1.f - beta;
+    const float *pg = g + blockIdx.y * g_mat;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < elems; i += gridDim.x * (int64_t)256) {
+        float mean = 0.f;
+        for (int w = 0; w < n; ++w) mean += pg[w * g_worker + i];
+        mean /= (float)n;
+        const float mi = beta * m[blockIdx.y * m_mat + i] + rest * mean;
+        m_out[blockIdx.y * m_out_mat + i] = mi;
+        update[blockIdx.y * elems + i] = nesterov ? beta * mi + rest * mean : mi;
+    }
+}
+
+// the words of X_0, and what they stand for
+template <int T, int KIND>
+__global__ void __launch_bounds__(256) k_ortho_words(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int64_t rows, int64_t cols, float eps,
+                                                     const double *part, OrthoScale *scale, uint16_t *x)
+{
+    __shared__ double norm;
+    if (threadIdx.x < 64) {
+        const double s = wave_sum(part[blockIdx.y * kNormSlices + threadIdx.x]);
+        if (threadIdx.x == 0) norm = sqrt(s);
+    }
+    __syncthreads();
+    int e = 0;
+    if (norm > 0 && isfinite(norm)) {
+        (void)frexp(norm, &e);
+        e = 15 - e;                                                  // norm * 2^e in [2^14, 2^15)
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const double sigma = norm > 0 ? ldexp(1.0 / (norm + (double)eps), -e) : (norm == 0 ? 0.0 : norm);
+        scale[blockIdx.y] = OrthoScale{(float)sigma, (float)(sigma * sigma), e};
+    }
+    const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat;
+    const int64_t width = row_numbers<KIND>(cols), ld = row_words<KIND>(cols), total = rows * width;
+    uint16_t *o = x + blockIdx.y * rows * ld;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += gridDim.x * (int64_t)256) {
+        const int64_t r = i / width, c = i - r * width;
+        put<KIND>(o + r * ld, c, c < cols ? (float)ldexp((double)(float)p[r * g_row + c], e) : 0.f);
+    }
+}
+
+struct OrthoDims {
+    int64_t rows, cols, small;          // of X; small = min(rows, cols)
+};
+
+typedef Shape<128, 128, 2, 2, 2> OrthoShape;
+
+// the tile of the lower triangle with a given number
+__device__ __forceinline__ void triangle(int id, int &i, int &j)
+{
+    i = (int)((sqrtf(8.f * (float)id + 1.f) - 1.f) * 0.5f);
+    while ((i + 1) * (i + 2) / 2 <= id) ++i;
+    while (i * (i + 1) / 2 > id) --i;
+    j = id - i * (i + 1) / 2;
+}
+
+// writes a symmetric matrix's tile and its mirror image, with zeros in what fills the rows up
+template <class S, int KIND, typename F>
+__device__ __forceinline__ void put_symmetric(uint16_t *o, int64_t ld, int64_t small, int64_t m0, int64_t n0, const f32x16 (&acc)[S::MI][S::NI], F value)
+{
+    const int64_t width = row_numbers<KIND>(small);
+    for_each<S>(acc, [&](int dm, int dn, float raw) {
+        const int64_t m = m0 + dm, n = n0 + dn;
+        if (m >= width || n >= width) return;
+        const float v = m < small && n < small ? value(m, n, raw) : 0.f;
+        if (m < small) put<KIND>(o + m * ld, n, v);
+        if (m0 != n0 && n < small) put<KIND>(o + n * ld, m, v);
+    });
+}
+
+// A = X X' (X' X where X is tall), times f2 and, in the first step, sigma^2
+template <class S, int KIND, bool TALL>
+__global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    int ti, tj;
+    triangle((int)blockIdx.x, ti, tj);
+    const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ldx = row_words<KIND>(d.cols), lds_ = row_words<KIND>(d.small);
+    const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, 0, TALL ? d.rows : d.cols, zeros, lds);
+    if (scale) f *= scale[blockIdx.y].sigma2;
+    put_symmetric<S, KIND>(gram + blockIdx.y * d.small * lds_, lds_, d.small, m0, n0, acc, [&](int64_t, int64_t, float raw) { return raw * f; });
+}
+
+// P = a I + b A + c A A
+template <class S, int KIND>
+__global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram, OrthoDims d, float a, float b, float c, uint16_t *poly, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    int ti, tj;
+    triangle((int)blockIdx.x, ti, tj);
+    const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ld = row_words<KIND>(d.small);
+    const Operand A{gram + blockIdx.y * d.small * ld, ld, d.small};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, false, false>(acc, A, m0, A, n0, 0, d.small, zeros, lds);
+    put_symmetric<S, KIND>(poly + blockIdx.y * d.small * ld, ld, d.small, m0, n0, acc,
+                           [&](int64_t m, int64_t n, float raw) { return (m == n ? a : 0.f) + b * get<KIND>(A.p + m * ld, n) + c * raw; });
+}
+
+// where the last step's X goes
+struct OrthoOut {
+    void *out;                          // the caller's tensor
+    int64_t out_mat, out_row;
+    const float *x;                     // or: parameters, x_out = keep * x - rate * X
+    int64_t x_mat;
+    float keep, rate;
+};
+
+// X' = P X (X P where X is tall), times f and, in the first step, sigma; LAST: to the caller (T: its type; with parameters f32)
+template <class S, int KIND, bool TALL, bool LAST, int T>
+__global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, int tiles_n, float f, const OrthoScale *scale,
+                                                            uint16_t *next, OrthoOut o, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * S::BM, n0 = (int64_t)(blockIdx.x % tiles_n) * S::BN;
+    const int64_t ldx = row_words<KIND>(d.cols), ldp = row_words<KIND>(d.small);
+    const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.rows : d.cols}, P{poly + blockIdx.y * d.small * ldp, ldp, d.small};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    if constexpr (TALL) tile_product<S, KIND, false, false>(acc, X, m0, P, n0, 0, d.small, zeros, lds);
+    else tile_product<S, KIND, false, true>(acc, P, m0, X, n0, 0, d.small, zeros, lds);
+    if (scale) f *= scale[blockIdx.y].sigma;
+    const int64_t width = row_numbers<KIND>(d.cols);
+    for_each<S>(acc, [&](int dm, int dn, float raw) {
+        const int64_t m = m0 + dm, n = n0 + dn;
+        if (m >= d.rows) return;
+        if constexpr (LAST) {
+            if (n >= d.cols) return;
+            if (o.x) ((float *)o.out)[blockIdx.y * o.out_mat + m * o.out_row + n] = o.keep * o.x[blockIdx.y * o.x_mat + m * d.cols + n] - o.rate * (raw * f);
+            else ((typename TypeOf<T>::type *)o.out)[blockIdx.y * o.out_mat + m * o.out_row + n] = (typename TypeOf<T>::type)(raw * f);
+        } else {
+            if (n < width) put<KIND>(next + blockIdx.y * d.rows * ldx + m * ldx, n, n < d.cols ? raw * f : 0.f);
+        }
+    });
+}
+
+// the largest of |a + b u + c u^2| * u^(odd ? 1/2 : 0) for 0 <= u <= u_max
+static double poly_bound(double a, double b, double c, double u_max, bool odd)
+{
+    auto f = [&](double u) { return fabs(a + b * u + c * u * u) * (odd ? sqrt(u) : 1.0); };
+    double best = fmax(f(0.0), f(u_max));
+    auto at = [&](double u) { if (u > 0 && u < u_max) best = fmax(best, f(u)); };
+    if (!odd) {
+        if (c != 0) at(-b / (2 * c));
+    } else if (c != 0) {                                             // d/ds (a s + b s^3 + c s^5) = a + 3 b u + 5 c u^2
+        const double disc = 9 * b * b - 20 * a * c;
+        if (disc >= 0) { at((-3 * b + sqrt(disc)) / (10 * c)); at((-3 * b - sqrt(disc)) / (10 * c)); }
+    } else if (b != 0) {
+        at(-a / (3 * b));
+    }
+    return best;
+}
+
+// power of two that takes a bound to about 2^14, a quarter of what a 16-bit float holds
+static int word_exponent(double bound)
+{
+    if (!(bound > 0) || !isfinite(bound)) return 0;
+    int e;
+    (void)frexp(bound, &e);
+    e = 14 - e;
+    return e > 60 ? 60 : e < -60 ? -60 : e;
+}
+
+template <int KIND, int T>
+static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *coef, const OrthoOut &o)
+{
+    typedef OrthoShape S;
+    const OrthoDims d{c->rows, c->cols, c->rows < c->cols ? c->rows : c->cols};
+    const bool tall = c->rows > c->cols;
+    uint16_t *gram = c->scratch.at<uint16_t>(c->gram), *poly = c->scratch.at<uint16_t>(c->poly);
+    const uint16_t *zeros = c->scratch.at<uint16_t>(c->zeros);
+    const OrthoScale *scale = c->scratch.at<OrthoScale>(c->scale);
+    const int64_t ts = (d.small + S::BM - 1) / S::BM, tm = (d.rows + S::BM - 1) / S::BM, tn = (d.cols + S::BN - 1) / S::BN;
+    double bound = 1.0;                                              // of X's singular values
+    int ex = 0;                                                      // words of X = X * 2^ex; the first: X = words * sigma
+    for (int s = 0; s < steps; ++s) {
+        const uint16_t *x = c->scratch.at<uint16_t>(c->x[s & 1]);
+        uint16_t *next = c->scratch.at<uint16_t>(c->x[(s + 1) & 1]);
+        const double a = coef[0], b = coef[1], cc = coef[2], u = bound * bound;
+        const double after = poly_bound(a, b, cc, u, true);
+        const int ea = word_exponent(u), ep = word_exponent(poly_bound(a, b, cc, u, false)), en = word_exponent(after);
+        const OrthoScale *first = s == 0 ? scale : nullptr;
+        const dim3 tri((unsigned)(ts * (ts + 1) / 2), (unsigned)batch), all((unsigned)(tm * tn), (unsigned)batch);
+        const float fg = (float)ldexp(1.0, ea - 2 * ex);
+        if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), tri, dim3(S::THREADS), 0, c->stream, x, d, fg, first, gram, zeros);
+        else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), tri, dim3(S::THREADS), 0, c->stream, x, d, fg, first, gram, zeros);
+        hipLaunchKernelGGL((k_ortho_poly<S, KIND>), tri, dim3(S::THREADS), 0, c->stream, gram, d, (float)ldexp(a, ep), (float)ldexp(b, ep - ea),
+                           (float)ldexp(cc, ep - 2 * ea), poly, zeros);
+        const bool last = s + 1 == steps;
+        const float fa = (float)ldexp(1.0, (last ? 0 : en) - ep - ex);
+        auto apply = [&](auto kernel) { hipLaunchKernelGGL(kernel, all, dim3(S::THREADS), 0, c->stream, poly, x, d, (int)tn, fa, first, next, o, zeros); };
+        if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
+        else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
+        else if (last) apply(k_ortho_apply<S, KIND, false, true, T>);
+        else apply(k_ortho_apply<S, KIND, false, false, T>);
+        SAMS_HIP(hipGetLastError());
+        ex = en;
+        bound = after;
+    }
+    return SAMS_OK;
+}
+
+// from a matrix in memory to the last step
+template <int T>
+static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, int steps, const float *coef, float eps, const OrthoOut &o)
+{
+    constexpr int KIND = T == SAMS_F32 ? SPLIT : F16;
+    typedef typename TypeOf<T>::type E;
+    double *part = c->scratch.at<double>(c->part);
+    hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, part);
+    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows * c->cols, 1024, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row,
+                       c->rows, c->cols, eps, part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
+    SAMS_HIP(hipGetLastError());
+    return enqueue_steps<KIND, T>(c, batch, steps, coef, o);
+}
+
+static bool coef_ok(const float *coef)
+{
+    return coef && isfinite(coef[0]) && isfinite(coef[1]) && isfinite(coef[2]);
+}
+
+}  // namespace sams
+
+using namespace sams;
+
+extern "C" {
+
+int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t cols, int32_t type, void *hip_stream)
+{
+    if (!out) return SAMS_EINVAL;
+    *out = nullptr;
+    if (batch < 1 || batch > SAMS_MAX_BATCH || rows < 1 || rows > SAMS_MAX_DIM || cols < 1 || cols > SAMS_MAX_DIM || !type_ok(type)) return SAMS_EINVAL;
+    sams_ortho *c = new (std::nothrow) sams_ortho();
+    if (!c) return SAMS_ENOMEM;
+    c->batch = batch; c->rows = rows; c->cols = cols; c->type = type;
+    c->stream = (hipStream_t)hip_stream;
+    const int64_t small = rows < cols ? rows : cols;
+    const int64_t ldx = type == SAMS_F32 ? row_words<SPLIT>(cols) : row_words<F16>(cols), ldp = type == SAMS_F32 ? row_words<SPLIT>(small) : row_words<F16>(small);
+    for (int q = 0; q < 2; ++q) c->x[q] = c->scratch.reserve(batch * rows * ldx * 2);
+    c->gram = c->scratch.reserve(batch * small * ldp * 2);
+    c->poly = c->scratch.reserve(batch * small * ldp * 2);
+    c->scale = c->scratch.reserve(batch * (int64_t)sizeof(OrthoScale));
+    c->part = c->scratch.reserve(batch * kNormSlices * 8);
+    c->update = type == SAMS_F32 ? c->scratch.reserve(batch * rows * cols * 4) : -1;
+    c->zeros = c->scratch.reserve(256);
+    int rc = c->scratch.take();
+    if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->zeros), 64, 0u);
+    if (rc != SAMS_OK) {
+        if (c->scratch.base) (void)hipFree(c->scratch.base);
+        delete c;
+        return rc;
+    }
+    *out = c;
+    return SAMS_OK;
+}
+
+int sams_ortho_destroy(sams_ortho *c)
+{
+    if (!c) return SAMS_OK;
+    hipError_t e = hipStreamSynchronize(c->stream);
+    if (c->scratch.base) (void)hipFree(c->scratch.base);
+    delete c;
+    if (e != hipSuccess) { g_last_hip_error = (int)e; return SAMS_EHIP; }
+    return SAMS_OK;
+}
+
+int64_t sams_ortho_scratch_bytes(const sams_ortho *c) { return c ? c->scratch.bytes : 0; }
+
+int orthogonalize(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, int32_t steps, const float *coef_host, float eps,
+                  void *out, int64_t out_mat, int64_t out_row)
+{
+    if (!c || batch < 0 || batch > c->batch || steps < 1 || steps > SAMS_MAX_ORTHO_STEPS || !coef_ok(coef_host) || !(eps >= 0.f)) return SAMS_EINVAL;
+    if (batch == 0) return SAMS_OK;
+    const int size = type_size(c->type);
+    if (!g || !out || !aligned_to(g, size) || !aligned_to(out, size) || g_mat < 0 || g_row < 0 || (c->rows > 1 && out_row < c->cols) || (batch > 1 && out_mat < c->cols)) return SAMS_EINVAL;
+    const OrthoOut o{out, out_mat, out_row, nullptr, 0, 0.f, 0.f};
+    SAMS_BY_TYPE(c->type, T, return enqueue_ortho<T>(c, batch, g, g_mat, g_row, steps, coef_host, eps, o));
+}
+
+int muon_update(sams_ortho *c, int32_t n, int64_t batch, const float *g, int64_t g_worker, int64_t g_mat, const float *m, int64_t m_mat, const float *x,
+                int64_t x_mat, float *m_out, int64_t m_out_mat, float *x_out, int64_t x_out_mat, float beta, int32_t nesterov, float lr, float scale,
+                float weight_decay, int32_t steps, const float *coef_host, float eps)
+{
+    if (!c || c->type != SAMS_F32 || n < 1 || n > kMaxWorkers || batch < 0 || batch > c->batch || steps < 1 || steps > SAMS_MAX_ORTHO_STEPS ||
+        !coef_ok(coef_host) || !(eps >= 0.f)) return SAMS_EINVAL;
+    if (batch == 0) return SAMS_OK;
+    if (!g || !m || !x || !m_out || !x_out || !aligned_to(g, 4) || !aligned_to(m, 4) || !aligned_to(x, 4) || !aligned_to(m_out, 4) || !aligned_to(x_out, 4)) return SAMS_EINVAL;
+    const int64_t elems = c->rows * c->cols;
+    if (g_worker < 0 || g_mat < 0 || m_mat < 0 || x_mat < 0 || (batch > 1 && (m_out_mat < elems || x_out_mat < elems))) return SAMS_EINVAL;
+    float *update = c->scratch.at<float>(c->update);
+    hipLaunchKernelGGL(k_muon_head, dim3((unsigned)grid_for(elems, 256, 4096), (unsigned)batch), dim3(256), 0, c->stream, g, g_worker, g_mat, n, m, m_mat, m_out, m_out_mat,
+                       beta, nesterov, update, elems);
+    SAMS_HIP(hipGetLastError());
+    const OrthoOut o{x_out, x_out_mat, c->cols, x, x_mat, 1.f - lr * weight_decay, lr * scale};
+    return enqueue_ortho<SAMS_F32>(c, batch, update, elems, c->cols, steps, coef_host, eps, o);
+}
+
+}  // extern "C"

@@ -1,0 +1,459 @@
+// Softmax cross entropy of an output layer, for n workers' tokens at once, with its gradients, and without the logits in memory.
+//
+//   z_i = W h_i,  lse_i = log sum_v exp(z_iv),  loss_w = mean over the labelled tokens of worker w of (lse_i - z_i,label)
+//   dz_iv = (exp(z_iv - lse_i) - [v = label_i]) * grad_w / count_w,  dh_i = sum_v dz_iv W_v,  dW^(w)_v = sum_i in w dz_iv h_i
+//
+// Forward: tiles of z = W H' stay in registers; a tile leaves, per token, its largest logit and its sum of exponentials, which a
+// second kernel joins over the vocabulary.  Backward: for one piece of the vocabulary after the other, the tiles of z again, from
+// which dz goes to scratch as 16-bit words, and from there into the two products.  (The logits kept as 32-bit numbers would save a
+// quarter of the products for rows * vocab * 8 bytes of traffic, and as 16-bit numbers would spoil exp(z).)
+//
+// Words: tensors of 16 bits are multiplied as they are; those of 32 bits as pairs of 16-bit floats (22 bits), scaled by the power of two
+// that takes the tensor's largest finite number to 2^14.  dz is kept without grad_w / count_w (which the products' results are
+// multiplied by), as words of the same kind: 8 or 11 bits beside 16-bit tensors, 22 beside 32-bit ones; in 16-bit floats times 2^14, so
+// that probabilities down to 2^-38 are not lost.
+#include <math.h>
+#include <new>
+
+#include "sams_gemm.h"
+#include "sams_train.h"
+
+struct sams_xent {
+    int32_t n, type, train;
+    int64_t t_max, dim, vocab, piece;
+    hipStream_t stream;
+    sams::Scratch scratch;
+    int64_t h, w, dz, dh, part, token, inv, amax, exps, zeros;
+};
+
+namespace sams {
+
+using namespace gemm;
+
+constexpr int64_t kXentPieceBytes = (int64_t)256 << 20;     // of dz, for one piece of the vocabulary
+constexpr int kAmaxBlocks = 256;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+typedef Shape<128, 128, 2, 2, 2> XentShape;
+
+template <int KIND> __host__ __device__ constexpr int dz_exponent() { return KIND == BF16 ? 0 : 14; }
+template <int T> constexpr int kind_of() { return T == SAMS_F32 ? SPLIT : T == SAMS_BF16 ? BF16 : F16; }
+
+__device__ __forceinline__ bool takes_part(const int64_t *labels, int64_t row, int64_t vocab)
+{
+    return (uint64_t)labels[row] < (uint64_t)vocab;
+}
+
+// largest finite |value| over the rows (those that take no part left out), one result per block: of H in the first blocks, of W in the others
+__global__ void __launch_bounds__(256) k_xent_amax(const float *h, Rows hs, int64_t t, int64_t rows, const int64_t *labels, const float *w, int64_t w_row,
+                                                   int64_t vocab, int64_t dim, float *amax)
+{
+    __shared__ float best[4];
+    const bool of_w = blockIdx.x >= kAmaxBlocks;
+    const int block = of_w ? blockIdx.x - kAmaxBlocks : blockIdx.x;
+    const int64_t count = of_w ? vocab : rows;
+    float m = 0.f;
+    for (int64_t r = block * (int64_t)4 + (threadIdx.x >> 6); r < count; r += kAmaxBlocks * 4) {
+        const float *p;
+        if (of_w) {
+            p = w + r * w_row;
+        } else {
+            if (!takes_part(labels, r, vocab)) continue;
+            p = h + r / t * hs.worker + r % t * hs.row;
+        }
+        for (int64_t i = threadIdx.x & 63; i < dim; i += 64) {
+            const float v = fabsf(p[i]);
+            if (v <= 3.402823466e38f) m = fmaxf(m, v);
+        }
+    }
+    m = wave_max(m);
+    if ((threadIdx.x & 63) == 0) best[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) amax[blockIdx.x] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+}
+
+// words of a tensor's rows; rows that take no part (labels given) become zeros, whatever they hold
+template <int T, int KIND>
+__global__ void __launch_bounds__(256) k_xent_pack(const typename TypeOf<T>::type *src, Rows s, int64_t t, int64_t rows, int64_t dim, const int64_t *labels, int64_t vocab,
+                                                   const float *amax, int32_t *exps, uint16_t *out)
+{
+    float scale = 1.f;
+    if constexpr (KIND == SPLIT) {
+        float m = 0.f;
+        for (int i = threadIdx.x & 63; i < kAmaxBlocks; i += 64) m = fmaxf(m, amax[i]);
+        m = wave_max(m);
+        int e = 0;
+        if (m > 0) {
+            (void)frexpf(m, &e);
+            e = 15 - e;                                              // the largest at 2^14 to 2^15
+            if (e > 126) e = 126;
+        }
+        scale = ldexpf(1.f, e);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *exps = e;
+    }
+    const int64_t width = row_numbers<KIND>(dim), ld = row_words<KIND>(dim);
+    for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * (int64_t)4) {
+        const bool used = !labels || takes_part(labels, r, vocab);
+        const typename TypeOf<T>::type *p = src + r / t * s.worker + r % t * s.row;
+        for (int64_t i = threadIdx.x & 63; i < width; i += 64) put<KIND>(out + r * ld, i, used && i < dim ? (float)p[i] * scale : 0.f);
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ float unscale(const int32_t *exps, int which)        // 1 / the scale of H (0), of W (1), of both (2)
+{
+    if constexpr (KIND != SPLIT) return 1.f;
+    return ldexpf(1.f, -(which == 0 ? exps[0] : which == 1 ? exps[1] : exps[0] + exps[1]));
+}
+
+// Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).
+template <class S, int KIND>
+__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, int tiles_v, const int32_t *exps, float2 *part, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN;
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
+    const float f = kLog2e * unscale<KIND>(exps, 2);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
+    float2 *joined = (float2 *)lds;                                  // [WAVES_M][BN]
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) {
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                const int64_t v = m0 + (wm * S::MI + i) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
+                acc[i][j][q] = v < W.size ? acc[i][j][q] * f : -INFINITY;
+                top = fmaxf(top, acc[i][j][q]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f(acc[i][j][q] - base);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 32) joined[wm * S::BN + (wn * S::NI + j) * 32 + lane] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < S::BN; i += S::THREADS) {
+        float2 a = joined[i];
+#pragma unroll
+        for (int w = 1; w < S::WAVES_M; ++w) {
+            const float2 b = joined[w * S::BN + i];
+            const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
+            a = make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
+        }
+        if (n0 + i < H.size) part[(blockIdx.x % tiles_v) * H.size + n0 + i] = a;
+    }
+}
+
+// A token's log-sum over the tiles, its label's logit, its loss; a wavefront per token.
+template <int T>
+__global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles_v, const typename TypeOf<T>::type *h, Rows hs, const typename TypeOf<T>::type *w, int64_t w_row,
+                                                   const int64_t *labels, int64_t t, int64_t rows, int64_t dim, int64_t vocab, float *lse, float *token)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    if (!takes_part(labels, row, vocab)) {
+        if (lane == 0) lse[row] = token[row] = 0.f;
+        return;
+    }
+    float top = -INFINITY;
+    for (int i = lane; i < tiles_v; i += 64) top = fmaxf(top, part[i * rows + row].x);
+    top = wave_max(top);
+    float sum = 0.f;
+    for (int i = lane; i < tiles_v; i += 64) {
+        const float2 p = part[i * rows + row];
+        sum += p.y * __builtin_amdgcn_exp2f(p.x - top);
+    }
+    sum = wave_sum(sum);
+    const typename TypeOf<T>::type *ph = h + row / t * hs.worker + row % t * hs.row, *pw = w + labels[row] * w_row;
+    float dot = 0.f;
+    for (int64_t i = lane; i < dim; i += 64) dot = __builtin_fmaf((float)ph[i], (float)pw[i], dot);
+    dot = wave_sum(dot);
+    if (lane == 0) {
+        const float l = top * (1.f / kLog2e) + logf(sum);
+        lse[row] = l;
+        token[row] = l - dot;
+    }
+}
+
+// a worker's mean; tokens are added up in the same order every time
+__global__ void __launch_bounds__(256) k_xent_loss(const float *token, const int64_t *labels, int64_t t, int64_t vocab, float *loss)
+{
+    __shared__ float sums[4];
+    __shared__ int64_t counts[4];
+    float s = 0.f;
+    int c = 0;
+    for (int64_t i = threadIdx.x; i < t; i += 256) {
+        s += token[blockIdx.x * t + i];
+        c += takes_part(labels, blockIdx.x * t + i, vocab);
+    }
+    s = wave_sum(s);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+    if ((threadIdx.x & 63) == 0) { sums[threadIdx.x >> 6] = s; counts[threadIdx.x >> 6] = c; }
+    __syncthreads();
+    if (threadIdx.x) return;
+    const int64_t count = counts[0] + counts[1] + counts[2] + counts[3];
+    loss[blockIdx.x] = count ? (sums[0] + sums[1] + sums[2] + sums[3]) / (float)count : 0.f;
+}
+
+// grad_w / count_w; 0 where a worker has no labelled token
+__global__ void __launch_bounds__(256) k_xent_inv(const int64_t *labels, int64_t t, int64_t vocab, const float *grad, float *inv)
+{
+    __shared__ int64_t counts[4];
+    int c = 0;
+    for (int64_t i = threadIdx.x; i < t; i += 256) c += takes_part(labels, blockIdx.x * t + i, vocab);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
+    __syncthreads();
+    if (threadIdx.x) return;
+    const int64_t count = counts[0] + counts[1] + counts[2] + counts[3];
+    inv[blockIdx.x] = count ? (grad ? grad[blockIdx.x] : 1.f) / (float)count : 0.f;
+}
+
+// dz of one piece of the vocabulary (W: the piece), a row of words per token
+template <class S, int KIND>
+__global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, int tiles_v, const int32_t *exps, const int64_t *labels, int64_t v0, int64_t vocab,
+                                                        const float *lse, uint16_t *dz, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN;
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
+    const float f = kLog2e * unscale<KIND>(exps, 2), up = (float)(1 << dz_exponent<KIND>());
+    const int64_t width = row_numbers<KIND>(W.size), ld = row_words<KIND>(W.size);
+    for_each<S>(acc, [&](int dm, int dn, float raw) {
+        const int64_t v = m0 + dm, row = n0 + dn;
+        if (v >= width || row >= H.size) return;
+        float g = 0.f;
+        if (v < W.size && takes_part(labels, row, vocab)) g = __builtin_amdgcn_exp2f(__builtin_fmaf(raw, f, -lse[row] * kLog2e)) - (v0 + v == labels[row] ? 1.f : 0.f);
+        put<KIND>(dz + row * ld, v, g * up);
+    });
+}
+
+// dW of one worker and piece
+template <class S, int KIND, int T>
+__global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, int tiles_v, const int32_t *exps, const float *inv,
+                                                        typename TypeOf<T>::type *dw, Rows ds, int accumulate, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN, worker = blockIdx.y;
+    const int64_t ldz = row_words<KIND>(piece), ldh = row_words<KIND>(dim);
+    const Operand Z{dz + worker * t * ldz, ldz, piece}, H{h + worker * t * ldh, ldh, dim};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, true, true>(acc, Z, m0, H, n0, 0, t, zeros, lds);
+    const float f = inv[worker] / (float)(1 << dz_exponent<KIND>()), fh = unscale<KIND>(exps, 0);       // apart: together they may be too small
+    typename TypeOf<T>::type *out = dw + worker * ds.worker;
+    for_each<S>(acc, [&](int dm, int dn, float raw) {
+        const int64_t v = m0 + dm, i = n0 + dn;
+        if (v >= piece || i >= dim) return;
+        typename TypeOf<T>::type *o = out + v * ds.row + i;
+        const float value = raw * f * fh;
+        *o = (typename TypeOf<T>::type)(accumulate ? (float)*o + value : value);
+    });
+}
+
+// dh over one piece, added to that of the pieces before; the last piece's call hands the sums over
+template <class S, int KIND, int T>
+__global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, int64_t t, int tiles_n, int first, int last,
+                                                        const int32_t *exps, const float *inv, float *sums, typename TypeOf<T>::type *dh, Rows ds, const uint16_t *zeros)
+{
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * S::BM, n0 = (int64_t)(blockIdx.x % tiles_n) * S::BN;
+    const Operand Z{dz, row_words<KIND>(piece), rows};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, false, true>(acc, Z, m0, W, n0, 0, piece, zeros, lds);
+    const float f = 1.f / (float)(1 << dz_exponent<KIND>()), fw = unscale<KIND>(exps, 1);
+    for_each<S>(acc, [&](int dm, int dn, float raw) {
+        const int64_t row = m0 + dm, i = n0 + dn;
+        if (row >= rows || i >= W.size) return;
+        float v = raw;
+        if (!first) v += sums[row * W.size + i];
+        if (!last) sums[row * W.size + i] = v;
+        else dh[row / t * ds.worker + row % t * ds.row + i] = (typename TypeOf<T>::type)(v * (f * inv[row / t]) * fw);
+    });
+}
+
+// W and H as operands; packed where the tensors themselves are not fit to be loaded from (or hold rows to be left out)
+template <int T, int KIND>
+static int enqueue_operands(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, bool clean, Operand *H, Operand *W)
+{
+    typedef typename TypeOf<T>::type E;
+    const int64_t rows = c->n * t;
+    float *amax = c->scratch.at<float>(c->amax);
+    int32_t *exps = c->scratch.at<int32_t>(c->exps);
+    if (KIND == SPLIT)
+        hipLaunchKernelGGL(k_xent_amax, dim3(2 * kAmaxBlocks), dim3(256), 0, c->stream, (const float *)h, hs, t, rows, labels, (const float *)w, w_row, c->vocab, c->dim, amax);
+    const bool fit = KIND != SPLIT && c->dim % 8 == 0;
+    const bool rows_even = c->n == 1 || hs.worker == t * hs.row;
+    if (fit && !clean && rows_even && hs.row % 8 == 0 && aligned16(h)) {
+        *H = Operand{(const uint16_t *)h, hs.row, rows};
+    } else {
+        uint16_t *hp = c->scratch.at<uint16_t>(c->h);
+        hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3((unsigned)grid_for(rows, 4, 4096)), dim3(256), 0, c->stream, (const E *)h, hs, t, rows, c->dim, labels, c->vocab, amax, exps, hp);
+        *H = Operand{hp, row_words<KIND>(c->dim), rows};
+    }
+    if (fit && w_row % 8 == 0 && aligned16(w)) {
+        *W = Operand{(const uint16_t *)w, w_row, c->vocab};
+    } else {
+        uint16_t *wp = c->scratch.at<uint16_t>(c->w);
+        hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3((unsigned)grid_for(c->vocab, 4, 4096)), dim3(256), 0, c->stream, (const E *)w, Rows{0, w_row}, c->vocab, c->vocab, c->dim,
+                           (const int64_t *)nullptr, c->vocab, amax + kAmaxBlocks, exps + 1, wp);
+        *W = Operand{wp, row_words<KIND>(c->dim), c->vocab};
+    }
+    SAMS_HIP(hipGetLastError());
+    return SAMS_OK;
+}
+
+template <int T>
+static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, float *loss, float *lse)
+{
+    constexpr int KIND = kind_of<T>();
+    typedef typename TypeOf<T>::type E;
+    typedef XentShape S;
+    const int64_t rows = c->n * t;
+    float *token = c->scratch.at<float>(c->token);
+    if (rows) {
+        Operand H, W;
+        SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, &H, &W)));
+        float2 *part = c->scratch.at<float2>(c->part);
+        const int64_t tv = (c->vocab + S::BM - 1) / S::BM, tn = (rows + S::BN - 1) / S::BN;
+        hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3((unsigned)(tv * tn)), dim3(S::THREADS), 0, c->stream, W, H, c->dim, (int)tv, c->scratch.at<int32_t>(c->exps), part,
+                           c->scratch.at<uint16_t>(c->zeros));
+        hipLaunchKernelGGL(k_xent_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)tv, (const E *)h, hs, (const E *)w, w_row, labels, t, rows, c->dim,
+                           c->vocab, lse, token);
+    }
+    hipLaunchKernelGGL(k_xent_loss, dim3((unsigned)c->n), dim3(256), 0, c->stream, token, labels, t, c->vocab, loss);
+    SAMS_HIP(hipGetLastError());
+    return SAMS_OK;
+}
+
+template <int T>
+static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, const float *lse, const float *grad,
+                            void *dh, Rows dhs, void *dw, Rows dws, int dw_type, int accumulate)
+{
+    constexpr int KIND = kind_of<T>();
+    typedef typename TypeOf<T>::type E;
+    typedef XentShape S;
+    const int64_t rows = c->n * t;
+    float *inv = c->scratch.at<float>(c->inv);
+    const int32_t *exps = c->scratch.at<int32_t>(c->exps);
+    const uint16_t *zeros = c->scratch.at<uint16_t>(c->zeros);
+    uint16_t *dz = c->scratch.at<uint16_t>(c->dz);
+    hipLaunchKernelGGL(k_xent_inv, dim3((unsigned)c->n), dim3(256), 0, c->stream, labels, t, c->vocab, grad, inv);
+    Operand H{c->scratch.at<uint16_t>(c->h), row_words<KIND>(c->dim), 0}, W{c->scratch.at<uint16_t>(c->w), row_words<KIND>(c->dim), c->vocab};
+    if (rows) SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, &H, &W)));
+    for (int64_t v0 = 0; v0 < c->vocab; v0 += c->piece) {
+        const int64_t piece = c->vocab - v0 < c->piece ? c->vocab - v0 : c->piece;
+        const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
+        const int64_t tv = (piece + S::BM - 1) / S::BM, tr = (rows + S::BN - 1) / S::BN, td = (c->dim + S::BN - 1) / S::BN;
+        if (rows)
+            hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3((unsigned)(tv * tr)), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, (int)tv, exps, labels, v0, c->vocab, lse, dz, zeros);
+        auto weight = [&](auto kernel, auto *out) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(tv * td), (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, (int)tv, exps, inv, out + v0 * dws.row, dws,
+                               accumulate, zeros);
+        };
+        if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32>, (float *)dw);
+        else weight(k_xent_dw<S, KIND, T>, (E *)dw);
+        if (rows)
+            hipLaunchKernelGGL((k_xent_dh<S, KIND, T>), dim3((unsigned)(tr * td)), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, t, (int)td, v0 == 0,
+                               v0 + piece == c->vocab, exps, inv, c->scratch.at<float>(c->dh), (E *)dh, dhs, zeros);
+        SAMS_HIP(hipGetLastError());
+    }
+    return SAMS_OK;
+}
+
+static bool inputs_ok(const sams_xent *c, int64_t t, const void *h, int64_t h_worker, int64_t h_row, const void *w, int64_t w_row, const int64_t *labels)
+{
+    const int size = type_size(c->type);
+    if (t < 0 || t > c->t_max || !w || !aligned_to(w, size) || w_row < 0 || h_worker < 0 || h_row < 0) return false;
+    return t == 0 || (h && labels && aligned_to(h, size) && aligned_to(labels, 8));
+}
+
+}  // namespace sams
+
+using namespace sams;
+
+extern "C" {
+
+int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int64_t vocab, int32_t type, int32_t train, void *hip_stream)
+{
+    if (!out) return SAMS_EINVAL;
+    *out = nullptr;
+    if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || dim < 1 || dim > SAMS_MAX_DIM || vocab < 1 || vocab > SAMS_MAX_VOCAB || !type_ok(type))
+        return SAMS_EINVAL;
+    if ((n * t_max / 128 + 1) * (vocab / 128 + 1) > INT32_MAX) return SAMS_EINVAL;       // tiles of one launch
+    sams_xent *c = new (std::nothrow) sams_xent();
+    if (!c) return SAMS_ENOMEM;
+    c->n = n; c->t_max = t_max; c->dim = dim; c->vocab = vocab; c->type = type; c->train = train != 0;
+    c->stream = (hipStream_t)hip_stream;
+    const int64_t rows = n * t_max, ld = type == SAMS_F32 ? row_words<SPLIT>(dim) : row_words<F16>(dim);
+    c->h = c->scratch.reserve(rows * ld * 2);
+    c->w = c->scratch.reserve(vocab * ld * 2);
+    c->part = c->scratch.reserve(rows * ((vocab + XentShape::BM - 1) / XentShape::BM) * 8);
+    c->token = c->scratch.reserve(rows * 4);
+    c->inv = c->scratch.reserve(n * 4);
+    c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
+    c->exps = c->scratch.reserve(2 * 4);
+    c->zeros = c->scratch.reserve(256);
+    if (train) {
+        const int64_t row_bytes = type == SAMS_F32 ? 4 : 2, whole = (vocab + 255) / 256 * 256;
+        c->piece = rows ? kXentPieceBytes / (rows * row_bytes) / 256 * 256 : whole;
+        if (c->piece < 1024) c->piece = 1024;
+        if (c->piece > whole) c->piece = whole;
+        c->dz = c->scratch.reserve(rows * c->piece * row_bytes);
+        c->dh = c->scratch.reserve(rows * dim * 4);
+    }
+    int rc = c->scratch.take();
+    if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->zeros), 64, 0u);
+    if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->exps), 2, 0u);
+    if (rc != SAMS_OK) {
+        if (c->scratch.base) (void)hipFree(c->scratch.base);
+        delete c;
+        return rc;
+    }
+    *out = c;
+    return SAMS_OK;
+}
+
+int sams_xent_destroy(sams_xent *c)
+{
+    if (!c) return SAMS_OK;
+    hipError_t e = hipStreamSynchronize(c->stream);
+    if (c->scratch.base) (void)hipFree(c->scratch.base);
+    delete c;
+    if (e != hipSuccess) { g_last_hip_error = (int)e; return SAMS_EHIP; }
+    return SAMS_OK;
+}
+
+int64_t sams_xent_scratch_bytes(const sams_xent *c) { return c ? c->scratch.bytes : 0; }
+
+int linear_xent_forward(sams_xent *c, int64_t t, const void *h, int64_t h_worker, int64_t h_row, const void *w, int64_t w_row, const int64_t *labels, float *loss, float *lse)
+{
+    if (!c || !inputs_ok(c, t, h, h_worker, h_row, w, w_row, labels) || !loss || !aligned_to(loss, 4) || (t > 0 && (!lse || !aligned_to(lse, 4)))) return SAMS_EINVAL;
+    SAMS_BY_TYPE(c->type, T, return enqueue_forward<T>(c, t, h, Rows{h_worker, h_row}, w, w_row, labels, loss, lse));
+}
+
+int linear_xent_backward(sams_xent *c, int64_t t, const void *h, int64_t h_worker, int64_t h_row, const void *w, int64_t w_row, const int64_t *labels, const float *lse,
+                         const float *grad_loss, void *dh, int64_t dh_worker, int64_t dh_row, void *dw, int64_t dw_worker, int64_t dw_row, int32_t dw_type, int32_t accumulate)
+{
+    if (!c || !c->train || !inputs_ok(c, t, h, h_worker, h_row, w, w_row, labels) || !aligned_to(grad_loss, 4)) return SAMS_EINVAL;
+    if (dw_type != c->type && dw_type != SAMS_F32) return SAMS_EINVAL;
+    if (!dw || !aligned_to(dw, type_size(dw_type)) || (c->vocab > 1 && dw_row < c->dim) || (c->n > 1 && dw_worker < c->dim)) return SAMS_EINVAL;
+    if (t > 0 && (!lse || !aligned_to(lse, 4) || !dh || !aligned_to(dh, type_size(c->type)) || (t > 1 && dh_row < c->dim) || (c->n > 1 && dh_worker < c->dim))) return SAMS_EINVAL;
+    SAMS_BY_TYPE(c->type, T, return enqueue_backward<T>(c, t, h, Rows{h_worker, h_row}, w, w_row, labels, lse, grad_loss, dh, Rows{dh_worker, dh_row}, dw,
+                                                        Rows{dw_worker, dw_row}, dw_type, accumulate));
+}
+
+}  // extern "C"

@@ -23,7 +23,10 @@ _ERR = {SAMS_EINVAL: "SAMS_EINVAL (bad argument)", SAMS_ENOMEM: "SAMS_ENOMEM (sc
 EXPORTS = ["sams_create", "sams_destroy", "sams_scratch_bytes", "sams_precondition_device_memory", "sams_last_hip_error", "sams_hash_dump",
            "sams_configure", "sams_sketch_mode", "sams_accumulate_variant", "sams_record_rows", "sams_profile_kernels", "sams_profile_name", "sams_profile_enable", "sams_profile_only", "sams_profile_read",
            "sketch_accumulate", "sketch_reduce", "unsketch_topk", "unsketch_estimates", "gather_topk", "topk_refine",
-           "amsgrad_ef_update", "amsgrad_ef_update_pa", "topk_refine_static", "topk_refine_static_max_candidates"]
+           "amsgrad_ef_update", "amsgrad_ef_update_pa", "topk_refine_static", "topk_refine_static_max_candidates",
+           "sams_norm_create", "sams_norm_destroy", "sams_norm_scratch_bytes", "layer_norm_forward", "layer_norm_backward",
+           "sams_xent_create", "sams_xent_destroy", "sams_xent_scratch_bytes", "linear_xent_forward", "linear_xent_backward",
+           "sams_ortho_create", "sams_ortho_destroy", "sams_ortho_scratch_bytes", "orthogonalize", "muon_update"]
 
 _lib = None
 _F32, _I32 = torch.float32, torch.int32
@@ -77,9 +80,22 @@ def load() -> ctypes.CDLL:
     lib.topk_refine_static.argtypes = [vp, vp, i64, i64, vp, vp, vp]
     lib.topk_refine_static_max_candidates.argtypes = []
     lib.topk_refine_static_max_candidates.restype = i64
+    lib.sams_norm_create.argtypes = [ctypes.POINTER(vp), i32, i64, i64, i32, vp]
+    lib.layer_norm_forward.argtypes = [vp, i64, vp, i64, i64, vp, vp, f32, vp, i64, i64, vp, vp]
+    lib.layer_norm_backward.argtypes = [vp, i64, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, i64, vp, i64, i32]
+    lib.sams_xent_create.argtypes = [ctypes.POINTER(vp), i32, i64, i64, i64, i32, i32, vp]
+    lib.linear_xent_forward.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, vp, vp]
+    lib.linear_xent_backward.argtypes = [vp, i64, vp, i64, i64, vp, i64, vp, vp, vp, vp, i64, i64, vp, i64, i64, i32, i32]
+    lib.sams_ortho_create.argtypes = [ctypes.POINTER(vp), i64, i64, i64, i32, vp]
+    lib.orthogonalize.argtypes = [vp, i64, vp, i64, i64, i32, vp, f32, vp, i64, i64]
+    lib.muon_update.argtypes = [vp, i32, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, f32, i32, f32, f32, f32, i32, vp, f32]
+    for name in ("sams_norm", "sams_xent", "sams_ortho"):
+        getattr(lib, name + "_destroy").argtypes = getattr(lib, name + "_scratch_bytes").argtypes = [vp]
+        getattr(lib, name + "_scratch_bytes").restype = i64
     for name in EXPORTS:
         if name not in ("sams_scratch_bytes", "sams_profile_name", "sams_precondition_device_memory",
-                        "topk_refine_static_max_candidates", "sams_record_rows"):
+                        "topk_refine_static_max_candidates", "sams_record_rows", "sams_norm_scratch_bytes",
+                        "sams_xent_scratch_bytes", "sams_ortho_scratch_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     lib.sams_profile_name.restype = ctypes.c_char_p
     _lib = lib
@@ -304,3 +320,148 @@ def run_step(ctx: Context, b: Buffers, beta1, beta2, lr, g_next=None, first=Fals
     ctx.unsketch_topk(b.S_mean, vh, b.idx, None)
     ctx.gather_topk(b.e_u, vh, b.idx, b.U_workers, b.delta)
     ctx.amsgrad_ef_update(g_next, b.m, b.e_u, b.v, b.vhat, b.x, b.idx, b.delta, ctx.k, beta1, beta2, lr)
+
+
+# ---- training operators ----
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}       # SAMS_F32, SAMS_BF16, SAMS_F16
+
+
+def _strided(t, dtype, shape, inner, name):
+    """(address, distances of the leading axes) of a tensor whose last `inner` axes are contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    strides, want = t.stride(), 1
+    for axis in range(len(shape) - 1, len(shape) - 1 - inner, -1):
+        if shape[axis] > 1 and strides[axis] != want:
+            raise ValueError(f"{name}: the last {inner} axes have to be contiguous")
+        want *= shape[axis]
+    return (t.data_ptr(), *strides[:len(shape) - inner])
+
+
+class _TrainContext:
+    """Owns one context of a training operator.  Work is enqueued on the stream given, or on the torch stream that is current at
+    creation; a call made while another one is current waits for that one's work, and that one waits for the call's."""
+
+    _name = ""
+
+    def __init__(self, dtype, stream, *sizes):
+        if not torch.cuda.is_available():
+            raise RuntimeError("paper_2210_07454_amd needs a GPU: no CPU fallback exists")
+        if dtype not in TYPES:
+            raise TypeError(f"expected one of {list(TYPES)}, got {dtype}")
+        self.dtype = dtype
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self._lib = load()
+        self._h = ctypes.c_void_p()
+        _check(getattr(self._lib, self._name + "_create")(ctypes.byref(self._h), *sizes, ctypes.c_void_p(self.stream.cuda_stream)),
+               self._name + "_create")
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            getattr(self._lib, self._name + "_destroy")(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    @property
+    def scratch_bytes(self) -> int:
+        return int(getattr(self._lib, self._name + "_scratch_bytes")(self._h))
+
+    def _call(self, name, *args):
+        current = torch.cuda.current_stream()
+        other = current.cuda_stream != self.stream.cuda_stream
+        if other:
+            self.stream.wait_stream(current)
+        code = getattr(self._lib, name)(self._h, *args)
+        if other:
+            current.wait_stream(self.stream)
+        if code:
+            _check(code, name)
+
+
+class LayerNorm(_TrainContext):
+    """Layer norm of [n][t][dim] tensors, t up to ``t_max``; see sams.h."""
+
+    _name = "sams_norm"
+
+    def __init__(self, n: int, t_max: int, dim: int, dtype=torch.float32, stream=None):
+        self.n, self.t_max, self.dim = n, t_max, dim
+        super().__init__(dtype, stream, n, t_max, dim, TYPES.get(dtype, -1))
+
+    def layer_norm_forward(self, x, weight, bias, y, mean, rstd, eps=1e-5):
+        t = x.shape[1]
+        full = (self.n, t, self.dim)
+        self._call("layer_norm_forward", t, *_strided(x, self.dtype, full, 1, "x"), _ptr(weight, _F32, (self.dim,), "weight"),
+                   _ptr(bias, _F32, (self.dim,), "bias"), eps, *_strided(y, self.dtype, full, 1, "y"),
+                   _ptr(mean, _F32, full[:2], "mean"), _ptr(rstd, _F32, full[:2], "rstd"))
+
+    def layer_norm_backward(self, dy, x, weight, mean, rstd, dx, dweight, dbias=None, accumulate=False):
+        t = x.shape[1]
+        full, sums = (self.n, t, self.dim), (self.n, self.dim)
+        self._call("layer_norm_backward", t, *_strided(dy, self.dtype, full, 1, "dy"), *_strided(x, self.dtype, full, 1, "x"),
+                   _ptr(weight, _F32, (self.dim,), "weight"), _ptr(mean, _F32, full[:2], "mean"), _ptr(rstd, _F32, full[:2], "rstd"),
+                   *_strided(dx, self.dtype, full, 1, "dx"), *_strided(dweight, _F32, sums, 1, "dweight"),
+                   *(_strided(dbias, _F32, sums, 1, "dbias") if dbias is not None else (None, 0)), int(bool(accumulate)))
+
+
+class LinearCrossEntropy(_TrainContext):
+    """Output layer and softmax cross entropy of [n][t][dim] hidden states, t up to ``t_max``; see sams.h."""
+
+    _name = "sams_xent"
+
+    def __init__(self, n: int, t_max: int, dim: int, vocab: int, dtype=torch.float32, train=True, stream=None):
+        self.n, self.t_max, self.dim, self.vocab = n, t_max, dim, vocab
+        super().__init__(dtype, stream, n, t_max, dim, vocab, TYPES.get(dtype, -1), int(bool(train)))
+
+    def _inputs(self, h, w, labels):
+        t = h.shape[1]
+        return (t, *_strided(h, self.dtype, (self.n, t, self.dim), 1, "h"), *_strided(w, self.dtype, (self.vocab, self.dim), 1, "w"),
+                _ptr(labels, torch.int64, (self.n, t), "labels"))
+
+    def linear_xent_forward(self, h, w, labels, loss, lse):
+        self._call("linear_xent_forward", *self._inputs(h, w, labels), _ptr(loss, _F32, (self.n,), "loss"),
+                   _ptr(lse, _F32, (self.n, h.shape[1]), "lse"))
+
+    def linear_xent_backward(self, h, w, labels, lse, grad_loss, dh, dw, accumulate=False):
+        t = h.shape[1]
+        kind = dw.dtype if isinstance(dw, torch.Tensor) and dw.dtype in (self.dtype, _F32) else self.dtype
+        self._call("linear_xent_backward", *self._inputs(h, w, labels), _ptr(lse, _F32, (self.n, t), "lse"),
+                   _ptr(grad_loss, _F32, (self.n,), "grad_loss"), *_strided(dh, self.dtype, (self.n, t, self.dim), 1, "dh"),
+                   *_strided(dw, kind, (self.n, self.vocab, self.dim), 1, "dw"), TYPES[kind], int(bool(accumulate)))
+
+
+class Orthogonalizer(_TrainContext):
+    """Newton-Schulz orthogonalisation of up to ``batch`` matrices of one shape, and the momentum update built on it; see sams.h."""
+
+    _name = "sams_ortho"
+
+    def __init__(self, batch: int, rows: int, cols: int, dtype=torch.float32, stream=None):
+        self.batch, self.rows, self.cols = batch, rows, cols
+        super().__init__(dtype, stream, batch, rows, cols, TYPES.get(dtype, -1))
+
+    def orthogonalize(self, g, out, steps=5, coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
+        full = (g.shape[0], self.rows, self.cols)
+        self._call("orthogonalize", full[0], *_strided(g, self.dtype, full, 1, "g"), steps, (ctypes.c_float * 3)(*coef), eps,
+                   *_strided(out, self.dtype, full, 1, "out"))
+
+    def muon_update(self, g, m, x, m_out, x_out, beta=0.95, nesterov=True, lr=0.02, scale=1.0, weight_decay=0.0, steps=5,
+                    coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
+        n, batch = g.shape[:2]
+        full = (batch, self.rows, self.cols)
+        self._call("muon_update", n, batch, *_strided(g, _F32, (n, *full), 2, "g"), *_strided(m, _F32, full, 2, "m"),
+                   *_strided(x, _F32, full, 2, "x"), *_strided(m_out, _F32, full, 2, "m_out"), *_strided(x_out, _F32, full, 2, "x_out"),
+                   beta, int(bool(nesterov)), lr, scale, weight_decay, steps, (ctypes.c_float * 3)(*coef), eps)
