@@ -206,19 +206,197 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[S::MI][S::NI])
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 }
 
-// f(m, n, value) for every number of the workgroup's tile that this thread holds, m and n counted from the tile's corner; four in
-// a row are m, m + 1, m + 2, m + 3 of one n, and 32 lanes hold 32 n's next to each other.
-template <class S, typename F>
-__device__ __forceinline__ void for_each(const f32x16 (&acc)[S::MI][S::NI], F f)
+// Between a wavefront's writes to LDS and its other lanes' reads of them (which LDS serves in order): the compiler keeps the order too.
+__device__ __forceinline__ void same_wave_lds() { asm volatile("" ::: "memory"); __builtin_amdgcn_wave_barrier(); }
+
+// Hands the tile over row by row: C[n][m], n the row, m along it.  A lane holds four m's next to each other of one n, and 32 lanes 32
+// rows, so that stores from the registers would touch 32 lines at once; each wavefront turns its 32 rows round in LDS and stores them in
+// pieces of 16 bytes, a row's pieces in lanes next to each other.
+//   row(n)            what the numbers of row n need (n counted from the tile's corner), computed once a lane and 32 rows
+//   pack(r, m, v)     four numbers from m on: 8 bytes (BYTES 2), 16 bytes (BYTES 4), or for pairs the first parts, then the second
+//   store(n, at, w)   16 bytes of row n, `at` bytes from the tile's corner
+template <class S, int BYTES, bool PAIRS, typename Row, typename Pack, typename Store>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[S::MI][S::NI], char *lds, Row row, Pack pack, Store store)
 {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int ROW = S::MI * 32 * BYTES, PIECES = ROW / 16;
+    static_assert(32 * ROW * S::WAVES_M * S::WAVES_N <= S::LDS_BYTES, "a wavefront's rows have to fit");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31;
     const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
+    char *mine = lds + wave * 32 * ROW, *mine_row = mine + r * ROW;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i)
+    for (int j = 0; j < S::NI; ++j) {
+        const auto what = row(wn + j * 32 + r);
 #pragma unroll
-        for (int j = 0; j < S::NI; ++j)
+        for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) f(wm + i * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3), wn + j * 32 + (lane & 31), acc[i][j][q]);
+            for (int q = 0; q < 4; ++q) {
+                const int m = i * 32 + q * 8 + (lane >> 5) * 4;
+                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                const auto w = pack(what, wm + m, v);
+                if constexpr (PAIRS) {
+                    const int at = i * 128 + (m & 31) * 2;
+                    *(u32x2 *)(mine_row + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = u32x2{w[0], w[1]};
+                    *(u32x2 *)(mine_row + ((((at + 64) >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = u32x2{w[2], w[3]};
+                } else {
+                    const int at = m * BYTES;
+                    *(decltype(pack(what, 0, v)) *)(mine_row + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = w;
+                }
+            }
+        same_wave_lds();
+#pragma unroll
+        for (int it = 0; it < PIECES / 2; ++it) {
+            const int slot = it * 64 + lane, n = slot / PIECES, c = slot % PIECES;
+            store(wn + j * 32 + n, wm * BYTES + c * 16, *(const u32x4 *)(mine + n * ROW + ((c ^ (n & (PIECES - 1))) << 4)));
+        }
+        same_wave_lds();
+    }
+}
+
+// The same with the numbers themselves in LDS: emit(n, m, v) gets eight numbers of row n from m on, so that what it reads beside them
+// comes in pieces of 16 bytes too.  MIRROR: of the transposed tile, C[m][n]; emit(m, n, v).
+template <class S, bool MIRROR, typename Emit>
+__device__ __forceinline__ void eights(const f32x16 (&acc)[S::MI][S::NI], char *lds, Emit emit)
+{
+    constexpr int ALONG = (MIRROR ? S::NI : S::MI) * 32, ROW = ALONG * 4, PIECES = ROW / 16, EIGHTS = ALONG / 8;
+    static_assert(32 * ROW * S::WAVES_M * S::WAVES_N <= S::LDS_BYTES, "a wavefront's rows have to fit");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
+    const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
+    char *mine = lds + wave * 32 * ROW;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int outer = 0; outer < (MIRROR ? S::MI : S::NI); ++outer) {
+#pragma unroll
+        for (int inner = 0; inner < (MIRROR ? S::NI : S::MI); ++inner)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16 &a = MIRROR ? acc[outer][inner] : acc[inner][outer];
+                if constexpr (MIRROR) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 8 * q + 4 * h + e, at = (inner * 32 + l) * 4;
+                        *(float *)(mine + r * ROW + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = a[4 * q + e];
+                    }
+                } else {
+                    const int c = (inner * 32 + 8 * q + 4 * h) >> 2;
+                    *(f32x4 *)(mine + l * ROW + ((c ^ (l & (PIECES - 1))) << 4)) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                }
+            }
+        same_wave_lds();
+#pragma unroll
+        for (int it = 0; it < EIGHTS / 2; ++it) {
+            const int slot = it * 64 + lane, r = slot / EIGHTS, c = slot % EIGHTS * 2;
+            const f32x4 lo = *(const f32x4 *)(mine + r * ROW + ((c ^ (r & (PIECES - 1))) << 4)), hi = *(const f32x4 *)(mine + r * ROW + (((c + 1) ^ (r & (PIECES - 1))) << 4));
+            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if constexpr (MIRROR) emit(wm + outer * 32 + r, wn + c * 4, v);
+            else emit(wn + outer * 32 + r, wm + c * 4, v);
+        }
+        same_wave_lds();
+    }
+}
+
+// eight numbers as words of an operand, whose row's number i (a multiple of 8) they start at; and back
+template <int KIND>
+__device__ __forceinline__ void put8(uint16_t *row, int64_t i, const float (&v)[8])
+{
+    if constexpr (KIND == BF16) {
+        bf16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
+        *(bf16x8 *)(row + i) = w;
+    } else {
+        half8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (_Float16)v[e];
+        if constexpr (KIND == SPLIT) {
+            half8 rest;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rest[e] = (_Float16)(v[e] - (float)w[e]);
+            uint16_t *p = row + (i >> 5) * 64 + (i & 31);
+            *(half8 *)p = w;
+            *(half8 *)(p + 32) = rest;
+        } else {
+            *(half8 *)(row + i) = w;
+        }
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ void get8(const uint16_t *row, int64_t i, float (&v)[8])
+{
+    const uint16_t *p = KIND == SPLIT ? row + (i >> 5) * 64 + (i & 31) : row + i;
+    const half8 w = *(const half8 *)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)w[e];
+    if constexpr (KIND == SPLIT) {
+        const half8 rest = *(const half8 *)(p + 32);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += (float)rest[e];
+    }
+}
+
+template <typename E>
+__device__ __forceinline__ uint32_t pair_of(float a, float b)
+{
+    typedef E e2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, e2{(E)a, (E)b});
+}
+
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+
+// four numbers as words of an operand, for store_rows
+template <int KIND>
+__device__ __forceinline__ auto pack_words(const float (&v)[4])
+{
+    if constexpr (KIND == SPLIT) {
+        float rest[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rest[i] = v[i] - (float)(_Float16)v[i];
+        return u32x4{pair_of<_Float16>(v[0], v[1]), pair_of<_Float16>(v[2], v[3]), pair_of<_Float16>(rest[0], rest[1]), pair_of<_Float16>(rest[2], rest[3])};
+    } else if constexpr (KIND == F16) {
+        return words2{pair_of<_Float16>(v[0], v[1]), pair_of<_Float16>(v[2], v[3])};
+    } else {
+        return words2{pair_of<__bf16>(v[0], v[1]), pair_of<__bf16>(v[2], v[3])};
+    }
+}
+
+// four numbers as a caller's type, for store_rows
+template <typename E>
+__device__ __forceinline__ auto pack_numbers(const float (&v)[4])
+{
+    if constexpr (sizeof(E) == 4) return u32x4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]), __builtin_bit_cast(uint32_t, v[3])};
+    else return words2{pair_of<E>(v[0], v[1]), pair_of<E>(v[2], v[3])};
+}
+
+// 16 bytes of a caller's row, of which numbers from `limit` on do not exist; rows start anywhere
+template <typename E>
+__device__ __forceinline__ void store_numbers(E *row, int64_t at, int64_t limit, u32x4 w)
+{
+    constexpr int N = 16 / sizeof(E);
+    typedef uint32_t anywhere __attribute__((ext_vector_type(4), aligned(2)));
+    if (at + N <= limit) {
+        *(anywhere *)(row + at) = w;
+    } else {
+        E e[N];
+        __builtin_memcpy(e, &w, 16);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (at + i < limit) row[at + i] = e[i];
+    }
+}
+
+// A workgroup's place in a grid of tiles.  Workgroups go round the eight XCDs one by one; each XCD gets a contiguous run of tiles, and a run
+// goes over `kTileGroup` columns of tiles at a time, so that what an XCD works on at once shares its operands in that XCD's L2.
+constexpr int kTileGroup = 8;
+__device__ __forceinline__ void tile_place(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni)
+{
+    const uint32_t total = tiles_m * tiles_n, xcd = id & 7, each = total >> 3, over = total & 7;
+    id = xcd * each + (xcd < over ? xcd : over) + (id >> 3);
+    const uint32_t group = id / (kTileGroup * tiles_n), first = group * kTileGroup;
+    const uint32_t wide = tiles_m - first < kTileGroup ? tiles_m - first : kTileGroup;
+    const uint32_t in = id - first * tiles_n;
+    mi = first + in % wide;
+    ni = in / wide;
 }
 
 // one number as the words of an operand whose row starts at `row`; its place among the row's numbers is i
@@ -237,18 +415,11 @@ __device__ __forceinline__ void put(uint16_t *row, int64_t i, float v)
     }
 }
 
-template <int KIND>
-__device__ __forceinline__ float get(const uint16_t *row, int64_t i)
-{
-    if constexpr (KIND == SPLIT) {
-        const uint16_t *p = row + (i >> 5) * 64 + (i & 31);
-        return (float)__builtin_bit_cast(_Float16, p[0]) + (float)__builtin_bit_cast(_Float16, p[32]);
-    } else if constexpr (KIND == F16) {
-        return (float)__builtin_bit_cast(_Float16, row[i]);
-    } else {
-        return (float)__builtin_bit_cast(__bf16, row[i]);
-    }
-}
+// The tiles in use.  Large: 128 x 64 numbers a wavefront, 128 KB of LDS, one workgroup a CU; 1.1 PFLOP/s at 8192^3 in 16 bits (400 TFLOP/s of
+// pairs), against 0.9 (340) of Middle, two of which share a CU, and 0.6 (270) of Small, which takes the fewest numbers to fill the chip.
+typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<128, 128, 2, 2, 2> Middle;
+typedef Shape<64, 64, 2, 2, 2> Small;
 
 // words of a row of `numbers` numbers: whole 128-byte lines
 template <int KIND> __host__ __device__ constexpr int64_t row_words(int64_t numbers)

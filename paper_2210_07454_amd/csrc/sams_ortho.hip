@@ -29,46 +29,73 @@ namespace sams {
 
 using namespace gemm;
 
-constexpr int kNormSlices = 64;         // of a matrix, for the sum of its squares
+constexpr int kNormSlices = 512;        // of a matrix, for the sum of its squares
+constexpr int64_t kFillTiles = 192;     // tiles that make a tile's size worth it: three for every four CUs
 
 struct OrthoScale {
     float sigma, sigma2;                // what the words of G still have to be multiplied by, and its square
     int32_t exponent;                   // words of G = G * 2^exponent
 };
 
-// sums of squares in 64 bits: no norm is too large or too small for its square
+// sums of squares in 64 bits: no norm is too large or too small for its square; a wavefront per row
 template <int T>
 __global__ void __launch_bounds__(256) k_ortho_squares(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int64_t rows, int64_t cols, double *part)
 {
     __shared__ double sums[4];
-    const int64_t elems = rows * cols, lo = elems * blockIdx.x / kNormSlices, hi = elems * (blockIdx.x + 1) / kNormSlices;
-    const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double s = 0;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += 256) {
-        const int64_t r = i / cols;
-        const double v = (double)(float)p[r * g_row + (i - r * cols)];
-        s += v * v;
+    for (int64_t r = blockIdx.x * 4 + wave; r < rows; r += kNormSlices * 4) {
+        const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat + r * g_row;
+        for (int64_t i = lane * 8; i < cols; i += 512) {
+            float v[8];
+            load8<T>(p, i, cols, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+        }
+    }
+    s = wave_sum(s);
+    if (lane == 0) sums[wave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.y * kNormSlices + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// m' = beta m + (1 - beta) mean_i g_i (workers in ascending order); the matrix to orthogonalise is m', or beta m' + (1 - beta) mean g,
+// and the sum of its squares is made on the way
+__global__ void __launch_bounds__(256) k_muon_head(const float *g, int64_t g_worker, int64_t g_mat, int32_t n, const float *m, int64_t m_mat, float *m_out, int64_t m_out_mat,
+                                                   float beta, int nesterov, float *update, int64_t elems, double *part)
+{
+    __shared__ double sums[4];
+    const float rest = 1.f - beta, workers = (float)n;
+    const float *pg = g + blockIdx.y * g_mat;
+    double s = 0;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < elems; i += kNormSlices * 1024) {
+        float mean[4] = {0.f, 0.f, 0.f, 0.f}, mi[4], u[4];
+#pragma unroll 4
+        for (int w = 0; w < n; ++w) {
+            uint32_t raw[4];
+            float v[4];
+            load_piece<SAMS_F32>(pg + w * g_worker, i, elems, raw);
+            widen<SAMS_F32>(raw, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mean[e] += v[e];
+        }
+        uint32_t raw[4];
+        load_piece<SAMS_F32>(m + blockIdx.y * m_mat, i, elems, raw);
+        widen<SAMS_F32>(raw, mi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float share = rest * (mean[e] / workers);
+            mi[e] = beta * mi[e] + share;
+            u[e] = nesterov ? beta * mi[e] + share : mi[e];
+            if (i + e < elems) s = __builtin_fma((double)u[e], (double)u[e], s);
+        }
+        store_piece<SAMS_F32>(m_out + blockIdx.y * m_out_mat, i, elems, mi);
+        store_piece<SAMS_F32>(update + blockIdx.y * elems, i, elems, u);
     }
     s = wave_sum(s);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
     if (threadIdx.x == 0) part[blockIdx.y * kNormSlices + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
-}
-
-// m' = beta m + (1 - beta) mean_i g_i (workers in ascending order); the matrix to orthogonalise is m', or beta m' + (1 - beta) mean g
-__global__ void __launch_bounds__(256) k_muon_head(const float *g, int64_t g_worker, int64_t g_mat, int32_t n, const float *m, int64_t m_mat, float *m_out, int64_t m_out_mat,
-                                                   float beta, int nesterov, float *update, int64_t elems)
-{
-    const float rest = 1.f - beta;
-    const float *pg = g + blockIdx.y * g_mat;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < elems; i += gridDim.x * (int64_t)256) {
-        float mean = 0.f;
-        for (int w = 0; w < n; ++w) mean += pg[w * g_worker + i];
-        mean /= (float)n;
-        const float mi = beta * m[blockIdx.y * m_mat + i] + rest * mean;
-        m_out[blockIdx.y * m_out_mat + i] = mi;
-        update[blockIdx.y * elems + i] = nesterov ? beta * mi + rest * mean : mi;
-    }
 }
 
 // the words of X_0, and what they stand for
@@ -78,7 +105,9 @@ __global__ void __launch_bounds__(256) k_ortho_words(const typename TypeOf<T>::t
 {
     __shared__ double norm;
     if (threadIdx.x < 64) {
-        const double s = wave_sum(part[blockIdx.y * kNormSlices + threadIdx.x]);
+        double s = 0;
+        for (int i = threadIdx.x; i < kNormSlices; i += 64) s += part[blockIdx.y * kNormSlices + i];
+        s = wave_sum(s);
         if (threadIdx.x == 0) norm = sqrt(s);
     }
     __syncthreads();
@@ -91,20 +120,24 @@ __global__ void __launch_bounds__(256) k_ortho_words(const typename TypeOf<T>::t
         const double sigma = norm > 0 ? ldexp(1.0 / (norm + (double)eps), -e) : (norm == 0 ? 0.0 : norm);
         scale[blockIdx.y] = OrthoScale{(float)sigma, (float)(sigma * sigma), e};
     }
-    const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat;
-    const int64_t width = row_numbers<KIND>(cols), ld = row_words<KIND>(cols), total = rows * width;
-    uint16_t *o = x + blockIdx.y * rows * ld;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += gridDim.x * (int64_t)256) {
-        const int64_t r = i / width, c = i - r * width;
-        put<KIND>(o + r * ld, c, c < cols ? (float)ldexp((double)(float)p[r * g_row + c], e) : 0.f);
+    const double by = ldexp(1.0, e);
+    const int64_t width = row_numbers<KIND>(cols), ld = row_words<KIND>(cols);
+    for (int64_t r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
+        const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat + r * g_row;
+        uint16_t *o = x + (blockIdx.y * rows + r) * ld;
+        for (int64_t i = (threadIdx.x & 63) * 8; i < width; i += 512) {
+            float v[8];
+            load8<T>(p, i, cols, v);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = (float)((double)v[q] * by);
+            put8<KIND>(o, i, v);
+        }
     }
 }
 
 struct OrthoDims {
     int64_t rows, cols, small;          // of X; small = min(rows, cols)
 };
-
-typedef Shape<128, 128, 2, 2, 2> OrthoShape;
 
 // the tile of the lower triangle with a given number
 __device__ __forceinline__ void triangle(int id, int &i, int &j)
@@ -115,34 +148,45 @@ __device__ __forceinline__ void triangle(int id, int &i, int &j)
     j = id - i * (i + 1) / 2;
 }
 
-// writes a symmetric matrix's tile and its mirror image, with zeros in what fills the rows up
+// Writes a symmetric matrix's tile and its mirror image, with zeros in what fills the rows up; value(row, col, v) makes eight numbers of them.
 template <class S, int KIND, typename F>
-__device__ __forceinline__ void put_symmetric(uint16_t *o, int64_t ld, int64_t small, int64_t m0, int64_t n0, const f32x16 (&acc)[S::MI][S::NI], F value)
+__device__ __forceinline__ void put_symmetric(uint16_t *o, int64_t ld, int64_t small, int64_t m0, int64_t n0, const f32x16 (&acc)[S::MI][S::NI], char *lds, F value)
 {
     const int64_t width = row_numbers<KIND>(small);
-    for_each<S>(acc, [&](int dm, int dn, float raw) {
-        const int64_t m = m0 + dm, n = n0 + dn;
-        if (m >= width || n >= width) return;
-        const float v = m < small && n < small ? value(m, n, raw) : 0.f;
-        if (m < small) put<KIND>(o + m * ld, n, v);
-        if (m0 != n0 && n < small) put<KIND>(o + n * ld, m, v);
-    });
+    auto emit = [&](int64_t row, int64_t col, const float (&raw)[8]) {
+        if (row >= small || col >= width) return;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = raw[e];
+        value(row, col, v);
+        if (col + 8 > small) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e >= small) v[e] = 0.f;
+        }
+        put8<KIND>(o + row * ld, col, v);
+    };
+    eights<S, false>(acc, lds, [&](int dn, int dm, const float (&raw)[8]) { emit(n0 + dn, m0 + dm, raw); });
+    if (m0 != n0) eights<S, true>(acc, lds, [&](int dm, int dn, const float (&raw)[8]) { emit(m0 + dm, n0 + dn, raw); });
 }
 
-// A = X X' (X' X where X is tall), times f2 and, in the first step, sigma^2
+// A = X X' (X' X where X is tall), times f and, in the first step, sigma^2
 template <class S, int KIND, bool TALL>
 __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram, const uint16_t *zeros)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     int ti, tj;
     triangle((int)blockIdx.x, ti, tj);
-    const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ldx = row_words<KIND>(d.cols), lds_ = row_words<KIND>(d.small);
+    const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ldx = row_words<KIND>(d.cols), ldg = row_words<KIND>(d.small);
     const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, 0, TALL ? d.rows : d.cols, zeros, lds);
     if (scale) f *= scale[blockIdx.y].sigma2;
-    put_symmetric<S, KIND>(gram + blockIdx.y * d.small * lds_, lds_, d.small, m0, n0, acc, [&](int64_t, int64_t, float raw) { return raw * f; });
+    put_symmetric<S, KIND>(gram + blockIdx.y * d.small * ldg, ldg, d.small, m0, n0, acc, lds, [&](int64_t, int64_t, float (&v)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+    });
 }
 
 // P = a I + b A + c A A
@@ -157,8 +201,12 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram,
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, A, m0, A, n0, 0, d.small, zeros, lds);
-    put_symmetric<S, KIND>(poly + blockIdx.y * d.small * ld, ld, d.small, m0, n0, acc,
-                           [&](int64_t m, int64_t n, float raw) { return (m == n ? a : 0.f) + b * get<KIND>(A.p + m * ld, n) + c * raw; });
+    put_symmetric<S, KIND>(poly + blockIdx.y * d.small * ld, ld, d.small, m0, n0, acc, lds, [&](int64_t row, int64_t col, float (&v)[8]) {
+        float g[8];
+        get8<KIND>(A.p + row * ld, col, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (row == col + e ? a : 0.f) + b * g[e] + c * v[e];
+    });
 }
 
 // where the last step's X goes
@@ -172,28 +220,47 @@ struct OrthoOut {
 
 // X' = P X (X P where X is tall), times f and, in the first step, sigma; LAST: to the caller (T: its type; with parameters f32)
 template <class S, int KIND, bool TALL, bool LAST, int T>
-__global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, int tiles_n, float f, const OrthoScale *scale,
-                                                            uint16_t *next, OrthoOut o, const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, uint32_t tiles_m, uint32_t tiles_n, float f,
+                                                            const OrthoScale *scale, uint16_t *next, OrthoOut o, const uint16_t *zeros)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * S::BM, n0 = (int64_t)(blockIdx.x % tiles_n) * S::BN;
+    uint32_t mi, ni;
+    tile_place(blockIdx.x, tiles_m, tiles_n, mi, ni);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;            // m: X's columns, n: its rows
     const int64_t ldx = row_words<KIND>(d.cols), ldp = row_words<KIND>(d.small);
     const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.rows : d.cols}, P{poly + blockIdx.y * d.small * ldp, ldp, d.small};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    if constexpr (TALL) tile_product<S, KIND, false, false>(acc, X, m0, P, n0, 0, d.small, zeros, lds);
-    else tile_product<S, KIND, false, true>(acc, P, m0, X, n0, 0, d.small, zeros, lds);
+    if constexpr (TALL) tile_product<S, KIND, false, false>(acc, P, m0, X, n0, 0, d.small, zeros, lds);
+    else tile_product<S, KIND, true, false>(acc, X, m0, P, n0, 0, d.small, zeros, lds);
     if (scale) f *= scale[blockIdx.y].sigma;
     const int64_t width = row_numbers<KIND>(d.cols);
-    for_each<S>(acc, [&](int dm, int dn, float raw) {
-        const int64_t m = m0 + dm, n = n0 + dn;
-        if (m >= d.rows) return;
+    eights<S, false>(acc, lds, [&](int dn, int dm, const float (&raw)[8]) {
+        const int64_t r = n0 + dn, col = m0 + dm;
+        if (r >= d.rows || col >= (LAST ? d.cols : width)) return;
         if constexpr (LAST) {
-            if (n >= d.cols) return;
-            if (o.x) ((float *)o.out)[blockIdx.y * o.out_mat + m * o.out_row + n] = o.keep * o.x[blockIdx.y * o.x_mat + m * d.cols + n] - o.rate * (raw * f);
-            else ((typename TypeOf<T>::type *)o.out)[blockIdx.y * o.out_mat + m * o.out_row + n] = (typename TypeOf<T>::type)(raw * f);
+            typedef typename TypeOf<T>::type E;
+            E *out = (E *)o.out + blockIdx.y * o.out_mat + r * o.out_row;
+            const float *px = o.x ? o.x + blockIdx.y * o.x_mat + r * d.cols : nullptr;
+            E e8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = raw[e] * f;
+                if constexpr (T == SAMS_F32) e8[e] = px ? (col + e < d.cols ? o.keep * px[col + e] - o.rate * v : 0.f) : v;
+                else e8[e] = (E)v;
+            }
+            u32x4 w;
+            __builtin_memcpy(&w, e8, 16);
+            store_numbers(out, col, d.cols, w);
+            if constexpr (T == SAMS_F32) {
+                __builtin_memcpy(&w, e8 + 4, 16);
+                store_numbers(out, col + 4, d.cols, w);
+            }
         } else {
-            if (n < width) put<KIND>(next + blockIdx.y * d.rows * ldx + m * ldx, n, n < d.cols ? raw * f : 0.f);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = col + e < d.cols ? raw[e] * f : 0.f;
+            put8<KIND>(next + blockIdx.y * d.rows * ldx + r * ldx, col, v);
         }
     });
 }
@@ -225,16 +292,27 @@ static int word_exponent(double bound)
     return e > 60 ? 60 : e < -60 ? -60 : e;
 }
 
+// calls f with the tile for a product of so many numbers: the largest of which there are about as many as CUs
+template <typename F>
+static void by_tiles(int64_t batch, int64_t m, int64_t n, bool triangular, F f)
+{
+    auto count = [&](int64_t size) {
+        const int64_t a = (m + size - 1) / size, b = (n + size - 1) / size;
+        return batch * (triangular ? a * (a + 1) / 2 : a * b);
+    };
+    if (count(256) >= kFillTiles) f(Large());
+    else if (count(128) >= kFillTiles) f(Middle());
+    else f(Small());
+}
+
 template <int KIND, int T>
 static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *coef, const OrthoOut &o)
 {
-    typedef OrthoShape S;
     const OrthoDims d{c->rows, c->cols, c->rows < c->cols ? c->rows : c->cols};
     const bool tall = c->rows > c->cols;
     uint16_t *gram = c->scratch.at<uint16_t>(c->gram), *poly = c->scratch.at<uint16_t>(c->poly);
     const uint16_t *zeros = c->scratch.at<uint16_t>(c->zeros);
     const OrthoScale *scale = c->scratch.at<OrthoScale>(c->scale);
-    const int64_t ts = (d.small + S::BM - 1) / S::BM, tm = (d.rows + S::BM - 1) / S::BM, tn = (d.cols + S::BN - 1) / S::BN;
     double bound = 1.0;                                              // of X's singular values
     int ex = 0;                                                      // words of X = X * 2^ex; the first: X = words * sigma
     for (int s = 0; s < steps; ++s) {
@@ -244,19 +322,29 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *c
         const double after = poly_bound(a, b, cc, u, true);
         const int ea = word_exponent(u), ep = word_exponent(poly_bound(a, b, cc, u, false)), en = word_exponent(after);
         const OrthoScale *first = s == 0 ? scale : nullptr;
-        const dim3 tri((unsigned)(ts * (ts + 1) / 2), (unsigned)batch), all((unsigned)(tm * tn), (unsigned)batch);
-        const float fg = (float)ldexp(1.0, ea - 2 * ex);
-        if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), tri, dim3(S::THREADS), 0, c->stream, x, d, fg, first, gram, zeros);
-        else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), tri, dim3(S::THREADS), 0, c->stream, x, d, fg, first, gram, zeros);
-        hipLaunchKernelGGL((k_ortho_poly<S, KIND>), tri, dim3(S::THREADS), 0, c->stream, gram, d, (float)ldexp(a, ep), (float)ldexp(b, ep - ea),
-                           (float)ldexp(cc, ep - 2 * ea), poly, zeros);
+        by_tiles(batch, d.small, d.small, true, [&](auto shape) {
+            typedef decltype(shape) S;
+            const int64_t ts = (d.small + S::BM - 1) / S::BM;
+            const dim3 grid((unsigned)(ts * (ts + 1) / 2), (unsigned)batch);
+            const float f = (float)ldexp(1.0, ea - 2 * ex);
+            if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram, zeros);
+            else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram, zeros);
+            hipLaunchKernelGGL((k_ortho_poly<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, gram, d, (float)ldexp(a, ep), (float)ldexp(b, ep - ea), (float)ldexp(cc, ep - 2 * ea),
+                               poly, zeros);
+        });
         const bool last = s + 1 == steps;
-        const float fa = (float)ldexp(1.0, (last ? 0 : en) - ep - ex);
-        auto apply = [&](auto kernel) { hipLaunchKernelGGL(kernel, all, dim3(S::THREADS), 0, c->stream, poly, x, d, (int)tn, fa, first, next, o, zeros); };
-        if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
-        else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
-        else if (last) apply(k_ortho_apply<S, KIND, false, true, T>);
-        else apply(k_ortho_apply<S, KIND, false, false, T>);
+        const float f = (float)ldexp(1.0, (last ? 0 : en) - ep - ex);
+        by_tiles(batch, d.cols, d.rows, false, [&](auto shape) {
+            typedef decltype(shape) S;
+            const uint32_t tm = (uint32_t)((d.cols + S::BM - 1) / S::BM), tn = (uint32_t)((d.rows + S::BN - 1) / S::BN);
+            auto apply = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, f, first, next, o, zeros);
+            };
+            if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
+            else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
+            else if (last) apply(k_ortho_apply<S, KIND, false, true, T>);
+            else apply(k_ortho_apply<S, KIND, false, false, T>);
+        });
         SAMS_HIP(hipGetLastError());
         ex = en;
         bound = after;
@@ -264,15 +352,14 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *c
     return SAMS_OK;
 }
 
-// from a matrix in memory to the last step
+// from a matrix in memory, the sum of its squares made, to the last step
 template <int T>
 static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, int steps, const float *coef, float eps, const OrthoOut &o)
 {
     constexpr int KIND = T == SAMS_F32 ? SPLIT : F16;
     typedef typename TypeOf<T>::type E;
     double *part = c->scratch.at<double>(c->part);
-    hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, part);
-    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows * c->cols, 1024, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row,
+    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows, 4, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row,
                        c->rows, c->cols, eps, part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
     SAMS_HIP(hipGetLastError());
     return enqueue_steps<KIND, T>(c, batch, steps, coef, o);
@@ -338,6 +425,8 @@ int orthogonalize(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, in
     const int size = type_size(c->type);
     if (!g || !out || !aligned_to(g, size) || !aligned_to(out, size) || g_mat < 0 || g_row < 0 || (c->rows > 1 && out_row < c->cols) || (batch > 1 && out_mat < c->cols)) return SAMS_EINVAL;
     const OrthoOut o{out, out_mat, out_row, nullptr, 0, 0.f, 0.f};
+    SAMS_BY_TYPE(c->type, T, hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const TypeOf<T>::type *)g, g_mat, g_row, c->rows,
+                                                c->cols, c->scratch.at<double>(c->part)));
     SAMS_BY_TYPE(c->type, T, return enqueue_ortho<T>(c, batch, g, g_mat, g_row, steps, coef_host, eps, o));
 }
 
@@ -352,8 +441,8 @@ int muon_update(sams_ortho *c, int32_t n, int64_t batch, const float *g, int64_t
     const int64_t elems = c->rows * c->cols;
     if (g_worker < 0 || g_mat < 0 || m_mat < 0 || x_mat < 0 || (batch > 1 && (m_out_mat < elems || x_out_mat < elems))) return SAMS_EINVAL;
     float *update = c->scratch.at<float>(c->update);
-    hipLaunchKernelGGL(k_muon_head, dim3((unsigned)grid_for(elems, 256, 4096), (unsigned)batch), dim3(256), 0, c->stream, g, g_worker, g_mat, n, m, m_mat, m_out, m_out_mat,
-                       beta, nesterov, update, elems);
+    hipLaunchKernelGGL(k_muon_head, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, g, g_worker, g_mat, n, m, m_mat, m_out, m_out_mat, beta, nesterov, update, elems,
+                       c->scratch.at<double>(c->part));
     SAMS_HIP(hipGetLastError());
     const OrthoOut o{x_out, x_out_mat, c->cols, x, x_mat, 1.f - lr * weight_decay, lr * scale};
     return enqueue_ortho<SAMS_F32>(c, batch, update, elems, c->cols, steps, coef_host, eps, o);

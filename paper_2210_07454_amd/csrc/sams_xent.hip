@@ -13,7 +13,9 @@
 // multiplied by), as words of the same kind: 8 or 11 bits beside 16-bit tensors, 22 beside 32-bit ones; in 16-bit floats times 2^14, so
 // that probabilities down to 2^-38 are not lost.
 #include <math.h>
+#include <algorithm>
 #include <new>
+#include <type_traits>
 
 #include "sams_gemm.h"
 #include "sams_train.h"
@@ -31,10 +33,12 @@ namespace sams {
 using namespace gemm;
 
 constexpr int64_t kXentPieceBytes = (int64_t)256 << 20;     // of dz, for one piece of the vocabulary
-constexpr int kAmaxBlocks = 256;
+constexpr int kAmaxBlocks = 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
 
-typedef Shape<128, 128, 2, 2, 2> XentShape;
+constexpr int64_t kFillTiles = 192;                         // tiles that make a tile's size worth it: three for every four CUs
+constexpr int64_t kPartBytes = (int64_t)256 << 20;          // of partial sums of dh, at most (but one for every token)
+constexpr int kMaxSplit = 64;
 
 template <int KIND> __host__ __device__ constexpr int dz_exponent() { return KIND == BF16 ? 0 : 14; }
 template <int T> constexpr int kind_of() { return T == SAMS_F32 ? SPLIT : T == SAMS_BF16 ? BF16 : F16; }
@@ -61,9 +65,14 @@ __global__ void __launch_bounds__(256) k_xent_amax(const float *h, Rows hs, int6
             if (!takes_part(labels, r, vocab)) continue;
             p = h + r / t * hs.worker + r % t * hs.row;
         }
-        for (int64_t i = threadIdx.x & 63; i < dim; i += 64) {
-            const float v = fabsf(p[i]);
-            if (v <= 3.402823466e38f) m = fmaxf(m, v);
+        for (int64_t i = (threadIdx.x & 63) * 4; i < dim; i += 256) {
+            uint32_t raw[4];
+            load_piece<SAMS_F32>(p, i, dim, raw);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = fabsf(__builtin_bit_cast(float, raw[e]));
+                m = v <= 3.402823466e38f ? fmaxf(m, v) : m;
+            }
         }
     }
     m = wave_max(m);
@@ -95,7 +104,13 @@ __global__ void __launch_bounds__(256) k_xent_pack(const typename TypeOf<T>::typ
     for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * (int64_t)4) {
         const bool used = !labels || takes_part(labels, r, vocab);
         const typename TypeOf<T>::type *p = src + r / t * s.worker + r % t * s.row;
-        for (int64_t i = threadIdx.x & 63; i < width; i += 64) put<KIND>(out + r * ld, i, used && i < dim ? (float)p[i] * scale : 0.f);
+        for (int64_t i = (threadIdx.x & 63) * 8; i < width; i += 512) {
+            float v[8];
+            load8<T>(p, i, used ? dim : 0, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= scale;
+            put8<KIND>(out + r * ld, i, v);
+        }
     }
 }
 
@@ -106,17 +121,30 @@ __device__ __forceinline__ float unscale(const int32_t *exps, int which)        
     return ldexpf(1.f, -(which == 0 ? exps[0] : which == 1 ? exps[1] : exps[0] + exps[1]));
 }
 
-// Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).
+// Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).  A lane holds numbers
+// of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, int tiles_v, const int32_t *exps, float2 *part, const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, float2 *part,
+                                                           const uint16_t *zeros)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN;
+    uint32_t mi, ni;
+    tile_place(blockIdx.x, tiles_v, tiles_t, mi, ni);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
     const float f = kLog2e * unscale<KIND>(exps, 2);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
+    if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+                if (m0 + (wm * S::MI + i) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3) >= W.size)
+#pragma unroll
+                    for (int j = 0; j < S::NI; ++j) acc[i][j][q] = -INFINITY;
+    }
     float2 *joined = (float2 *)lds;                                  // [WAVES_M][BN]
 #pragma unroll
     for (int j = 0; j < S::NI; ++j) {
@@ -124,17 +152,13 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const int64_t v = m0 + (wm * S::MI + i) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
-                acc[i][j][q] = v < W.size ? acc[i][j][q] * f : -INFINITY;
-                top = fmaxf(top, acc[i][j][q]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 32));
+            for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * f;
         const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-            for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f(acc[i][j][q] - base);
+            for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][q], f, -base));
         sum += __shfl_xor(sum, 32);
         if (lane < 32) joined[wm * S::BN + (wn * S::NI + j) * 32 + lane] = make_float2(top, sum);
     }
@@ -147,7 +171,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
             const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
             a = make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
         }
-        if (n0 + i < H.size) part[(blockIdx.x % tiles_v) * H.size + n0 + i] = a;
+        if (n0 + i < H.size) part[mi * H.size + n0 + i] = a;
     }
 }
 
@@ -221,68 +245,168 @@ __global__ void __launch_bounds__(256) k_xent_inv(const int64_t *labels, int64_t
 
 // dz of one piece of the vocabulary (W: the piece), a row of words per token
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, int tiles_v, const int32_t *exps, const int64_t *labels, int64_t v0, int64_t vocab,
-                                                        const float *lse, uint16_t *dz, const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
+                                                        int64_t vocab, const float *lse, uint16_t *dz, const uint16_t *zeros)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN;
+    uint32_t mi, ni;
+    tile_place(blockIdx.x, tiles_v, tiles_t, mi, ni);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
-    const float f = kLog2e * unscale<KIND>(exps, 2), up = (float)(1 << dz_exponent<KIND>());
-    const int64_t width = row_numbers<KIND>(W.size), ld = row_words<KIND>(W.size);
-    for_each<S>(acc, [&](int dm, int dn, float raw) {
-        const int64_t v = m0 + dm, row = n0 + dn;
-        if (v >= width || row >= H.size) return;
-        float g = 0.f;
-        if (v < W.size && takes_part(labels, row, vocab)) g = __builtin_amdgcn_exp2f(__builtin_fmaf(raw, f, -lse[row] * kLog2e)) - (v0 + v == labels[row] ? 1.f : 0.f);
-        put<KIND>(dz + row * ld, v, g * up);
-    });
+    const float f = kLog2e * unscale<KIND>(exps, 2), one = (float)(1 << dz_exponent<KIND>());
+    const int limit = W.size - m0 < S::BM ? (int)(W.size - m0) : S::BM;          // of the tile's words, in the vocabulary
+    constexpr int BYTES = KIND == SPLIT ? 4 : 2;
+    const int64_t row_bytes = row_words<KIND>(W.size) * 2;
+    char *corner = (char *)dz + n0 * row_bytes + m0 * BYTES;
+    struct Token { float base; int label; };
+    store_rows<S, BYTES, KIND == SPLIT>(
+        acc, lds,
+        [&](int n) {
+            const int64_t row = n0 + n;
+            Token k = {-INFINITY, -1};                               // takes no part: 2^(0 - infinity) = 0
+            if (row < H.size && takes_part(labels, row, vocab)) {
+                const int64_t at = labels[row] - v0 - m0;
+                k.base = dz_exponent<KIND>() - lse[row] * kLog2e;
+                k.label = at >= 0 && at < S::BM ? (int)at : -1;
+            }
+            return k;
+        },
+        [&](const Token &k, int m, const float (&z)[4]) {
+            float g[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                g[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, k.base));
+                if (m + e == k.label) g[e] -= one;
+            }
+            if (limit < S::BM) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (m + e >= limit) g[e] = 0.f;
+            }
+            return pack_words<KIND>(g);
+        },
+        [&](int n, int at, u32x4 w) {
+            if (n0 + n < H.size && m0 * BYTES + at < row_bytes) *(u32x4 *)(corner + n * row_bytes + at) = w;
+        });
 }
 
-// dW of one worker and piece
-template <class S, int KIND, int T>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, int tiles_v, const int32_t *exps, const float *inv,
-                                                        typename TypeOf<T>::type *dw, Rows ds, int accumulate, const uint16_t *zeros)
+// dW of one worker and piece.  ADD: to what is there, as 32-bit numbers.
+template <class S, int KIND, int T, bool ADD>
+__global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, uint32_t tiles_d, uint32_t tiles_v,
+                                                        const int32_t *exps, const float *inv, typename TypeOf<T>::type *dw, Rows ds, const uint16_t *zeros)
 {
+    typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    const int64_t m0 = (int64_t)(blockIdx.x % tiles_v) * S::BM, n0 = (int64_t)(blockIdx.x / tiles_v) * S::BN, worker = blockIdx.y;
+    uint32_t mi, ni;
+    tile_place(blockIdx.x, tiles_d, tiles_v, mi, ni);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN, worker = blockIdx.y;
     const int64_t ldz = row_words<KIND>(piece), ldh = row_words<KIND>(dim);
     const Operand Z{dz + worker * t * ldz, ldz, piece}, H{h + worker * t * ldh, ldh, dim};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, true, true>(acc, Z, m0, H, n0, 0, t, zeros, lds);
+    tile_product<S, KIND, true, true>(acc, H, m0, Z, n0, 0, t, zeros, lds);
     const float f = inv[worker] / (float)(1 << dz_exponent<KIND>()), fh = unscale<KIND>(exps, 0);       // apart: together they may be too small
-    typename TypeOf<T>::type *out = dw + worker * ds.worker;
-    for_each<S>(acc, [&](int dm, int dn, float raw) {
-        const int64_t v = m0 + dm, i = n0 + dn;
-        if (v >= piece || i >= dim) return;
-        typename TypeOf<T>::type *o = out + v * ds.row + i;
-        const float value = raw * f * fh;
-        *o = (typename TypeOf<T>::type)(accumulate ? (float)*o + value : value);
-    });
+    E *out = dw + worker * ds.worker + n0 * ds.row;
+    typedef typename std::conditional<ADD, float, E>::type Staged;
+    store_rows<S, sizeof(Staged), false>(
+        acc, lds, [](int) { return 0; },
+        [&](int, int, const float (&v)[4]) {
+            const float r[4] = {v[0] * f * fh, v[1] * f * fh, v[2] * f * fh, v[3] * f * fh};
+            return pack_numbers<Staged>(r);
+        },
+        [&](int n, int at, u32x4 w) {
+            const int64_t i = m0 + at / (int)sizeof(Staged);
+            if (n0 + n >= piece || i >= dim) return;
+            E *row = out + n * ds.row;
+            if constexpr (ADD) {
+                float v[4];
+                __builtin_memcpy(v, &w, 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < dim) row[i + e] = (E)((float)row[i + e] + v[e]);
+            } else {
+                store_numbers(row, i, dim, w);
+            }
+        });
 }
 
-// dh over one piece, added to that of the pieces before; the last piece's call hands the sums over
-template <class S, int KIND, int T>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, int64_t t, int tiles_n, int first, int last,
-                                                        const int32_t *exps, const float *inv, float *sums, typename TypeOf<T>::type *dh, Rows ds, const uint16_t *zeros)
+// dh over one piece, its vocabulary cut into gridDim.y parts; a part's sums are added to those of the pieces before.  part: [parts][rows][pitch]
+template <class S, int KIND>
+__global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
+                                                        int64_t pitch, const uint16_t *zeros)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * S::BM, n0 = (int64_t)(blockIdx.x % tiles_n) * S::BN;
+    uint32_t mi, ni;
+    tile_place(blockIdx.x, tiles_d, tiles_t, mi, ni);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+    const int64_t steps = (piece + tile_k<KIND>() - 1) / tile_k<KIND>();
+    const int64_t lo = steps * blockIdx.y / gridDim.y * tile_k<KIND>(), hi = steps * (blockIdx.y + 1) / gridDim.y * tile_k<KIND>();
     const Operand Z{dz, row_words<KIND>(piece), rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, false, true>(acc, Z, m0, W, n0, 0, piece, zeros, lds);
-    const float f = 1.f / (float)(1 << dz_exponent<KIND>()), fw = unscale<KIND>(exps, 1);
-    for_each<S>(acc, [&](int dm, int dn, float raw) {
-        const int64_t row = m0 + dm, i = n0 + dn;
-        if (row >= rows || i >= W.size) return;
-        float v = raw;
-        if (!first) v += sums[row * W.size + i];
-        if (!last) sums[row * W.size + i] = v;
-        else dh[row / t * ds.worker + row % t * ds.row + i] = (typename TypeOf<T>::type)(v * (f * inv[row / t]) * fw);
-    });
+    tile_product<S, KIND, true, false>(acc, W, m0, Z, n0, lo, (hi < piece ? hi : piece) - lo, zeros, lds);
+    float *out = part + (blockIdx.y * rows + n0) * pitch + m0;
+    store_rows<S, 4, false>(acc, lds, [](int) { return 0; }, [](int, int, const float (&v)[4]) { return pack_numbers<float>(v); },
+                            [&](int n, int at, u32x4 w) {
+                                if (n0 + n >= rows || m0 + at / 4 >= pitch) return;
+                                float *o = out + n * pitch + at / 4, v[4];
+                                __builtin_memcpy(v, &w, 16);
+                                const float4 was = first ? make_float4(0.f, 0.f, 0.f, 0.f) : *(const float4 *)o;
+                                *(float4 *)o = make_float4(was.x + v[0], was.y + v[1], was.z + v[2], was.w + v[3]);
+                            });
+}
+
+// joins the parts, in ascending order; a wavefront per row
+template <int KIND, int T>
+__global__ void __launch_bounds__(256) k_xent_dh_join(const float *part, int parts, int64_t rows, int64_t pitch, int64_t t, int64_t dim, const int32_t *exps, const float *inv,
+                                                      typename TypeOf<T>::type *dh, Rows ds)
+{
+    const int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const float f = inv[row / t] / (float)(1 << dz_exponent<KIND>()), fw = unscale<KIND>(exps, 1);       // apart: together they may be too small
+    typename TypeOf<T>::type *out = dh + row / t * ds.worker + row % t * ds.row;
+    constexpr int N = kPiece<T>;
+    for (int64_t i = (threadIdx.x & 63) * N; i < dim; i += 64 * N) {
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = 0.f;
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            const float *at = part + (p * rows + row) * pitch + i;
+#pragma unroll
+            for (int e = 0; e < N; e += 4) {
+                const float4 a = i + e < pitch ? *(const float4 *)(at + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[e] += a.x; v[e + 1] += a.y; v[e + 2] += a.z; v[e + 3] += a.w;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = v[e] * f * fw;
+        store_piece<T>(out, i, dim, v);
+    }
+}
+
+// calls f with the tile for a product of so many numbers: the largest of which there are about as many as CUs
+template <typename F>
+static void by_tiles(int64_t batch, int64_t m, int64_t n, F f)
+{
+    auto count = [&](int64_t size) { return batch * ((m + size - 1) / size) * ((n + size - 1) / size); };
+    if (count(256) >= kFillTiles) f(Large());
+    else f(Middle());
+}
+
+static int64_t dh_pitch(int64_t dim) { return (dim + 3) / 4 * 4; }
+
+// parts that the vocabulary is cut into for dh: until there are two tiles of 128 for every CU, each with 8 steps at least
+static int64_t dh_parts(int64_t rows, int64_t dim, int64_t piece)
+{
+    const int64_t tiles = ((rows + 127) / 128) * ((dim + 127) / 128), room = kPartBytes / (rows * dh_pitch(dim) * 4 + 1);
+    int64_t parts = (512 + tiles - 1) / tiles;
+    if (parts > kMaxSplit) parts = kMaxSplit;
+    if (parts > (piece + 511) / 512) parts = (piece + 511) / 512;
+    if (parts > room) parts = room;
+    return parts < 1 ? 1 : parts;
 }
 
 // W and H as operands; packed where the tensors themselves are not fit to be loaded from (or hold rows to be left out)
@@ -321,16 +445,20 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
 {
     constexpr int KIND = kind_of<T>();
     typedef typename TypeOf<T>::type E;
-    typedef XentShape S;
     const int64_t rows = c->n * t;
     float *token = c->scratch.at<float>(c->token);
     if (rows) {
         Operand H, W;
         SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, &H, &W)));
         float2 *part = c->scratch.at<float2>(c->part);
-        const int64_t tv = (c->vocab + S::BM - 1) / S::BM, tn = (rows + S::BN - 1) / S::BN;
-        hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3((unsigned)(tv * tn)), dim3(S::THREADS), 0, c->stream, W, H, c->dim, (int)tv, c->scratch.at<int32_t>(c->exps), part,
-                           c->scratch.at<uint16_t>(c->zeros));
+        uint32_t tv = 0;
+        by_tiles(1, c->vocab, rows, [&](auto shape) {
+            typedef decltype(shape) S;
+            tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
+            const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), part,
+                               c->scratch.at<uint16_t>(c->zeros));
+        });
         hipLaunchKernelGGL(k_xent_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)tv, (const E *)h, hs, (const E *)w, w_row, labels, t, rows, c->dim,
                            c->vocab, lse, token);
     }
@@ -345,7 +473,6 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
 {
     constexpr int KIND = kind_of<T>();
     typedef typename TypeOf<T>::type E;
-    typedef XentShape S;
     const int64_t rows = c->n * t;
     float *inv = c->scratch.at<float>(c->inv);
     const int32_t *exps = c->scratch.at<int32_t>(c->exps);
@@ -354,23 +481,40 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
     hipLaunchKernelGGL(k_xent_inv, dim3((unsigned)c->n), dim3(256), 0, c->stream, labels, t, c->vocab, grad, inv);
     Operand H{c->scratch.at<uint16_t>(c->h), row_words<KIND>(c->dim), 0}, W{c->scratch.at<uint16_t>(c->w), row_words<KIND>(c->dim), c->vocab};
     if (rows) SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, &H, &W)));
+    float *part = c->scratch.at<float>(c->dh);
+    const int64_t parts = rows ? dh_parts(rows, c->dim, c->piece) : 0, pitch = dh_pitch(c->dim);
     for (int64_t v0 = 0; v0 < c->vocab; v0 += c->piece) {
         const int64_t piece = c->vocab - v0 < c->piece ? c->vocab - v0 : c->piece;
         const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
-        const int64_t tv = (piece + S::BM - 1) / S::BM, tr = (rows + S::BN - 1) / S::BN, td = (c->dim + S::BN - 1) / S::BN;
         if (rows)
-            hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3((unsigned)(tv * tr)), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, (int)tv, exps, labels, v0, c->vocab, lse, dz, zeros);
-        auto weight = [&](auto kernel, auto *out) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(tv * td), (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, (int)tv, exps, inv, out + v0 * dws.row, dws,
-                               accumulate, zeros);
-        };
-        if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32>, (float *)dw);
-        else weight(k_xent_dw<S, KIND, T>, (E *)dw);
+            by_tiles(1, piece, rows, [&](auto shape) {
+                typedef decltype(shape) S;
+                const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
+                hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, labels, v0, c->vocab, lse, dz, zeros);
+            });
+        by_tiles(c->n, c->dim, piece, [&](auto shape) {
+            typedef decltype(shape) S;
+            const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
+            auto weight = [&](auto kernel, auto *out) {
+                hipLaunchKernelGGL(kernel, dim3(td * tv, (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws, zeros);
+            };
+            if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
+            else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
+            else if (accumulate) weight(k_xent_dw<S, KIND, T, true>, (E *)dw);
+            else weight(k_xent_dw<S, KIND, T, false>, (E *)dw);
+        });
         if (rows)
-            hipLaunchKernelGGL((k_xent_dh<S, KIND, T>), dim3((unsigned)(tr * td)), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, t, (int)td, v0 == 0,
-                               v0 + piece == c->vocab, exps, inv, c->scratch.at<float>(c->dh), (E *)dh, dhs, zeros);
+            by_tiles(parts, c->dim, rows, [&](auto shape) {
+                typedef decltype(shape) S;
+                const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
+                hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt, (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt, v0 == 0,
+                                   part, pitch, zeros);
+            });
         SAMS_HIP(hipGetLastError());
     }
+    if (rows)
+        hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)parts, rows, pitch, t, c->dim, exps, inv, (E *)dh, dhs);
+    SAMS_HIP(hipGetLastError());
     return SAMS_OK;
 }
 
@@ -401,7 +545,7 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     const int64_t rows = n * t_max, ld = type == SAMS_F32 ? row_words<SPLIT>(dim) : row_words<F16>(dim);
     c->h = c->scratch.reserve(rows * ld * 2);
     c->w = c->scratch.reserve(vocab * ld * 2);
-    c->part = c->scratch.reserve(rows * ((vocab + XentShape::BM - 1) / XentShape::BM) * 8);
+    c->part = c->scratch.reserve(rows * ((vocab + Middle::BM - 1) / Middle::BM) * 8);
     c->token = c->scratch.reserve(rows * 4);
     c->inv = c->scratch.reserve(n * 4);
     c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
@@ -413,7 +557,8 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
         if (c->piece < 1024) c->piece = 1024;
         if (c->piece > whole) c->piece = whole;
         c->dz = c->scratch.reserve(rows * c->piece * row_bytes);
-        c->dh = c->scratch.reserve(rows * dim * 4);
+        // for fewer tokens there may be more parts, in as much memory
+        c->dh = c->scratch.reserve(std::max(rows * dh_pitch(dim) * 4, std::min(kPartBytes, rows * dh_pitch(dim) * 4 * kMaxSplit)));
     }
     int rc = c->scratch.take();
     if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->zeros), 64, 0u);
