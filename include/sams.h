@@ -403,8 +403,8 @@ int layer_norm_backward(sams_norm *ctx, int64_t t, const void *dy, int64_t dy_wo
  * 16-bit tensors are multiplied as they are, and dz is held as numbers of their type between the products (so dw and dh carry
  * its rounding whatever dw_type); 32-bit ones to 22 bits of mantissa, of numbers below 2^-17 of the tensor's largest fewer.
  * train == 0 at creation: the forward pass only, and less scratch (backward then returns SAMS_EINVAL).
- * Scratch: copies of h and w; 8 bytes per token and 128 words of the vocabulary; for training the dz of one piece of the vocabulary
- * (about 256 MiB, or the whole of a smaller one; at least 1024 words per token) and up to 256 MiB, or 4*dim bytes per token, of partial sums of dh.
+ * Scratch: copies of h and w; 8 bytes per token and 64 words of the vocabulary; for training the dz of one piece of the vocabulary
+ * (up to 1 GiB, or 1024 words per token if that is more) and up to 256 MiB, or 4*dim bytes per token, of partial sums of dh.
  */
 int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int64_t vocab, int32_t type, int32_t train,
                      void *hip_stream);

@@ -1,6 +1,9 @@
 // Products of 16-bit matrices on the matrix cores: C[m][n] = sum_k A(m, k) B(n, k) for one tile of C per workgroup, with
 // 32-bit accumulators that stay in registers for whatever the kernel does with its tile.
 #pragma once
+#include <math.h>
+#include <algorithm>
+
 #include "sams_ctx.h"
 
 namespace sams {
@@ -20,7 +23,7 @@ enum Kind { BF16 = 0, F16 = 1, SPLIT = 2 };
 // One operand.  K_ROWS false: row m (or n) has its k's next to each other; true: a row holds one k of all m (or n).
 struct Operand {
     const uint16_t *p;
-    int64_t ld;         // words from row to row, a multiple of 8
+    int64_t ld;         // words from row to row, a multiple of 8, at most kMaxRowWords
     int64_t size;       // extent along m (or n), in numbers
 };
 
@@ -50,49 +53,68 @@ __device__ __forceinline__ int swizzle_k(int k) { return ((k & 3) << 2) | (k & 2
 
 template <int KIND> __host__ __device__ constexpr int tile_k() { return KIND == SPLIT ? 32 : 64; }      // numbers of k in a stage
 
-// Loads of one operand's tile straight into LDS, 64 words of k (32 numbers of k where they are split) a stage.
+// Loads of one operand's tile straight into LDS, 64 words of k (32 numbers of k where they are split) a stage.  They are buffer loads: an
+// address that all threads share and moves on, each thread's distances from it, and zeros for a distance past kTileSpan, which rows and
+// k's that do not exist are given.
+constexpr uint32_t kTileSpan = 0x80000000u;
+constexpr int64_t kMaxRowWords = 1 << 22;                           // a tile (256 rows, or 64 k's) spans less than that
+
+// a number that all lanes share, as the instructions that want it in a scalar register need it
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// 16 bytes a lane from a buffer, to LDS from address `at` on, lane by lane.  No register is written, so nothing can be overwritten while
+// it is under way.  Written out because the compiler waits for every such load of its own before it lets a transposing read go
+// ahead (also of the stage that landed long ago): those who read the stage wait for it, in wait_and_meet.
+__device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t off, uint32_t at)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(buffer), "s"(at) : "memory");
+}
+
 template <int ROWS, int THREADS, int KIND, bool K_ROWS>
 struct Loader {
     static constexpr int N = ROWS * 8 / THREADS;                    // 16-byte pieces a thread brings
     static constexpr int PIECES = K_ROWS ? (KIND == SPLIT ? ROWS / 4 : ROWS / 8) : 8;       // of a row of the tile
-    const uint16_t *p[N];
-    int kpos[N];                                                    // where a piece starts, in k
+    const char *base;
+    uint32_t off[N];
     int64_t step;
+
+    __device__ __forceinline__ static int row_of(int i, int tid) { return (i * THREADS + tid) / PIECES; }
+    __device__ __forceinline__ static int piece_of(int i, int tid)
+    {
+        const int row = row_of(i, tid), c = (i * THREADS + tid) % PIECES;
+        return K_ROWS ? c ^ (swizzle_k(row) & (PIECES - 1)) : c ^ swizzle(row);
+    }
+    // where a piece starts, in k
+    __device__ __forceinline__ static int k_of(int i, int tid) { return K_ROWS ? row_of(i, tid) : (KIND == SPLIT ? piece_of(i, tid) & 3 : piece_of(i, tid)) * 8; }
 
     __device__ __forceinline__ void init(const Operand &op, int64_t first, int64_t k_first, int tid)
     {
+        const int64_t wide = KIND == SPLIT ? 2 : 1;
+        if constexpr (K_ROWS) base = (const char *)(op.p + k_first * op.ld + first * wide);
+        else base = (const char *)(op.p + first * op.ld + k_first * wide);
+        const int64_t words = (KIND == SPLIT ? (op.size + 31) / 32 * 64 : (op.size + 7) / 8 * 8) - first * wide;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int slot = i * THREADS + tid;
-            const int row = slot / PIECES;
-            if constexpr (K_ROWS) {
-                const int c = (slot % PIECES) ^ (swizzle_k(row) & (PIECES - 1));
-                const int64_t words = KIND == SPLIT ? (op.size + 31) / 32 * 64 : (op.size + 7) / 8 * 8;
-                int64_t w = (KIND == SPLIT ? 2 * first : first) + c * 8;
-                if (w >= words) w = 0;                              // columns that no output asks for
-                p[i] = op.p + (k_first + row) * op.ld + w;
-                kpos[i] = row;
-            } else {
-                const int c = (slot % PIECES) ^ swizzle(row);
-                int64_t r = first + row;
-                if (r >= op.size) r = op.size - 1;                  // rows that no output asks for
-                p[i] = op.p + r * op.ld + (KIND == SPLIT ? 2 * k_first : k_first) + c * 8;
-                kpos[i] = KIND == SPLIT ? (c & 3) * 8 : c * 8;
-            }
+            const int row = row_of(i, tid), c = piece_of(i, tid);
+            const bool there = K_ROWS ? c * 8 < words : row < op.size - first;
+            off[i] = there ? (uint32_t)(row * (uint32_t)op.ld * 2 + c * 16) : kTileSpan;
         }
-        step = K_ROWS ? tile_k<KIND>() * op.ld : 64;
+        step = K_ROWS ? tile_k<KIND>() * op.ld * 2 : 128;
     }
 
-    // left: k's from the start of this stage on; a piece past them is read from the zeros
-    __device__ __forceinline__ void load(char *lds, int wave, const uint16_t *zeros, int64_t left)
+    // left: k's from the start of this stage on
+    __device__ __forceinline__ void load(char *lds, int wave, int tid, int left)
     {
+        if (left < tile_k<KIND>()) {                                 // the last stage
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint16_t *src = kpos[i] < left ? p[i] : zeros;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t *)src,
-                                             (__attribute__((address_space(3))) uint32_t *)(lds + (i * THREADS + wave * 64) * 16), 16, 0, 0);
-            p[i] += step;
+            for (int i = 0; i < N; ++i)
+                if (k_of(i, tid) >= left) off[i] = kTileSpan;
         }
+        const u32x4 buffer = {uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffff), kTileSpan, 0x00020000};
+        const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_to_lds(buffer, off[i], uniform(at + i * THREADS * 16));
+        base += step;
     }
 };
 
@@ -128,71 +150,82 @@ __device__ __forceinline__ void wait_and_meet()
 }
 
 // acc += the tile's product over k numbers from k_first on.  `lds`: S::LDS_BYTES, 16-byte aligned; every thread of the workgroup
-// calls it, and LDS is free again when it returns.  Pieces past k come from `zeros` (16 bytes of them).
+// calls it, and LDS is free again when it returns.
+//
+// A wavefront has the fragments of the next 16 k's on their way while the matrix instructions of these run, across stages too: the
+// one barrier of a stage stands before its last fragments are used, when they are in registers and the next stage has
+// landed; behind it the stage just read is filled anew.
 template <class S, int KIND, bool A_K_ROWS, bool B_K_ROWS>
 __device__ __forceinline__ void tile_product(f32x16 (&acc)[S::MI][S::NI], const Operand &A, int64_t m0, const Operand &B, int64_t n0, int64_t k_first,
-                                             int64_t k, const uint16_t *zeros, char *lds)
+                                             int64_t k, char *lds)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
-    constexpr int BK = tile_k<KIND>(), STAGE = S::A_BYTES + S::B_BYTES;
+    constexpr int BK = tile_k<KIND>(), STAGE = S::A_BYTES + S::B_BYTES, HALVES = KIND == SPLIT ? 2 : 1, GROUPS = BK / 16;
     typedef Loader<S::BM, S::THREADS, KIND, A_K_ROWS> LA;
     typedef Loader<S::BN, S::THREADS, KIND, B_K_ROWS> LB;
     LA la;
     LB lb;
     la.init(A, m0, k_first, tid);
     lb.init(B, n0, k_first, tid);
-    const int64_t steps = (k + BK - 1) / BK;
-    int64_t left = k;
-#pragma unroll
-    for (int s = 0; s < S::STAGES - 1; ++s) {
-        la.load(lds + s * STAGE, wave, zeros, left);
-        lb.load(lds + s * STAGE + S::A_BYTES, wave, zeros, left);
+    int left = (int)k;
+    auto fetch = [&](char *to) {
+        la.load(to, wave, tid, left);
+        lb.load(to + S::A_BYTES, wave, tid, left);
         left -= BK;
-    }
-    int cur = 0, nxt = S::STAGES - 1;
-    for (int64_t s = 0; s < steps; ++s) {
-        wait_and_meet<(S::STAGES - 2) * (LA::N + LB::N)>();
-        la.load(lds + nxt * STAGE, wave, zeros, left);
-        lb.load(lds + nxt * STAGE + S::A_BYTES, wave, zeros, left);
-        left -= BK;
-        const char *ta = lds + cur * STAGE, *tb = ta + S::A_BYTES;
-        if constexpr (KIND != SPLIT) {
+    };
+    if (k <= 0) return;
+    u32x4 fa[2][HALVES][S::MI], fb[2][HALVES][S::NI];
+    auto read = [&](const char *stage, int group, int into) {
 #pragma unroll
-            for (int ks = 0; ks < 64; ks += 16) {
-                u32x4 a[S::MI], b[S::NI];
+        for (int h = 0; h < HALVES; ++h) {
 #pragma unroll
-                for (int i = 0; i < S::MI; ++i) a[i] = fragment<S::BM, KIND, A_K_ROWS>(ta, wm + i * 32, ks, 0, lane);
+            for (int i = 0; i < S::MI; ++i) fa[into][h][i] = fragment<S::BM, KIND, A_K_ROWS>(stage, wm + i * 32, group * 16, h, lane);
 #pragma unroll
-                for (int j = 0; j < S::NI; ++j) b[j] = fragment<S::BN, KIND, B_K_ROWS>(tb, wn + j * 32, ks, 0, lane);
-#pragma unroll
-                for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                    for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(a[i], b[j], acc[i][j]);
-            }
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < 32; ks += 16) {
-                u32x4 a[2][S::MI], b[2][S::NI];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (int i = 0; i < S::MI; ++i) a[h][i] = fragment<S::BM, KIND, A_K_ROWS>(ta, wm + i * 32, ks, h, lane);
-#pragma unroll
-                    for (int j = 0; j < S::NI; ++j) b[h][j] = fragment<S::BN, KIND, B_K_ROWS>(tb, wn + j * 32, ks, h, lane);
-                }
-#pragma unroll
-                for (int q = 0; q < 3; ++q)
-#pragma unroll
-                    for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                        for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(a[q == 2][i], b[q == 1][j], acc[i][j]);
-            }
+            for (int j = 0; j < S::NI; ++j) fb[into][h][j] = fragment<S::BN, KIND, B_K_ROWS>(stage + S::A_BYTES, wn + j * 32, group * 16, h, lane);
         }
-        cur = cur + 1 == S::STAGES ? 0 : cur + 1;
-        nxt = nxt + 1 == S::STAGES ? 0 : nxt + 1;
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int q = 0; q < (KIND == SPLIT ? 3 : 1); ++q)
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(fa[from][q == 2 ? HALVES - 1 : 0][i], fb[from][q == 1 ? HALVES - 1 : 0][j], acc[i][j]);
+    };
+    // the order of a group's instructions: after each matrix instruction a share of the reads, which LDS then serves in its shadow
+    auto interleave = [&]() {
+        constexpr int PRODUCTS = S::MI * S::NI * (KIND == SPLIT ? 3 : 1), READS = HALVES * (S::MI * (A_K_ROWS ? 2 : 1) + S::NI * (B_K_ROWS ? 2 : 1));
+        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+        for (int p = 0; p < PRODUCTS; ++p) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int AHEAD = (S::STAGES - 2) * (LA::N + LB::N);         // loads that may be under way when the next stage is read
+#pragma unroll
+    for (int s = 0; s < S::STAGES; ++s) fetch(lds + s * STAGE);      // past k: zeros, so that the count holds
+    wait_and_meet<AHEAD + LA::N + LB::N>();
+    char *cur = lds, *nxt = lds + STAGE, *const end = lds + S::STAGES * STAGE;
+    read(cur, 0, 0);
+    for (int todo = (int)k; todo > 0; todo -= BK) {
+#pragma unroll
+        for (int g = 0; g + 1 < GROUPS; ++g) {
+            read(cur, g + 1, (g + 1) & 1);
+            multiply(g & 1);
+            interleave();
+        }
+        wait_and_meet<AHEAD>();
+        if (S::STAGES > 2 || left > 0) fetch(cur);
+        read(nxt, 0, 0);                                             // after the last stage: what nobody uses
+        multiply((GROUPS - 1) & 1);
+        interleave();
+        cur = nxt;
+        nxt = nxt + STAGE == end ? lds : nxt + STAGE;
     }
-    wait_and_meet<0>();
+    if constexpr (S::STAGES > 2) wait_and_meet<0>();
 }
 
 template <class S>
@@ -415,11 +448,51 @@ __device__ __forceinline__ void put(uint16_t *row, int64_t i, float v)
     }
 }
 
-// The tiles in use.  Large: 128 x 64 numbers a wavefront, 128 KB of LDS, one workgroup a CU; 1.1 PFLOP/s at 8192^3 in 16 bits (400 TFLOP/s of
-// pairs), against 0.9 (340) of Middle, two of which share a CU, and 0.6 (270) of Small, which takes the fewest numbers to fill the chip.
+// The tiles in use.  At 8192^3 (16 bits; pairs), Large reaches 1.27 PFLOP/s (0.45), 83 % of the library's 1.54 in 16 bits and three times
+// its 0.15 in 32, the card's clock down to 1.85 GHz (1.55) by then; Middle 1.1 (0.40), two workgroups on a CU; Small 0.65 (0.29).  Small's four
+// stages cover a load's way where a CU has one workgroup: 640 x 640 x 12800 takes it 56 us (92), with two stages 95 (186), Middle 134 (267).
 typedef Shape<256, 256, 2, 4, 2> Large;
 typedef Shape<128, 128, 2, 2, 2> Middle;
-typedef Shape<64, 64, 2, 2, 2> Small;
+typedef Shape<64, 64, 2, 2, 4> Small;
+
+// What a product of m x n x k numbers, `batch` times, is estimated to take in tiles of a size (1 Large, 2 Middle, 3 Small), its k cut into
+// `parts`, in ns: a CU's workgroups one after the other, each at the pace it has beside others or, alone on its CU, by itself
+// (measured as above), and what a tile costs before and after its k's.
+struct TileCost { int size; double pace16, alone16, pace_pairs, alone_pairs, fixed; };
+constexpr TileCost kTileCosts[3] = {{256, 26, 26, 75, 75, 5000}, {128, 7.5, 10.5, 21.4, 21.4, 1700}, {64, 3.0, 4.4, 6.9, 7.2, 700}};
+
+static inline double tile_estimate(int shape, bool pairs, double tiles, double k, int parts)
+{
+    const TileCost &c = kTileCosts[shape - 1];
+    const double rounds = ceil(tiles * parts / 256), each = k / parts;
+    return std::max(rounds * (pairs ? c.pace_pairs : c.pace16), pairs ? c.alone_pairs : c.alone16) * each + rounds * c.fixed;
+}
+
+struct TileChoice { int shape, parts; };
+
+// part_ns: what another part costs (its sums are written and read once more); triangular: tiles on and under the diagonal only
+static inline TileChoice choose_tiles(bool pairs, int64_t batch, int64_t m, int64_t n, bool triangular, int64_t k, int most_parts, double part_ns)
+{
+    TileChoice best{2, 1};
+    double least = 1e30;
+    for (int shape = 1; shape <= 3; ++shape) {
+        const int64_t size = kTileCosts[shape - 1].size, a = (m + size - 1) / size, b = (n + size - 1) / size;
+        const double tiles = (double)batch * (triangular ? a * (a + 1) / 2 : a * b);
+        for (int parts = 1; parts <= most_parts; ++parts) {
+            const double ns = tile_estimate(shape, pairs, tiles, (double)k, parts) + (most_parts > 1 ? parts * part_ns : 0.0);
+            if (ns < least) { least = ns; best = TileChoice{shape, parts}; }
+        }
+    }
+    return best;
+}
+
+template <typename F>
+static void with_tile(int shape, F f)
+{
+    if (shape == 1) f(Large());
+    else if (shape == 2) f(Middle());
+    else f(Small());
+}
 
 // words of a row of `numbers` numbers: whole 128-byte lines
 template <int KIND> __host__ __device__ constexpr int64_t row_words(int64_t numbers)

@@ -22,7 +22,7 @@ struct sams_ortho {
     int32_t type;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t x[2], gram, poly, scale, part, update, zeros;       // offsets in the scratch
+    int64_t x[2], gram, poly, scale, part, update;       // offsets in the scratch
 };
 
 namespace sams {
@@ -30,7 +30,6 @@ namespace sams {
 using namespace gemm;
 
 constexpr int kNormSlices = 512;        // of a matrix, for the sum of its squares
-constexpr int64_t kFillTiles = 192;     // tiles that make a tile's size worth it: three for every four CUs
 
 struct OrthoScale {
     float sigma, sigma2;                // what the words of G still have to be multiplied by, and its square
@@ -172,7 +171,7 @@ __device__ __forceinline__ void put_symmetric(uint16_t *o, int64_t ld, int64_t s
 
 // A = X X' (X' X where X is tall), times f and, in the first step, sigma^2
 template <class S, int KIND, bool TALL>
-__global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram, const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     int ti, tj;
@@ -181,7 +180,7 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, Or
     const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, 0, TALL ? d.rows : d.cols, zeros, lds);
+    tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, 0, TALL ? d.rows : d.cols, lds);
     if (scale) f *= scale[blockIdx.y].sigma2;
     put_symmetric<S, KIND>(gram + blockIdx.y * d.small * ldg, ldg, d.small, m0, n0, acc, lds, [&](int64_t, int64_t, float (&v)[8]) {
 #pragma unroll
@@ -191,7 +190,7 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, Or
 
 // P = a I + b A + c A A
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram, OrthoDims d, float a, float b, float c, uint16_t *poly, const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram, OrthoDims d, float a, float b, float c, uint16_t *poly)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     int ti, tj;
@@ -200,7 +199,7 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram,
     const Operand A{gram + blockIdx.y * d.small * ld, ld, d.small};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, false, false>(acc, A, m0, A, n0, 0, d.small, zeros, lds);
+    tile_product<S, KIND, false, false>(acc, A, m0, A, n0, 0, d.small, lds);
     put_symmetric<S, KIND>(poly + blockIdx.y * d.small * ld, ld, d.small, m0, n0, acc, lds, [&](int64_t row, int64_t col, float (&v)[8]) {
         float g[8];
         get8<KIND>(A.p + row * ld, col, g);
@@ -221,7 +220,7 @@ struct OrthoOut {
 // X' = P X (X P where X is tall), times f and, in the first step, sigma; LAST: to the caller (T: its type; with parameters f32)
 template <class S, int KIND, bool TALL, bool LAST, int T>
 __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, uint32_t tiles_m, uint32_t tiles_n, float f,
-                                                            const OrthoScale *scale, uint16_t *next, OrthoOut o, const uint16_t *zeros)
+                                                            const OrthoScale *scale, uint16_t *next, OrthoOut o)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni;
@@ -231,8 +230,8 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
     const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.rows : d.cols}, P{poly + blockIdx.y * d.small * ldp, ldp, d.small};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    if constexpr (TALL) tile_product<S, KIND, false, false>(acc, P, m0, X, n0, 0, d.small, zeros, lds);
-    else tile_product<S, KIND, true, false>(acc, X, m0, P, n0, 0, d.small, zeros, lds);
+    if constexpr (TALL) tile_product<S, KIND, false, false>(acc, P, m0, X, n0, 0, d.small, lds);
+    else tile_product<S, KIND, true, false>(acc, X, m0, P, n0, 0, d.small, lds);
     if (scale) f *= scale[blockIdx.y].sigma;
     const int64_t width = row_numbers<KIND>(d.cols);
     eights<S, false>(acc, lds, [&](int dn, int dm, const float (&raw)[8]) {
@@ -292,27 +291,16 @@ static int word_exponent(double bound)
     return e > 60 ? 60 : e < -60 ? -60 : e;
 }
 
-// calls f with the tile for a product of so many numbers: the largest of which there are about as many as CUs
-template <typename F>
-static void by_tiles(int64_t batch, int64_t m, int64_t n, bool triangular, F f)
-{
-    auto count = [&](int64_t size) {
-        const int64_t a = (m + size - 1) / size, b = (n + size - 1) / size;
-        return batch * (triangular ? a * (a + 1) / 2 : a * b);
-    };
-    if (count(256) >= kFillTiles) f(Large());
-    else if (count(128) >= kFillTiles) f(Middle());
-    else f(Small());
-}
-
 template <int KIND, int T>
 static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *coef, const OrthoOut &o)
 {
     const OrthoDims d{c->rows, c->cols, c->rows < c->cols ? c->rows : c->cols};
     const bool tall = c->rows > c->cols;
     uint16_t *gram = c->scratch.at<uint16_t>(c->gram), *poly = c->scratch.at<uint16_t>(c->poly);
-    const uint16_t *zeros = c->scratch.at<uint16_t>(c->zeros);
     const OrthoScale *scale = c->scratch.at<OrthoScale>(c->scale);
+    const int64_t large = d.rows + d.cols - d.small;
+    const TileChoice square = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, (large + d.small) / 2, 1, 0),
+                     whole = choose_tiles(KIND == SPLIT, batch, d.cols, d.rows, false, d.small, 1, 0);
     double bound = 1.0;                                              // of X's singular values
     int ex = 0;                                                      // words of X = X * 2^ex; the first: X = words * sigma
     for (int s = 0; s < steps; ++s) {
@@ -322,23 +310,23 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *c
         const double after = poly_bound(a, b, cc, u, true);
         const int ea = word_exponent(u), ep = word_exponent(poly_bound(a, b, cc, u, false)), en = word_exponent(after);
         const OrthoScale *first = s == 0 ? scale : nullptr;
-        by_tiles(batch, d.small, d.small, true, [&](auto shape) {
+        with_tile(square.shape, [&](auto shape) {
             typedef decltype(shape) S;
             const int64_t ts = (d.small + S::BM - 1) / S::BM;
             const dim3 grid((unsigned)(ts * (ts + 1) / 2), (unsigned)batch);
             const float f = (float)ldexp(1.0, ea - 2 * ex);
-            if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram, zeros);
-            else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram, zeros);
+            if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram);
+            else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram);
             hipLaunchKernelGGL((k_ortho_poly<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, gram, d, (float)ldexp(a, ep), (float)ldexp(b, ep - ea), (float)ldexp(cc, ep - 2 * ea),
-                               poly, zeros);
+                               poly);
         });
         const bool last = s + 1 == steps;
         const float f = (float)ldexp(1.0, (last ? 0 : en) - ep - ex);
-        by_tiles(batch, d.cols, d.rows, false, [&](auto shape) {
+        with_tile(whole.shape, [&](auto shape) {
             typedef decltype(shape) S;
             const uint32_t tm = (uint32_t)((d.cols + S::BM - 1) / S::BM), tn = (uint32_t)((d.rows + S::BN - 1) / S::BN);
             auto apply = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, f, first, next, o, zeros);
+                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, f, first, next, o);
             };
             if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
             else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
@@ -393,14 +381,8 @@ int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t col
     c->scale = c->scratch.reserve(batch * (int64_t)sizeof(OrthoScale));
     c->part = c->scratch.reserve(batch * kNormSlices * 8);
     c->update = type == SAMS_F32 ? c->scratch.reserve(batch * rows * cols * 4) : -1;
-    c->zeros = c->scratch.reserve(256);
-    int rc = c->scratch.take();
-    if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->zeros), 64, 0u);
-    if (rc != SAMS_OK) {
-        if (c->scratch.base) (void)hipFree(c->scratch.base);
-        delete c;
-        return rc;
-    }
+    const int rc = c->scratch.take();
+    if (rc != SAMS_OK) { delete c; return rc; }
     *out = c;
     return SAMS_OK;
 }

@@ -25,18 +25,17 @@ struct sams_xent {
     int64_t t_max, dim, vocab, piece;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t h, w, dz, dh, part, token, inv, amax, exps, zeros;
+    int64_t h, w, dz, dh, part, token, inv, amax, exps;
 };
 
 namespace sams {
 
 using namespace gemm;
 
-constexpr int64_t kXentPieceBytes = (int64_t)256 << 20;     // of dz, for one piece of the vocabulary
+constexpr int64_t kXentPieceBytes = (int64_t)1 << 30;        // of dz, for one piece of the vocabulary
 constexpr int kAmaxBlocks = 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
 
-constexpr int64_t kFillTiles = 192;                         // tiles that make a tile's size worth it: three for every four CUs
 constexpr int64_t kPartBytes = (int64_t)256 << 20;          // of partial sums of dh, at most (but one for every token)
 constexpr int kMaxSplit = 64;
 
@@ -124,8 +123,7 @@ __device__ __forceinline__ float unscale(const int32_t *exps, int which)        
 // Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).  A lane holds numbers
 // of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, float2 *part,
-                                                           const uint16_t *zeros)
+__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, float2 *part)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni;
@@ -133,7 +131,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
+    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
     const float f = kLog2e * unscale<KIND>(exps, 2);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
     if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
@@ -246,7 +244,7 @@ __global__ void __launch_bounds__(256) k_xent_inv(const int64_t *labels, int64_t
 // dz of one piece of the vocabulary (W: the piece), a row of words per token
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
-                                                        int64_t vocab, const float *lse, uint16_t *dz, const uint16_t *zeros)
+                                                        int64_t vocab, const float *lse, uint16_t *dz)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni;
@@ -254,7 +252,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, zeros, lds);
+    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
     const float f = kLog2e * unscale<KIND>(exps, 2), one = (float)(1 << dz_exponent<KIND>());
     const int limit = W.size - m0 < S::BM ? (int)(W.size - m0) : S::BM;          // of the tile's words, in the vocabulary
     constexpr int BYTES = KIND == SPLIT ? 4 : 2;
@@ -295,7 +293,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
 // dW of one worker and piece.  ADD: to what is there, as 32-bit numbers.
 template <class S, int KIND, int T, bool ADD>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, uint32_t tiles_d, uint32_t tiles_v,
-                                                        const int32_t *exps, const float *inv, typename TypeOf<T>::type *dw, Rows ds, const uint16_t *zeros)
+                                                        const int32_t *exps, const float *inv, typename TypeOf<T>::type *dw, Rows ds)
 {
     typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) char lds[S::LDS_BYTES];
@@ -306,7 +304,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
     const Operand Z{dz + worker * t * ldz, ldz, piece}, H{h + worker * t * ldh, ldh, dim};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, true, true>(acc, H, m0, Z, n0, 0, t, zeros, lds);
+    tile_product<S, KIND, true, true>(acc, H, m0, Z, n0, 0, t, lds);
     const float f = inv[worker] / (float)(1 << dz_exponent<KIND>()), fh = unscale<KIND>(exps, 0);       // apart: together they may be too small
     E *out = dw + worker * ds.worker + n0 * ds.row;
     typedef typename std::conditional<ADD, float, E>::type Staged;
@@ -335,7 +333,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
 // dh over one piece, its vocabulary cut into gridDim.y parts; a part's sums are added to those of the pieces before.  part: [parts][rows][pitch]
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
-                                                        int64_t pitch, const uint16_t *zeros)
+                                                        int64_t pitch)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni;
@@ -346,7 +344,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int6
     const Operand Z{dz, row_words<KIND>(piece), rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
-    tile_product<S, KIND, true, false>(acc, W, m0, Z, n0, lo, (hi < piece ? hi : piece) - lo, zeros, lds);
+    tile_product<S, KIND, true, false>(acc, W, m0, Z, n0, lo, (hi < piece ? hi : piece) - lo, lds);
     float *out = part + (blockIdx.y * rows + n0) * pitch + m0;
     store_rows<S, 4, false>(acc, lds, [](int) { return 0; }, [](int, int, const float (&v)[4]) { return pack_numbers<float>(v); },
                             [&](int n, int at, u32x4 w) {
@@ -387,26 +385,13 @@ __global__ void __launch_bounds__(256) k_xent_dh_join(const float *part, int par
     }
 }
 
-// calls f with the tile for a product of so many numbers: the largest of which there are about as many as CUs
-template <typename F>
-static void by_tiles(int64_t batch, int64_t m, int64_t n, F f)
-{
-    auto count = [&](int64_t size) { return batch * ((m + size - 1) / size) * ((n + size - 1) / size); };
-    if (count(256) >= kFillTiles) f(Large());
-    else f(Middle());
-}
-
 static int64_t dh_pitch(int64_t dim) { return (dim + 3) / 4 * 4; }
 
-// parts that the vocabulary is cut into for dh: until there are two tiles of 128 for every CU, each with 8 steps at least
-static int64_t dh_parts(int64_t rows, int64_t dim, int64_t piece)
+// the tile of dh's product over one piece, and the parts that the vocabulary is cut into for it
+static TileChoice dh_tiles(bool pairs, int64_t rows, int64_t dim, int64_t piece)
 {
-    const int64_t tiles = ((rows + 127) / 128) * ((dim + 127) / 128), room = kPartBytes / (rows * dh_pitch(dim) * 4 + 1);
-    int64_t parts = (512 + tiles - 1) / tiles;
-    if (parts > kMaxSplit) parts = kMaxSplit;
-    if (parts > (piece + 511) / 512) parts = (piece + 511) / 512;
-    if (parts > room) parts = room;
-    return parts < 1 ? 1 : parts;
+    const int64_t bytes = rows * dh_pitch(dim) * 4, room = kPartBytes / bytes, most = std::min<int64_t>(kMaxSplit, (piece + 255) / 256);
+    return choose_tiles(pairs, 1, dim, rows, false, piece, (int)std::max<int64_t>(1, std::min(room, most)), bytes * 2 / 4000.0);      // 4 TB/s
 }
 
 // W and H as operands; packed where the tensors themselves are not fit to be loaded from (or hold rows to be left out)
@@ -419,16 +404,16 @@ static int enqueue_operands(sams_xent *c, int64_t t, const void *h, Rows hs, con
     int32_t *exps = c->scratch.at<int32_t>(c->exps);
     if (KIND == SPLIT)
         hipLaunchKernelGGL(k_xent_amax, dim3(2 * kAmaxBlocks), dim3(256), 0, c->stream, (const float *)h, hs, t, rows, labels, (const float *)w, w_row, c->vocab, c->dim, amax);
-    const bool fit = KIND != SPLIT && c->dim % 8 == 0;
+    auto fit = [&](int64_t row, const void *p) { return KIND != SPLIT && c->dim % 8 == 0 && row % 8 == 0 && row <= kMaxRowWords && aligned16(p); };
     const bool rows_even = c->n == 1 || hs.worker == t * hs.row;
-    if (fit && !clean && rows_even && hs.row % 8 == 0 && aligned16(h)) {
+    if (!clean && rows_even && fit(hs.row, h)) {
         *H = Operand{(const uint16_t *)h, hs.row, rows};
     } else {
         uint16_t *hp = c->scratch.at<uint16_t>(c->h);
         hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3((unsigned)grid_for(rows, 4, 4096)), dim3(256), 0, c->stream, (const E *)h, hs, t, rows, c->dim, labels, c->vocab, amax, exps, hp);
         *H = Operand{hp, row_words<KIND>(c->dim), rows};
     }
-    if (fit && w_row % 8 == 0 && aligned16(w)) {
+    if (fit(w_row, w)) {
         *W = Operand{(const uint16_t *)w, w_row, c->vocab};
     } else {
         uint16_t *wp = c->scratch.at<uint16_t>(c->w);
@@ -452,12 +437,11 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
         SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, &H, &W)));
         float2 *part = c->scratch.at<float2>(c->part);
         uint32_t tv = 0;
-        by_tiles(1, c->vocab, rows, [&](auto shape) {
+        with_tile(choose_tiles(KIND == SPLIT, 1, c->vocab, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
             typedef decltype(shape) S;
             tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
             const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), part,
-                               c->scratch.at<uint16_t>(c->zeros));
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), part);
         });
         hipLaunchKernelGGL(k_xent_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)tv, (const E *)h, hs, (const E *)w, w_row, labels, t, rows, c->dim,
                            c->vocab, lse, token);
@@ -476,27 +460,28 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
     const int64_t rows = c->n * t;
     float *inv = c->scratch.at<float>(c->inv);
     const int32_t *exps = c->scratch.at<int32_t>(c->exps);
-    const uint16_t *zeros = c->scratch.at<uint16_t>(c->zeros);
     uint16_t *dz = c->scratch.at<uint16_t>(c->dz);
     hipLaunchKernelGGL(k_xent_inv, dim3((unsigned)c->n), dim3(256), 0, c->stream, labels, t, c->vocab, grad, inv);
     Operand H{c->scratch.at<uint16_t>(c->h), row_words<KIND>(c->dim), 0}, W{c->scratch.at<uint16_t>(c->w), row_words<KIND>(c->dim), c->vocab};
     if (rows) SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, &H, &W)));
     float *part = c->scratch.at<float>(c->dh);
-    const int64_t parts = rows ? dh_parts(rows, c->dim, c->piece) : 0, pitch = dh_pitch(c->dim);
+    const int64_t pitch = dh_pitch(c->dim);
+    const TileChoice hidden = rows ? dh_tiles(KIND == SPLIT, rows, c->dim, c->piece) : TileChoice{2, 0};
+    const int parts = hidden.parts;
     for (int64_t v0 = 0; v0 < c->vocab; v0 += c->piece) {
         const int64_t piece = c->vocab - v0 < c->piece ? c->vocab - v0 : c->piece;
         const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
         if (rows)
-            by_tiles(1, piece, rows, [&](auto shape) {
+            with_tile(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
                 typedef decltype(shape) S;
                 const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, labels, v0, c->vocab, lse, dz, zeros);
+                hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, labels, v0, c->vocab, lse, dz);
             });
-        by_tiles(c->n, c->dim, piece, [&](auto shape) {
+        with_tile(choose_tiles(KIND == SPLIT, c->n, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
             typedef decltype(shape) S;
             const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
             auto weight = [&](auto kernel, auto *out) {
-                hipLaunchKernelGGL(kernel, dim3(td * tv, (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws, zeros);
+                hipLaunchKernelGGL(kernel, dim3(td * tv, (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws);
             };
             if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
             else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
@@ -504,16 +489,16 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
             else weight(k_xent_dw<S, KIND, T, false>, (E *)dw);
         });
         if (rows)
-            by_tiles(parts, c->dim, rows, [&](auto shape) {
+            with_tile(hidden.shape, [&](auto shape) {
                 typedef decltype(shape) S;
                 const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
                 hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt, (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt, v0 == 0,
-                                   part, pitch, zeros);
+                                   part, pitch);
             });
         SAMS_HIP(hipGetLastError());
     }
     if (rows)
-        hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)parts, rows, pitch, t, c->dim, exps, inv, (E *)dh, dhs);
+        hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, parts, rows, pitch, t, c->dim, exps, inv, (E *)dh, dhs);
     SAMS_HIP(hipGetLastError());
     return SAMS_OK;
 }
@@ -537,7 +522,7 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     *out = nullptr;
     if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || dim < 1 || dim > SAMS_MAX_DIM || vocab < 1 || vocab > SAMS_MAX_VOCAB || !type_ok(type))
         return SAMS_EINVAL;
-    if ((n * t_max / 128 + 1) * (vocab / 128 + 1) > INT32_MAX) return SAMS_EINVAL;       // tiles of one launch
+    if ((n * t_max / Small::BN + 1) * (vocab / Small::BM + 1) > INT32_MAX) return SAMS_EINVAL;       // tiles of one launch
     sams_xent *c = new (std::nothrow) sams_xent();
     if (!c) return SAMS_ENOMEM;
     c->n = n; c->t_max = t_max; c->dim = dim; c->vocab = vocab; c->type = type; c->train = train != 0;
@@ -545,23 +530,21 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     const int64_t rows = n * t_max, ld = type == SAMS_F32 ? row_words<SPLIT>(dim) : row_words<F16>(dim);
     c->h = c->scratch.reserve(rows * ld * 2);
     c->w = c->scratch.reserve(vocab * ld * 2);
-    c->part = c->scratch.reserve(rows * ((vocab + Middle::BM - 1) / Middle::BM) * 8);
+    c->part = c->scratch.reserve(rows * ((vocab + Small::BM - 1) / Small::BM) * 8);
     c->token = c->scratch.reserve(rows * 4);
     c->inv = c->scratch.reserve(n * 4);
     c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
     c->exps = c->scratch.reserve(2 * 4);
-    c->zeros = c->scratch.reserve(256);
     if (train) {
         const int64_t row_bytes = type == SAMS_F32 ? 4 : 2, whole = (vocab + 255) / 256 * 256;
         c->piece = rows ? kXentPieceBytes / (rows * row_bytes) / 256 * 256 : whole;
         if (c->piece < 1024) c->piece = 1024;
-        if (c->piece > whole) c->piece = whole;
+        c->piece = std::min({c->piece, whole, kMaxRowWords / 2});
         c->dz = c->scratch.reserve(rows * c->piece * row_bytes);
         // for fewer tokens there may be more parts, in as much memory
         c->dh = c->scratch.reserve(std::max(rows * dh_pitch(dim) * 4, std::min(kPartBytes, rows * dh_pitch(dim) * 4 * kMaxSplit)));
     }
     int rc = c->scratch.take();
-    if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->zeros), 64, 0u);
     if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->exps), 2, 0u);
     if (rc != SAMS_OK) {
         if (c->scratch.base) (void)hipFree(c->scratch.base);
