@@ -50,6 +50,8 @@ __device__ __forceinline__ f32x16 mfma(u32x4 a, u32x4 b, f32x16 c)
 // c ^ swizzle_k(k), so that the four k's of a transposing read do.
 __device__ __forceinline__ int swizzle(int row) { return ((row ^ (row >> 3)) & 1) | (row & 6); }
 __device__ __forceinline__ int swizzle_k(int k) { return ((k & 3) << 2) | (k & 2); }
+// the part of it that stays within a row of so many pieces
+template <int PIECES> constexpr int kPieceMask = (PIECES & -PIECES) - 1;
 
 template <int KIND> __host__ __device__ constexpr int tile_k() { return KIND == SPLIT ? 32 : 64; }      // numbers of k in a stage
 
@@ -82,7 +84,7 @@ struct Loader {
     __device__ __forceinline__ static int piece_of(int i, int tid)
     {
         const int row = row_of(i, tid), c = (i * THREADS + tid) % PIECES;
-        return K_ROWS ? c ^ (swizzle_k(row) & (PIECES - 1)) : c ^ swizzle(row);
+        return K_ROWS ? c ^ (swizzle_k(row) & kPieceMask<PIECES>) : c ^ swizzle(row);
     }
     // where a piece starts, in k
     __device__ __forceinline__ static int k_of(int i, int tid) { return K_ROWS ? row_of(i, tid) : (KIND == SPLIT ? piece_of(i, tid) & 3 : piece_of(i, tid)) * 8; }
@@ -129,7 +131,7 @@ __device__ __forceinline__ u32x4 fragment(const char *tile, int row0, int kbase,
         const int g = lane >> 4, q = lane & 15;
         const int k = kbase + 8 * (g >> 1) + (q >> 2);
         const int w = (KIND == SPLIT ? row0 * 2 + half * 32 : row0) + (g & 1) * 16 + (q & 3) * 4;
-        const char *at = tile + k * (PIECES * 16) + (((w >> 3) ^ (swizzle_k(k) & (PIECES - 1))) << 4) + (w & 7) * 2;
+        const char *at = tile + k * (PIECES * 16) + (((w >> 3) ^ (swizzle_k(k) & kPieceMask<PIECES>)) << 4) + (w & 7) * 2;
         typedef __attribute__((address_space(3))) short4v *lds_ptr;
         const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
         const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * (PIECES * 16)));
@@ -239,6 +241,14 @@ __device__ __forceinline__ void clear(f32x16 (&acc)[S::MI][S::NI])
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
 }
 
+// A number as it stands in 32 bits.  The two parts of a pair are made from it; without this the compiler may round the first part
+// straight from the factors of the product that the number is, once for the pair and once, otherwise, for what is left of it.
+__device__ __forceinline__ float settled(float v)
+{
+    asm("" : "+v"(v));
+    return v;
+}
+
 // Between a wavefront's writes to LDS and its other lanes' reads of them (which LDS serves in order): the compiler keeps the order too.
 __device__ __forceinline__ void same_wave_lds() { asm volatile("" ::: "memory"); __builtin_amdgcn_wave_barrier(); }
 
@@ -269,18 +279,18 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[S::MI][S::NI], ch
                 const auto w = pack(what, wm + m, v);
                 if constexpr (PAIRS) {
                     const int at = i * 128 + (m & 31) * 2;
-                    *(u32x2 *)(mine_row + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = u32x2{w[0], w[1]};
-                    *(u32x2 *)(mine_row + ((((at + 64) >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = u32x2{w[2], w[3]};
+                    *(u32x2 *)(mine_row + (((at >> 4) ^ (r & kPieceMask<PIECES>)) << 4) + (at & 15)) = u32x2{w[0], w[1]};
+                    *(u32x2 *)(mine_row + ((((at + 64) >> 4) ^ (r & kPieceMask<PIECES>)) << 4) + (at & 15)) = u32x2{w[2], w[3]};
                 } else {
                     const int at = m * BYTES;
-                    *(decltype(pack(what, 0, v)) *)(mine_row + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = w;
+                    *(decltype(pack(what, 0, v)) *)(mine_row + (((at >> 4) ^ (r & kPieceMask<PIECES>)) << 4) + (at & 15)) = w;
                 }
             }
         same_wave_lds();
 #pragma unroll
         for (int it = 0; it < PIECES / 2; ++it) {
             const int slot = it * 64 + lane, n = slot / PIECES, c = slot % PIECES;
-            store(wn + j * 32 + n, wm * BYTES + c * 16, *(const u32x4 *)(mine + n * ROW + ((c ^ (n & (PIECES - 1))) << 4)));
+            store(wn + j * 32 + n, wm * BYTES + c * 16, *(const u32x4 *)(mine + n * ROW + ((c ^ (n & kPieceMask<PIECES>)) << 4)));
         }
         same_wave_lds();
     }
@@ -308,18 +318,18 @@ __device__ __forceinline__ void eights(const f32x16 (&acc)[S::MI][S::NI], char *
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int r = 8 * q + 4 * h + e, at = (inner * 32 + l) * 4;
-                        *(float *)(mine + r * ROW + (((at >> 4) ^ (r & (PIECES - 1))) << 4) + (at & 15)) = a[4 * q + e];
+                        *(float *)(mine + r * ROW + (((at >> 4) ^ (r & kPieceMask<PIECES>)) << 4) + (at & 15)) = a[4 * q + e];
                     }
                 } else {
                     const int c = (inner * 32 + 8 * q + 4 * h) >> 2;
-                    *(f32x4 *)(mine + l * ROW + ((c ^ (l & (PIECES - 1))) << 4)) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
+                    *(f32x4 *)(mine + l * ROW + ((c ^ (l & kPieceMask<PIECES>)) << 4)) = f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]};
                 }
             }
         same_wave_lds();
 #pragma unroll
         for (int it = 0; it < EIGHTS / 2; ++it) {
             const int slot = it * 64 + lane, r = slot / EIGHTS, c = slot % EIGHTS * 2;
-            const f32x4 lo = *(const f32x4 *)(mine + r * ROW + ((c ^ (r & (PIECES - 1))) << 4)), hi = *(const f32x4 *)(mine + r * ROW + (((c + 1) ^ (r & (PIECES - 1))) << 4));
+            const f32x4 lo = *(const f32x4 *)(mine + r * ROW + ((c ^ (r & kPieceMask<PIECES>)) << 4)), hi = *(const f32x4 *)(mine + r * ROW + (((c + 1) ^ (r & kPieceMask<PIECES>)) << 4));
             const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             if constexpr (MIRROR) emit(wm + outer * 32 + r, wn + c * 4, v);
             else emit(wn + outer * 32 + r, wm + c * 4, v);
@@ -339,12 +349,16 @@ __device__ __forceinline__ void put8(uint16_t *row, int64_t i, const float (&v)[
         *(bf16x8 *)(row + i) = w;
     } else {
         half8 w;
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (_Float16)v[e];
+        for (int e = 0; e < 8; ++e) {
+            x[e] = KIND == SPLIT ? settled(v[e]) : v[e];
+            w[e] = (_Float16)x[e];
+        }
         if constexpr (KIND == SPLIT) {
             half8 rest;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rest[e] = (_Float16)(v[e] - (float)w[e]);
+            for (int e = 0; e < 8; ++e) rest[e] = (_Float16)(x[e] - (float)w[e]);
             uint16_t *p = row + (i >> 5) * 64 + (i & 31);
             *(half8 *)p = w;
             *(half8 *)(p + 32) = rest;
@@ -382,10 +396,17 @@ template <int KIND>
 __device__ __forceinline__ auto pack_words(const float (&v)[4])
 {
     if constexpr (KIND == SPLIT) {
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+        _Float16 first[4];
         float rest[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rest[i] = v[i] - (float)(_Float16)v[i];
-        return u32x4{pair_of<_Float16>(v[0], v[1]), pair_of<_Float16>(v[2], v[3]), pair_of<_Float16>(rest[0], rest[1]), pair_of<_Float16>(rest[2], rest[3])};
+        for (int i = 0; i < 4; ++i) {
+            const float x = settled(v[i]);
+            first[i] = (_Float16)x;
+            rest[i] = x - (float)first[i];
+        }
+        return u32x4{__builtin_bit_cast(uint32_t, half2v{first[0], first[1]}), __builtin_bit_cast(uint32_t, half2v{first[2], first[3]}), pair_of<_Float16>(rest[0], rest[1]),
+                     pair_of<_Float16>(rest[2], rest[3])};
     } else if constexpr (KIND == F16) {
         return words2{pair_of<_Float16>(v[0], v[1]), pair_of<_Float16>(v[2], v[3])};
     } else {
@@ -432,38 +453,24 @@ __device__ __forceinline__ void tile_place(uint32_t id, uint32_t tiles_m, uint32
     ni = in / wide;
 }
 
-// one number as the words of an operand whose row starts at `row`; its place among the row's numbers is i
-template <int KIND>
-__device__ __forceinline__ void put(uint16_t *row, int64_t i, float v)
-{
-    if constexpr (KIND == SPLIT) {
-        const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
-        uint16_t *p = row + (i >> 5) * 64 + (i & 31);
-        p[0] = __builtin_bit_cast(uint16_t, hi);
-        p[32] = __builtin_bit_cast(uint16_t, lo);
-    } else if constexpr (KIND == F16) {
-        row[i] = __builtin_bit_cast(uint16_t, (_Float16)v);
-    } else {
-        row[i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-    }
-}
-
 // The tiles in use.  At 8192^3 (16 bits; pairs), Large reaches 1.27 PFLOP/s (0.45), 83 % of the library's 1.54 in 16 bits and three times
-// its 0.15 in 32, the card's clock down to 1.85 GHz (1.55) by then; Middle 1.1 (0.40), two workgroups on a CU; Small 0.65 (0.29).  Small's four
+// its 0.15 in 32, the card's clock down to 1.85 GHz (1.55) by then; Wide 1.05 (0.36), there for products that make a CU's worth of its tiles
+// but few of Large's; Middle 1.1 (0.40), two workgroups on a CU; Small 0.65 (0.29).  Small's four
 // stages cover a load's way where a CU has one workgroup: 640 x 640 x 12800 takes it 56 us (92), with two stages 95 (186), Middle 134 (267).
 typedef Shape<256, 256, 2, 4, 2> Large;
+typedef Shape<192, 192, 2, 2, 2> Wide;
 typedef Shape<128, 128, 2, 2, 2> Middle;
 typedef Shape<64, 64, 2, 2, 4> Small;
 
-// What a product of m x n x k numbers, `batch` times, is estimated to take in tiles of a size (1 Large, 2 Middle, 3 Small), its k cut into
+// What a product of m x n x k numbers, `batch` times, is estimated to take in tiles of a size (Large, Wide, Middle, Small), its k cut into
 // `parts`, in ns: a CU's workgroups one after the other, each at the pace it has beside others or, alone on its CU, by itself
 // (measured as above), and what a tile costs before and after its k's.
 struct TileCost { int size; double pace16, alone16, pace_pairs, alone_pairs, fixed; };
-constexpr TileCost kTileCosts[3] = {{256, 26, 26, 75, 75, 5000}, {128, 7.5, 10.5, 21.4, 21.4, 1700}, {64, 3.0, 4.4, 6.9, 7.2, 700}};
+constexpr TileCost kTileCosts[4] = {{256, 26, 26, 75, 75, 5000}, {192, 17, 17, 47.4, 47.4, 3500}, {128, 7.5, 10.5, 21.4, 21.4, 1700}, {64, 3.0, 4.4, 6.9, 7.2, 700}};
 
 static inline double tile_estimate(int shape, bool pairs, double tiles, double k, int parts)
 {
-    const TileCost &c = kTileCosts[shape - 1];
+    const TileCost &c = kTileCosts[shape];
     const double rounds = ceil(tiles * parts / 256), each = k / parts;
     return std::max(rounds * (pairs ? c.pace_pairs : c.pace16), pairs ? c.alone_pairs : c.alone16) * each + rounds * c.fixed;
 }
@@ -475,8 +482,8 @@ static inline TileChoice choose_tiles(bool pairs, int64_t batch, int64_t m, int6
 {
     TileChoice best{2, 1};
     double least = 1e30;
-    for (int shape = 1; shape <= 3; ++shape) {
-        const int64_t size = kTileCosts[shape - 1].size, a = (m + size - 1) / size, b = (n + size - 1) / size;
+    for (int shape = 0; shape < 4; ++shape) {
+        const int64_t size = kTileCosts[shape].size, a = (m + size - 1) / size, b = (n + size - 1) / size;
         const double tiles = (double)batch * (triangular ? a * (a + 1) / 2 : a * b);
         for (int parts = 1; parts <= most_parts; ++parts) {
             const double ns = tile_estimate(shape, pairs, tiles, (double)k, parts) + (most_parts > 1 ? parts * part_ns : 0.0);
@@ -489,7 +496,8 @@ static inline TileChoice choose_tiles(bool pairs, int64_t batch, int64_t m, int6
 template <typename F>
 static void with_tile(int shape, F f)
 {
-    if (shape == 1) f(Large());
+    if (shape == 0) f(Large());
+    else if (shape == 1) f(Wide());
     else if (shape == 2) f(Middle());
     else f(Small());
 }

@@ -36,6 +36,17 @@ struct OrthoScale {
     int32_t exponent;                   // words of G = G * 2^exponent
 };
 
+__device__ __forceinline__ OrthoScale ortho_scale(double norm, float eps)
+{
+    int e = 0;
+    if (norm > 0 && isfinite(norm)) {
+        (void)frexp(norm, &e);
+        e = 15 - e;                                                  // norm * 2^e in [2^14, 2^15)
+    }
+    const double sigma = norm > 0 ? ldexp(1.0 / (norm + (double)eps), -e) : (norm == 0 ? 0.0 : norm);
+    return OrthoScale{(float)sigma, (float)(sigma * sigma), e};
+}
+
 // sums of squares in 64 bits: no norm is too large or too small for its square; a wavefront per row
 template <int T>
 __global__ void __launch_bounds__(256) k_ortho_squares(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int64_t rows, int64_t cols, double *part)
@@ -110,16 +121,9 @@ __global__ void __launch_bounds__(256) k_ortho_words(const typename TypeOf<T>::t
         if (threadIdx.x == 0) norm = sqrt(s);
     }
     __syncthreads();
-    int e = 0;
-    if (norm > 0 && isfinite(norm)) {
-        (void)frexp(norm, &e);
-        e = 15 - e;                                                  // norm * 2^e in [2^14, 2^15)
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        const double sigma = norm > 0 ? ldexp(1.0 / (norm + (double)eps), -e) : (norm == 0 ? 0.0 : norm);
-        scale[blockIdx.y] = OrthoScale{(float)sigma, (float)(sigma * sigma), e};
-    }
-    const double by = ldexp(1.0, e);
+    const OrthoScale by_norm = ortho_scale(norm, eps);
+    if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = by_norm;
+    const double by = ldexp(1.0, by_norm.exponent);
     const int64_t width = row_numbers<KIND>(cols), ld = row_words<KIND>(cols);
     for (int64_t r = blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * 4) {
         const typename TypeOf<T>::type *p = g + blockIdx.y * g_mat + r * g_row;
@@ -264,6 +268,233 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
     });
 }
 
+// ---- matrices that fit one workgroup's LDS: all steps in one launch ----
+//
+// X and one square matrix (A, then P in its place) stay in LDS as planes of 16-bit floats (the first parts, then the second ones where
+// numbers are pairs), rows 16 bytes longer than whole fragments, so that rows next to each other start on other banks.  Sixteen wavefronts
+// share out 32 x 32 tiles, hold their results until all have read what these replace, and write them over it.
+constexpr int kSmallWaves = 16, kSmallTiles = 3;                    // tiles a wavefront can hold
+constexpr int kSmallLds = 163840 - 1024;
+
+struct SmallLayout {
+    int rows32, cols32, small32, pitch_x, pitch_s;                  // in numbers: padded extents, words from row to row
+    int plane_x, plane_s;                                           // words of a plane
+};
+static inline __host__ __device__ SmallLayout small_layout(int64_t rows, int64_t cols)
+{
+    SmallLayout l;
+    l.rows32 = (int)(rows + 31) / 32 * 32;
+    l.cols32 = (int)(cols + 31) / 32 * 32;
+    l.small32 = l.rows32 < l.cols32 ? l.rows32 : l.cols32;
+    l.pitch_x = l.cols32 + 8;
+    l.pitch_s = l.small32 + 8;
+    l.plane_x = l.rows32 * l.pitch_x;
+    l.plane_s = l.small32 * l.pitch_s;
+    return l;
+}
+static bool small_fits(int64_t rows, int64_t cols, bool pairs)
+{
+    if (rows > 4096 || cols > 4096) return false;
+    const SmallLayout l = small_layout(rows, cols);
+    return (int64_t)(l.plane_x + l.plane_s) * (pairs ? 4 : 2) <= kSmallLds && l.rows32 / 32 * (l.cols32 / 32) <= kSmallWaves * kSmallTiles &&
+           l.small32 / 32 * (l.small32 / 32) <= kSmallWaves * kSmallTiles;
+}
+
+// what the host knows of a step: the polynomial, and the powers of two between the words
+struct SmallStep { float f_gram, a, b, c, f_apply; };
+struct SmallSteps { int count; SmallStep step[SAMS_MAX_ORTHO_STEPS]; };
+
+// a lane's 8 k's (from k0 + 8 * (lane / 32) on) of row r0 + lane % 32, or, where rows are k's, of column r0 + lane % 32
+__device__ __forceinline__ u32x4 small_fragment(const uint16_t *m, int pitch, int r0, int k0, int lane) { return *(const u32x4 *)(m + (r0 + (lane & 31)) * pitch + k0 + 8 * (lane >> 5)); }
+__device__ __forceinline__ u32x4 small_fragment_k(const uint16_t *m, int pitch, int r0, int k0, int lane)
+{
+    const int g = lane >> 4, q = lane & 15;
+    typedef __attribute__((address_space(3))) short4v *lds_ptr;
+    const uint16_t *at = m + (k0 + 8 * (g >> 1) + (q >> 2)) * pitch + r0 + (g & 1) * 16 + (q & 3) * 4;
+    const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * pitch));
+    const words2 a = __builtin_bit_cast(words2, lo), b = __builtin_bit_cast(words2, hi);
+    return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// acc[t] = the product of tile (m, n) number wave + kSmallWaves t, n fastest, over k (a multiple of 32); A_K, B_K: rows are k's
+template <bool PAIRS, bool A_K, bool B_K>
+__device__ __forceinline__ void small_product(f32x16 (&acc)[kSmallTiles], const uint16_t *a, int pitch_a, int plane_a, const uint16_t *b, int pitch_b, int plane_b, int tiles,
+                                              int tiles_n, int k, int lane, int wave)
+{
+#pragma unroll
+    for (int t = 0; t < kSmallTiles; ++t) {
+        const int id = wave + t * kSmallWaves;
+        if (id >= tiles) break;
+        asm volatile("" : "+v"(lane));                               // addresses made here, not kept for every tile over all steps
+        const int m0 = id / tiles_n * 32, n0 = id % tiles_n * 32;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[t][q] = 0.f;
+        for (int k0 = 0; k0 < k; k0 += 32) {
+            u32x4 fa[2][2], fb[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int h = 0; h < (PAIRS ? 2 : 1); ++h) {
+                    const int at = k0 + 16 * u;
+                    fa[u][h] = A_K ? small_fragment_k(a + h * plane_a, pitch_a, m0, at, lane) : small_fragment(a + h * plane_a, pitch_a, m0, at, lane);
+                    fb[u][h] = B_K ? small_fragment_k(b + h * plane_b, pitch_b, n0, at, lane) : small_fragment(b + h * plane_b, pitch_b, n0, at, lane);
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                acc[t] = mfma<F16>(fa[u][0], fb[u][0], acc[t]);
+                if constexpr (PAIRS) {
+                    acc[t] = mfma<F16>(fa[u][0], fb[u][1], acc[t]);
+                    acc[t] = mfma<F16>(fa[u][1], fb[u][0], acc[t]);
+                }
+            }
+        }
+    }
+}
+
+// f(row, column, numbers) for the fours of a wavefront's tiles: n are rows, m columns
+template <typename F>
+__device__ __forceinline__ void small_fours(const f32x16 (&acc)[kSmallTiles], int tiles, int tiles_n, int lane, int wave, F f)
+{
+#pragma unroll
+    for (int t = 0; t < kSmallTiles; ++t) {
+        const int id = wave + t * kSmallWaves;
+        if (id >= tiles) break;
+        asm volatile("" : "+v"(lane));
+        const int m0 = id / tiles_n * 32, n0 = id % tiles_n * 32;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {acc[t][4 * q], acc[t][4 * q + 1], acc[t][4 * q + 2], acc[t][4 * q + 3]};
+            f(n0 + (lane & 31), m0 + 8 * q + 4 * (lane >> 5), v);
+        }
+    }
+}
+
+template <bool PAIRS>
+__device__ __forceinline__ void small_put(uint16_t *at, int plane, const float (&v)[4])
+{
+    if constexpr (PAIRS) {
+        const u32x4 w = pack_words<SPLIT>(v);
+        *(words2 *)at = words2{w[0], w[1]};
+        *(words2 *)(at + plane) = words2{w[2], w[3]};
+    } else {
+        *(words2 *)at = pack_words<F16>(v);
+    }
+}
+
+template <bool PAIRS>
+__device__ __forceinline__ void small_get(const uint16_t *at, int plane, float (&v)[4])
+{
+    typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+    const half4 a = *(const half4 *)at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)a[e];
+    if constexpr (PAIRS) {
+        const half4 b = *(const half4 *)(at + plane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += (float)b[e];
+    }
+}
+
+// part: the sums of squares where they are made already (part_count of them a matrix), else null
+template <int T, bool TALL>
+__global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int rows, int cols, float eps, const double *part,
+                                                                  SmallSteps steps, OrthoOut o)
+{
+    constexpr bool PAIRS = T == SAMS_F32;
+    typedef typename TypeOf<T>::type E;
+    __shared__ __align__(16) uint16_t lds[kSmallLds / 2];
+    __shared__ double sums[kSmallWaves];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int lane = tid & 63;
+    const SmallLayout l = small_layout(rows, cols);
+    uint16_t *x = lds, *sq = lds + l.plane_x * (PAIRS ? 2 : 1);
+    const E *pg = g + blockIdx.x * g_mat;
+    const int fours = l.cols32 / 4, small = rows < cols ? rows : cols;
+    auto load4 = [&](int r, int c, float (&v)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = r < rows && c + e < cols ? (float)pg[r * g_row + c + e] : 0.f;
+    };
+    double s = 0;
+    if (part) {
+        for (int i = tid; i < kNormSlices; i += 64 * kSmallWaves) s += part[blockIdx.x * kNormSlices + i];
+    } else {
+        for (int i = tid; i < rows * fours; i += 64 * kSmallWaves) {
+            float v[4];
+            load4(i / fours, i % fours * 4, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_fma((double)v[e], (double)v[e], s);
+        }
+    }
+    s = wave_sum(s);
+    if (lane == 0) sums[wave] = s;
+    __syncthreads();
+    double norm = 0;
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) norm += sums[w];
+    norm = sqrt(norm);
+    const OrthoScale scale = ortho_scale(norm, eps);
+    const double by = ldexp(1.0, scale.exponent);
+    for (int i = tid; i < l.rows32 * fours; i += 64 * kSmallWaves) {
+        const int r = i / fours, c = i % fours * 4;
+        float v[4];
+        load4(r, c, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)((double)v[e] * by);
+        small_put<PAIRS>(x + r * l.pitch_x + c, l.plane_x, v);
+    }
+    __syncthreads();
+    f32x16 acc[kSmallTiles];
+    const int ts = l.small32 / 32, square = ts * ts, tr = l.rows32 / 32, tiles = tr * (l.cols32 / 32), large32 = TALL ? l.rows32 : l.cols32;
+    for (int step = 0; step < steps.count; ++step) {
+        const SmallStep p = steps.step[step];
+        const float fg = step ? p.f_gram : p.f_gram * scale.sigma2, fa = step ? p.f_apply : p.f_apply * scale.sigma;
+        small_product<PAIRS, TALL, TALL>(acc, x, l.pitch_x, l.plane_x, x, l.pitch_x, l.plane_x, square, ts, large32, lane, wave);
+        small_fours(acc, square, ts, lane, wave, [&](int r, int c, const float (&v)[4]) {
+            const float w[4] = {v[0] * fg, v[1] * fg, v[2] * fg, v[3] * fg};
+            small_put<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, w);
+        });
+        __syncthreads();
+        small_product<PAIRS, false, false>(acc, sq, l.pitch_s, l.plane_s, sq, l.pitch_s, l.plane_s, square, ts, l.small32, lane, wave);
+#pragma unroll
+        for (int t = 0; t < kSmallTiles; ++t) {                      // P, still in registers: A is read by the others
+            const int id = wave + t * kSmallWaves;
+            if (id >= square) break;
+            asm volatile("" : "+v"(lane));
+            const int m0 = id / ts * 32, n0 = id % ts * 32;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = n0 + (lane & 31), c = m0 + 8 * q + 4 * (lane >> 5);
+                float w[4];
+                small_get<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t][4 * q + e] = r < small && c + e < small ? (r == c + e ? p.a : 0.f) + p.b * w[e] + p.c * acc[t][4 * q + e] : 0.f;
+            }
+        }
+        __syncthreads();
+        small_fours(acc, square, ts, lane, wave, [&](int r, int c, const float (&v)[4]) { small_put<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, v); });
+        __syncthreads();
+        if constexpr (TALL) small_product<PAIRS, false, false>(acc, sq, l.pitch_s, l.plane_s, x, l.pitch_x, l.plane_x, tiles, tr, l.small32, lane, wave);
+        else small_product<PAIRS, true, false>(acc, x, l.pitch_x, l.plane_x, sq, l.pitch_s, l.plane_s, tiles, tr, l.small32, lane, wave);
+        if (step + 1 < steps.count) {
+            __syncthreads();
+            small_fours(acc, tiles, tr, lane, wave, [&](int r, int c, const float (&v)[4]) {
+                const float w[4] = {v[0] * fa, v[1] * fa, v[2] * fa, v[3] * fa};
+                small_put<PAIRS>(x + r * l.pitch_x + c, l.plane_x, w);
+            });
+            __syncthreads();
+        } else {
+            small_fours(acc, tiles, tr, lane, wave, [&](int r, int c, const float (&v)[4]) {
+                if (r >= rows) return;
+                E *out = (E *)o.out + blockIdx.x * o.out_mat + r * o.out_row;
+                const float *px = o.x ? o.x + blockIdx.x * o.x_mat + (int64_t)r * cols : nullptr;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < cols) out[c + e] = (E)(px ? o.keep * px[c + e] - o.rate * (v[e] * fa) : v[e] * fa);
+            });
+        }
+    }
+}
+
 // the largest of |a + b u + c u^2| * u^(odd ? 1/2 : 0) for 0 <= u <= u_max
 static double poly_bound(double a, double b, double c, double u_max, bool odd)
 {
@@ -291,42 +522,56 @@ static int word_exponent(double bound)
     return e > 60 ? 60 : e < -60 ? -60 : e;
 }
 
+// the steps' factors, from bounds of X's singular values: words of X = X * 2^ex (the first: X = words * sigma), A's and P's likewise
+static void plan_steps(int steps, const float *coef, SmallSteps *plan)
+{
+    const double a = coef[0], b = coef[1], c = coef[2];
+    double bound = 1.0;
+    int ex = 0;
+    plan->count = steps;
+    for (int s = 0; s < steps; ++s) {
+        const double u = bound * bound, after = poly_bound(a, b, c, u, true);
+        const int ea = word_exponent(u), ep = word_exponent(poly_bound(a, b, c, u, false)), en = s + 1 == steps ? 0 : word_exponent(after);
+        plan->step[s] = SmallStep{(float)ldexp(1.0, ea - 2 * ex), (float)ldexp(a, ep), (float)ldexp(b, ep - ea), (float)ldexp(c, ep - 2 * ea), (float)ldexp(1.0, en - ep - ex)};
+        ex = en;
+        bound = after;
+    }
+}
+
 template <int KIND, int T>
-static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *coef, const OrthoOut &o)
+static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, const OrthoOut &o)
 {
     const OrthoDims d{c->rows, c->cols, c->rows < c->cols ? c->rows : c->cols};
     const bool tall = c->rows > c->cols;
     uint16_t *gram = c->scratch.at<uint16_t>(c->gram), *poly = c->scratch.at<uint16_t>(c->poly);
     const OrthoScale *scale = c->scratch.at<OrthoScale>(c->scale);
     const int64_t large = d.rows + d.cols - d.small;
-    const TileChoice square = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, (large + d.small) / 2, 1, 0),
-                     whole = choose_tiles(KIND == SPLIT, batch, d.cols, d.rows, false, d.small, 1, 0);
-    double bound = 1.0;                                              // of X's singular values
-    int ex = 0;                                                      // words of X = X * 2^ex; the first: X = words * sigma
-    for (int s = 0; s < steps; ++s) {
+    const int of_gram = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, large, 1, 0).shape, of_poly = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, d.small, 1, 0).shape,
+              of_apply = choose_tiles(KIND == SPLIT, batch, d.cols, d.rows, false, d.small, 1, 0).shape;
+    for (int s = 0; s < plan.count; ++s) {
         const uint16_t *x = c->scratch.at<uint16_t>(c->x[s & 1]);
         uint16_t *next = c->scratch.at<uint16_t>(c->x[(s + 1) & 1]);
-        const double a = coef[0], b = coef[1], cc = coef[2], u = bound * bound;
-        const double after = poly_bound(a, b, cc, u, true);
-        const int ea = word_exponent(u), ep = word_exponent(poly_bound(a, b, cc, u, false)), en = word_exponent(after);
+        const SmallStep &p = plan.step[s];
         const OrthoScale *first = s == 0 ? scale : nullptr;
-        with_tile(square.shape, [&](auto shape) {
+        auto square = [&](auto shape) {
+            const int64_t ts = (d.small + decltype(shape)::BM - 1) / decltype(shape)::BM;
+            return dim3((unsigned)(ts * (ts + 1) / 2), (unsigned)batch);
+        };
+        with_tile(of_gram, [&](auto shape) {
             typedef decltype(shape) S;
-            const int64_t ts = (d.small + S::BM - 1) / S::BM;
-            const dim3 grid((unsigned)(ts * (ts + 1) / 2), (unsigned)batch);
-            const float f = (float)ldexp(1.0, ea - 2 * ex);
-            if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram);
-            else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), grid, dim3(S::THREADS), 0, c->stream, x, d, f, first, gram);
-            hipLaunchKernelGGL((k_ortho_poly<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, gram, d, (float)ldexp(a, ep), (float)ldexp(b, ep - ea), (float)ldexp(cc, ep - 2 * ea),
-                               poly);
+            if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
+            else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
         });
-        const bool last = s + 1 == steps;
-        const float f = (float)ldexp(1.0, (last ? 0 : en) - ep - ex);
-        with_tile(whole.shape, [&](auto shape) {
+        with_tile(of_poly, [&](auto shape) {
+            typedef decltype(shape) S;
+            hipLaunchKernelGGL((k_ortho_poly<S, KIND>), square(shape), dim3(S::THREADS), 0, c->stream, gram, d, p.a, p.b, p.c, poly);
+        });
+        const bool last = s + 1 == plan.count;
+        with_tile(of_apply, [&](auto shape) {
             typedef decltype(shape) S;
             const uint32_t tm = (uint32_t)((d.cols + S::BM - 1) / S::BM), tn = (uint32_t)((d.rows + S::BN - 1) / S::BN);
             auto apply = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, f, first, next, o);
+                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, p.f_apply, first, next, o);
             };
             if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
             else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
@@ -334,23 +579,35 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, int steps, const float *c
             else apply(k_ortho_apply<S, KIND, false, false, T>);
         });
         SAMS_HIP(hipGetLastError());
-        ex = en;
-        bound = after;
     }
     return SAMS_OK;
 }
 
-// from a matrix in memory, the sum of its squares made, to the last step
+// from a matrix in memory to the last step; squares_made: the sums of its squares are in the scratch
 template <int T>
-static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, int steps, const float *coef, float eps, const OrthoOut &o)
+static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, bool squares_made, int steps, const float *coef, float eps, const OrthoOut &o)
 {
     constexpr int KIND = T == SAMS_F32 ? SPLIT : F16;
     typedef typename TypeOf<T>::type E;
     double *part = c->scratch.at<double>(c->part);
-    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows, 4, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row,
-                       c->rows, c->cols, eps, part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
+    SmallSteps plan;
+    plan_steps(steps, coef, &plan);
+    if (small_fits(c->rows, c->cols, KIND == SPLIT)) {
+        auto all = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(64 * kSmallWaves), 0, c->stream, (const E *)g, g_mat, g_row, (int)c->rows, (int)c->cols, eps,
+                               squares_made ? part : nullptr, plan, o);
+        };
+        if (c->rows > c->cols) all(k_ortho_small<T, true>);
+        else all(k_ortho_small<T, false>);
+        SAMS_HIP(hipGetLastError());
+        return SAMS_OK;
+    }
+    if (!squares_made)
+        hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, part);
+    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows, 4, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, eps,
+                       part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
     SAMS_HIP(hipGetLastError());
-    return enqueue_steps<KIND, T>(c, batch, steps, coef, o);
+    return enqueue_steps<KIND, T>(c, batch, plan, o);
 }
 
 static bool coef_ok(const float *coef)
@@ -407,9 +664,7 @@ int orthogonalize(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, in
     const int size = type_size(c->type);
     if (!g || !out || !aligned_to(g, size) || !aligned_to(out, size) || g_mat < 0 || g_row < 0 || (c->rows > 1 && out_row < c->cols) || (batch > 1 && out_mat < c->cols)) return SAMS_EINVAL;
     const OrthoOut o{out, out_mat, out_row, nullptr, 0, 0.f, 0.f};
-    SAMS_BY_TYPE(c->type, T, hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const TypeOf<T>::type *)g, g_mat, g_row, c->rows,
-                                                c->cols, c->scratch.at<double>(c->part)));
-    SAMS_BY_TYPE(c->type, T, return enqueue_ortho<T>(c, batch, g, g_mat, g_row, steps, coef_host, eps, o));
+    SAMS_BY_TYPE(c->type, T, return enqueue_ortho<T>(c, batch, g, g_mat, g_row, false, steps, coef_host, eps, o));
 }
 
 int muon_update(sams_ortho *c, int32_t n, int64_t batch, const float *g, int64_t g_worker, int64_t g_mat, const float *m, int64_t m_mat, const float *x,
@@ -427,7 +682,7 @@ int muon_update(sams_ortho *c, int32_t n, int64_t batch, const float *g, int64_t
                        c->scratch.at<double>(c->part));
     SAMS_HIP(hipGetLastError());
     const OrthoOut o{x_out, x_out_mat, c->cols, x, x_mat, 1.f - lr * weight_decay, lr * scale};
-    return enqueue_ortho<SAMS_F32>(c, batch, update, elems, c->cols, steps, coef_host, eps, o);
+    return enqueue_ortho<SAMS_F32>(c, batch, update, elems, c->cols, true, steps, coef_host, eps, o);
 }
 
 }  // extern "C"

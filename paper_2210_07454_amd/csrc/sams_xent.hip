@@ -80,15 +80,46 @@ __global__ void __launch_bounds__(256) k_xent_amax(const float *h, Rows hs, int6
     if (threadIdx.x == 0) amax[blockIdx.x] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
 }
 
-// words of a tensor's rows; rows that take no part (labels given) become zeros, whatever they hold
+// what k_xent_pack packs: rows of a tensor into rows of words; rows that take no part (labels given) become zeros, whatever they hold
+struct Packed {
+    const void *src;
+    Rows at;
+    int64_t t, rows;                    // rows of a worker, rows; none: nothing to pack
+    const int64_t *labels;
+    uint16_t *out;
+};
+
+// H by the first blocks, W by the next, and grad_w / count_w (0 where a worker has no labelled token) by the last n, where asked for
 template <int T, int KIND>
-__global__ void __launch_bounds__(256) k_xent_pack(const typename TypeOf<T>::type *src, Rows s, int64_t t, int64_t rows, int64_t dim, const int64_t *labels, int64_t vocab,
-                                                   const float *amax, int32_t *exps, uint16_t *out)
+__global__ void __launch_bounds__(256) k_xent_pack(Packed H, unsigned blocks_h, Packed W, unsigned blocks_w, int64_t dim, int64_t vocab, const float *amax, int32_t *exps,
+                                                   const int64_t *labels, int64_t t, const float *grad, float *inv)
 {
+    if (blockIdx.x >= blocks_h + blocks_w) {
+        __shared__ int64_t counts[4];
+        const int64_t worker = blockIdx.x - blocks_h - blocks_w;
+        int c = 0;
+        for (int64_t i = threadIdx.x; i < t; i += 256) c += takes_part(labels, worker * t + i, vocab);
+#pragma unroll
+        for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
+        if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
+        __syncthreads();
+        const int64_t count = counts[0] + counts[1] + counts[2] + counts[3];
+        if (threadIdx.x == 0) inv[worker] = count ? (grad ? grad[worker] : 1.f) / (float)count : 0.f;
+        return;
+    }
+    const bool of_w = blockIdx.x >= blocks_h;
+    const Packed p = of_w ? W : H;
+    const unsigned block = of_w ? blockIdx.x - blocks_h : blockIdx.x, blocks = of_w ? blocks_w : blocks_h;
+    const int lane = threadIdx.x & 63;
     float scale = 1.f;
     if constexpr (KIND == SPLIT) {
         float m = 0.f;
-        for (int i = threadIdx.x & 63; i < kAmaxBlocks; i += 64) m = fmaxf(m, amax[i]);
+        static_assert(kAmaxBlocks % 256 == 0, "");
+#pragma unroll
+        for (int i = 0; i < kAmaxBlocks / 256; ++i) {
+            const float4 a = ((const float4 *)(amax + (of_w ? kAmaxBlocks : 0)))[i * 64 + lane];
+            m = fmaxf(m, fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)));
+        }
         m = wave_max(m);
         int e = 0;
         if (m > 0) {
@@ -97,18 +128,18 @@ __global__ void __launch_bounds__(256) k_xent_pack(const typename TypeOf<T>::typ
             if (e > 126) e = 126;
         }
         scale = ldexpf(1.f, e);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *exps = e;
+        if (block == 0 && threadIdx.x == 0) exps[of_w] = e;
     }
     const int64_t width = row_numbers<KIND>(dim), ld = row_words<KIND>(dim);
-    for (int64_t r = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); r < rows; r += gridDim.x * (int64_t)4) {
-        const bool used = !labels || takes_part(labels, r, vocab);
-        const typename TypeOf<T>::type *p = src + r / t * s.worker + r % t * s.row;
-        for (int64_t i = (threadIdx.x & 63) * 8; i < width; i += 512) {
+    for (int64_t r = block * (int64_t)4 + (threadIdx.x >> 6); r < p.rows; r += blocks * (int64_t)4) {
+        const bool used = !p.labels || takes_part(p.labels, r, vocab);
+        const typename TypeOf<T>::type *from = (const typename TypeOf<T>::type *)p.src + r / p.t * p.at.worker + r % p.t * p.at.row;
+        for (int64_t i = lane * 8; i < width; i += 512) {
             float v[8];
-            load8<T>(p, i, used ? dim : 0, v);
+            load8<T>(from, i, used ? dim : 0, v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= scale;
-            put8<KIND>(out + r * ld, i, v);
+            put8<KIND>(p.out + r * ld, i, v);
         }
     }
 }
@@ -224,21 +255,6 @@ __global__ void __launch_bounds__(256) k_xent_loss(const float *token, const int
     if (threadIdx.x) return;
     const int64_t count = counts[0] + counts[1] + counts[2] + counts[3];
     loss[blockIdx.x] = count ? (sums[0] + sums[1] + sums[2] + sums[3]) / (float)count : 0.f;
-}
-
-// grad_w / count_w; 0 where a worker has no labelled token
-__global__ void __launch_bounds__(256) k_xent_inv(const int64_t *labels, int64_t t, int64_t vocab, const float *grad, float *inv)
-{
-    __shared__ int64_t counts[4];
-    int c = 0;
-    for (int64_t i = threadIdx.x; i < t; i += 256) c += takes_part(labels, blockIdx.x * t + i, vocab);
-#pragma unroll
-    for (int o = 32; o; o >>= 1) c += __shfl_xor(c, o);
-    if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = c;
-    __syncthreads();
-    if (threadIdx.x) return;
-    const int64_t count = counts[0] + counts[1] + counts[2] + counts[3];
-    inv[blockIdx.x] = count ? (grad ? grad[blockIdx.x] : 1.f) / (float)count : 0.f;
 }
 
 // dz of one piece of the vocabulary (W: the piece), a row of words per token
@@ -394,33 +410,33 @@ static TileChoice dh_tiles(bool pairs, int64_t rows, int64_t dim, int64_t piece)
     return choose_tiles(pairs, 1, dim, rows, false, piece, (int)std::max<int64_t>(1, std::min(room, most)), bytes * 2 / 4000.0);      // 4 TB/s
 }
 
-// W and H as operands; packed where the tensors themselves are not fit to be loaded from (or hold rows to be left out)
+// H and W as operands, packed where the tensors themselves are not fit to be loaded from; backward: H without the rows that take no part,
+// and inv
 template <int T, int KIND>
-static int enqueue_operands(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, bool clean, Operand *H, Operand *W)
+static int enqueue_operands(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, bool backward, const float *grad, Operand *H,
+                            Operand *W)
 {
-    typedef typename TypeOf<T>::type E;
-    const int64_t rows = c->n * t;
+    const int64_t rows = c->n * t, ld = row_words<KIND>(c->dim);
     float *amax = c->scratch.at<float>(c->amax);
-    int32_t *exps = c->scratch.at<int32_t>(c->exps);
-    if (KIND == SPLIT)
-        hipLaunchKernelGGL(k_xent_amax, dim3(2 * kAmaxBlocks), dim3(256), 0, c->stream, (const float *)h, hs, t, rows, labels, (const float *)w, w_row, c->vocab, c->dim, amax);
     auto fit = [&](int64_t row, const void *p) { return KIND != SPLIT && c->dim % 8 == 0 && row % 8 == 0 && row <= kMaxRowWords && aligned16(p); };
-    const bool rows_even = c->n == 1 || hs.worker == t * hs.row;
-    if (!clean && rows_even && fit(hs.row, h)) {
+    Packed ph = {h, hs, t, rows, labels, c->scratch.at<uint16_t>(c->h)}, pw = {w, Rows{0, w_row}, c->vocab, c->vocab, nullptr, c->scratch.at<uint16_t>(c->w)};
+    *H = Operand{ph.out, ld, rows};
+    *W = Operand{pw.out, ld, c->vocab};
+    if (!backward && (c->n == 1 || hs.worker == t * hs.row) && fit(hs.row, h)) {
         *H = Operand{(const uint16_t *)h, hs.row, rows};
-    } else {
-        uint16_t *hp = c->scratch.at<uint16_t>(c->h);
-        hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3((unsigned)grid_for(rows, 4, 4096)), dim3(256), 0, c->stream, (const E *)h, hs, t, rows, c->dim, labels, c->vocab, amax, exps, hp);
-        *H = Operand{hp, row_words<KIND>(c->dim), rows};
+        ph.rows = 0;
     }
     if (fit(w_row, w)) {
         *W = Operand{(const uint16_t *)w, w_row, c->vocab};
-    } else {
-        uint16_t *wp = c->scratch.at<uint16_t>(c->w);
-        hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3((unsigned)grid_for(c->vocab, 4, 4096)), dim3(256), 0, c->stream, (const E *)w, Rows{0, w_row}, c->vocab, c->vocab, c->dim,
-                           (const int64_t *)nullptr, c->vocab, amax + kAmaxBlocks, exps + 1, wp);
-        *W = Operand{wp, row_words<KIND>(c->dim), c->vocab};
+        pw.rows = 0;
     }
+    if (rows == 0) ph.rows = pw.rows = 0;
+    const unsigned blocks_h = ph.rows ? grid_for(ph.rows, 4, 2048) : 0, blocks_w = pw.rows ? grid_for(pw.rows, 4, 4096) : 0, blocks = blocks_h + blocks_w + (backward ? c->n : 0);
+    if (KIND == SPLIT && rows)
+        hipLaunchKernelGGL(k_xent_amax, dim3(2 * kAmaxBlocks), dim3(256), 0, c->stream, (const float *)h, hs, t, rows, labels, (const float *)w, w_row, c->vocab, c->dim, amax);
+    if (blocks)
+        hipLaunchKernelGGL((k_xent_pack<T, KIND>), dim3(blocks), dim3(256), 0, c->stream, ph, blocks_h, pw, blocks_w, c->dim, c->vocab, amax, c->scratch.at<int32_t>(c->exps), labels, t,
+                           grad, c->scratch.at<float>(c->inv));
     SAMS_HIP(hipGetLastError());
     return SAMS_OK;
 }
@@ -434,7 +450,7 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
     float *token = c->scratch.at<float>(c->token);
     if (rows) {
         Operand H, W;
-        SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, &H, &W)));
+        SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, nullptr, &H, &W)));
         float2 *part = c->scratch.at<float2>(c->part);
         uint32_t tv = 0;
         with_tile(choose_tiles(KIND == SPLIT, 1, c->vocab, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
@@ -461,9 +477,8 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
     float *inv = c->scratch.at<float>(c->inv);
     const int32_t *exps = c->scratch.at<int32_t>(c->exps);
     uint16_t *dz = c->scratch.at<uint16_t>(c->dz);
-    hipLaunchKernelGGL(k_xent_inv, dim3((unsigned)c->n), dim3(256), 0, c->stream, labels, t, c->vocab, grad, inv);
-    Operand H{c->scratch.at<uint16_t>(c->h), row_words<KIND>(c->dim), 0}, W{c->scratch.at<uint16_t>(c->w), row_words<KIND>(c->dim), c->vocab};
-    if (rows) SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, &H, &W)));
+    Operand H, W;
+    SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, grad, &H, &W)));
     float *part = c->scratch.at<float>(c->dh);
     const int64_t pitch = dh_pitch(c->dim);
     const TileChoice hidden = rows ? dh_tiles(KIND == SPLIT, rows, c->dim, c->piece) : TileChoice{2, 0};

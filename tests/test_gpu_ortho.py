@@ -89,6 +89,21 @@ def test_against_64_bits(sams, kind, shape):
     check(out, want, bounds, kind, shape)
 
 
+@pytest.mark.parametrize("shape", [(4, 96, 128), (4, 120, 84), (2, 300, 400), (2, 400, 130)], ids=str)
+def test_no_number_stands_out(sams, shape):
+    """The bound above is on the whole matrix, where one number that lost its second part (an error of 2^-12 of it) would hide.  Roundings
+    spread over a matrix: no number is off by more than eight times what the bound leaves each on the average."""
+    for seed in range(6):
+        g = matrices(*shape, torch.float32, seed=100 * seed)
+        want, bounds = reference(g, steps=2)
+        out = torch.empty_like(g, device="cuda")
+        with sams.Orthogonalizer(*shape) as op:
+            op.orthogonalize(g.cuda(), out, steps=2)
+        for i in range(shape[0]):
+            each = 16 * UNIT[torch.float32] * bounds[i] / math.sqrt(want[i].numel())
+            assert float((out[i].cpu().double() - want[i]).abs().max()) <= 8 * each, (seed, i)
+
+
 @pytest.mark.parametrize("kind", TYPES, ids=str)
 @pytest.mark.parametrize("steps,coef", [(1, COEF), (2, CUBIC), (10, CUBIC), (3, (2.0, -1.5, 0.5)), (7, COEF), (2, (0.0, 1.0, 0.0)), (2, (1.0, 0.0, 0.0))], ids=str)
 def test_steps_and_coefficients(sams, kind, steps, coef):
