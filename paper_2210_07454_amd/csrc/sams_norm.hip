@@ -22,6 +22,7 @@ constexpr int64_t kNormForwardThreads = 1024 * 256;      // of the forward pass:
 constexpr int kNormBlocks = 512;        // workgroups of the backward pass that leave sums (all workers'): two for every CU
 
 template <int TPR> constexpr int kNormBlock = TPR == 64 ? 256 : TPR;        // threads of a workgroup: a row's, or four rows' wavefronts
+template <int TPR> constexpr int kNormBackBlock = TPR < 512 ? 512 : TPR;    // of the backward pass: several rows', whose sums are joined in LDS
 
 template <int N>
 __device__ __forceinline__ void load_floats(const float *p, int64_t at, int64_t dim, float (&v)[N])
@@ -43,12 +44,12 @@ __device__ __forceinline__ float2 row_sum(float a, float b, float2 (&buf)[2][16]
     a = wave_sum(a);
     b = wave_sum(b);
     if constexpr (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
+        const int wave = threadIdx.x >> 6, first = wave & ~(TPR / 64 - 1);
         if ((threadIdx.x & 63) == 0) buf[turn][wave] = make_float2(a, b);
         __syncthreads();
         a = b = 0.f;
 #pragma unroll
-        for (int w = 0; w < TPR / 64; ++w) { a += buf[turn][w].x; b += buf[turn][w].y; }
+        for (int w = 0; w < TPR / 64; ++w) { a += buf[turn][first + w].x; b += buf[turn][first + w].y; }
         turn ^= 1;
     }
     return make_float2(a, b);
@@ -118,11 +119,11 @@ __global__ void __launch_bounds__(kNormBlock<TPR>) k_norm_forward(const typename
 // The same for the backward pass.  A workgroup has rows of one worker (part blockIdx.x of gridDim.x, worker blockIdx.y), and a thread
 // its columns of all of them, so that dw and db are added up in registers beside dx; a workgroup's sums are left in `part`.
 template <int T, int TPR, int CH>
-__global__ void __launch_bounds__(kNormBlock<TPR>) k_norm_backward(const typename TypeOf<T>::type *dy, Rows dys, const typename TypeOf<T>::type *x, Rows xs, const float *w,
+__global__ void __launch_bounds__(kNormBackBlock<TPR>, 4) k_norm_backward(const typename TypeOf<T>::type *dy, Rows dys, const typename TypeOf<T>::type *x, Rows xs, const float *w,
                                                                          const float *mean, const float *rstd, typename TypeOf<T>::type *dx, Rows dxs, float *part, uint32_t t,
                                                                          int64_t dim)
 {
-    constexpr int N = kPiece<T>, GROUPS = kNormBlock<TPR> / TPR;
+    constexpr int N = kPiece<T>, GROUPS = kNormBackBlock<TPR> / TPR;
     __shared__ float2 buf[2][16];
     extern __shared__ float joined[];                                // GROUPS > 1: [GROUPS / 2][2][dim]
     int turn = 0;
@@ -138,6 +139,10 @@ __global__ void __launch_bounds__(kNormBlock<TPR>) k_norm_backward(const typenam
     }
     const float over = 1.f / (float)dim;
     uint32_t rx[CH][4], rd[CH][4];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rx[c][i] = rd[c][i] = 0;
     float mu = 0.f, s = 0.f;
     auto fetch = [&](uint32_t r) {
         const typename TypeOf<T>::type *px = x + worker * xs.worker + r * xs.row, *pd = dy + worker * dys.worker + r * dys.row;
@@ -150,11 +155,18 @@ __global__ void __launch_bounds__(kNormBlock<TPR>) k_norm_backward(const typenam
         s = rstd[(int64_t)worker * t + r];
     };
     if (lo + group < hi) fetch(lo + group);
-    for (uint32_t r = lo + group; r < hi; r += GROUPS) {
+    for (uint32_t first = lo; first < hi; first += GROUPS) {         // as often for every row's threads: they meet in row_sum
+        const uint32_t r = first + group;
         float z[CH][N], d[CH][N];
         const float scale = s, shift = mu;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) { widen<T>(rx[c], z[c]); widen<T>(rd[c], d[c]); }
+        for (int c = 0; c < CH; ++c) {
+            widen<T>(rx[c], z[c]);
+            widen<T>(rd[c], d[c]);
+            if (GROUPS > 1 && r >= hi)
+#pragma unroll
+                for (int i = 0; i < N; ++i) z[c][i] = d[c][i] = 0.f;
+        }
         if (r + GROUPS < hi) fetch(r + GROUPS);
         float sa = 0.f, saz = 0.f;
 #pragma unroll
@@ -169,6 +181,7 @@ __global__ void __launch_bounds__(kNormBlock<TPR>) k_norm_backward(const typenam
                 saz = __builtin_fmaf(d[c][i], z[c][i], saz);
             }
         const float2 sums = row_sum<TPR>(sa, saz, buf, turn);
+        if (GROUPS > 1 && r >= hi) continue;
         const float ma = sums.x * over, maz = sums.y * over;
         typename TypeOf<T>::type *o = dx + worker * dxs.worker + r * dxs.row;
 #pragma unroll
@@ -342,7 +355,7 @@ static bool by_row(int64_t dim, F f)
 // parts that the rows of a worker are split into, in the backward pass
 static int norm_parts(int32_t n, int64_t t)
 {
-    const int64_t most = (kNormBlocks + n - 1) / n, some = (t + 3) / 4;
+    const int64_t most = n < kNormBlocks ? kNormBlocks / n : 1, some = (t + 3) / 4;       // no workgroup left for a second round
     return (int)(some < 1 ? 1 : some < most ? some : most);
 }
 
@@ -421,7 +434,7 @@ int layer_norm_backward(sams_norm *c, int64_t t, const void *dy, int64_t dy_work
     SAMS_BY_TYPE(c->type, T, {
         typedef TypeOf<T>::type E;
         if (!by_row<T, T == SAMS_F32 ? 2 : 1>(c->dim, [&](auto tpr, auto ch) {
-                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, BLOCK = kNormBlock<TPR>, GROUPS = BLOCK / TPR;
+                constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, BLOCK = kNormBackBlock<TPR>, GROUPS = BLOCK / TPR;
                 hipLaunchKernelGGL((k_norm_backward<T, TPR, CH>), dim3((unsigned)parts, (unsigned)c->n), dim3(BLOCK), (unsigned)(GROUPS / 2 * 2 * c->dim * 4), c->stream,
                                    (const E *)dy, Rows{dy_worker, dy_row}, (const E *)x, Rows{x_worker, x_row}, weight, mean, rstd, (E *)dx, Rows{dx_worker, dx_row}, part, (uint32_t)t,
                                    c->dim);
