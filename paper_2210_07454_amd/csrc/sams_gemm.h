@@ -3,6 +3,7 @@
 #pragma once
 #include <math.h>
 #include <algorithm>
+#include <type_traits>
 
 #include "sams_ctx.h"
 
@@ -27,8 +28,9 @@ struct Operand {
     int64_t size;       // extent along m (or n), in numbers
 };
 
-template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_>
+template <int BM_, int BN_, int WAVES_M_, int WAVES_N_, int STAGES_, bool SPREAD16_ = false, bool SPREAD_PAIRS_ = false>
 struct Shape {
+    static constexpr bool SPREAD16 = SPREAD16_, SPREAD_PAIRS = SPREAD_PAIRS_;      // loads spread over two groups (see tile_product)
     static constexpr int BM = BM_, BN = BN_, WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, STAGES = STAGES_;
     static constexpr int THREADS = 64 * WAVES_M * WAVES_N;
     static constexpr int MI = BM / WAVES_M / 32, NI = BN / WAVES_N / 32;
@@ -104,20 +106,22 @@ struct Loader {
         step = K_ROWS ? tile_k<KIND>() * op.ld * 2 : 128;
     }
 
-    // left: k's from the start of this stage on
-    __device__ __forceinline__ void load(char *lds, int wave, int tid, int left)
+    // before a stage's pieces are loaded.  left: k's from its start on
+    __device__ __forceinline__ void begin(int tid, int left)
     {
         if (left < tile_k<KIND>()) {                                 // the last stage
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (k_of(i, tid) >= left) off[i] = kTileSpan;
         }
+    }
+    __device__ __forceinline__ void load(char *lds, int wave, int i)
+    {
         const u32x4 buffer = {uniform((uint32_t)(uintptr_t)base), uniform((uint32_t)((uintptr_t)base >> 32) & 0xffff), kTileSpan, 0x00020000};
         const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
-#pragma unroll
-        for (int i = 0; i < N; ++i) load_to_lds(buffer, off[i], uniform(at + i * THREADS * 16));
-        base += step;
+        load_to_lds(buffer, off[i], uniform(at + i * THREADS * 16));
     }
+    __device__ __forceinline__ void next() { base += step; }
 };
 
 // A lane's 8 k's of its row (lane % 32) for one matrix instruction: k = kbase + 8 * (lane / 32) .. + 7, of part `half` where split.
@@ -156,7 +160,10 @@ __device__ __forceinline__ void wait_and_meet()
 //
 // A wavefront has the fragments of the next 16 k's on their way while the matrix instructions of these run, across stages too: the
 // one barrier of a stage stands before its last fragments are used, when they are in registers and the next stage has
-// landed; behind it the stage just read is filled anew.
+// landed; behind it the stage just read is filled anew.  The order of instructions is written out: after each matrix instruction a
+// share of the reads of fragments.  Large tiles of 16-bit numbers have the loads spread over the two groups behind the barrier too
+// (issued at once they hold a wavefront back for as long as a group takes: 4096^3 121 us, spread 112); the others need them early more
+// (pairs in Middle, one tile a CU, k = 1536: 31 us at once, 40 spread).
 template <class S, int KIND, bool A_K_ROWS, bool B_K_ROWS>
 __device__ __forceinline__ void tile_product(f32x16 (&acc)[S::MI][S::NI], const Operand &A, int64_t m0, const Operand &B, int64_t n0, int64_t k_first,
                                              int64_t k, char *lds)
@@ -171,63 +178,86 @@ __device__ __forceinline__ void tile_product(f32x16 (&acc)[S::MI][S::NI], const 
     la.init(A, m0, k_first, tid);
     lb.init(B, n0, k_first, tid);
     int left = (int)k;
-    auto fetch = [&](char *to) {
-        la.load(to, wave, tid, left);
-        lb.load(to + S::A_BYTES, wave, tid, left);
+    constexpr int LOADS = LA::N + LB::N, PRODUCTS = S::MI * S::NI * (KIND == SPLIT ? 3 : 1), FRAGMENTS = HALVES * (S::MI + S::NI);
+    auto load = [&](char *to, int i) {
+        if (i < LA::N) la.load(to, wave, i);
+        else lb.load(to + S::A_BYTES, wave, i - LA::N);
+    };
+    auto begin = [&]() {
+        la.begin(tid, left);
+        lb.begin(tid, left);
         left -= BK;
+    };
+    auto next = [&]() {
+        la.next();
+        lb.next();
+    };
+    auto fetch = [&](char *to) {
+        begin();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(to, i);
+        next();
     };
     if (k <= 0) return;
     u32x4 fa[2][HALVES][S::MI], fb[2][HALVES][S::NI];
-    auto read = [&](const char *stage, int group, int into) {
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) fa[into][h][i] = fragment<S::BM, KIND, A_K_ROWS>(stage, wm + i * 32, group * 16, h, lane);
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) fb[into][h][j] = fragment<S::BN, KIND, B_K_ROWS>(stage + S::A_BYTES, wn + j * 32, group * 16, h, lane);
-        }
+    auto read = [&](const char *stage, int group, int into, int f) {     // first parts first
+        const int h = f / (S::MI + S::NI), e = f % (S::MI + S::NI);
+        if (e < S::MI) fa[into][h][e] = fragment<S::BM, KIND, A_K_ROWS>(stage, wm + e * 32, group * 16, h, lane);
+        else fb[into][h][e - S::MI] = fragment<S::BN, KIND, B_K_ROWS>(stage + S::A_BYTES, wn + (e - S::MI) * 32, group * 16, h, lane);
     };
-    auto multiply = [&](int from) {
-#pragma unroll
-        for (int q = 0; q < (KIND == SPLIT ? 3 : 1); ++q)
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                for (int j = 0; j < S::NI; ++j) acc[i][j] = mfma<KIND>(fa[from][q == 2 ? HALVES - 1 : 0][i], fb[from][q == 1 ? HALVES - 1 : 0][j], acc[i][j]);
-    };
-    // the order of a group's instructions: after each matrix instruction a share of the reads, which LDS then serves in its shadow
-    auto interleave = [&]() {
-        constexpr int PRODUCTS = S::MI * S::NI * (KIND == SPLIT ? 3 : 1), READS = HALVES * (S::MI * (A_K_ROWS ? 2 : 1) + S::NI * (B_K_ROWS ? 2 : 1));
-        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+    constexpr int BEHIND = (KIND == SPLIT ? S::SPREAD_PAIRS : S::SPREAD16) ? LOADS / 2 : LOADS;        // loads of a stage that the group behind the barrier begins
+    // one group: its matrix instructions, the reads of another one, loads from `first` to `last` of a stage
+    auto work = [&](int from, const char *stage, int group, int into, char *to, int first, int last) {
 #pragma unroll
         for (int p = 0; p < PRODUCTS; ++p) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+            const int q = p / (S::MI * S::NI), i = p / S::NI % S::MI, j = p % S::NI;
+            acc[i][j] = mfma<KIND>(fa[from][q == 2 ? HALVES - 1 : 0][i], fb[from][q == 1 ? HALVES - 1 : 0][j], acc[i][j]);
+#pragma unroll
+            for (int f = FRAGMENTS * p / PRODUCTS; f < FRAGMENTS * (p + 1) / PRODUCTS; ++f) read(stage, group, into, f);
+            if (first < last)
+#pragma unroll
+                for (int l = first + (last - first) * p / PRODUCTS; l < first + (last - first) * (p + 1) / PRODUCTS; ++l) load(to, l);
+            if constexpr (BEHIND < LOADS) __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (BEHIND == LOADS) {                             // the same order, without the compiler's hands tied in each place
+            constexpr int READS = HALVES * (S::MI * (A_K_ROWS ? 2 : 1) + S::NI * (B_K_ROWS ? 2 : 1));
+#pragma unroll
+            for (int p = 0; p < PRODUCTS; ++p) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    constexpr int AHEAD = (S::STAGES - 2) * (LA::N + LB::N);         // loads that may be under way when the next stage is read
+    constexpr int AHEAD = (S::STAGES - 2) * LOADS;                   // loads that may be under way when the next stage is read
+    char *cur = lds, *nxt = lds + STAGE, *const end = lds + S::STAGES * STAGE, *fill = end - STAGE;
 #pragma unroll
-    for (int s = 0; s < S::STAGES; ++s) fetch(lds + s * STAGE);      // past k: zeros, so that the count holds
-    wait_and_meet<AHEAD + LA::N + LB::N>();
-    char *cur = lds, *nxt = lds + STAGE, *const end = lds + S::STAGES * STAGE;
-    read(cur, 0, 0);
+    for (int s = 0; s + 1 < S::STAGES; ++s) fetch(lds + s * STAGE);  // past k: zeros, here and below, so that the count of loads holds
+    begin();
+#pragma unroll
+    for (int i = 0; i < BEHIND; ++i) load(fill, i);
+    wait_and_meet<AHEAD + BEHIND>();
+#pragma unroll
+    for (int f = 0; f < FRAGMENTS; ++f) read(cur, 0, 0, f);
     for (int todo = (int)k; todo > 0; todo -= BK) {
+        work(0, cur, 1, 1, fill, BEHIND, LOADS);                     // the second half of what the last group began to load
+        next();
 #pragma unroll
-        for (int g = 0; g + 1 < GROUPS; ++g) {
-            read(cur, g + 1, (g + 1) & 1);
-            multiply(g & 1);
-            interleave();
-        }
+        for (int g = 1; g + 1 < GROUPS; ++g) work(g & 1, cur, g + 1, (g + 1) & 1, nullptr, 0, 0);
         wait_and_meet<AHEAD>();
-        if (S::STAGES > 2 || left > 0) fetch(cur);
-        read(nxt, 0, 0);                                             // after the last stage: what nobody uses
-        multiply((GROUPS - 1) & 1);
-        interleave();
+        begin();
+        if constexpr (BEHIND == LOADS) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load(cur, i);
+            work((GROUPS - 1) & 1, nxt, 0, 0, nullptr, 0, 0);
+        } else {
+            work((GROUPS - 1) & 1, nxt, 0, 0, cur, 0, BEHIND);
+        }                                                            // (reads after the last stage: what nobody uses)
+        fill = cur;
         cur = nxt;
         nxt = nxt + STAGE == end ? lds : nxt + STAGE;
     }
-    if constexpr (S::STAGES > 2) wait_and_meet<0>();
+    wait_and_meet<0>();
 }
 
 template <class S>
@@ -439,13 +469,20 @@ __device__ __forceinline__ void store_numbers(E *row, int64_t at, int64_t limit,
     }
 }
 
-// A workgroup's place in a grid of tiles.  Workgroups go round the eight XCDs one by one; each XCD gets a contiguous run of tiles, and a run
-// goes over `kTileGroup` columns of tiles at a time, so that what an XCD works on at once shares its operands in that XCD's L2.
+// A workgroup's place in `batch` grids of tiles.  Workgroups go round the eight XCDs one by one; each XCD gets a contiguous run of tiles,
+// so that the tiles of a product meet their operands in few XCDs' L2 (12 products of 768^3 spread over all eight read them from the
+// memory side at 11 TB/s), and a run goes over `kTileGroup` columns of tiles at a time.
 constexpr int kTileGroup = 8;
-__device__ __forceinline__ void tile_place(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni)
+__device__ __forceinline__ uint32_t tile_run(uint32_t id, uint32_t total)
 {
-    const uint32_t total = tiles_m * tiles_n, xcd = id & 7, each = total >> 3, over = total & 7;
-    id = xcd * each + (xcd < over ? xcd : over) + (id >> 3);
+    const uint32_t xcd = id & 7, each = total >> 3, over = total & 7;
+    return xcd * each + (xcd < over ? xcd : over) + (id >> 3);
+}
+__device__ __forceinline__ void tile_place(uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
+{
+    uint32_t id = tile_run(blockIdx.x, gridDim.x);
+    batch = id / (tiles_m * tiles_n);
+    id -= batch * tiles_m * tiles_n;
     const uint32_t group = id / (kTileGroup * tiles_n), first = group * kTileGroup;
     const uint32_t wide = tiles_m - first < kTileGroup ? tiles_m - first : kTileGroup;
     const uint32_t in = id - first * tiles_n;
@@ -455,18 +492,20 @@ __device__ __forceinline__ void tile_place(uint32_t id, uint32_t tiles_m, uint32
 
 // The tiles in use.  At 8192^3 (16 bits; pairs), Large reaches 1.27 PFLOP/s (0.45), 83 % of the library's 1.54 in 16 bits and three times
 // its 0.15 in 32, the card's clock down to 1.85 GHz (1.55) by then; Wide 1.05 (0.36), there for products that make a CU's worth of its tiles
-// but few of Large's; Middle 1.1 (0.40), two workgroups on a CU; Small 0.65 (0.29).  Small's four
-// stages cover a load's way where a CU has one workgroup: 640 x 640 x 12800 takes it 56 us (92), with two stages 95 (186), Middle 134 (267).
-typedef Shape<256, 256, 2, 4, 2> Large;
+// but few of Large's; Middle 1.1, two workgroups on a CU; MiddlePairs (0.39), one; Small 0.65 (0.29).  Small's four
+// stages cover a load's way where a CU has one workgroup: 640 x 640 x 12800 takes it 56 us (92), with two stages 95 (186), Middle 134 and, for
+// pairs, with its two stages 267, MiddlePairs 150.
+typedef Shape<256, 256, 2, 4, 2, true> Large;
 typedef Shape<192, 192, 2, 2, 2> Wide;
 typedef Shape<128, 128, 2, 2, 2> Middle;
+typedef Shape<128, 128, 2, 2, 3, false, true> MiddlePairs;
 typedef Shape<64, 64, 2, 2, 4> Small;
 
 // What a product of m x n x k numbers, `batch` times, is estimated to take in tiles of a size (Large, Wide, Middle, Small), its k cut into
 // `parts`, in ns: a CU's workgroups one after the other, each at the pace it has beside others or, alone on its CU, by itself
 // (measured as above), and what a tile costs before and after its k's.
 struct TileCost { int size; double pace16, alone16, pace_pairs, alone_pairs, fixed; };
-constexpr TileCost kTileCosts[4] = {{256, 26, 26, 75, 75, 5000}, {192, 17, 17, 47.4, 47.4, 3500}, {128, 7.5, 10.5, 21.4, 21.4, 1700}, {64, 3.0, 4.4, 6.9, 7.2, 700}};
+constexpr TileCost kTileCosts[4] = {{256, 26, 26, 75, 75, 5000}, {192, 17, 17, 47.4, 47.4, 3500}, {128, 7.5, 10.5, 22, 12, 3000}, {64, 3.0, 4.4, 6.9, 7.2, 1200}};
 
 static inline double tile_estimate(int shape, bool pairs, double tiles, double k, int parts)
 {
@@ -493,12 +532,12 @@ static inline TileChoice choose_tiles(bool pairs, int64_t batch, int64_t m, int6
     return best;
 }
 
-template <typename F>
+template <int KIND, typename F>
 static void with_tile(int shape, F f)
 {
     if (shape == 0) f(Large());
     else if (shape == 1) f(Wide());
-    else if (shape == 2) f(Middle());
+    else if (shape == 2) f(typename std::conditional<KIND == SPLIT, MiddlePairs, Middle>::type());
     else f(Small());
 }
 

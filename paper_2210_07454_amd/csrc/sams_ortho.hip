@@ -8,9 +8,10 @@
 //
 // Numbers.  Every matrix of the iteration has a bound that the coefficients give on the host: |x_ij| <= the largest singular value,
 // which p keeps below max |p| over the range before.  So they are held as fixed-point-like words: 16-bit floats (11 bits) after
-// scaling by a power of two that puts the bound near the top of their range, one word where the caller's tensors have 16 bits, two
-// (22 bits) where they have 32.  bfloat16 would have 8 bits for the same cost, and nothing here needs its range.  G itself is only
-// scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the first step's products.
+// scaling by a power of two that puts the bound near the top of their range; one word where the caller's tensors are bfloat16 (whose
+// own 8 bits cost the same and would add up to several roundings of the result; nothing here needs their range), two (22 bits)
+// where they are 32-bit or 16-bit floats: with one word 16-bit floats come out eight times as far off as their rounding.  G itself
+// is only scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the first step's products.
 #include <math.h>
 #include <new>
 
@@ -28,6 +29,9 @@ struct sams_ortho {
 namespace sams {
 
 using namespace gemm;
+
+// words between the products: one where the result is rounded to 8 bits anyway, pairs elsewhere
+constexpr int ortho_kind(int type) { return type == SAMS_BF16 ? F16 : SPLIT; }
 
 constexpr int kNormSlices = 512;        // of a matrix, for the sum of its squares
 
@@ -142,9 +146,12 @@ struct OrthoDims {
     int64_t rows, cols, small;          // of X; small = min(rows, cols)
 };
 
-// the tile of the lower triangle with a given number
-__device__ __forceinline__ void triangle(int id, int &i, int &j)
+// a workgroup's tile of the lower triangle, and its matrix
+__device__ __forceinline__ void triangle(int64_t tiles, int &i, int &j, int64_t &matrix)
 {
+    const uint32_t run = tile_run(blockIdx.x, gridDim.x), each = (uint32_t)(tiles * (tiles + 1) / 2);
+    matrix = run / each;
+    const int id = (int)(run % each);
     i = (int)((sqrtf(8.f * (float)id + 1.f) - 1.f) * 0.5f);
     while ((i + 1) * (i + 2) / 2 <= id) ++i;
     while (i * (i + 1) / 2 > id) --i;
@@ -179,14 +186,15 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, Or
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     int ti, tj;
-    triangle((int)blockIdx.x, ti, tj);
+    int64_t matrix;
+    triangle((d.small + S::BM - 1) / S::BM, ti, tj, matrix);
     const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ldx = row_words<KIND>(d.cols), ldg = row_words<KIND>(d.small);
-    const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
+    const Operand X{x + matrix * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, 0, TALL ? d.rows : d.cols, lds);
-    if (scale) f *= scale[blockIdx.y].sigma2;
-    put_symmetric<S, KIND>(gram + blockIdx.y * d.small * ldg, ldg, d.small, m0, n0, acc, lds, [&](int64_t, int64_t, float (&v)[8]) {
+    if (scale) f *= scale[matrix].sigma2;
+    put_symmetric<S, KIND>(gram + matrix * d.small * ldg, ldg, d.small, m0, n0, acc, lds, [&](int64_t, int64_t, float (&v)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
     });
@@ -198,13 +206,14 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram,
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     int ti, tj;
-    triangle((int)blockIdx.x, ti, tj);
+    int64_t matrix;
+    triangle((d.small + S::BM - 1) / S::BM, ti, tj, matrix);
     const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ld = row_words<KIND>(d.small);
-    const Operand A{gram + blockIdx.y * d.small * ld, ld, d.small};
+    const Operand A{gram + matrix * d.small * ld, ld, d.small};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, A, m0, A, n0, 0, d.small, lds);
-    put_symmetric<S, KIND>(poly + blockIdx.y * d.small * ld, ld, d.small, m0, n0, acc, lds, [&](int64_t row, int64_t col, float (&v)[8]) {
+    put_symmetric<S, KIND>(poly + matrix * d.small * ld, ld, d.small, m0, n0, acc, lds, [&](int64_t row, int64_t col, float (&v)[8]) {
         float g[8];
         get8<KIND>(A.p + row * ld, col, g);
 #pragma unroll
@@ -227,24 +236,25 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
                                                             const OrthoScale *scale, uint16_t *next, OrthoOut o)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni;
-    tile_place(blockIdx.x, tiles_m, tiles_n, mi, ni);
+    uint32_t mi, ni, batch;
+    tile_place(tiles_m, tiles_n, mi, ni, batch);
+    const int64_t matrix = batch;
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;            // m: X's columns, n: its rows
     const int64_t ldx = row_words<KIND>(d.cols), ldp = row_words<KIND>(d.small);
-    const Operand X{x + blockIdx.y * d.rows * ldx, ldx, TALL ? d.rows : d.cols}, P{poly + blockIdx.y * d.small * ldp, ldp, d.small};
+    const Operand X{x + matrix * d.rows * ldx, ldx, TALL ? d.rows : d.cols}, P{poly + matrix * d.small * ldp, ldp, d.small};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     if constexpr (TALL) tile_product<S, KIND, false, false>(acc, P, m0, X, n0, 0, d.small, lds);
     else tile_product<S, KIND, true, false>(acc, X, m0, P, n0, 0, d.small, lds);
-    if (scale) f *= scale[blockIdx.y].sigma;
+    if (scale) f *= scale[matrix].sigma;
     const int64_t width = row_numbers<KIND>(d.cols);
     eights<S, false>(acc, lds, [&](int dn, int dm, const float (&raw)[8]) {
         const int64_t r = n0 + dn, col = m0 + dm;
         if (r >= d.rows || col >= (LAST ? d.cols : width)) return;
         if constexpr (LAST) {
             typedef typename TypeOf<T>::type E;
-            E *out = (E *)o.out + blockIdx.y * o.out_mat + r * o.out_row;
-            const float *px = o.x ? o.x + blockIdx.y * o.x_mat + r * d.cols : nullptr;
+            E *out = (E *)o.out + matrix * o.out_mat + r * o.out_row;
+            const float *px = o.x ? o.x + matrix * o.x_mat + r * d.cols : nullptr;
             E e8[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -263,7 +273,7 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = col + e < d.cols ? raw[e] * f : 0.f;
-            put8<KIND>(next + blockIdx.y * d.rows * ldx + r * ldx, col, v);
+            put8<KIND>(next + matrix * d.rows * ldx + r * ldx, col, v);
         }
     });
 }
@@ -400,7 +410,7 @@ template <int T, bool TALL>
 __global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int rows, int cols, float eps, const double *part,
                                                                   SmallSteps steps, OrthoOut o)
 {
-    constexpr bool PAIRS = T == SAMS_F32;
+    constexpr bool PAIRS = ortho_kind(T) == SPLIT;
     typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) uint16_t lds[kSmallLds / 2];
     __shared__ double sums[kSmallWaves];
@@ -555,23 +565,23 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
         const OrthoScale *first = s == 0 ? scale : nullptr;
         auto square = [&](auto shape) {
             const int64_t ts = (d.small + decltype(shape)::BM - 1) / decltype(shape)::BM;
-            return dim3((unsigned)(ts * (ts + 1) / 2), (unsigned)batch);
+            return dim3((unsigned)(ts * (ts + 1) / 2 * batch));
         };
-        with_tile(of_gram, [&](auto shape) {
+        with_tile<KIND>(of_gram, [&](auto shape) {
             typedef decltype(shape) S;
             if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
             else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
         });
-        with_tile(of_poly, [&](auto shape) {
+        with_tile<KIND>(of_poly, [&](auto shape) {
             typedef decltype(shape) S;
             hipLaunchKernelGGL((k_ortho_poly<S, KIND>), square(shape), dim3(S::THREADS), 0, c->stream, gram, d, p.a, p.b, p.c, poly);
         });
         const bool last = s + 1 == plan.count;
-        with_tile(of_apply, [&](auto shape) {
+        with_tile<KIND>(of_apply, [&](auto shape) {
             typedef decltype(shape) S;
             const uint32_t tm = (uint32_t)((d.cols + S::BM - 1) / S::BM), tn = (uint32_t)((d.rows + S::BN - 1) / S::BN);
             auto apply = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3(tm * tn, (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, p.f_apply, first, next, o);
+                hipLaunchKernelGGL(kernel, dim3(tm * tn * (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, p.f_apply, first, next, o);
             };
             if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
             else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);
@@ -587,7 +597,7 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
 template <int T>
 static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, bool squares_made, int steps, const float *coef, float eps, const OrthoOut &o)
 {
-    constexpr int KIND = T == SAMS_F32 ? SPLIT : F16;
+    constexpr int KIND = ortho_kind(T);
     typedef typename TypeOf<T>::type E;
     double *part = c->scratch.at<double>(c->part);
     SmallSteps plan;
@@ -631,7 +641,8 @@ int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t col
     c->batch = batch; c->rows = rows; c->cols = cols; c->type = type;
     c->stream = (hipStream_t)hip_stream;
     const int64_t small = rows < cols ? rows : cols;
-    const int64_t ldx = type == SAMS_F32 ? row_words<SPLIT>(cols) : row_words<F16>(cols), ldp = type == SAMS_F32 ? row_words<SPLIT>(small) : row_words<F16>(small);
+    const bool pairs = ortho_kind(type) == SPLIT;
+    const int64_t ldx = pairs ? row_words<SPLIT>(cols) : row_words<F16>(cols), ldp = pairs ? row_words<SPLIT>(small) : row_words<F16>(small);
     for (int q = 0; q < 2; ++q) c->x[q] = c->scratch.reserve(batch * rows * ldx * 2);
     c->gram = c->scratch.reserve(batch * small * ldp * 2);
     c->poly = c->scratch.reserve(batch * small * ldp * 2);

@@ -25,7 +25,7 @@ struct sams_xent {
     int64_t t_max, dim, vocab, piece;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t h, w, dz, dh, part, token, inv, amax, exps;
+    int64_t h, w, dz, dh, part, token, at_label, inv, amax, exps;
 };
 
 namespace sams {
@@ -151,20 +151,36 @@ __device__ __forceinline__ float unscale(const int32_t *exps, int which)        
     return ldexpf(1.f, -(which == 0 ? exps[0] : which == 1 ? exps[1] : exps[0] + exps[1]));
 }
 
+// (largest, sum of 2^(number - largest)) of two sets of numbers
+__device__ __forceinline__ float2 join_sums(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
+    return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
+}
+
 // Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).  A lane holds numbers
-// of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.
+// of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's logit, in the same units, is
+// left in `at_label` by the lane that holds it: the loss, the difference of the two, keeps its digits where the label is nearly certain.
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, float2 *part)
+__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels,
+                                                           float2 *part, float *at_label)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni;
-    tile_place(blockIdx.x, tiles_v, tiles_t, mi, ni);
+    uint32_t mi, ni, batch;
+    tile_place(tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
+    int label[S::NI];                                                // where a token's label lies among the wavefront's words; -1: elsewhere
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) {
+        const int64_t row = n0 + (wn * S::NI + j) * 32 + (lane & 31), at = row < H.size ? labels[row] : -1;
+        const int64_t in = at - m0 - wm * S::MI * 32;
+        label[j] = at < W.size && in >= 0 && in < S::MI * 32 ? (int)in : -1;
+    }
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
     const float f = kLog2e * unscale<KIND>(exps, 2);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
     if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
 #pragma unroll
         for (int i = 0; i < S::MI; ++i)
@@ -182,6 +198,14 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
         for (int i = 0; i < S::MI; ++i)
 #pragma unroll
             for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
+        if (__any(label[j] >= 0)) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) z = (label[j] & ~4) == i * 32 + 8 * (q >> 2) + (q & 3) ? acc[i][j][q] : z;
+            if (label[j] >= 0 && (label[j] >> 2 & 1) == lane >> 5) at_label[n0 + (wn * S::NI + j) * 32 + (lane & 31)] = z * f;
+        }
         top = fmaxf(top, __shfl_xor(top, 32)) * f;
         const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
@@ -195,45 +219,35 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
     for (int i = threadIdx.x; i < S::BN; i += S::THREADS) {
         float2 a = joined[i];
 #pragma unroll
-        for (int w = 1; w < S::WAVES_M; ++w) {
-            const float2 b = joined[w * S::BN + i];
-            const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
-            a = make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
-        }
+        for (int w = 1; w < S::WAVES_M; ++w) a = join_sums(a, joined[w * S::BN + i]);
         if (n0 + i < H.size) part[mi * H.size + n0 + i] = a;
     }
 }
 
-// A token's log-sum over the tiles, its label's logit, its loss; a wavefront per token.
-template <int T>
-__global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles_v, const typename TypeOf<T>::type *h, Rows hs, const typename TypeOf<T>::type *w, int64_t w_row,
-                                                   const int64_t *labels, int64_t t, int64_t rows, int64_t dim, int64_t vocab, float *lse, float *token)
+// A token's log-sum over the tiles and its loss: 16 tokens a workgroup (a line of `part`), each tile's by one of 16 threads in turn.
+__global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles_v, const float *at_label, const int64_t *labels, int64_t rows, int64_t vocab, float *lse,
+                                                   float *token)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
+    __shared__ float2 joined[4][16];
+    const int r = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t row = blockIdx.x * (int64_t)16 + r;
+    float2 sums = make_float2(-INFINITY, 0.f);
+    if (row < rows)
+#pragma unroll 4
+        for (int i = g; i < tiles_v; i += 16) sums = join_sums(sums, part[i * rows + row]);
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) sums = join_sums(sums, make_float2(__shfl_xor(sums.x, o), __shfl_xor(sums.y, o)));
+    if ((threadIdx.x & 63) < 16) joined[threadIdx.x >> 6][r] = sums;
+    __syncthreads();
+    if (threadIdx.x >= 16 || row >= rows) return;
     if (!takes_part(labels, row, vocab)) {
-        if (lane == 0) lse[row] = token[row] = 0.f;
+        lse[row] = token[row] = 0.f;
         return;
     }
-    float top = -INFINITY;
-    for (int i = lane; i < tiles_v; i += 64) top = fmaxf(top, part[i * rows + row].x);
-    top = wave_max(top);
-    float sum = 0.f;
-    for (int i = lane; i < tiles_v; i += 64) {
-        const float2 p = part[i * rows + row];
-        sum += p.y * __builtin_amdgcn_exp2f(p.x - top);
-    }
-    sum = wave_sum(sum);
-    const typename TypeOf<T>::type *ph = h + row / t * hs.worker + row % t * hs.row, *pw = w + labels[row] * w_row;
-    float dot = 0.f;
-    for (int64_t i = lane; i < dim; i += 64) dot = __builtin_fmaf((float)ph[i], (float)pw[i], dot);
-    dot = wave_sum(dot);
-    if (lane == 0) {
-        const float l = top * (1.f / kLog2e) + logf(sum);
-        lse[row] = l;
-        token[row] = l - dot;
-    }
+    sums = join_sums(join_sums(joined[0][r], joined[1][r]), join_sums(joined[2][r], joined[3][r]));
+    const float log_sum = log2f(sums.y);
+    lse[row] = (sums.x + log_sum) * (1.f / kLog2e);
+    token[row] = ((sums.x - at_label[row]) + log_sum) * (1.f / kLog2e);
 }
 
 // a worker's mean; tokens are added up in the same order every time
@@ -263,8 +277,8 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
                                                         int64_t vocab, const float *lse, uint16_t *dz)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni;
-    tile_place(blockIdx.x, tiles_v, tiles_t, mi, ni);
+    uint32_t mi, ni, batch;
+    tile_place(tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
@@ -313,9 +327,9 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
 {
     typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni;
-    tile_place(blockIdx.x, tiles_d, tiles_v, mi, ni);
-    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN, worker = blockIdx.y;
+    uint32_t mi, ni, batch;
+    tile_place(tiles_d, tiles_v, mi, ni, batch);
+    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN, worker = batch;
     const int64_t ldz = row_words<KIND>(piece), ldh = row_words<KIND>(dim);
     const Operand Z{dz + worker * t * ldz, ldz, piece}, H{h + worker * t * ldh, ldh, dim};
     f32x16 acc[S::MI][S::NI];
@@ -346,22 +360,22 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
         });
 }
 
-// dh over one piece, its vocabulary cut into gridDim.y parts; a part's sums are added to those of the pieces before.  part: [parts][rows][pitch]
+// dh over one piece, its vocabulary cut into parts; a part's sums are added to those of the pieces before.  part: [parts][rows][pitch]
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
-                                                        int64_t pitch)
+                                                        int64_t pitch, uint32_t parts)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni;
-    tile_place(blockIdx.x, tiles_d, tiles_t, mi, ni);
+    uint32_t mi, ni, batch;
+    tile_place(tiles_d, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     const int64_t steps = (piece + tile_k<KIND>() - 1) / tile_k<KIND>();
-    const int64_t lo = steps * blockIdx.y / gridDim.y * tile_k<KIND>(), hi = steps * (blockIdx.y + 1) / gridDim.y * tile_k<KIND>();
+    const int64_t lo = steps * batch / parts * tile_k<KIND>(), hi = steps * (batch + 1) / parts * tile_k<KIND>();
     const Operand Z{dz, row_words<KIND>(piece), rows};
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, true, false>(acc, W, m0, Z, n0, lo, (hi < piece ? hi : piece) - lo, lds);
-    float *out = part + (blockIdx.y * rows + n0) * pitch + m0;
+    float *out = part + (batch * rows + n0) * pitch + m0;
     store_rows<S, 4, false>(acc, lds, [](int) { return 0; }, [](int, int, const float (&v)[4]) { return pack_numbers<float>(v); },
                             [&](int n, int at, u32x4 w) {
                                 if (n0 + n >= rows || m0 + at / 4 >= pitch) return;
@@ -445,22 +459,20 @@ template <int T>
 static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, float *loss, float *lse)
 {
     constexpr int KIND = kind_of<T>();
-    typedef typename TypeOf<T>::type E;
     const int64_t rows = c->n * t;
-    float *token = c->scratch.at<float>(c->token);
+    float *token = c->scratch.at<float>(c->token), *at_label = c->scratch.at<float>(c->at_label);
     if (rows) {
         Operand H, W;
         SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, nullptr, &H, &W)));
         float2 *part = c->scratch.at<float2>(c->part);
         uint32_t tv = 0;
-        with_tile(choose_tiles(KIND == SPLIT, 1, c->vocab, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
+        with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, c->vocab, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
             typedef decltype(shape) S;
             tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
             const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), part);
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), labels, part, at_label);
         });
-        hipLaunchKernelGGL(k_xent_join<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, (int)tv, (const E *)h, hs, (const E *)w, w_row, labels, t, rows, c->dim,
-                           c->vocab, lse, token);
+        hipLaunchKernelGGL(k_xent_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, part, (int)tv, at_label, labels, rows, c->vocab, lse, token);
     }
     hipLaunchKernelGGL(k_xent_loss, dim3((unsigned)c->n), dim3(256), 0, c->stream, token, labels, t, c->vocab, loss);
     SAMS_HIP(hipGetLastError());
@@ -487,16 +499,16 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
         const int64_t piece = c->vocab - v0 < c->piece ? c->vocab - v0 : c->piece;
         const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
         if (rows)
-            with_tile(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
+            with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
                 typedef decltype(shape) S;
                 const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
                 hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, labels, v0, c->vocab, lse, dz);
             });
-        with_tile(choose_tiles(KIND == SPLIT, c->n, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
+        with_tile<KIND>(choose_tiles(KIND == SPLIT, c->n, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
             typedef decltype(shape) S;
             const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
             auto weight = [&](auto kernel, auto *out) {
-                hipLaunchKernelGGL(kernel, dim3(td * tv, (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws);
+                hipLaunchKernelGGL(kernel, dim3(td * tv * (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws);
             };
             if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
             else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
@@ -504,11 +516,11 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
             else weight(k_xent_dw<S, KIND, T, false>, (E *)dw);
         });
         if (rows)
-            with_tile(hidden.shape, [&](auto shape) {
+            with_tile<KIND>(hidden.shape, [&](auto shape) {
                 typedef decltype(shape) S;
                 const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt, (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt, v0 == 0,
-                                   part, pitch);
+                hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt * (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt, v0 == 0,
+                                   part, pitch, (uint32_t)parts);
             });
         SAMS_HIP(hipGetLastError());
     }
@@ -547,6 +559,7 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     c->w = c->scratch.reserve(vocab * ld * 2);
     c->part = c->scratch.reserve(rows * ((vocab + Small::BM - 1) / Small::BM) * 8);
     c->token = c->scratch.reserve(rows * 4);
+    c->at_label = c->scratch.reserve(rows * 4);
     c->inv = c->scratch.reserve(n * 4);
     c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
     c->exps = c->scratch.reserve(2 * 4);
