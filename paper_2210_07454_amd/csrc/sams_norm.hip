@@ -353,9 +353,9 @@ static bool by_row(int64_t dim, F f)
 }
 
 // parts that the rows of a worker are split into, in the backward pass
-static int norm_parts(int32_t n, int64_t t)
+static int norm_parts(int32_t n, int64_t t, bool wide)
 {
-    const int64_t most = n < kNormBlocks ? kNormBlocks / n : 1, some = (t + 3) / 4;       // no workgroup left for a second round
+    const int64_t blocks = wide ? kNormBlocks / 2 : kNormBlocks, most = n < blocks ? blocks / n : 1, some = (t + 3) / 4;        // no workgroup left for a second round
     return (int)(some < 1 ? 1 : some < most ? some : most);
 }
 
@@ -374,7 +374,7 @@ int sams_norm_create(sams_norm **out, int32_t n, int64_t t_max, int64_t dim, int
     if (!c) return SAMS_ENOMEM;
     c->n = n; c->t_max = t_max; c->dim = dim; c->type = type;
     c->stream = (hipStream_t)hip_stream;
-    c->part = c->scratch.reserve((int64_t)n * norm_parts(n, t_max) * 2 * dim * 4);
+    c->part = c->scratch.reserve((int64_t)n * norm_parts(n, t_max, false) * 2 * dim * 4);
     const int rc = c->scratch.take();
     if (rc != SAMS_OK) { delete c; return rc; }
     *out = c;
@@ -430,11 +430,12 @@ int layer_norm_backward(sams_norm *c, int64_t t, const void *dy, int64_t dy_work
     }
     const int64_t rows = c->n * t;
     float *part = c->scratch.at<float>(c->part);
-    const int parts = norm_parts(c->n, t);
+    int parts = norm_parts(c->n, t, false);
     SAMS_BY_TYPE(c->type, T, {
         typedef TypeOf<T>::type E;
         if (!by_row<T, T == SAMS_F32 ? 2 : 1>(c->dim, [&](auto tpr, auto ch) {
                 constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value, BLOCK = kNormBackBlock<TPR>, GROUPS = BLOCK / TPR;
+                parts = norm_parts(c->n, t, BLOCK > 512);
                 hipLaunchKernelGGL((k_norm_backward<T, TPR, CH>), dim3((unsigned)parts, (unsigned)c->n), dim3(BLOCK), (unsigned)(GROUPS / 2 * 2 * c->dim * 4), c->stream,
                                    (const E *)dy, Rows{dy_worker, dy_row}, (const E *)x, Rows{x_worker, x_row}, weight, mean, rstd, (E *)dx, Rows{dx_worker, dx_row}, part, (uint32_t)t,
                                    c->dim);
