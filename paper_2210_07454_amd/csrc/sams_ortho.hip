@@ -8,10 +8,10 @@
 //
 // Numbers.  Every matrix of the iteration has a bound that the coefficients give on the host: |x_ij| <= the largest singular value,
 // which p keeps below max |p| over the range before.  So they are held as fixed-point-like words: 16-bit floats (11 bits) after
-// scaling by a power of two that puts the bound near the top of their range; one word where the caller's tensors are bfloat16 (whose
-// own 8 bits cost the same and would add up to several roundings of the result; nothing here needs their range), two (22 bits)
-// where they are 32-bit or 16-bit floats: with one word 16-bit floats come out eight times as far off as their rounding.  G itself
-// is only scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the first step's products.
+// scaling by a power of two that puts the bound near the top of their range: pairs of words (22 bits), or single ones for large bfloat16
+// matrices (bfloat16's own 8 bits cost the same and would add up to several roundings of the result; nothing here needs their
+// range).  G itself is only scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the
+// first step's products.
 #include <math.h>
 #include <new>
 
@@ -30,8 +30,11 @@ namespace sams {
 
 using namespace gemm;
 
-// words between the products: one where the result is rounded to 8 bits anyway, pairs elsewhere
-constexpr int ortho_kind(int type) { return type == SAMS_BF16 ? F16 : SPLIT; }
+// Words between the products are pairs, but single ones for large bfloat16 matrices: there the roundings of a matrix's many numbers average
+// out against its singular directions.  Off the 64-bit result (2-norm; bfloat16's own rounding is 1.7e-3 of it): single words 3.6e-3 at
+// 32 x 768, 2.3e-3 at 512 x 8013, 2.0e-3 at 1024 x 1024, 1.9e-3 at 4096 x 8192, where pairs would take about twice the time.
+constexpr int64_t kSingleMin = 1024;    // of the shorter side
+static bool ortho_pairs(int type, int64_t rows, int64_t cols) { return type != SAMS_BF16 || rows < kSingleMin || cols < kSingleMin; }
 
 constexpr int kNormSlices = 512;        // of a matrix, for the sum of its squares
 
@@ -280,8 +283,8 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
 
 // ---- matrices that fit one workgroup's LDS: all steps in one launch ----
 //
-// X and one square matrix (A, then P in its place) stay in LDS as planes of 16-bit floats (the first parts, then the second ones where
-// numbers are pairs), rows 16 bytes longer than whole fragments, so that rows next to each other start on other banks.  Sixteen wavefronts
+// X and one square matrix (A, then P in its place) stay in LDS as planes of 16-bit floats (the pairs' first parts, then the second
+// ones), rows 16 bytes longer than whole fragments, so that rows next to each other start on other banks.  Sixteen wavefronts
 // share out 32 x 32 tiles, hold their results until all have read what these replace, and write them over it.
 constexpr int kSmallWaves = 16, kSmallTiles = 3;                    // tiles a wavefront can hold
 constexpr int kSmallLds = 163840 - 1024;
@@ -302,11 +305,11 @@ static inline __host__ __device__ SmallLayout small_layout(int64_t rows, int64_t
     l.plane_s = l.small32 * l.pitch_s;
     return l;
 }
-static bool small_fits(int64_t rows, int64_t cols, bool pairs)
+static bool small_fits(int64_t rows, int64_t cols)
 {
     if (rows > 4096 || cols > 4096) return false;
     const SmallLayout l = small_layout(rows, cols);
-    return (int64_t)(l.plane_x + l.plane_s) * (pairs ? 4 : 2) <= kSmallLds && l.rows32 / 32 * (l.cols32 / 32) <= kSmallWaves * kSmallTiles &&
+    return (int64_t)(l.plane_x + l.plane_s) * 4 <= kSmallLds && l.rows32 / 32 * (l.cols32 / 32) <= kSmallWaves * kSmallTiles &&
            l.small32 / 32 * (l.small32 / 32) <= kSmallWaves * kSmallTiles;
 }
 
@@ -327,7 +330,7 @@ __device__ __forceinline__ u32x4 small_fragment_k(const uint16_t *m, int pitch, 
 }
 
 // acc[t] = the product of tile (m, n) number wave + kSmallWaves t, n fastest, over k (a multiple of 32); A_K, B_K: rows are k's
-template <bool PAIRS, bool A_K, bool B_K>
+template <bool A_K, bool B_K>
 __device__ __forceinline__ void small_product(f32x16 (&acc)[kSmallTiles], const uint16_t *a, int pitch_a, int plane_a, const uint16_t *b, int pitch_b, int plane_b, int tiles,
                                               int tiles_n, int k, int lane, int wave)
 {
@@ -344,7 +347,7 @@ __device__ __forceinline__ void small_product(f32x16 (&acc)[kSmallTiles], const 
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int h = 0; h < (PAIRS ? 2 : 1); ++h) {
+                for (int h = 0; h < 2; ++h) {
                     const int at = k0 + 16 * u;
                     fa[u][h] = A_K ? small_fragment_k(a + h * plane_a, pitch_a, m0, at, lane) : small_fragment(a + h * plane_a, pitch_a, m0, at, lane);
                     fb[u][h] = B_K ? small_fragment_k(b + h * plane_b, pitch_b, n0, at, lane) : small_fragment(b + h * plane_b, pitch_b, n0, at, lane);
@@ -352,10 +355,8 @@ __device__ __forceinline__ void small_product(f32x16 (&acc)[kSmallTiles], const 
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 acc[t] = mfma<F16>(fa[u][0], fb[u][0], acc[t]);
-                if constexpr (PAIRS) {
-                    acc[t] = mfma<F16>(fa[u][0], fb[u][1], acc[t]);
-                    acc[t] = mfma<F16>(fa[u][1], fb[u][0], acc[t]);
-                }
+                acc[t] = mfma<F16>(fa[u][0], fb[u][1], acc[t]);
+                acc[t] = mfma<F16>(fa[u][1], fb[u][0], acc[t]);
             }
         }
     }
@@ -379,30 +380,19 @@ __device__ __forceinline__ void small_fours(const f32x16 (&acc)[kSmallTiles], in
     }
 }
 
-template <bool PAIRS>
 __device__ __forceinline__ void small_put(uint16_t *at, int plane, const float (&v)[4])
 {
-    if constexpr (PAIRS) {
-        const u32x4 w = pack_words<SPLIT>(v);
-        *(words2 *)at = words2{w[0], w[1]};
-        *(words2 *)(at + plane) = words2{w[2], w[3]};
-    } else {
-        *(words2 *)at = pack_words<F16>(v);
-    }
+    const u32x4 w = pack_words<SPLIT>(v);
+    *(words2 *)at = words2{w[0], w[1]};
+    *(words2 *)(at + plane) = words2{w[2], w[3]};
 }
 
-template <bool PAIRS>
 __device__ __forceinline__ void small_get(const uint16_t *at, int plane, float (&v)[4])
 {
     typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-    const half4 a = *(const half4 *)at;
+    const half4 a = *(const half4 *)at, b = *(const half4 *)(at + plane);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)a[e];
-    if constexpr (PAIRS) {
-        const half4 b = *(const half4 *)(at + plane);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += (float)b[e];
-    }
+    for (int e = 0; e < 4; ++e) v[e] = (float)a[e] + (float)b[e];
 }
 
 // part: the sums of squares where they are made already (part_count of them a matrix), else null
@@ -410,14 +400,13 @@ template <int T, bool TALL>
 __global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename TypeOf<T>::type *g, int64_t g_mat, int64_t g_row, int rows, int cols, float eps, const double *part,
                                                                   SmallSteps steps, OrthoOut o)
 {
-    constexpr bool PAIRS = ortho_kind(T) == SPLIT;
     typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) uint16_t lds[kSmallLds / 2];
     __shared__ double sums[kSmallWaves];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int lane = tid & 63;
     const SmallLayout l = small_layout(rows, cols);
-    uint16_t *x = lds, *sq = lds + l.plane_x * (PAIRS ? 2 : 1);
+    uint16_t *x = lds, *sq = lds + l.plane_x * 2;
     const E *pg = g + blockIdx.x * g_mat;
     const int fours = l.cols32 / 4, small = rows < cols ? rows : cols;
     auto load4 = [&](int r, int c, float (&v)[4]) {
@@ -450,7 +439,7 @@ __global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename
         load4(r, c, v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = (float)((double)v[e] * by);
-        small_put<PAIRS>(x + r * l.pitch_x + c, l.plane_x, v);
+        small_put(x + r * l.pitch_x + c, l.plane_x, v);
     }
     __syncthreads();
     f32x16 acc[kSmallTiles];
@@ -458,13 +447,13 @@ __global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename
     for (int step = 0; step < steps.count; ++step) {
         const SmallStep p = steps.step[step];
         const float fg = step ? p.f_gram : p.f_gram * scale.sigma2, fa = step ? p.f_apply : p.f_apply * scale.sigma;
-        small_product<PAIRS, TALL, TALL>(acc, x, l.pitch_x, l.plane_x, x, l.pitch_x, l.plane_x, square, ts, large32, lane, wave);
+        small_product<TALL, TALL>(acc, x, l.pitch_x, l.plane_x, x, l.pitch_x, l.plane_x, square, ts, large32, lane, wave);
         small_fours(acc, square, ts, lane, wave, [&](int r, int c, const float (&v)[4]) {
             const float w[4] = {v[0] * fg, v[1] * fg, v[2] * fg, v[3] * fg};
-            small_put<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, w);
+            small_put(sq + r * l.pitch_s + c, l.plane_s, w);
         });
         __syncthreads();
-        small_product<PAIRS, false, false>(acc, sq, l.pitch_s, l.plane_s, sq, l.pitch_s, l.plane_s, square, ts, l.small32, lane, wave);
+        small_product<false, false>(acc, sq, l.pitch_s, l.plane_s, sq, l.pitch_s, l.plane_s, square, ts, l.small32, lane, wave);
 #pragma unroll
         for (int t = 0; t < kSmallTiles; ++t) {                      // P, still in registers: A is read by the others
             const int id = wave + t * kSmallWaves;
@@ -475,21 +464,21 @@ __global__ void __launch_bounds__(64 * kSmallWaves) k_ortho_small(const typename
             for (int q = 0; q < 4; ++q) {
                 const int r = n0 + (lane & 31), c = m0 + 8 * q + 4 * (lane >> 5);
                 float w[4];
-                small_get<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, w);
+                small_get(sq + r * l.pitch_s + c, l.plane_s, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[t][4 * q + e] = r < small && c + e < small ? (r == c + e ? p.a : 0.f) + p.b * w[e] + p.c * acc[t][4 * q + e] : 0.f;
             }
         }
         __syncthreads();
-        small_fours(acc, square, ts, lane, wave, [&](int r, int c, const float (&v)[4]) { small_put<PAIRS>(sq + r * l.pitch_s + c, l.plane_s, v); });
+        small_fours(acc, square, ts, lane, wave, [&](int r, int c, const float (&v)[4]) { small_put(sq + r * l.pitch_s + c, l.plane_s, v); });
         __syncthreads();
-        if constexpr (TALL) small_product<PAIRS, false, false>(acc, sq, l.pitch_s, l.plane_s, x, l.pitch_x, l.plane_x, tiles, tr, l.small32, lane, wave);
-        else small_product<PAIRS, true, false>(acc, x, l.pitch_x, l.plane_x, sq, l.pitch_s, l.plane_s, tiles, tr, l.small32, lane, wave);
+        if constexpr (TALL) small_product<false, false>(acc, sq, l.pitch_s, l.plane_s, x, l.pitch_x, l.plane_x, tiles, tr, l.small32, lane, wave);
+        else small_product<true, false>(acc, x, l.pitch_x, l.plane_x, sq, l.pitch_s, l.plane_s, tiles, tr, l.small32, lane, wave);
         if (step + 1 < steps.count) {
             __syncthreads();
             small_fours(acc, tiles, tr, lane, wave, [&](int r, int c, const float (&v)[4]) {
                 const float w[4] = {v[0] * fa, v[1] * fa, v[2] * fa, v[3] * fa};
-                small_put<PAIRS>(x + r * l.pitch_x + c, l.plane_x, w);
+                small_put(x + r * l.pitch_x + c, l.plane_x, w);
             });
             __syncthreads();
         } else {
@@ -597,12 +586,11 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
 template <int T>
 static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_mat, int64_t g_row, bool squares_made, int steps, const float *coef, float eps, const OrthoOut &o)
 {
-    constexpr int KIND = ortho_kind(T);
     typedef typename TypeOf<T>::type E;
     double *part = c->scratch.at<double>(c->part);
     SmallSteps plan;
     plan_steps(steps, coef, &plan);
-    if (small_fits(c->rows, c->cols, KIND == SPLIT)) {
+    if (small_fits(c->rows, c->cols)) {
         auto all = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)batch), dim3(64 * kSmallWaves), 0, c->stream, (const E *)g, g_mat, g_row, (int)c->rows, (int)c->cols, eps,
                                squares_made ? part : nullptr, plan, o);
@@ -614,10 +602,16 @@ static int enqueue_ortho(sams_ortho *c, int64_t batch, const void *g, int64_t g_
     }
     if (!squares_made)
         hipLaunchKernelGGL(k_ortho_squares<T>, dim3(kNormSlices, (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, part);
-    hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows, 4, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols, eps,
-                       part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
-    SAMS_HIP(hipGetLastError());
-    return enqueue_steps<KIND, T>(c, batch, plan, o);
+    auto large = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        hipLaunchKernelGGL((k_ortho_words<T, KIND>), dim3((unsigned)grid_for(c->rows, 4, 1024), (unsigned)batch), dim3(256), 0, c->stream, (const E *)g, g_mat, g_row, c->rows, c->cols,
+                           eps, part, c->scratch.at<OrthoScale>(c->scale), c->scratch.at<uint16_t>(c->x[0]));
+        SAMS_HIP(hipGetLastError());
+        return enqueue_steps<KIND, T>(c, batch, plan, o);
+    };
+    if constexpr (T == SAMS_BF16)
+        if (!ortho_pairs(T, c->rows, c->cols)) return large(std::integral_constant<int, F16>());
+    return large(std::integral_constant<int, SPLIT>());
 }
 
 static bool coef_ok(const float *coef)
@@ -641,7 +635,7 @@ int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t col
     c->batch = batch; c->rows = rows; c->cols = cols; c->type = type;
     c->stream = (hipStream_t)hip_stream;
     const int64_t small = rows < cols ? rows : cols;
-    const bool pairs = ortho_kind(type) == SPLIT;
+    const bool pairs = ortho_pairs(type, rows, cols);
     const int64_t ldx = pairs ? row_words<SPLIT>(cols) : row_words<F16>(cols), ldp = pairs ? row_words<SPLIT>(small) : row_words<F16>(small);
     for (int q = 0; q < 2; ++q) c->x[q] = c->scratch.reserve(batch * rows * ldx * 2);
     c->gram = c->scratch.reserve(batch * small * ldp * 2);
