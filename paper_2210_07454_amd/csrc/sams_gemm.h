@@ -505,13 +505,13 @@ typedef Shape<64, 64, 2, 2, 4> Small;
 // `parts`, in ns: a CU's workgroups one after the other, each at the pace it has beside others or, alone on its CU, by itself
 // (measured as above), and what a tile costs before and after its k's.
 struct TileCost { int size; double pace16, alone16, pace_pairs, alone_pairs, fixed; };
-constexpr TileCost kTileCosts[4] = {{256, 26, 26, 75, 75, 5000}, {192, 17, 17, 47.4, 47.4, 3500}, {128, 7.5, 10.5, 22, 12, 3000}, {64, 3.0, 4.4, 6.9, 7.2, 1200}};
+constexpr TileCost kTileCosts[4] = {{256, 26, 26, 75, 75, 5000}, {192, 17, 17, 47.4, 47.4, 3500}, {128, 7.5, 10.5, 22, 17, 3000}, {64, 3.0, 4.4, 6.9, 7.2, 1200}};
 
 static inline double tile_estimate(int shape, bool pairs, double tiles, double k, int parts)
 {
     const TileCost &c = kTileCosts[shape];
     const double rounds = ceil(tiles * parts / 256), each = k / parts;
-    return std::max(rounds * (pairs ? c.pace_pairs : c.pace16), pairs ? c.alone_pairs : c.alone16) * each + rounds * c.fixed;
+    return (rounds > 1 ? rounds * (pairs ? c.pace_pairs : c.pace16) : pairs ? c.alone_pairs : c.alone16) * each + rounds * c.fixed;
 }
 
 struct TileChoice { int shape, parts; };
