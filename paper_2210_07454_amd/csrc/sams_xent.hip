@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <new>
 #include <type_traits>
+#include <utility>
 
 #include "sams_gemm.h"
 #include "sams_train.h"
@@ -170,16 +171,22 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
     tile_place(tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
-    int label[S::NI];                                                // where a token's label lies among the wavefront's words; -1: elsewhere
+    int64_t at[S::NI];                                               // the tokens' labels, under way during the product
 #pragma unroll
     for (int j = 0; j < S::NI; ++j) {
-        const int64_t row = n0 + (wn * S::NI + j) * 32 + (lane & 31), at = row < H.size ? labels[row] : -1;
-        const int64_t in = at - m0 - wm * S::MI * 32;
-        label[j] = at < W.size && in >= 0 && in < S::MI * 32 ? (int)in : -1;
+        const int64_t row = n0 + (wn * S::NI + j) * 32 + (lane & 31);
+        at[j] = row < H.size ? labels[row] : -1;
     }
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
+    int label[S::NI];                                                // where they lie among the wavefront's words; -1: elsewhere
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) {
+        asm volatile("" : "+v"(at[j]));                              // not looked at before
+        const int64_t in = at[j] - m0 - wm * S::MI * 32;
+        label[j] = at[j] < W.size && in >= 0 && in < S::MI * 32 ? (int)in : -1;
+    }
     const float f = kLog2e * unscale<KIND>(exps, 2);
     if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
 #pragma unroll
@@ -302,41 +309,52 @@ __global__ void __launch_bounds__(256) k_xent_loss(const float *token, const int
 }
 
 // dz of one piece of the vocabulary (W: the piece), a row of words per token
+struct Token { float base; int label; };                             // log2 of the scale less the log-sum; the label's place in the tile
+constexpr int kNoLabel = -1;
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
                                                         int64_t vocab, const float *lse, uint16_t *dz)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
+    __shared__ Token tokens[S::BN];
     uint32_t mi, ni, batch;
     tile_place(tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+    static_assert(S::BN <= S::THREADS, "a thread for each of the tile's tokens");
+    const int64_t row = n0 + threadIdx.x;
+    const bool mine = threadIdx.x < S::BN && row < H.size;
+    int64_t label = mine ? labels[row] : -1;                         // under way during the product
+    float log_sum = mine ? lse[row] : 0.f;
     f32x16 acc[S::MI][S::NI];
     clear<S>(acc);
     tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
+    asm volatile("" : "+v"(label), "+v"(log_sum));                   // not looked at before
+    if (threadIdx.x < S::BN) {
+        const int64_t at = label - v0 - m0;
+        const bool part = label >= 0 && label < vocab;               // elsewhere 2^(0 - infinity) = 0
+        tokens[threadIdx.x] = Token{part ? dz_exponent<KIND>() - log_sum * kLog2e : -INFINITY, part && at >= 0 && at < S::BM ? (int)at : kNoLabel};
+    }
+    __syncthreads();
     const float f = kLog2e * unscale<KIND>(exps, 2), one = (float)(1 << dz_exponent<KIND>());
     const int limit = W.size - m0 < S::BM ? (int)(W.size - m0) : S::BM;          // of the tile's words, in the vocabulary
     constexpr int BYTES = KIND == SPLIT ? 4 : 2;
     const int64_t row_bytes = row_words<KIND>(W.size) * 2;
     char *corner = (char *)dz + n0 * row_bytes + m0 * BYTES;
-    struct Token { float base; int label; };
     store_rows<S, BYTES, KIND == SPLIT>(
         acc, lds,
         [&](int n) {
-            const int64_t row = n0 + n;
-            Token k = {-INFINITY, -1};                               // takes no part: 2^(0 - infinity) = 0
-            if (row < H.size && takes_part(labels, row, vocab)) {
-                const int64_t at = labels[row] - v0 - m0;
-                k.base = dz_exponent<KIND>() - lse[row] * kLog2e;
-                k.label = at >= 0 && at < S::BM ? (int)at : -1;
-            }
-            return k;
+            const Token k = tokens[n];
+            return std::make_pair(k, __any(k.label != kNoLabel) != 0);
         },
-        [&](const Token &k, int m, const float (&z)[4]) {
+        [&](const std::pair<Token, bool> &kl, int m, const float (&z)[4]) {
+            const Token &k = kl.first;
             float g[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                g[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, k.base));
-                if (m + e == k.label) g[e] -= one;
+            for (int e = 0; e < 4; ++e) g[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, k.base));
+            if (kl.second) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (m + e == k.label) g[e] -= one;
             }
             if (limit < S::BM) {
 #pragma unroll
