@@ -164,100 +164,121 @@ __device__ __forceinline__ void wait_and_meet()
 // share of the reads of fragments.  Large tiles of 16-bit numbers have the loads spread over the two groups behind the barrier too
 // (issued at once they hold a wavefront back for as long as a group takes: 4096^3 121 us, spread 112); the others need them early more
 // (pairs in Middle, one tile a CU, k = 1536: 31 us at once, 40 spread).
+// In two steps for those who have something else to do while the first stages are on their way: start() begins to load them, into all
+// stages of LDS but the last, which is the caller's until finish().
+template <class S, int KIND, bool A_K_ROWS, bool B_K_ROWS>
+struct Product {
+    typedef Loader<S::BM, S::THREADS, KIND, A_K_ROWS> LA;
+    typedef Loader<S::BN, S::THREADS, KIND, B_K_ROWS> LB;
+    static constexpr int BK = tile_k<KIND>(), STAGE = S::A_BYTES + S::B_BYTES, LOADS = LA::N + LB::N;
+    LA la;
+    LB lb;
+    int left;
+
+    __device__ __forceinline__ void load(char *to, int wave, int i)
+    {
+        if (i < LA::N) la.load(to, wave, i);
+        else lb.load(to + S::A_BYTES, wave, i - LA::N);
+    }
+    __device__ __forceinline__ void begin()
+    {
+        la.begin(threadIdx.x, left);
+        lb.begin(threadIdx.x, left);
+        left -= BK;
+    }
+    __device__ __forceinline__ void next()
+    {
+        la.next();
+        lb.next();
+    }
+    __device__ __forceinline__ void start(const Operand &A, int64_t m0, const Operand &B, int64_t n0, int64_t k_first, int64_t k, char *lds)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        la.init(A, m0, k_first, threadIdx.x);
+        lb.init(B, n0, k_first, threadIdx.x);
+        left = (int)k;
+        if (k <= 0) return;
+#pragma unroll
+        for (int s = 0; s + 1 < S::STAGES; ++s) {                    // past k: zeros, here and below, so that the count of loads holds
+            begin();
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load(lds + s * STAGE, wave, i);
+            next();
+        }
+    }
+    __device__ __forceinline__ void finish(f32x16 (&acc)[S::MI][S::NI], int64_t k, char *lds)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
+        constexpr int HALVES = KIND == SPLIT ? 2 : 1, GROUPS = BK / 16, PRODUCTS = S::MI * S::NI * (KIND == SPLIT ? 3 : 1), FRAGMENTS = HALVES * (S::MI + S::NI);
+        if (k <= 0) return;
+        u32x4 fa[2][HALVES][S::MI], fb[2][HALVES][S::NI];
+        auto read = [&](const char *stage, int group, int into, int f) {     // first parts first
+            const int h = f / (S::MI + S::NI), e = f % (S::MI + S::NI);
+            if (e < S::MI) fa[into][h][e] = fragment<S::BM, KIND, A_K_ROWS>(stage, wm + e * 32, group * 16, h, lane);
+            else fb[into][h][e - S::MI] = fragment<S::BN, KIND, B_K_ROWS>(stage + S::A_BYTES, wn + (e - S::MI) * 32, group * 16, h, lane);
+        };
+        constexpr int BEHIND = (KIND == SPLIT ? S::SPREAD_PAIRS : S::SPREAD16) ? LOADS / 2 : LOADS;        // loads of a stage that the group behind the barrier begins
+        // one group: its matrix instructions, the reads of another one, loads from `first` to `last` of a stage
+        auto work = [&](int from, const char *stage, int group, int into, char *to, int first, int last) {
+#pragma unroll
+            for (int p = 0; p < PRODUCTS; ++p) {
+                const int q = p / (S::MI * S::NI), i = p / S::NI % S::MI, j = p % S::NI;
+                acc[i][j] = mfma<KIND>(fa[from][q == 2 ? HALVES - 1 : 0][i], fb[from][q == 1 ? HALVES - 1 : 0][j], acc[i][j]);
+#pragma unroll
+                for (int f = FRAGMENTS * p / PRODUCTS; f < FRAGMENTS * (p + 1) / PRODUCTS; ++f) read(stage, group, into, f);
+                if (first < last)
+#pragma unroll
+                    for (int l = first + (last - first) * p / PRODUCTS; l < first + (last - first) * (p + 1) / PRODUCTS; ++l) load(to, wave, l);
+                if constexpr (BEHIND < LOADS) __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (BEHIND == LOADS) {                             // the same order, without the compiler's hands tied in each place
+                constexpr int READS = HALVES * (S::MI * (A_K_ROWS ? 2 : 1) + S::NI * (B_K_ROWS ? 2 : 1));
+#pragma unroll
+                for (int p = 0; p < PRODUCTS; ++p) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        constexpr int AHEAD = (S::STAGES - 2) * LOADS;                   // loads that may be under way when the next stage is read
+        char *cur = lds, *nxt = lds + STAGE, *const end = lds + S::STAGES * STAGE, *fill = end - STAGE;
+        begin();
+#pragma unroll
+        for (int i = 0; i < BEHIND; ++i) load(fill, wave, i);
+        wait_and_meet<AHEAD + BEHIND>();
+#pragma unroll
+        for (int f = 0; f < FRAGMENTS; ++f) read(cur, 0, 0, f);
+        for (int todo = (int)k; todo > 0; todo -= BK) {
+            work(0, cur, 1, 1, fill, BEHIND, LOADS);                     // the second half of what the last group began to load
+            next();
+#pragma unroll
+            for (int g = 1; g + 1 < GROUPS; ++g) work(g & 1, cur, g + 1, (g + 1) & 1, nullptr, 0, 0);
+            wait_and_meet<AHEAD>();
+            begin();
+            if constexpr (BEHIND == LOADS) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) load(cur, wave, i);
+                work((GROUPS - 1) & 1, nxt, 0, 0, nullptr, 0, 0);
+            } else {
+                work((GROUPS - 1) & 1, nxt, 0, 0, cur, 0, BEHIND);
+            }                                                            // (reads after the last stage: what nobody uses)
+            fill = cur;
+            cur = nxt;
+            nxt = nxt + STAGE == end ? lds : nxt + STAGE;
+        }
+        wait_and_meet<0>();
+    }
+};
+
 template <class S, int KIND, bool A_K_ROWS, bool B_K_ROWS>
 __device__ __forceinline__ void tile_product(f32x16 (&acc)[S::MI][S::NI], const Operand &A, int64_t m0, const Operand &B, int64_t n0, int64_t k_first,
                                              int64_t k, char *lds)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
-    constexpr int BK = tile_k<KIND>(), STAGE = S::A_BYTES + S::B_BYTES, HALVES = KIND == SPLIT ? 2 : 1, GROUPS = BK / 16;
-    typedef Loader<S::BM, S::THREADS, KIND, A_K_ROWS> LA;
-    typedef Loader<S::BN, S::THREADS, KIND, B_K_ROWS> LB;
-    LA la;
-    LB lb;
-    la.init(A, m0, k_first, tid);
-    lb.init(B, n0, k_first, tid);
-    int left = (int)k;
-    constexpr int LOADS = LA::N + LB::N, PRODUCTS = S::MI * S::NI * (KIND == SPLIT ? 3 : 1), FRAGMENTS = HALVES * (S::MI + S::NI);
-    auto load = [&](char *to, int i) {
-        if (i < LA::N) la.load(to, wave, i);
-        else lb.load(to + S::A_BYTES, wave, i - LA::N);
-    };
-    auto begin = [&]() {
-        la.begin(tid, left);
-        lb.begin(tid, left);
-        left -= BK;
-    };
-    auto next = [&]() {
-        la.next();
-        lb.next();
-    };
-    auto fetch = [&](char *to) {
-        begin();
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load(to, i);
-        next();
-    };
-    if (k <= 0) return;
-    u32x4 fa[2][HALVES][S::MI], fb[2][HALVES][S::NI];
-    auto read = [&](const char *stage, int group, int into, int f) {     // first parts first
-        const int h = f / (S::MI + S::NI), e = f % (S::MI + S::NI);
-        if (e < S::MI) fa[into][h][e] = fragment<S::BM, KIND, A_K_ROWS>(stage, wm + e * 32, group * 16, h, lane);
-        else fb[into][h][e - S::MI] = fragment<S::BN, KIND, B_K_ROWS>(stage + S::A_BYTES, wn + (e - S::MI) * 32, group * 16, h, lane);
-    };
-    constexpr int BEHIND = (KIND == SPLIT ? S::SPREAD_PAIRS : S::SPREAD16) ? LOADS / 2 : LOADS;        // loads of a stage that the group behind the barrier begins
-    // one group: its matrix instructions, the reads of another one, loads from `first` to `last` of a stage
-    auto work = [&](int from, const char *stage, int group, int into, char *to, int first, int last) {
-#pragma unroll
-        for (int p = 0; p < PRODUCTS; ++p) {
-            const int q = p / (S::MI * S::NI), i = p / S::NI % S::MI, j = p % S::NI;
-            acc[i][j] = mfma<KIND>(fa[from][q == 2 ? HALVES - 1 : 0][i], fb[from][q == 1 ? HALVES - 1 : 0][j], acc[i][j]);
-#pragma unroll
-            for (int f = FRAGMENTS * p / PRODUCTS; f < FRAGMENTS * (p + 1) / PRODUCTS; ++f) read(stage, group, into, f);
-            if (first < last)
-#pragma unroll
-                for (int l = first + (last - first) * p / PRODUCTS; l < first + (last - first) * (p + 1) / PRODUCTS; ++l) load(to, l);
-            if constexpr (BEHIND < LOADS) __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (BEHIND == LOADS) {                             // the same order, without the compiler's hands tied in each place
-            constexpr int READS = HALVES * (S::MI * (A_K_ROWS ? 2 : 1) + S::NI * (B_K_ROWS ? 2 : 1));
-#pragma unroll
-            for (int p = 0; p < PRODUCTS; ++p) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, (READS + PRODUCTS - 1) / PRODUCTS, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    constexpr int AHEAD = (S::STAGES - 2) * LOADS;                   // loads that may be under way when the next stage is read
-    char *cur = lds, *nxt = lds + STAGE, *const end = lds + S::STAGES * STAGE, *fill = end - STAGE;
-#pragma unroll
-    for (int s = 0; s + 1 < S::STAGES; ++s) fetch(lds + s * STAGE);  // past k: zeros, here and below, so that the count of loads holds
-    begin();
-#pragma unroll
-    for (int i = 0; i < BEHIND; ++i) load(fill, i);
-    wait_and_meet<AHEAD + BEHIND>();
-#pragma unroll
-    for (int f = 0; f < FRAGMENTS; ++f) read(cur, 0, 0, f);
-    for (int todo = (int)k; todo > 0; todo -= BK) {
-        work(0, cur, 1, 1, fill, BEHIND, LOADS);                     // the second half of what the last group began to load
-        next();
-#pragma unroll
-        for (int g = 1; g + 1 < GROUPS; ++g) work(g & 1, cur, g + 1, (g + 1) & 1, nullptr, 0, 0);
-        wait_and_meet<AHEAD>();
-        begin();
-        if constexpr (BEHIND == LOADS) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) load(cur, i);
-            work((GROUPS - 1) & 1, nxt, 0, 0, nullptr, 0, 0);
-        } else {
-            work((GROUPS - 1) & 1, nxt, 0, 0, cur, 0, BEHIND);
-        }                                                            // (reads after the last stage: what nobody uses)
-        fill = cur;
-        cur = nxt;
-        nxt = nxt + STAGE == end ? lds : nxt + STAGE;
-    }
-    wait_and_meet<0>();
+    Product<S, KIND, A_K_ROWS, B_K_ROWS> product;
+    product.start(A, m0, B, n0, k_first, k, lds);
+    product.finish(acc, k, lds);
 }
 
 template <class S>
@@ -478,9 +499,9 @@ __device__ __forceinline__ uint32_t tile_run(uint32_t id, uint32_t total)
     const uint32_t xcd = id & 7, each = total >> 3, over = total & 7;
     return xcd * each + (xcd < over ? xcd : over) + (id >> 3);
 }
-__device__ __forceinline__ void tile_place(uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
+__device__ __forceinline__ void tile_place(uint32_t at, uint32_t total, uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
 {
-    uint32_t id = tile_run(blockIdx.x, gridDim.x);
+    uint32_t id = tile_run(at, total);
     batch = id / (tiles_m * tiles_n);
     id -= batch * tiles_m * tiles_n;
     const uint32_t group = id / (kTileGroup * tiles_n), first = group * kTileGroup;
@@ -488,6 +509,10 @@ __device__ __forceinline__ void tile_place(uint32_t tiles_m, uint32_t tiles_n, u
     const uint32_t in = id - first * tiles_n;
     mi = first + in % wide;
     ni = in / wide;
+}
+__device__ __forceinline__ void tile_place(uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
+{
+    tile_place(blockIdx.x, gridDim.x, tiles_m, tiles_n, mi, ni, batch);
 }
 
 // The tiles in use.  At 8192^3 (16 bits; pairs), Large reaches 1.27 PFLOP/s (0.45), 83 % of the library's 1.54 in 16 bits and three times
@@ -531,6 +556,9 @@ static inline TileChoice choose_tiles(bool pairs, int64_t batch, int64_t m, int6
     }
     return best;
 }
+
+// workgroups of a kernel that goes from tile to tile: as many as the chip holds at once
+template <class S> static uint32_t at_once(uint32_t tiles) { return std::min<uint32_t>(tiles, 256 * (163840 / S::LDS_BYTES)); }
 
 template <int KIND, typename F>
 static void with_tile(int shape, F f)

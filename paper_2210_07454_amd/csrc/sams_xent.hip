@@ -159,6 +159,11 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b)
     return make_float2(top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base));
 }
 
+// Whether the workgroups go from tile to tile, the next tile's first stage on its way while the sums of one are made: 16-bit words do (8192 x
+// 50257 x 768: 655 -> 618 us; 4096 x 32000 x 1024: 257 -> 245), pairs, whose tiles of 256 leave no registers for it, gain nothing
+// (2044 x 50257 x 768: 464, 461).
+template <int KIND> constexpr bool kStatsInTurn = KIND != SPLIT;
+
 // Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).  A lane holds numbers
 // of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's logit, in the same units, is
 // left in `at_label` by the lane that holds it: the loss, the difference of the two, keeps its digits where the label is nearly certain.
@@ -167,67 +172,84 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
                                                            float2 *part, float *at_label)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
-    uint32_t mi, ni, batch;
-    tile_place(tiles_v, tiles_t, mi, ni, batch);
-    const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+    typedef Product<S, KIND, false, false> Logits;
+    constexpr bool ON = kStatsInTurn<KIND>;
+    float2 *joined = (float2 *)(lds + (ON ? (S::STAGES - 1) * Logits::STAGE : 0));           // [WAVES_M][BN]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
-    int64_t at[S::NI];                                               // the tokens' labels, under way during the product
+    const uint32_t tiles = tiles_v * tiles_t;
+    uint32_t id = blockIdx.x, mi, ni, batch;
+    tile_place(id, tiles, tiles_v, tiles_t, mi, ni, batch);
+    Logits logits;
+    logits.start(W, (int64_t)mi * S::BM, H, (int64_t)ni * S::BN, 0, dim, lds);
+    for (;;) {
+        const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
+        const uint32_t tile_v = mi;
+        int64_t at[S::NI];                                               // the tokens' labels, under way during the product
 #pragma unroll
-    for (int j = 0; j < S::NI; ++j) {
-        const int64_t row = n0 + (wn * S::NI + j) * 32 + (lane & 31);
-        at[j] = row < H.size ? labels[row] : -1;
-    }
-    f32x16 acc[S::MI][S::NI];
-    clear<S>(acc);
-    tile_product<S, KIND, false, false>(acc, W, m0, H, n0, 0, dim, lds);
-    int label[S::NI];                                                // where they lie among the wavefront's words; -1: elsewhere
+        for (int j = 0; j < S::NI; ++j) {
+            const int64_t row = n0 + (wn * S::NI + j) * 32 + (lane & 31);
+            at[j] = row < H.size ? labels[row] : -1;
+        }
+        f32x16 acc[S::MI][S::NI];
+        clear<S>(acc);
+        logits.finish(acc, dim, lds);
+        if constexpr (ON) {
+            id += gridDim.x;
+            if (id < tiles) {
+                tile_place(id, tiles, tiles_v, tiles_t, mi, ni, batch);
+                logits.start(W, (int64_t)mi * S::BM, H, (int64_t)ni * S::BN, 0, dim, lds);
+            }
+        }
+        int label[S::NI];                                                // where they lie among the wavefront's words; -1: elsewhere
 #pragma unroll
-    for (int j = 0; j < S::NI; ++j) {
-        asm volatile("" : "+v"(at[j]));                              // not looked at before
-        const int64_t in = at[j] - m0 - wm * S::MI * 32;
-        label[j] = at[j] < W.size && in >= 0 && in < S::MI * 32 ? (int)in : -1;
-    }
-    const float f = kLog2e * unscale<KIND>(exps, 2);
-    if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-                if (m0 + (wm * S::MI + i) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3) >= W.size)
-#pragma unroll
-                    for (int j = 0; j < S::NI; ++j) acc[i][j][q] = -INFINITY;
-    }
-    float2 *joined = (float2 *)lds;                                  // [WAVES_M][BN]
-#pragma unroll
-    for (int j = 0; j < S::NI; ++j) {
-        float top = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
-        if (__any(label[j] >= 0)) {
-            float z = 0.f;
+        for (int j = 0; j < S::NI; ++j) {
+            asm volatile("" : "+v"(at[j]));                              // not looked at before
+            const int64_t in = at[j] - m0 - wm * S::MI * 32;
+            label[j] = at[j] < W.size && in >= 0 && in < S::MI * 32 ? (int)in : -1;
+        }
+        const float f = kLog2e * unscale<KIND>(exps, 2);
+        if (m0 + S::BM > W.size) {                                       // rows past the vocabulary
 #pragma unroll
             for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-                for (int q = 0; q < 16; ++q) z = (label[j] & ~4) == i * 32 + 8 * (q >> 2) + (q & 3) ? acc[i][j][q] : z;
-            if (label[j] >= 0 && (label[j] >> 2 & 1) == lane >> 5) at_label[n0 + (wn * S::NI + j) * 32 + (lane & 31)] = z * f;
+                for (int q = 0; q < 16; ++q)
+                    if (m0 + (wm * S::MI + i) * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3) >= W.size)
+#pragma unroll
+                        for (int j = 0; j < S::NI; ++j) acc[i][j][q] = -INFINITY;
         }
-        top = fmaxf(top, __shfl_xor(top, 32)) * f;
-        const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int i = 0; i < S::MI; ++i)
+        for (int j = 0; j < S::NI; ++j) {
+            float top = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][q], f, -base));
-        sum += __shfl_xor(sum, 32);
-        if (lane < 32) joined[wm * S::BN + (wn * S::NI + j) * 32 + lane] = make_float2(top, sum);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < S::BN; i += S::THREADS) {
-        float2 a = joined[i];
+            for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-        for (int w = 1; w < S::WAVES_M; ++w) a = join_sums(a, joined[w * S::BN + i]);
-        if (n0 + i < H.size) part[mi * H.size + n0 + i] = a;
+                for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
+            if (__any(label[j] >= 0)) {
+                float z = 0.f;
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) z = (label[j] & ~4) == i * 32 + 8 * (q >> 2) + (q & 3) ? acc[i][j][q] : z;
+                if (label[j] >= 0 && (label[j] >> 2 & 1) == lane >> 5) at_label[n0 + (wn * S::NI + j) * 32 + (lane & 31)] = z * f;
+            }
+            top = fmaxf(top, __shfl_xor(top, 32)) * f;
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][q], f, -base));
+            sum += __shfl_xor(sum, 32);
+            if (lane < 32) joined[wm * S::BN + (wn * S::NI + j) * 32 + lane] = make_float2(top, sum);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < S::BN; i += S::THREADS) {
+            float2 a = joined[i];
+#pragma unroll
+            for (int w = 1; w < S::WAVES_M; ++w) a = join_sums(a, joined[w * S::BN + i]);
+            if (n0 + i < H.size) part[tile_v * H.size + n0 + i] = a;
+        }
+        if (!ON || id >= tiles) return;
+        __syncthreads();                                             // the stage that `joined` lies in is loaded next
     }
 }
 
@@ -518,7 +540,7 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
             typedef decltype(shape) S;
             tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
             const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), labels, part, at_label);
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), labels, part, at_label);
         });
         if (t <= kJoinTokens && tv <= kJoinTiles) {
             hipLaunchKernelGGL(k_xent_join_few, dim3((unsigned)c->n), dim3(256), 0, c->stream, part, (int)tv, at_label, labels, (int)t, rows, c->vocab, lse, loss);
