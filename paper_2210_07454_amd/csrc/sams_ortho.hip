@@ -224,6 +224,21 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram,
     });
 }
 
+// eight parameters from `at` on, of which those from `limit` on do not exist (0): in pieces of 16 bytes where they do (one by one, the last
+// step's products of 12 matrices of 768 x 768 take 70 us, so 57)
+__device__ __forceinline__ void load_numbers(const float *row, int64_t at, int64_t limit, float (&v)[8])
+{
+    typedef float anywhere __attribute__((ext_vector_type(4), aligned(4)));
+    if (at + 8 <= limit) {
+        const anywhere a = *(const anywhere *)(row + at), b = *(const anywhere *)(row + at + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = at + e < limit ? row[at + e] : 0.f;
+    }
+}
+
 // where the last step's X goes
 struct OrthoOut {
     void *out;                          // the caller's tensor
@@ -259,10 +274,13 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly
             E *out = (E *)o.out + matrix * o.out_mat + r * o.out_row;
             const float *px = o.x ? o.x + matrix * o.x_mat + r * d.cols : nullptr;
             E e8[8];
+            float was[8];
+            if constexpr (T == SAMS_F32)
+                if (px) load_numbers(px, col, d.cols, was);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = raw[e] * f;
-                if constexpr (T == SAMS_F32) e8[e] = px ? (col + e < d.cols ? o.keep * px[col + e] - o.rate * v : 0.f) : v;
+                if constexpr (T == SAMS_F32) e8[e] = px ? o.keep * was[e] - o.rate * v : v;
                 else e8[e] = (E)v;
             }
             u32x4 w;
