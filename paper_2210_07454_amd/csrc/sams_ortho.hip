@@ -27,7 +27,7 @@ struct sams_ortho {
     int32_t type;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t x[2], gram, poly, scale, part, update;       // offsets in the scratch
+    int64_t x[2], gram, poly, scale, part, update, sums; // offsets in the scratch
 };
 
 namespace sams {
@@ -153,16 +153,20 @@ struct OrthoDims {
     int64_t rows, cols, small;          // of X; small = min(rows, cols)
 };
 
-// a workgroup's tile of the lower triangle, and its matrix
-__device__ __forceinline__ void triangle(int64_t tiles, int &i, int &j, int64_t &matrix)
+// tile number `run` of the lower triangles, and its matrix
+__device__ __forceinline__ void triangle_at(uint32_t run, int64_t tiles, int &i, int &j, int64_t &matrix)
 {
-    const uint32_t run = tile_run(blockIdx.x, gridDim.x), each = (uint32_t)(tiles * (tiles + 1) / 2);
+    const uint32_t each = (uint32_t)(tiles * (tiles + 1) / 2);
     matrix = run / each;
     const int id = (int)(run % each);
     i = (int)((sqrtf(8.f * (float)id + 1.f) - 1.f) * 0.5f);
     while ((i + 1) * (i + 2) / 2 <= id) ++i;
     while (i * (i + 1) / 2 > id) --i;
     j = id - i * (i + 1) / 2;
+}
+__device__ __forceinline__ void triangle(int64_t tiles, int &i, int &j, int64_t &matrix)           // a workgroup's
+{
+    triangle_at(tile_run(blockIdx.x, gridDim.x), tiles, i, j, matrix);
 }
 
 // Writes a symmetric matrix's tile and its mirror image, with zeros in what fills the rows up; value(row, col, v) makes eight numbers of them.
@@ -206,6 +210,61 @@ __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, Or
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
     });
+}
+
+// The same where a few tiles' k's are long: the k's in parts, whose sums of 64 x 64 numbers lie one after the other (tiles fastest) and
+// are added up in ascending order by k_ortho_gram_join.  Orthogonalised in 32 bits: 8 of 64 x
+// 5145 275 us whole, 188 cut; 3 of 320 x 8192 513, 353; one of 256 x 1024 125, 133, and not cut.
+constexpr int kGramParts = 32;          // of k, at most, and as many as make a tile for every CU
+constexpr int kGramTiles = 256;         // parts of all tiles, at most
+template <int KIND, bool TALL>
+__global__ void __launch_bounds__(Small::THREADS) k_ortho_gram_part(const uint16_t *x, OrthoDims d, uint32_t tiles, uint32_t parts, float *sums)
+{
+    typedef Small S;
+    __shared__ __align__(16) char lds[S::LDS_BYTES];
+    const uint32_t part = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    int ti, tj;
+    int64_t matrix;
+    triangle_at(tile, (d.small + S::BM - 1) / S::BM, ti, tj, matrix);
+    const int64_t m0 = (int64_t)ti * S::BM, n0 = (int64_t)tj * S::BN, ldx = row_words<KIND>(d.cols), k = TALL ? d.rows : d.cols;
+    const int64_t steps = (k + tile_k<KIND>() - 1) / tile_k<KIND>();
+    const int64_t lo = steps * part / parts * tile_k<KIND>(), hi = steps * (part + 1) / parts * tile_k<KIND>();
+    const Operand X{x + matrix * d.rows * ldx, ldx, TALL ? d.cols : d.rows};
+    f32x16 acc[S::MI][S::NI];
+    clear<S>(acc);
+    tile_product<S, KIND, TALL, TALL>(acc, X, m0, X, n0, lo, (hi < k ? hi : k) - lo, lds);
+    float *out = sums + (int64_t)blockIdx.x * (S::BM * S::BN);
+    eights<S, false>(acc, lds, [&](int dn, int dm, const float (&v)[8]) {
+        float4 *o = (float4 *)(out + dn * S::BM + dm);
+        o[0] = make_float4(v[0], v[1], v[2], v[3]);
+        o[1] = make_float4(v[4], v[5], v[6], v[7]);
+    });
+}
+
+// a quarter of a tile and of its mirror image (blockIdx.y) by a workgroup
+template <int KIND>
+__global__ void __launch_bounds__(256) k_ortho_gram_join(const float *sums, uint32_t tiles, uint32_t parts, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram)
+{
+    constexpr int B = Small::BM;
+    int ti, tj;
+    int64_t matrix;
+    triangle_at(blockIdx.x, (d.small + B - 1) / B, ti, tj, matrix);
+    const bool mirror = threadIdx.x >= 128;
+    if (mirror && ti == tj) return;
+    const int at = blockIdx.y * 128 + (threadIdx.x & 127), r = at / (B / 8), c = at % (B / 8) * 8;
+    const int64_t row = (int64_t)(mirror ? ti : tj) * B + r, col = (int64_t)(mirror ? tj : ti) * B + c;
+    if (row >= d.small || col >= row_numbers<KIND>(d.small)) return;
+    if (scale) f *= scale[matrix].sigma2;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (uint32_t p = 0; p < parts; ++p) {
+        const float *tile = sums + ((int64_t)p * tiles + blockIdx.x) * (B * B);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += mirror ? tile[(c + e) * B + r] : tile[r * B + c + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = col + e < d.small ? v[e] * f : 0.f;
+    const int64_t ld = row_words<KIND>(d.small);
+    put8<KIND>(gram + matrix * d.small * ld + row * ld, col, v);
 }
 
 // P = a I + b A + c A A: 102 us at 4096, 0.67 PFLOP/s of the half that is computed, 253 tiles of 192 on 256 CUs.
@@ -564,6 +623,24 @@ static void plan_steps(int steps, const float *coef, SmallSteps *plan)
     }
 }
 
+// tiles of 64 x 64 on and under the diagonals
+static int64_t gram_tiles(int64_t batch, int64_t small)
+{
+    const int64_t a = (small + Small::BM - 1) / Small::BM;
+    return batch * (a * (a + 1) / 2);
+}
+
+// The parts that the k's of A's tiles are cut into (pairs): where a tile for every CU by parts, and a launch more to join them (6.5 us), is
+// estimated to be the faster way.
+static uint32_t gram_parts(int64_t batch, int64_t small, int64_t large, int shape)
+{
+    const int64_t tiles = gram_tiles(batch, small), parts = std::min<int64_t>(std::min<int64_t>(kGramParts, kGramTiles / tiles), large / 128);
+    if (parts < 2) return 1;
+    const int64_t size = kTileCosts[shape].size, a = (small + size - 1) / size;
+    const double whole = tile_estimate(shape, true, (double)(batch * (a * (a + 1) / 2)), (double)large, 1), cut = tile_estimate(3, true, (double)tiles, (double)large, (int)parts) + 6500.0;
+    return cut < whole ? (uint32_t)parts : 1;
+}
+
 template <int KIND, int T>
 static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, const OrthoOut &o)
 {
@@ -574,6 +651,7 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
     const int64_t large = d.rows + d.cols - d.small;
     const int of_gram = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, large, 1, 0).shape, of_poly = choose_tiles(KIND == SPLIT, batch, d.small, d.small, true, d.small, 1, 0).shape,
               of_apply = choose_tiles(KIND == SPLIT, batch, d.cols, d.rows, false, d.small, 1, 0).shape;
+    const uint32_t parts = KIND == SPLIT ? gram_parts(batch, d.small, large, of_gram) : 1, tiles = (uint32_t)gram_tiles(batch, d.small);
     for (int s = 0; s < plan.count; ++s) {
         const uint16_t *x = c->scratch.at<uint16_t>(c->x[s & 1]);
         uint16_t *next = c->scratch.at<uint16_t>(c->x[(s + 1) & 1]);
@@ -583,7 +661,15 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
             const int64_t ts = (d.small + decltype(shape)::BM - 1) / decltype(shape)::BM;
             return dim3((unsigned)(ts * (ts + 1) / 2 * batch));
         };
-        with_tile<KIND>(of_gram, [&](auto shape) {
+        if (parts > 1) {
+            if constexpr (KIND == SPLIT) {                           // (a bfloat16 matrix of single words has tiles enough)
+                float *sums = c->scratch.at<float>(c->sums);
+                auto cut = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(tiles * parts), dim3(Small::THREADS), 0, c->stream, x, d, tiles, parts, sums); };
+                if (tall) cut(k_ortho_gram_part<KIND, true>);
+                else cut(k_ortho_gram_part<KIND, false>);
+                hipLaunchKernelGGL((k_ortho_gram_join<KIND>), dim3(tiles, 4), dim3(256), 0, c->stream, sums, tiles, parts, d, p.f_gram, first, gram);
+            }
+        } else with_tile<KIND>(of_gram, [&](auto shape) {
             typedef decltype(shape) S;
             if (tall) hipLaunchKernelGGL((k_ortho_gram<S, KIND, true>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
             else hipLaunchKernelGGL((k_ortho_gram<S, KIND, false>), square(shape), dim3(S::THREADS), 0, c->stream, x, d, p.f_gram, first, gram);
@@ -669,6 +755,7 @@ int sams_ortho_create(sams_ortho **out, int64_t batch, int64_t rows, int64_t col
     c->poly = c->scratch.reserve(batch * small * ldp * 2);
     c->scale = c->scratch.reserve(batch * (int64_t)sizeof(OrthoScale));
     c->part = c->scratch.reserve(batch * kNormSlices * 8);
+    c->sums = pairs && gram_tiles(1, small) < kGramTiles ? c->scratch.reserve((int64_t)kGramTiles * Small::BM * Small::BN * 4) : -1;
     c->update = type == SAMS_F32 ? c->scratch.reserve(batch * rows * cols * 4) : -1;
     const int rc = c->scratch.take();
     if (rc != SAMS_OK) { delete c; return rc; }

@@ -215,3 +215,15 @@ def test_equal_inputs_give_equal_results(sams):
         for o in outs:
             op.orthogonalize(g, o)
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+@pytest.mark.parametrize("shape", [(1, 1, 6000), (2, 19, 3617), (3, 1801, 33), (1, 130, 2500), (1, 2311, 200)], ids=str)
+def test_long_thin_matrices(sams, kind, shape):
+    """A short side beside a long one, whose products are cut along it."""
+    g = matrices(*shape, kind)
+    want, bounds = reference(g)
+    out = torch.full_like(g, float("nan"), device="cuda")
+    with sams.Orthogonalizer(*shape, kind) as op:
+        op.orthogonalize(g.cuda(), out)
+    check(out, want, bounds, kind, shape)
