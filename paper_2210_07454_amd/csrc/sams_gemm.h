@@ -68,10 +68,12 @@ __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__bui
 
 // 16 bytes a lane from a buffer, to LDS from address `at` on, lane by lane.  No register is written, so nothing can be overwritten while
 // it is under way.  Written out because the compiler waits for every such load of its own before it lets a transposing read go
-// ahead (also of the stage that landed long ago): those who read the stage wait for it, in wait_and_meet.
+// ahead (also of the stage that landed long ago): those who read the stage wait for it, in wait_and_meet.  The buffer's scalar registers
+// may come from a readfirstlane right before: what the vector unit writes may be read by a load of it five wait states later, which the
+// compiler does not add to instructions it has not made itself; the move to m0 is one, the s_nop four.  (m0 belongs to no value of the compiler's: it is a reserved register, written anew where it is used.)
 __device__ __forceinline__ void load_to_lds(u32x4 buffer, uint32_t off, uint32_t at)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(buffer), "s"(at) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(buffer), "s"(at) : "memory");
 }
 
 template <int ROWS, int THREADS, int KIND, bool K_ROWS>
