@@ -350,15 +350,18 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[S::MI][S::NI], ch
 }
 
 // The same with the numbers themselves in LDS: emit(n, m, v) gets eight numbers of row n from m on, so that what it reads beside them
-// comes in pieces of 16 bytes too.  MIRROR: of the transposed tile, C[m][n]; emit(m, n, v).
+// comes in pieces of 16 bytes too.  MIRROR: of the transposed tile, C[m][n]; emit(m, n, v).  A wavefront has the same bytes of LDS in either
+// order, whichever side of its part of the tile is longer: one may be through with the tile and at its mirror image while another still
+// reads the tile, and nothing but a wavefront's own order keeps the two apart.
 template <class S, bool MIRROR, typename Emit>
 __device__ __forceinline__ void eights(const f32x16 (&acc)[S::MI][S::NI], char *lds, Emit emit)
 {
     constexpr int ALONG = (MIRROR ? S::NI : S::MI) * 32, ROW = ALONG * 4, PIECES = ROW / 16, EIGHTS = ALONG / 8;
-    static_assert(32 * ROW * S::WAVES_M * S::WAVES_N <= S::LDS_BYTES, "a wavefront's rows have to fit");
+    constexpr int MINE = 32 * 32 * 4 * (S::MI > S::NI ? S::MI : S::NI);
+    static_assert(32 * ROW <= MINE && MINE * S::WAVES_M * S::WAVES_N <= S::LDS_BYTES, "a wavefront's rows have to fit");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
     const int wm = wave / S::WAVES_N * S::MI * 32, wn = wave % S::WAVES_N * S::NI * 32;
-    char *mine = lds + wave * 32 * ROW;
+    char *mine = lds + wave * MINE;
     typedef float f32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int outer = 0; outer < (MIRROR ? S::MI : S::NI); ++outer) {
