@@ -172,9 +172,9 @@ template <int KIND> constexpr bool kStatsInTurn = KIND != SPLIT;
 // Bound by the matrix cores, and by the exponentials while these wait: 8192 tokens of 768 and 50,257
 // words 618 us, 1.02 PFLOP/s in bf16; pairs 0.35.
 //
-// Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest).  A lane holds numbers
-// of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's logit, in the same units, is
-// left in `at_label` by the lane that holds it: the loss, the difference of the two, keeps its digits where the label is nearly certain.
+// Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest) over the words but the
+// label.  A lane holds numbers of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's
+// product is left in `at_label`, as it is, by the lane that holds it: see token_loss.
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels,
                                                            float2 *part, float *at_label)
@@ -233,12 +233,17 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
 #pragma unroll
                 for (int q = 0; q < 16; ++q) top = fmaxf(top, acc[i][j][q]);
             if (__any(label[j] >= 0)) {
+                const int own = label[j] >= 0 && (label[j] >> 2 & 1) == lane >> 5 ? label[j] & ~4 : -1;
                 float z = 0.f;
 #pragma unroll
                 for (int i = 0; i < S::MI; ++i)
 #pragma unroll
-                    for (int q = 0; q < 16; ++q) z = (label[j] & ~4) == i * 32 + 8 * (q >> 2) + (q & 3) ? acc[i][j][q] : z;
-                if (label[j] >= 0 && (label[j] >> 2 & 1) == lane >> 5) at_label[n0 + (wn * S::NI + j) * 32 + (lane & 31)] = z * f;
+                    for (int q = 0; q < 16; ++q)
+                        if (own == i * 32 + 8 * (q >> 2) + (q & 3)) {
+                            z = acc[i][j][q];
+                            acc[i][j][q] = -INFINITY;
+                        }
+                if (own >= 0) at_label[n0 + (wn * S::NI + j) * 32 + (lane & 31)] = z;
             }
             top = fmaxf(top, __shfl_xor(top, 32)) * f;
             const float base = top == -INFINITY ? 0.f : top;
@@ -263,8 +268,13 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
 
 // The log-sums over the tiles and the losses of 16 tokens (a line of `part`) by a workgroup, each tile's by one of 16 threads in turn;
 // the first 16 threads get their token's loss.
-__device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, const float *at_label, const int64_t *labels, int64_t first, int64_t end, int64_t rows, int64_t vocab,
-                                            float *lse, float2 (&joined)[4][16])
+//
+// With S the sum of 2^(z_v - top) over the words but the label, and d = top - z_label, a token's loss is log(1 + S 2^d).  d comes from
+// the label's product by one fma, against the same rounded `top` that the terms of S were taken against, so that the loss keeps its
+// digits where the label is nearly certain, however large the logits, and is never below 0.
+template <int KIND>
+__device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, const int64_t *labels, int64_t first, int64_t end,
+                                            int64_t rows, int64_t vocab, float *lse, float2 (&joined)[4][16])
 {
     const int r = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t row = first + r;
@@ -282,24 +292,27 @@ __device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, con
         return 0.f;
     }
     sums = join_sums(join_sums(joined[0][r], joined[1][r]), join_sums(joined[2][r], joined[3][r]));
-    const float log_sum = log2f(sums.y);
-    lse[row] = (sums.x + log_sum) * (1.f / kLog2e);
-    return ((sums.x - at_label[row]) + log_sum) * (1.f / kLog2e);
+    const float top = sums.x == -INFINITY ? 0.f : sums.x;
+    const float d = -__builtin_fmaf(at_label[row], kLog2e * unscale<KIND>(exps, 2), -top), log_sum = log2f(sums.y + exp2f(-d));
+    lse[row] = (top + log_sum) * (1.f / kLog2e);
+    return d > 32.f ? (d + log_sum) * (1.f / kLog2e) : log1pf(sums.y * exp2f(d));      // (2^d may be too large where 2^-d is small)
 }
 
-__global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles_v, const float *at_label, const int64_t *labels, int64_t rows, int64_t vocab, float *lse,
+template <int KIND>
+__global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, const int64_t *labels, int64_t rows, int64_t vocab, float *lse,
                                                    float *token)
 {
     __shared__ float2 joined[4][16];
     const int64_t first = blockIdx.x * (int64_t)16;
-    const float loss = token_loss(part, tiles_v, at_label, labels, first, rows, rows, vocab, lse, joined);
+    const float loss = token_loss<KIND>(part, tiles_v, at_label, exps, labels, first, rows, rows, vocab, lse, joined);
     if (threadIdx.x < 16 && first + threadIdx.x < rows) token[first + threadIdx.x] = loss;
 }
 
 // The same and the mean over a worker's tokens in one launch, a workgroup per worker, where there are few (kJoinTokens, kJoinTiles): 1.5 us
 // less of 48.8 for 4 x 5 tokens.
 constexpr int kJoinTokens = 64, kJoinTiles = 2048;
-__global__ void __launch_bounds__(256) k_xent_join_few(const float2 *part, int tiles_v, const float *at_label, const int64_t *labels, int t, int64_t rows, int64_t vocab, float *lse,
+template <int KIND>
+__global__ void __launch_bounds__(256) k_xent_join_few(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, const int64_t *labels, int t, int64_t rows, int64_t vocab, float *lse,
                                                        float *loss)
 {
     __shared__ float2 joined[4][16];
@@ -307,7 +320,7 @@ __global__ void __launch_bounds__(256) k_xent_join_few(const float2 *part, int t
     float sum = 0.f;
     int count = 0;
     for (int i = 0; i < t; i += 16) {
-        sum += token_loss(part, tiles_v, at_label, labels, begin + i, begin + t, rows, vocab, lse, joined);
+        sum += token_loss<KIND>(part, tiles_v, at_label, exps, labels, begin + i, begin + t, rows, vocab, lse, joined);
         if (threadIdx.x < 16 && i + threadIdx.x < t) count += takes_part(labels, begin + i + threadIdx.x, vocab);
         __syncthreads();
     }
@@ -544,6 +557,7 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
     constexpr int KIND = kind_of<T>();
     const int64_t rows = c->n * t;
     float *token = c->scratch.at<float>(c->token), *at_label = c->scratch.at<float>(c->at_label);
+    const int32_t *exps = c->scratch.at<int32_t>(c->exps);
     if (rows) {
         Operand H, W;
         SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, nullptr, &H, &W)));
@@ -553,14 +567,14 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
             typedef decltype(shape) S;
             tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
             const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, c->scratch.at<int32_t>(c->exps), labels, part, at_label);
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, exps, labels, part, at_label);
         });
         if (t <= kJoinTokens && tv <= kJoinTiles) {
-            hipLaunchKernelGGL(k_xent_join_few, dim3((unsigned)c->n), dim3(256), 0, c->stream, part, (int)tv, at_label, labels, (int)t, rows, c->vocab, lse, loss);
+            hipLaunchKernelGGL(k_xent_join_few<KIND>, dim3((unsigned)c->n), dim3(256), 0, c->stream, part, (int)tv, at_label, exps, labels, (int)t, rows, c->vocab, lse, loss);
             SAMS_HIP(hipGetLastError());
             return SAMS_OK;
         }
-        hipLaunchKernelGGL(k_xent_join, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, part, (int)tv, at_label, labels, rows, c->vocab, lse, token);
+        hipLaunchKernelGGL(k_xent_join<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, part, (int)tv, at_label, exps, labels, rows, c->vocab, lse, token);
     }
     hipLaunchKernelGGL(k_xent_loss, dim3((unsigned)c->n), dim3(256), 0, c->stream, token, labels, t, c->vocab, loss);
     SAMS_HIP(hipGetLastError());
