@@ -398,13 +398,16 @@ int layer_norm_backward(sams_norm *ctx, int64_t t, const void *dy, int64_t dy_wo
  * included) and changes nothing.  A worker without a token that takes part has loss 0 and gradients 0.
  * Backward, of sum_i grad_loss[i] * loss[i] (grad_loss NULL: all 1), from the lse of the forward pass:
  *     dh = dz w,   dw[i] = sum over worker i's tokens of dz' h,   dz = (exp(z - lse) - onehot(label)) * grad_loss / count
+ * where, for a label above 1/2, dz at it is made as minus the sum of the token's others, exp(z - lse) - 1 without its cancellation:
+ * gradients of tokens whose label is nearly certain keep their digits.
  *   dh [n][t][dim] of `type`     dw [n][vocab][dim] of dw_type (`type` or SAMS_F32), with the distances from worker to worker and from
- *   row to row; accumulate != 0 adds to what dw holds.  The logits are computed again, in pieces of the vocabulary.
+ *   row to row; accumulate != 0 adds to what dw holds.  The logits are computed again (twice, if one worker's dz finds no
+ *   room in the scratch: it goes by pieces of the vocabulary then).
  * 16-bit tensors are multiplied as they are, and dz is held as numbers of their type between the products (so dw and dh carry
  * its rounding whatever dw_type); 32-bit ones to 22 bits of mantissa, of numbers below 2^-17 of the tensor's largest fewer.
  * train == 0 at creation: the forward pass only, and less scratch (backward then returns SAMS_EINVAL).
- * Scratch: copies of h and w; 8 bytes per token and 64 words of the vocabulary; for training the dz of one piece of the vocabulary
- * (up to 1 GiB, or 1024 words per token if that is more) and up to 256 MiB, or 4*dim bytes per token, of partial sums of dh.
+ * Scratch: copies of h and w; 8 bytes per token and 64 words of the vocabulary; for training the dz of some workers' tokens (up to 1 GiB;
+ * of one worker's up to 4 GiB, if there is as much memory; at least 1024 words per token of one worker) and up to 256 MiB, or 4*dim bytes per token, of partial sums of dh.
  */
 int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int64_t vocab, int32_t type, int32_t train,
                      void *hip_stream);

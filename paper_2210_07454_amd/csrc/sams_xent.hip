@@ -4,9 +4,15 @@
 //   dz_iv = (exp(z_iv - lse_i) - [v = label_i]) * grad_w / count_w,  dh_i = sum_v dz_iv W_v,  dW^(w)_v = sum_i in w dz_iv h_i
 //
 // Forward: tiles of z = W H' stay in registers; a tile leaves, per token, its largest logit and its sum of exponentials, which a
-// second kernel joins over the vocabulary.  Backward: for one piece of the vocabulary after the other, the tiles of z again, from
+// second kernel joins over the vocabulary.  Backward: for some workers after the others, the tiles of z again, from
 // which dz goes to scratch as 16-bit words, and from there into the two products.  (The logits kept as 32-bit numbers would save a
 // quarter of the products for rows * vocab * 8 bytes of traffic, and as 16-bit numbers would spoil exp(z).)
+//
+// dz at the label, p - 1, is minus the sum of the token's other probabilities too, and made so where that is below 1/2: where the label is
+// nearly certain, 1 - p is far smaller than what the rounding of lse to 32 bits leaves uncertain of p (a token whose loss was 4e-5 beside
+// a log-sum of 190 had gradients 16 % off).  The tiles that make dz add the others up; the word of such a label is written when the whole
+// vocabulary is there.  Only where one worker's dz is too large for the scratch does it go by pieces of the vocabulary, with a pass over
+// the logits before them for the sums.
 //
 // All but the smallest are bound by the matrix cores: 8 x 1024 tokens of 768 against 50,257 words in bf16 take 2.4 ms for four products
 // of 632 GFLOP, 1.05 PFLOP/s with everything between them (the library's largest plain product: 1.54); in 32 bits 4 x 511 tokens
@@ -28,7 +34,7 @@
 
 struct sams_xent {
     int32_t n, type, train;
-    int64_t t_max, dim, vocab, piece;
+    int64_t t_max, dim, vocab, piece, dz_bytes;
     hipStream_t stream;
     sams::Scratch scratch;
     int64_t h, w, dz, dh, part, token, at_label, inv, amax, exps;
@@ -38,7 +44,9 @@ namespace sams {
 
 using namespace gemm;
 
-constexpr int64_t kXentPieceBytes = (int64_t)1 << 30;        // of dz, for one piece of the vocabulary
+constexpr int64_t kXentPieceBytes = (int64_t)1 << 30;        // of dz, of some workers' tokens or one piece of the vocabulary
+// of one worker's dz, if there is as much memory: by pieces the backward pass of 16,384 tokens of 768 and 50,257 words takes 5.0 ms, whole 3.9
+constexpr int64_t kXentWorkerBytes = (int64_t)4 << 30;
 constexpr int kAmaxBlocks = 1024;
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -266,15 +274,16 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
     }
 }
 
-// The log-sums over the tiles and the losses of 16 tokens (a line of `part`) by a workgroup, each tile's by one of 16 threads in turn;
-// the first 16 threads get their token's loss.
+// What the tiles left of 16 tokens (a line of `part`) joined over the vocabulary by a workgroup, each tile's by one of 16 threads in turn;
+// the first 16 threads get their token's.
 //
 // With S the sum of 2^(z_v - top) over the words but the label, and d = top - z_label, a token's loss is log(1 + S 2^d).  d comes from
 // the label's product by one fma, against the same rounded `top` that the terms of S were taken against, so that the loss keeps its
 // digits where the label is nearly certain, however large the logits, and is never below 0.
+struct TokenSums { float top, rest, d; };
 template <int KIND>
-__device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, const int64_t *labels, int64_t first, int64_t end,
-                                            int64_t rows, int64_t vocab, float *lse, float2 (&joined)[4][16])
+__device__ __forceinline__ TokenSums token_sums(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, int64_t first, int64_t end, int64_t rows,
+                                                float2 (&joined)[4][16])
 {
     const int r = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t row = first + r;
@@ -286,16 +295,25 @@ __device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, con
     for (int o = 16; o < 64; o <<= 1) sums = join_sums(sums, make_float2(__shfl_xor(sums.x, o), __shfl_xor(sums.y, o)));
     if ((threadIdx.x & 63) < 16) joined[threadIdx.x >> 6][r] = sums;
     __syncthreads();
+    sums = join_sums(join_sums(joined[0][r], joined[1][r]), join_sums(joined[2][r], joined[3][r]));
+    const float top = sums.x == -INFINITY ? 0.f : sums.x;
+    return TokenSums{top, sums.y, row < end ? -__builtin_fmaf(at_label[row], kLog2e * unscale<KIND>(exps, 2), -top) : 0.f};
+}
+
+template <int KIND>
+__device__ __forceinline__ float token_loss(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, const int64_t *labels, int64_t first, int64_t end,
+                                            int64_t rows, int64_t vocab, float *lse, float2 (&joined)[4][16])
+{
+    const TokenSums k = token_sums<KIND>(part, tiles_v, at_label, exps, first, end, rows, joined);
+    const int64_t row = first + threadIdx.x;
     if (threadIdx.x >= 16 || row >= end) return 0.f;
     if (!takes_part(labels, row, vocab)) {
         lse[row] = 0.f;
         return 0.f;
     }
-    sums = join_sums(join_sums(joined[0][r], joined[1][r]), join_sums(joined[2][r], joined[3][r]));
-    const float top = sums.x == -INFINITY ? 0.f : sums.x;
-    const float d = -__builtin_fmaf(at_label[row], kLog2e * unscale<KIND>(exps, 2), -top), log_sum = log2f(sums.y + exp2f(-d));
-    lse[row] = (top + log_sum) * (1.f / kLog2e);
-    return d > 32.f ? (d + log_sum) * (1.f / kLog2e) : log1pf(sums.y * exp2f(d));      // (2^d may be too large where 2^-d is small)
+    const float log_sum = log2f(k.rest + exp2f(-k.d));
+    lse[row] = (k.top + log_sum) * (1.f / kLog2e);
+    return k.d > 32.f ? (k.d + log_sum) * (1.f / kLog2e) : log1pf(k.rest * exp2f(k.d));      // (2^d may be too large where 2^-d is small)
 }
 
 template <int KIND>
@@ -353,14 +371,20 @@ __global__ void __launch_bounds__(256) k_xent_loss(const float *token, const int
 
 // dz of one piece of the vocabulary (W: the piece), a row of words per token.  705 us at 8192 x 50,257 x 768 in bf16, 0.90 PFLOP/s: beside
 // the product an exponential each, and 823 MB written, a wavefront's rows through LDS so that they leave in whole lines.
-struct Token { float base; int label; };                             // log2 of the scale less the log-sum; the label's place in the tile
+//
+// rest == NULL: dz at the label is p - 1 for now, and `sums` [tiles_v][rows] gets each token's sum over the tile of the others; else `rest` is
+// the sum over all.
+struct Token { float base; int label; float rest; };                 // log2 of the scale less the log-sum; the label's place in the tile; the others' sum, if known
 constexpr int kNoLabel = -1;
+// whether dz at the label is -rest (in dz's scale)
+template <int KIND> __device__ __forceinline__ bool mostly_label(float rest) { return rest < 0.5f * (float)(1 << dz_exponent<KIND>()); }
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
-                                                        int64_t vocab, const float *lse, uint16_t *dz)
+                                                        int64_t vocab, const float *lse, uint16_t *dz, const float *rest, float *sums)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     __shared__ Token tokens[S::BN];
+    __shared__ float joined[S::WAVES_M][S::BN];
     uint32_t mi, ni, batch;
     tile_place(tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
@@ -376,10 +400,14 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
     if (threadIdx.x < S::BN) {
         const int64_t at = label - v0 - m0;
         const bool part = label >= 0 && label < vocab;               // elsewhere 2^(0 - infinity) = 0
-        tokens[threadIdx.x] = Token{part ? dz_exponent<KIND>() - log_sum * kLog2e : -INFINITY, part && at >= 0 && at < S::BM ? (int)at : kNoLabel};
+        const bool here = part && at >= 0 && at < S::BM;
+        tokens[threadIdx.x] = Token{part ? dz_exponent<KIND>() - log_sum * kLog2e : -INFINITY, here ? (int)at : kNoLabel, here && rest ? rest[row] : INFINITY};
     }
     __syncthreads();
     const float f = kLog2e * unscale<KIND>(exps, 2), one = (float)(1 << dz_exponent<KIND>());
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
+    float sum[S::NI];
+    int block = -1;
     const int limit = W.size - m0 < S::BM ? (int)(W.size - m0) : S::BM;          // of the tile's words, in the vocabulary
     constexpr int BYTES = KIND == SPLIT ? 4 : 2;
     const int64_t row_bytes = row_words<KIND>(W.size) * 2;
@@ -388,6 +416,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
         acc, lds,
         [&](int n) {
             const Token k = tokens[n];
+            sum[++block] = 0.f;
             return std::make_pair(k, __any(k.label != kNoLabel) != 0);
         },
         [&](const std::pair<Token, bool> &kl, int m, const float (&z)[4]) {
@@ -395,21 +424,81 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, in
             float g[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) g[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[e], f, k.base));
-            if (kl.second) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (m + e == k.label) g[e] -= one;
-            }
             if (limit < S::BM) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (m + e >= limit) g[e] = 0.f;
             }
+            float four = (g[0] + g[1]) + (g[2] + g[3]);
+            if (kl.second) {
+                float others[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool it = m + e == k.label;
+                    others[e] = it ? 0.f : g[e];
+                    g[e] = it ? (mostly_label<KIND>(k.rest) ? -k.rest : g[e] - one) : g[e];
+                }
+                four = (others[0] + others[1]) + (others[2] + others[3]);
+            }
+            sum[block] += four;
             return pack_words<KIND>(g);
         },
         [&](int n, int at, u32x4 w) {
             if (n0 + n < H.size && m0 * BYTES + at < row_bytes) *(u32x4 *)(corner + n * row_bytes + at) = w;
         });
+    if (rest) return;
+#pragma unroll
+    for (int j = 0; j < S::NI; ++j) {
+        sum[j] += __shfl_xor(sum[j], 32);
+        if (lane < 32) joined[wm][(wn * S::NI + j) * 32 + lane] = sum[j];
+    }
+    __syncthreads();
+    if (!mine) return;
+    float all = joined[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < S::WAVES_M; ++w) all += joined[w][threadIdx.x];
+    sums[mi * H.size + row] = all;
+}
+
+// The words of nearly certain labels, minus the sum of the others: 16 tokens by a workgroup, each tile's sums by one of 16 threads in turn.
+template <int KIND>
+__global__ void __launch_bounds__(256) k_xent_dz_label(const float *sums, int tiles_v, const int64_t *labels, int64_t rows, int64_t vocab, uint16_t *dz, int64_t ld)
+{
+    __shared__ float joined[4][16];
+    const int r = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t row = blockIdx.x * (int64_t)16 + r;
+    float sum = 0.f;
+    if (row < rows)
+#pragma unroll 4
+        for (int i = g; i < tiles_v; i += 16) sum += sums[i * rows + row];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if ((threadIdx.x & 63) < 16) joined[threadIdx.x >> 6][r] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 16 || row >= rows || !takes_part(labels, row, vocab)) return;
+    sum = (joined[0][r] + joined[1][r]) + (joined[2][r] + joined[3][r]);
+    if (!mostly_label<KIND>(sum)) return;
+    const float v[4] = {-sum, 0.f, 0.f, 0.f};
+    const auto w = pack_words<KIND>(v);
+    const int64_t label = labels[row];
+    if constexpr (KIND == SPLIT) {
+        uint16_t *p = dz + row * ld + (label >> 5) * 64 + (label & 31);
+        p[0] = (uint16_t)w[0];
+        p[32] = (uint16_t)w[2];
+    } else {
+        dz[row * ld + label] = (uint16_t)w[0];
+    }
+}
+
+// The same sums from the log-sums' parts, in dz's scale: 1 - p = S 2^d / (1 + S 2^d).
+template <int KIND>
+__global__ void __launch_bounds__(256) k_xent_rest(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, int64_t rows, float *rest)
+{
+    __shared__ float2 joined[4][16];
+    const int64_t first = blockIdx.x * (int64_t)16;
+    const TokenSums k = token_sums<KIND>(part, tiles_v, at_label, exps, first, rows, rows, joined);
+    if (threadIdx.x >= 16 || first + threadIdx.x >= rows) return;
+    rest[first + threadIdx.x] = (float)(1 << dz_exponent<KIND>()) * (k.rest / (k.rest + exp2f(-k.d)));
 }
 
 // dW of one worker and piece.  ADD: to what is there, as 32-bit numbers.  Both operands lie with their k's, the tokens, as rows; a worker's
@@ -511,6 +600,7 @@ __global__ void __launch_bounds__(256) k_xent_dh_join(const float *part, int par
     }
 }
 
+static int64_t dz_words(int64_t vocab) { return (vocab + 255) / 256 * 256; }       // room for a token's, in numbers
 static int64_t dh_pitch(int64_t dim) { return (dim + 3) / 4 * 4; }
 
 // the tile of dh's product over one piece, and the parts that the vocabulary is cut into for it
@@ -551,6 +641,21 @@ static int enqueue_operands(sams_xent *c, int64_t t, const void *h, Rows hs, con
     return SAMS_OK;
 }
 
+// the log-sums' parts of rows tokens; the tiles of the vocabulary
+template <int KIND>
+static uint32_t enqueue_stats(sams_xent *c, const Operand &W, const Operand &H, const int64_t *labels)
+{
+    uint32_t tv = 0;
+    with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, c->vocab, H.size, false, c->dim, 1, 0).shape, [&](auto shape) {
+        typedef decltype(shape) S;
+        tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
+        const uint32_t tt = (uint32_t)((H.size + S::BN - 1) / S::BN);
+        hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt,
+                           c->scratch.at<int32_t>(c->exps), labels, c->scratch.at<float2>(c->part), c->scratch.at<float>(c->at_label));
+    });
+    return tv;
+}
+
 template <int T>
 static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, const void *w, int64_t w_row, const int64_t *labels, float *loss, float *lse)
 {
@@ -562,13 +667,7 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
         Operand H, W;
         SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, false, nullptr, &H, &W)));
         float2 *part = c->scratch.at<float2>(c->part);
-        uint32_t tv = 0;
-        with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, c->vocab, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
-            typedef decltype(shape) S;
-            tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
-            const uint32_t tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-            hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt, exps, labels, part, at_label);
-        });
+        const uint32_t tv = enqueue_stats<KIND>(c, W, H, labels);
         if (t <= kJoinTokens && tv <= kJoinTiles) {
             hipLaunchKernelGGL(k_xent_join_few<KIND>, dim3((unsigned)c->n), dim3(256), 0, c->stream, part, (int)tv, at_label, exps, labels, (int)t, rows, c->vocab, lse, loss);
             SAMS_HIP(hipGetLastError());
@@ -587,48 +686,65 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
 {
     constexpr int KIND = kind_of<T>();
     typedef typename TypeOf<T>::type E;
-    const int64_t rows = c->n * t;
-    float *inv = c->scratch.at<float>(c->inv);
     const int32_t *exps = c->scratch.at<int32_t>(c->exps);
     uint16_t *dz = c->scratch.at<uint16_t>(c->dz);
-    Operand H, W;
-    SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, grad, &H, &W)));
-    float *part = c->scratch.at<float>(c->dh);
-    const int64_t pitch = dh_pitch(c->dim);
-    const TileChoice hidden = rows ? dh_tiles(KIND == SPLIT, rows, c->dim, c->piece) : TileChoice{2, 0};
-    const int parts = hidden.parts;
-    for (int64_t v0 = 0; v0 < c->vocab; v0 += c->piece) {
-        const int64_t piece = c->vocab - v0 < c->piece ? c->vocab - v0 : c->piece;
-        const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
-        if (rows)
-            with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
+    Operand allH, W;
+    SAMS_TRY((enqueue_operands<T, KIND>(c, t, h, hs, w, w_row, labels, true, grad, &allH, &W)));
+    float *part = c->scratch.at<float>(c->dh), *sums = c->scratch.at<float>(c->part), *rest = nullptr;
+    const int64_t pitch = dh_pitch(c->dim), whole = dz_words(c->vocab), worker_bytes = t * whole * type_size(c->type);
+    // as many workers at a time as the scratch has room for, evenly; or a worker by pieces of the vocabulary
+    const bool pieces = t && (worker_bytes > c->dz_bytes || whole > kMaxRowWords / 2);
+    const int64_t most = pieces ? 1 : worker_bytes ? std::min<int64_t>(c->n, c->dz_bytes / worker_bytes) : c->n, turns = (c->n + most - 1) / most, each = (c->n + turns - 1) / turns;
+    for (int64_t first = 0; first < c->n; first += each) {
+        const int64_t workers = std::min(each, c->n - first), rows = workers * t, row0 = first * t, size = pieces ? c->piece : c->vocab;
+        const int64_t *label = labels + row0;
+        const float *log_sums = lse + row0, *inv = c->scratch.at<float>(c->inv) + first;
+        const Operand H{allH.p + row0 * allH.ld, allH.ld, rows};
+        if (pieces) {
+            rest = c->scratch.at<float>(c->token);
+            const uint32_t tv = enqueue_stats<KIND>(c, W, H, label);
+            hipLaunchKernelGGL(k_xent_rest<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, c->scratch.at<float2>(c->part), (int)tv, c->scratch.at<float>(c->at_label),
+                               exps, rows, rest);
+        }
+        const TileChoice hidden = rows ? dh_tiles(KIND == SPLIT, rows, c->dim, size) : TileChoice{2, 0};
+        const int parts = hidden.parts;
+        for (int64_t v0 = 0; v0 < c->vocab; v0 += size) {
+            const int64_t piece = std::min(size, c->vocab - v0);
+            const Operand Wp{W.p + v0 * W.ld, W.ld, piece};
+            if (rows)
+                with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
+                    typedef decltype(shape) S;
+                    const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
+                    hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, label, v0, c->vocab, log_sums, dz, rest, sums);
+                    if (!rest)
+                        hipLaunchKernelGGL(k_xent_dz_label<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, sums, (int)tv, label, rows, c->vocab, dz, row_words<KIND>(piece));
+                });
+            with_tile<KIND>(choose_tiles(KIND == SPLIT, workers, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
                 typedef decltype(shape) S;
-                const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, labels, v0, c->vocab, lse, dz);
+                const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
+                auto weight = [&](auto kernel, auto *out) {
+                    hipLaunchKernelGGL(kernel, dim3(td * tv * (unsigned)workers), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv,
+                                       out + first * dws.worker + v0 * dws.row, dws);
+                };
+                if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
+                else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
+                else if (accumulate) weight(k_xent_dw<S, KIND, T, true>, (E *)dw);
+                else weight(k_xent_dw<S, KIND, T, false>, (E *)dw);
             });
-        with_tile<KIND>(choose_tiles(KIND == SPLIT, c->n, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
-            typedef decltype(shape) S;
-            const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
-            auto weight = [&](auto kernel, auto *out) {
-                hipLaunchKernelGGL(kernel, dim3(td * tv * (unsigned)c->n), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv, out + v0 * dws.row, dws);
-            };
-            if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
-            else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
-            else if (accumulate) weight(k_xent_dw<S, KIND, T, true>, (E *)dw);
-            else weight(k_xent_dw<S, KIND, T, false>, (E *)dw);
-        });
+            if (rows)
+                with_tile<KIND>(hidden.shape, [&](auto shape) {
+                    typedef decltype(shape) S;
+                    const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
+                    hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt * (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt,
+                                       v0 == 0, part, pitch, (uint32_t)parts);
+                });
+            SAMS_HIP(hipGetLastError());
+        }
         if (rows)
-            with_tile<KIND>(hidden.shape, [&](auto shape) {
-                typedef decltype(shape) S;
-                const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt * (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt, v0 == 0,
-                                   part, pitch, (uint32_t)parts);
-            });
+            hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, parts, rows, pitch, t, c->dim, exps, inv,
+                               (E *)dh + first * dhs.worker, dhs);
         SAMS_HIP(hipGetLastError());
     }
-    if (rows)
-        hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, parts, rows, pitch, t, c->dim, exps, inv, (E *)dh, dhs);
-    SAMS_HIP(hipGetLastError());
     return SAMS_OK;
 }
 
@@ -656,25 +772,35 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     if (!c) return SAMS_ENOMEM;
     c->n = n; c->t_max = t_max; c->dim = dim; c->vocab = vocab; c->type = type; c->train = train != 0;
     c->stream = (hipStream_t)hip_stream;
-    const int64_t rows = n * t_max, ld = type == SAMS_F32 ? row_words<SPLIT>(dim) : row_words<F16>(dim);
-    c->h = c->scratch.reserve(rows * ld * 2);
-    c->w = c->scratch.reserve(vocab * ld * 2);
-    c->part = c->scratch.reserve(rows * ((vocab + Small::BM - 1) / Small::BM) * 8);
-    c->token = c->scratch.reserve(rows * 4);
-    c->at_label = c->scratch.reserve(rows * 4);
-    c->inv = c->scratch.reserve(n * 4);
-    c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
-    c->exps = c->scratch.reserve(2 * 4);
-    if (train) {
-        const int64_t row_bytes = type == SAMS_F32 ? 4 : 2, whole = (vocab + 255) / 256 * 256;
-        c->piece = rows ? kXentPieceBytes / (rows * row_bytes) / 256 * 256 : whole;
-        if (c->piece < 1024) c->piece = 1024;
-        c->piece = std::min({c->piece, whole, kMaxRowWords / 2});
-        c->dz = c->scratch.reserve(rows * c->piece * row_bytes);
-        // for fewer tokens there may be more parts, in as much memory
-        c->dh = c->scratch.reserve(std::max(rows * dh_pitch(dim) * 4, std::min(kPartBytes, rows * dh_pitch(dim) * 4 * kMaxSplit)));
-    }
-    int rc = c->scratch.take();
+    const int64_t rows = n * t_max, ld = type == SAMS_F32 ? row_words<SPLIT>(dim) : row_words<F16>(dim), row_bytes = type_size(type), whole = dz_words(vocab),
+                  worker_bytes = t_max * whole * row_bytes;
+    auto take = [&](int64_t most) {                                  // most: of a worker's dz that is not cut into pieces
+        c->scratch = Scratch{};
+        c->h = c->scratch.reserve(rows * ld * 2);
+        c->w = c->scratch.reserve(vocab * ld * 2);
+        c->part = c->scratch.reserve(rows * ((vocab + Small::BM - 1) / Small::BM) * 8);
+        c->token = c->scratch.reserve(rows * 4);
+        c->at_label = c->scratch.reserve(rows * 4);
+        c->inv = c->scratch.reserve(n * 4);
+        c->amax = c->scratch.reserve(2 * kAmaxBlocks * 4);
+        c->exps = c->scratch.reserve(2 * 4);
+        if (train) {
+            if (worker_bytes <= most && whole <= kMaxRowWords / 2) {
+                c->piece = whole;
+                c->dz_bytes = worker_bytes * (worker_bytes ? std::min<int64_t>(n, std::max<int64_t>(1, kXentPieceBytes / worker_bytes)) : 0);
+            } else {
+                c->piece = t_max ? kXentPieceBytes / (t_max * row_bytes) / 256 * 256 : whole;
+                c->piece = std::min({std::max<int64_t>(c->piece, 1024), whole, kMaxRowWords / 2});
+                c->dz_bytes = t_max * c->piece * row_bytes;
+            }
+            c->dz = c->scratch.reserve(c->dz_bytes);
+            // for fewer tokens there may be more parts, in as much memory
+            c->dh = c->scratch.reserve(std::max(rows * dh_pitch(dim) * 4, std::min(kPartBytes, rows * dh_pitch(dim) * 4 * kMaxSplit)));
+        }
+        return c->scratch.take();
+    };
+    int rc = take(kXentWorkerBytes);
+    if (rc == SAMS_ENOMEM && train && worker_bytes > kXentPieceBytes && worker_bytes <= kXentWorkerBytes) rc = take(kXentPieceBytes);
     if (rc == SAMS_OK) rc = enqueue_fill_u32_on(nullptr, c->stream, c->scratch.at<uint32_t>(c->exps), 2, 0u);
     if (rc != SAMS_OK) {
         if (c->scratch.base) (void)hipFree(c->scratch.base);

@@ -67,3 +67,60 @@ def test_labels_far_from_the_largest_logit(sams, kind):
     want = torch.logsumexp(z, 0) - z
     assert ((loss.cpu().double() - want).abs() <= 2.0 ** -22 * want).all(), loss
     assert ((lse.cpu().double() - 160).abs() <= 2.0 ** -22 * 160).all()
+
+
+WORD = {torch.float32: 2.0 ** -21, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+HALF_ULP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
+
+
+def check_gradients(sams, h, w, labels):
+    """Gradients against 64 bits, a worker at a time on the GPU.  A probability's exponent carries the roundings of lse, of its product with
+    log2 e, of log2 e itself and of an fma, each 2^-24 of a logit's size: 2^-22 |z| of the probability, and 2^-18 of exp2 and of the sum
+    over the vocabulary; dz is that far off in each number, the label's too, rounded to the words it is held in (and 2^-38), and the products
+    add 2^-20 of the magnitudes they add up."""
+    (n, t, dim), vocab, kind = h.shape, w.shape[0], h.dtype
+    h, w, labels = h.cuda(), w.cuda(), labels.cuda()
+    loss, lse = torch.empty((n,), device="cuda"), torch.empty((n, t), device="cuda")
+    dh, dw = torch.full_like(h, float("nan")), torch.full((n, vocab, dim), float("nan"), device="cuda", dtype=kind)
+    with sams.LinearCrossEntropy(n, t, dim, vocab, kind) as op:
+        op.linear_xent_forward(h, w, labels, loss, lse)
+        op.linear_xent_backward(h, w, labels, lse, None, dh, dw)
+    wd = w.double()
+    for i in range(n):
+        want_dw, tol_dw = torch.zeros((2, vocab, dim), device="cuda", dtype=torch.float64)
+        for lo in range(0, t, 1 << 16):
+            part = slice(lo, min(t, lo + (1 << 16)))
+            hd, at = h[i, part].double(), labels[i, part, None]
+            z = hd @ wd.t().contiguous()
+            most = float(z.abs().max())
+            p = torch.exp(z - z.gather(-1, at)).scatter_(-1, at, 0.0)
+            rest = p.sum(-1, keepdim=True)
+            p /= 1 + rest
+            dz = p.scatter_(-1, at, -rest / (1 + rest)) / t
+            edz = dz.abs() * (2.0 ** -22 * most + 2.0 ** -18 + 2.0 ** -20 + WORD[kind]) + 2.0 ** -38 / t
+            compare(("dh", i, (n, t, vocab), kind), dh[i, part], dz @ wd, edz @ wd.abs())
+            want_dw += dz.t().contiguous() @ hd
+            tol_dw += edz.t().contiguous() @ hd.abs()
+        compare(("dw", i, (n, t, vocab), kind), dw[i], want_dw, tol_dw)
+
+
+def compare(what, got, want, tol):
+    slack = tol + HALF_ULP[got.dtype] * (want.abs() + tol) + TINY[got.dtype]
+    off = (got.double() - want).abs()
+    print(*what, "off by %.3g of what is allowed" % float((off / slack.clamp(min=1e-300)).max()))
+    assert (off <= slack).all(), what
+
+
+@pytest.mark.parametrize("common", [188.0, 0.0, -192.0])
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+@pytest.mark.parametrize("n,t,vocab", [(24, 1, 1000), (5, 70, 777), (2, 300, 5003), (2, 3, 1), (1, 1, 257)])
+def test_gradients_keep_their_digits(sams, n, t, vocab, kind, common):
+    check_gradients(sams, *make(n, t, vocab, kind, common))
+
+
+@pytest.mark.parametrize("n,t,vocab,kind", [(3, 22000, 9001, torch.bfloat16), (2, 70000, 5003, torch.float32), (1, 530000, 4001, torch.bfloat16), (2, 3, 2100001, torch.float32),
+                                            (1, 3, 4300007, torch.float16)], ids=str)
+def test_more_than_the_scratch_has_room_for(sams, n, t, vocab, kind):
+    """dz of some workers after the others (two of three, one of two), and by pieces of the vocabulary where a worker's has no room or is too wide."""
+    check_gradients(sams, *make(n, t, vocab, kind, 24.0, dim=24))
