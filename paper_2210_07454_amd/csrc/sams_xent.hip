@@ -158,11 +158,13 @@ __global__ void __launch_bounds__(256) k_xent_pack(Packed H, unsigned blocks_h, 
     }
 }
 
+// 1 / the scale of H (0), of W (1), of both (2).  Of both, at least 2^-126: a product of words is below 2^48, and a logit of 2^-78 in place of
+// a smaller one moves nothing, whereas 0 would make NaN of the -infinity that stands for words which are none.
 template <int KIND>
-__device__ __forceinline__ float unscale(const int32_t *exps, int which)        // 1 / the scale of H (0), of W (1), of both (2)
+__device__ __forceinline__ float unscale(const int32_t *exps, int which)
 {
     if constexpr (KIND != SPLIT) return 1.f;
-    return ldexpf(1.f, -(which == 0 ? exps[0] : which == 1 ? exps[1] : exps[0] + exps[1]));
+    return ldexpf(1.f, -(which == 0 ? exps[0] : which == 1 ? exps[1] : min(exps[0] + exps[1], 126)));
 }
 
 // (largest, sum of 2^(number - largest)) of two sets of numbers
