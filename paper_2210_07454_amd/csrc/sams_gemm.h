@@ -515,9 +515,18 @@ __device__ __forceinline__ void tile_place(uint32_t at, uint32_t total, uint32_t
     mi = first + in % wide;
     ni = in / wide;
 }
-__device__ __forceinline__ void tile_place(uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
+// A launch's share of the tiles: a grid may have fewer than 2^32 threads, which thin matrices' tiles can exceed.
+struct Launch { uint32_t first, total; };
+__device__ __forceinline__ void tile_place(Launch l, uint32_t tiles_m, uint32_t tiles_n, uint32_t &mi, uint32_t &ni, uint32_t &batch)
 {
-    tile_place(blockIdx.x, gridDim.x, tiles_m, tiles_n, mi, ni, batch);
+    tile_place(l.first + blockIdx.x, l.total, tiles_m, tiles_n, mi, ni, batch);
+}
+// f(workgroups, share) for as many launches as the tiles take; a first one that is a multiple of 8 leaves the XCDs' runs as they are
+template <typename F>
+static void in_launches(int64_t tiles, int threads, F f)
+{
+    const int64_t most = ((int64_t)1 << 31) / threads;
+    for (int64_t first = 0; first < tiles; first += most) f(dim3((unsigned)std::min(most, tiles - first)), Launch{(uint32_t)first, (uint32_t)tiles});
 }
 
 // The tiles in use.  At 8192^3 (16 bits; pairs), Large reaches 1.27 PFLOP/s (0.45), 83 % of the library's 1.54 in 16 bits and three times

@@ -316,12 +316,12 @@ struct OrthoOut {
 //
 // X' = P X (X P where X is tall), times f and, in the first step, sigma; LAST: to the caller (T: its type; with parameters f32)
 template <class S, int KIND, bool TALL, bool LAST, int T>
-__global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, uint32_t tiles_m, uint32_t tiles_n, float f,
+__global__ void __launch_bounds__(S::THREADS) k_ortho_apply(const uint16_t *poly, const uint16_t *x, OrthoDims d, Launch launch, uint32_t tiles_m, uint32_t tiles_n, float f,
                                                             const OrthoScale *scale, uint16_t *next, OrthoOut o)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni, batch;
-    tile_place(tiles_m, tiles_n, mi, ni, batch);
+    tile_place(launch, tiles_m, tiles_n, mi, ni, batch);
     const int64_t matrix = batch;
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;            // m: X's columns, n: its rows
     const int64_t ldx = row_words<KIND>(d.cols), ldp = row_words<KIND>(d.small);
@@ -683,7 +683,9 @@ static int enqueue_steps(sams_ortho *c, int64_t batch, const SmallSteps &plan, c
             typedef decltype(shape) S;
             const uint32_t tm = (uint32_t)((d.cols + S::BM - 1) / S::BM), tn = (uint32_t)((d.rows + S::BN - 1) / S::BN);
             auto apply = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3(tm * tn * (unsigned)batch), dim3(S::THREADS), 0, c->stream, poly, x, d, tm, tn, p.f_apply, first, next, o);
+                in_launches((int64_t)tm * tn * batch, S::THREADS, [&](dim3 grid, Launch l) {
+                    hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), 0, c->stream, poly, x, d, l, tm, tn, p.f_apply, first, next, o);
+                });
             };
             if (tall && last) apply(k_ortho_apply<S, KIND, true, true, T>);
             else if (tall) apply(k_ortho_apply<S, KIND, true, false, T>);

@@ -52,6 +52,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 
 constexpr int64_t kPartBytes = (int64_t)256 << 20;          // of partial sums of dh, at most (but one for every token)
 constexpr int kMaxSplit = 64;
+constexpr int64_t kMostBlocks = 1 << 20;                    // workgroups of 256 that go from row to row
 
 template <int KIND> __host__ __device__ constexpr int dz_exponent() { return KIND == BF16 ? 0 : 14; }
 template <int T> constexpr int kind_of() { return T == SAMS_F32 ? SPLIT : T == SAMS_BF16 ? BF16 : F16; }
@@ -186,7 +187,7 @@ template <int KIND> constexpr bool kStatsInTurn = KIND != SPLIT;
 // label.  A lane holds numbers of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's
 // product is left in `at_label`, as it is, by the lane that holds it: see token_loss.
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels,
+__global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H, int64_t dim, uint32_t first, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels,
                                                            float2 *part, float *at_label)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_stats(Operand W, Operand H,
     float2 *joined = (float2 *)(lds + (ON ? (S::STAGES - 1) * Logits::STAGE : 0));           // [WAVES_M][BN]
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / S::WAVES_N, wn = wave % S::WAVES_N;
     const uint32_t tiles = tiles_v * tiles_t;
-    uint32_t id = blockIdx.x, mi, ni, batch;
+    uint32_t id = first + blockIdx.x, mi, ni, batch;
     tile_place(id, tiles, tiles_v, tiles_t, mi, ni, batch);
     Logits logits;
     logits.start(W, (int64_t)mi * S::BM, H, (int64_t)ni * S::BN, 0, dim, lds);
@@ -323,9 +324,11 @@ __global__ void __launch_bounds__(256) k_xent_join(const float2 *part, int tiles
                                                    float *token)
 {
     __shared__ float2 joined[4][16];
-    const int64_t first = blockIdx.x * (int64_t)16;
-    const float loss = token_loss<KIND>(part, tiles_v, at_label, exps, labels, first, rows, rows, vocab, lse, joined);
-    if (threadIdx.x < 16 && first + threadIdx.x < rows) token[first + threadIdx.x] = loss;
+    for (int64_t first = blockIdx.x * (int64_t)16; first < rows; first += gridDim.x * (int64_t)16) {
+        const float loss = token_loss<KIND>(part, tiles_v, at_label, exps, labels, first, rows, rows, vocab, lse, joined);
+        if (threadIdx.x < 16 && first + threadIdx.x < rows) token[first + threadIdx.x] = loss;
+        __syncthreads();
+    }
 }
 
 // The same and the mean over a worker's tokens in one launch, a workgroup per worker, where there are few (kJoinTokens, kJoinTiles): 1.5 us
@@ -381,14 +384,14 @@ constexpr int kNoLabel = -1;
 // whether dz at the label is -rest (in dz's scale)
 template <int KIND> __device__ __forceinline__ bool mostly_label(float rest) { return rest < 0.5f * (float)(1 << dz_exponent<KIND>()); }
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
+__global__ void __launch_bounds__(S::THREADS) k_xent_dz(Operand W, Operand H, int64_t dim, Launch launch, uint32_t tiles_v, uint32_t tiles_t, const int32_t *exps, const int64_t *labels, int64_t v0,
                                                         int64_t vocab, const float *lse, uint16_t *dz, const float *rest, float *sums)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     __shared__ Token tokens[S::BN];
     __shared__ float joined[S::WAVES_M][S::BN];
     uint32_t mi, ni, batch;
-    tile_place(tiles_v, tiles_t, mi, ni, batch);
+    tile_place(launch, tiles_v, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     static_assert(S::BN <= S::THREADS, "a thread for each of the tile's tokens");
     const int64_t row = n0 + threadIdx.x;
@@ -468,27 +471,29 @@ __global__ void __launch_bounds__(256) k_xent_dz_label(const float *sums, int ti
 {
     __shared__ float joined[4][16];
     const int r = threadIdx.x & 15, g = threadIdx.x >> 4;
-    const int64_t row = blockIdx.x * (int64_t)16 + r;
-    float sum = 0.f;
-    if (row < rows)
+    for (int64_t first = blockIdx.x * (int64_t)16; first < rows; first += gridDim.x * (int64_t)16) {
+        const int64_t row = first + r;
+        float sum = 0.f;
+        if (row < rows)
 #pragma unroll 4
-        for (int i = g; i < tiles_v; i += 16) sum += sums[i * rows + row];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if ((threadIdx.x & 63) < 16) joined[threadIdx.x >> 6][r] = sum;
-    __syncthreads();
-    if (threadIdx.x >= 16 || row >= rows || !takes_part(labels, row, vocab)) return;
-    sum = (joined[0][r] + joined[1][r]) + (joined[2][r] + joined[3][r]);
-    if (!mostly_label<KIND>(sum)) return;
-    const float v[4] = {-sum, 0.f, 0.f, 0.f};
-    const auto w = pack_words<KIND>(v);
-    const int64_t label = labels[row];
-    if constexpr (KIND == SPLIT) {
-        uint16_t *p = dz + row * ld + (label >> 5) * 64 + (label & 31);
-        p[0] = (uint16_t)w[0];
-        p[32] = (uint16_t)w[2];
-    } else {
-        dz[row * ld + label] = (uint16_t)w[0];
+            for (int i = g; i < tiles_v; i += 16) sum += sums[i * rows + row];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if ((threadIdx.x & 63) < 16) joined[threadIdx.x >> 6][r] = sum;
+        __syncthreads();
+        sum = (joined[0][r] + joined[1][r]) + (joined[2][r] + joined[3][r]);
+        __syncthreads();
+        if (threadIdx.x >= 16 || row >= rows || !takes_part(labels, row, vocab) || !mostly_label<KIND>(sum)) continue;
+        const float v[4] = {-sum, 0.f, 0.f, 0.f};
+        const auto w = pack_words<KIND>(v);
+        const int64_t label = labels[row];
+        if constexpr (KIND == SPLIT) {
+            uint16_t *p = dz + row * ld + (label >> 5) * 64 + (label & 31);
+            p[0] = (uint16_t)w[0];
+            p[32] = (uint16_t)w[2];
+        } else {
+            dz[row * ld + label] = (uint16_t)w[0];
+        }
     }
 }
 
@@ -497,23 +502,24 @@ template <int KIND>
 __global__ void __launch_bounds__(256) k_xent_rest(const float2 *part, int tiles_v, const float *at_label, const int32_t *exps, int64_t rows, float *rest)
 {
     __shared__ float2 joined[4][16];
-    const int64_t first = blockIdx.x * (int64_t)16;
-    const TokenSums k = token_sums<KIND>(part, tiles_v, at_label, exps, first, rows, rows, joined);
-    if (threadIdx.x >= 16 || first + threadIdx.x >= rows) return;
-    rest[first + threadIdx.x] = (float)(1 << dz_exponent<KIND>()) * (k.rest / (k.rest + exp2f(-k.d)));
+    for (int64_t first = blockIdx.x * (int64_t)16; first < rows; first += gridDim.x * (int64_t)16) {
+        const TokenSums k = token_sums<KIND>(part, tiles_v, at_label, exps, first, rows, rows, joined);
+        if (threadIdx.x < 16 && first + threadIdx.x < rows) rest[first + threadIdx.x] = (float)(1 << dz_exponent<KIND>()) * (k.rest / (k.rest + exp2f(-k.d)));
+        __syncthreads();
+    }
 }
 
 // dW of one worker and piece.  ADD: to what is there, as 32-bit numbers.  Both operands lie with their k's, the tokens, as rows; a worker's
 // products are its own, so that there are tiles enough without a split of k.  690 us at 8 x 1024 x 50,257 x 768 in bf16, 0.92 PFLOP/s,
 // with 617 MB written.
 template <class S, int KIND, int T, bool ADD>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, uint32_t tiles_d, uint32_t tiles_v,
+__global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, Launch launch, uint32_t tiles_d, uint32_t tiles_v,
                                                         const int32_t *exps, const float *inv, typename TypeOf<T>::type *dw, Rows ds)
 {
     typedef typename TypeOf<T>::type E;
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni, batch;
-    tile_place(tiles_d, tiles_v, mi, ni, batch);
+    tile_place(launch, tiles_d, tiles_v, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN, worker = batch;
     const int64_t ldz = row_words<KIND>(piece), ldh = row_words<KIND>(dim);
     const Operand Z{dz + worker * t * ldz, ldz, piece}, H{h + worker * t * ldh, ldh, dim};
@@ -549,12 +555,12 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
 // The result has few tiles (96 of 256 x 256 for 8192 tokens of 768) and k is the vocabulary: the parts make them enough for the chip.
 // 586 us at 8192 x 50,257 x 768 in bf16, 1.08 PFLOP/s, and 23 us to join the parts.
 template <class S, int KIND>
-__global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
+__global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, Launch launch, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
                                                         int64_t pitch, uint32_t parts)
 {
     __shared__ __align__(16) char lds[S::LDS_BYTES];
     uint32_t mi, ni, batch;
-    tile_place(tiles_d, tiles_t, mi, ni, batch);
+    tile_place(launch, tiles_d, tiles_t, mi, ni, batch);
     const int64_t m0 = (int64_t)mi * S::BM, n0 = (int64_t)ni * S::BN;
     const int64_t steps = (piece + tile_k<KIND>() - 1) / tile_k<KIND>();
     const int64_t lo = steps * batch / parts * tile_k<KIND>(), hi = steps * (batch + 1) / parts * tile_k<KIND>();
@@ -578,27 +584,27 @@ template <int KIND, int T>
 __global__ void __launch_bounds__(256) k_xent_dh_join(const float *part, int parts, int64_t rows, int64_t pitch, int64_t t, int64_t dim, const int32_t *exps, const float *inv,
                                                       typename TypeOf<T>::type *dh, Rows ds)
 {
-    const int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const float f = inv[row / t] / (float)(1 << dz_exponent<KIND>()), fw = unscale<KIND>(exps, 1);       // apart: together they may be too small
-    typename TypeOf<T>::type *out = dh + row / t * ds.worker + row % t * ds.row;
-    constexpr int N = kPiece<T>;
-    for (int64_t i = (threadIdx.x & 63) * N; i < dim; i += 64 * N) {
-        float v[N];
+    for (int64_t row = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * (int64_t)4) {
+        const float f = inv[row / t] / (float)(1 << dz_exponent<KIND>()), fw = unscale<KIND>(exps, 1);   // apart: together they may be too small
+        typename TypeOf<T>::type *out = dh + row / t * ds.worker + row % t * ds.row;
+        constexpr int N = kPiece<T>;
+        for (int64_t i = (threadIdx.x & 63) * N; i < dim; i += 64 * N) {
+            float v[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = 0.f;
+            for (int e = 0; e < N; ++e) v[e] = 0.f;
 #pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const float *at = part + (p * rows + row) * pitch + i;
+            for (int p = 0; p < parts; ++p) {
+                const float *at = part + (p * rows + row) * pitch + i;
 #pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const float4 a = i + e < pitch ? *(const float4 *)(at + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-                v[e] += a.x; v[e + 1] += a.y; v[e + 2] += a.z; v[e + 3] += a.w;
+                for (int e = 0; e < N; e += 4) {
+                    const float4 a = i + e < pitch ? *(const float4 *)(at + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    v[e] += a.x; v[e + 1] += a.y; v[e + 2] += a.z; v[e + 3] += a.w;
+                }
             }
-        }
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = v[e] * f * fw;
-        store_piece<T>(out, i, dim, v);
+            for (int e = 0; e < N; ++e) v[e] = v[e] * f * fw;
+            store_piece<T>(out, i, dim, v);
+        }
     }
 }
 
@@ -652,8 +658,12 @@ static uint32_t enqueue_stats(sams_xent *c, const Operand &W, const Operand &H, 
         typedef decltype(shape) S;
         tv = (uint32_t)((c->vocab + S::BM - 1) / S::BM);
         const uint32_t tt = (uint32_t)((H.size + S::BN - 1) / S::BN);
-        hipLaunchKernelGGL((k_xent_stats<S, KIND>), dim3(kStatsInTurn<KIND> ? at_once<S>(tv * tt) : tv * tt), dim3(S::THREADS), 0, c->stream, W, H, c->dim, tv, tt,
-                           c->scratch.at<int32_t>(c->exps), labels, c->scratch.at<float2>(c->part), c->scratch.at<float>(c->at_label));
+        auto launch = [&](dim3 grid, uint32_t first) {
+            hipLaunchKernelGGL((k_xent_stats<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, W, H, c->dim, first, tv, tt, c->scratch.at<int32_t>(c->exps), labels,
+                               c->scratch.at<float2>(c->part), c->scratch.at<float>(c->at_label));
+        };
+        if (kStatsInTurn<KIND>) launch(dim3(at_once<S>(tv * tt)), 0);
+        else in_launches((int64_t)tv * tt, S::THREADS, [&](dim3 grid, Launch l) { launch(grid, l.first); });
     });
     return tv;
 }
@@ -675,7 +685,7 @@ static int enqueue_forward(sams_xent *c, int64_t t, const void *h, Rows hs, cons
             SAMS_HIP(hipGetLastError());
             return SAMS_OK;
         }
-        hipLaunchKernelGGL(k_xent_join<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, part, (int)tv, at_label, exps, labels, rows, c->vocab, lse, token);
+        hipLaunchKernelGGL(k_xent_join<KIND>, dim3((unsigned)grid_for(rows, 16, kMostBlocks)), dim3(256), 0, c->stream, part, (int)tv, at_label, exps, labels, rows, c->vocab, lse, token);
     }
     hipLaunchKernelGGL(k_xent_loss, dim3((unsigned)c->n), dim3(256), 0, c->stream, token, labels, t, c->vocab, loss);
     SAMS_HIP(hipGetLastError());
@@ -705,7 +715,7 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
         if (pieces) {
             rest = c->scratch.at<float>(c->token);
             const uint32_t tv = enqueue_stats<KIND>(c, W, H, label);
-            hipLaunchKernelGGL(k_xent_rest<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, c->scratch.at<float2>(c->part), (int)tv, c->scratch.at<float>(c->at_label),
+            hipLaunchKernelGGL(k_xent_rest<KIND>, dim3((unsigned)grid_for(rows, 16, kMostBlocks)), dim3(256), 0, c->stream, c->scratch.at<float2>(c->part), (int)tv, c->scratch.at<float>(c->at_label),
                                exps, rows, rest);
         }
         const TileChoice hidden = rows ? dh_tiles(KIND == SPLIT, rows, c->dim, size) : TileChoice{2, 0};
@@ -717,16 +727,19 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
                 with_tile<KIND>(choose_tiles(KIND == SPLIT, 1, piece, rows, false, c->dim, 1, 0).shape, [&](auto shape) {
                     typedef decltype(shape) S;
                     const uint32_t tv = (uint32_t)((piece + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                    hipLaunchKernelGGL((k_xent_dz<S, KIND>), dim3(tv * tt), dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, tv, tt, exps, label, v0, c->vocab, log_sums, dz, rest, sums);
+                    in_launches((int64_t)tv * tt, S::THREADS, [&](dim3 grid, Launch l) {
+                        hipLaunchKernelGGL((k_xent_dz<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, Wp, H, c->dim, l, tv, tt, exps, label, v0, c->vocab, log_sums, dz, rest, sums);
+                    });
                     if (!rest)
-                        hipLaunchKernelGGL(k_xent_dz_label<KIND>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, c->stream, sums, (int)tv, label, rows, c->vocab, dz, row_words<KIND>(piece));
+                        hipLaunchKernelGGL(k_xent_dz_label<KIND>, dim3((unsigned)grid_for(rows, 16, kMostBlocks)), dim3(256), 0, c->stream, sums, (int)tv, label, rows, c->vocab, dz, row_words<KIND>(piece));
                 });
             with_tile<KIND>(choose_tiles(KIND == SPLIT, workers, c->dim, piece, false, t, 1, 0).shape, [&](auto shape) {
                 typedef decltype(shape) S;
                 const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tv = (uint32_t)((piece + S::BN - 1) / S::BN);
                 auto weight = [&](auto kernel, auto *out) {
-                    hipLaunchKernelGGL(kernel, dim3(td * tv * (unsigned)workers), dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, td, tv, exps, inv,
-                                       out + first * dws.worker + v0 * dws.row, dws);
+                    in_launches((int64_t)td * tv * workers, S::THREADS, [&](dim3 grid, Launch l) {
+                        hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), 0, c->stream, dz, piece, H.p, c->dim, t, l, td, tv, exps, inv, out + first * dws.worker + v0 * dws.row, dws);
+                    });
                 };
                 if (dw_type == SAMS_F32 && accumulate) weight(k_xent_dw<S, KIND, SAMS_F32, true>, (float *)dw);
                 else if (dw_type == SAMS_F32) weight(k_xent_dw<S, KIND, SAMS_F32, false>, (float *)dw);
@@ -737,13 +750,15 @@ static int enqueue_backward(sams_xent *c, int64_t t, const void *h, Rows hs, con
                 with_tile<KIND>(hidden.shape, [&](auto shape) {
                     typedef decltype(shape) S;
                     const uint32_t td = (uint32_t)((c->dim + S::BM - 1) / S::BM), tt = (uint32_t)((rows + S::BN - 1) / S::BN);
-                    hipLaunchKernelGGL((k_xent_dh<S, KIND>), dim3(td * tt * (unsigned)parts), dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, td, tt,
-                                       v0 == 0, part, pitch, (uint32_t)parts);
+                    in_launches((int64_t)td * tt * parts, S::THREADS, [&](dim3 grid, Launch l) {
+                        hipLaunchKernelGGL((k_xent_dh<S, KIND>), grid, dim3(S::THREADS), 0, c->stream, dz, piece, Operand{Wp.p, Wp.ld, c->dim}, rows, l, td, tt, v0 == 0, part, pitch,
+                                           (uint32_t)parts);
+                    });
                 });
             SAMS_HIP(hipGetLastError());
         }
         if (rows)
-            hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, c->stream, part, parts, rows, pitch, t, c->dim, exps, inv,
+            hipLaunchKernelGGL((k_xent_dh_join<KIND, T>), dim3((unsigned)grid_for(rows, 4, kMostBlocks)), dim3(256), 0, c->stream, part, parts, rows, pitch, t, c->dim, exps, inv,
                                (E *)dh + first * dhs.worker, dhs);
         SAMS_HIP(hipGetLastError());
     }
@@ -769,7 +784,7 @@ int sams_xent_create(sams_xent **out, int32_t n, int64_t t_max, int64_t dim, int
     *out = nullptr;
     if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || dim < 1 || dim > SAMS_MAX_DIM || vocab < 1 || vocab > SAMS_MAX_VOCAB || !type_ok(type))
         return SAMS_EINVAL;
-    if ((n * t_max / Small::BN + 1) * (vocab / Small::BM + 1) > INT32_MAX) return SAMS_EINVAL;       // tiles of one launch
+    if ((n * t_max / Small::BN + 1) * (vocab / Small::BM + 1) > INT32_MAX) return SAMS_EINVAL;       // tiles are counted in 32 bits
     sams_xent *c = new (std::nothrow) sams_xent();
     if (!c) return SAMS_ENOMEM;
     c->n = n; c->t_max = t_max; c->dim = dim; c->vocab = vocab; c->type = type; c->train = train != 0;
