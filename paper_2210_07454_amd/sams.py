@@ -350,6 +350,22 @@ def _strided(t, dtype, shape, inner, name):
     return (t.data_ptr(), *strides[:len(shape) - inner])
 
 
+def _leading(t, axes, name):
+    """Extents of a tensor that a call goes by, before its shape is compared with them."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    if t.dim() != axes:
+        raise ValueError(f"{name}: expected {axes} axes, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def _coefficients(coef):
+    coef = tuple(coef)
+    if len(coef) != 3:
+        raise ValueError(f"coef: expected three numbers, got {len(coef)}")
+    return (ctypes.c_float * 3)(*coef)
+
+
 class _TrainContext:
     """Owns one context of a training operator.  Work is enqueued on the stream given, or on the torch stream that is current at
     creation; a call made while another one is current waits for that one's work, and that one waits for the call's."""
@@ -412,14 +428,14 @@ class LayerNorm(_TrainContext):
         super().__init__(dtype, stream, n, t_max, dim, TYPES.get(dtype, -1))
 
     def layer_norm_forward(self, x, weight, bias, y, mean, rstd, eps=1e-5):
-        t = x.shape[1]
+        t = _leading(x, 3, "x")[1]
         full = (self.n, t, self.dim)
         self._call("layer_norm_forward", t, *_strided(x, self.dtype, full, 1, "x"), _ptr(weight, _F32, (self.dim,), "weight"),
                    _ptr(bias, _F32, (self.dim,), "bias"), eps, *_strided(y, self.dtype, full, 1, "y"),
                    _ptr(mean, _F32, full[:2], "mean"), _ptr(rstd, _F32, full[:2], "rstd"))
 
     def layer_norm_backward(self, dy, x, weight, mean, rstd, dx, dweight, dbias=None, accumulate=False):
-        t = x.shape[1]
+        t = _leading(x, 3, "x")[1]
         full, sums = (self.n, t, self.dim), (self.n, self.dim)
         self._call("layer_norm_backward", t, *_strided(dy, self.dtype, full, 1, "dy"), *_strided(x, self.dtype, full, 1, "x"),
                    _ptr(weight, _F32, (self.dim,), "weight"), _ptr(mean, _F32, full[:2], "mean"), _ptr(rstd, _F32, full[:2], "rstd"),
@@ -437,7 +453,7 @@ class LinearCrossEntropy(_TrainContext):
         super().__init__(dtype, stream, n, t_max, dim, vocab, TYPES.get(dtype, -1), int(bool(train)))
 
     def _inputs(self, h, w, labels):
-        t = h.shape[1]
+        t = _leading(h, 3, "h")[1]
         return (t, *_strided(h, self.dtype, (self.n, t, self.dim), 1, "h"), *_strided(w, self.dtype, (self.vocab, self.dim), 1, "w"),
                 _ptr(labels, torch.int64, (self.n, t), "labels"))
 
@@ -446,7 +462,7 @@ class LinearCrossEntropy(_TrainContext):
                    _ptr(lse, _F32, (self.n, h.shape[1]), "lse"))
 
     def linear_xent_backward(self, h, w, labels, lse, grad_loss, dh, dw, accumulate=False):
-        t = h.shape[1]
+        t = _leading(h, 3, "h")[1]
         kind = dw.dtype if isinstance(dw, torch.Tensor) and dw.dtype in (self.dtype, _F32) else self.dtype
         self._call("linear_xent_backward", *self._inputs(h, w, labels), _ptr(lse, _F32, (self.n, t), "lse"),
                    _ptr(grad_loss, _F32, (self.n,), "grad_loss"), *_strided(dh, self.dtype, (self.n, t, self.dim), 1, "dh"),
@@ -463,14 +479,14 @@ class Orthogonalizer(_TrainContext):
         super().__init__(dtype, stream, batch, rows, cols, TYPES.get(dtype, -1))
 
     def orthogonalize(self, g, out, steps=5, coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
-        full = (g.shape[0], self.rows, self.cols)
-        self._call("orthogonalize", full[0], *_strided(g, self.dtype, full, 1, "g"), steps, (ctypes.c_float * 3)(*coef), eps,
+        full = (_leading(g, 3, "g")[0], self.rows, self.cols)
+        self._call("orthogonalize", full[0], *_strided(g, self.dtype, full, 1, "g"), steps, _coefficients(coef), eps,
                    *_strided(out, self.dtype, full, 1, "out"))
 
     def muon_update(self, g, m, x, m_out, x_out, beta=0.95, nesterov=True, lr=0.02, scale=1.0, weight_decay=0.0, steps=5,
                     coef=(3.4445, -4.7750, 2.0315), eps=1e-7):
-        n, batch = g.shape[:2]
+        n, batch = _leading(g, 4, "g")[:2]
         full = (batch, self.rows, self.cols)
         self._call("muon_update", n, batch, *_strided(g, _F32, (n, *full), 2, "g"), *_strided(m, _F32, full, 2, "m"),
                    *_strided(x, _F32, full, 2, "x"), *_strided(m_out, _F32, full, 2, "m_out"), *_strided(x_out, _F32, full, 2, "x_out"),
-                   beta, int(bool(nesterov)), lr, scale, weight_decay, steps, (ctypes.c_float * 3)(*coef), eps)
+                   beta, int(bool(nesterov)), lr, scale, weight_decay, steps, _coefficients(coef), eps)
