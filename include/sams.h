@@ -424,7 +424,8 @@ int linear_xent_backward(sams_xent *ctx, int64_t t, const void *h, int64_t h_wor
  *     X_0 = G / (|G|_F + eps),   X <- a X + b (X X') X + c (X X')^2 X   `steps` times,   (a, b, c) = coef_host[0..2]
  *   g, out [batch][rows][cols] of `type`, with the distances from matrix to matrix and from row to row; out may be g
  *   coef_host  HOST pointer, three finite numbers, read during the call      1 <= steps <= SAMS_MAX_ORTHO_STEPS
- * Between the products, matrices are held to 22 bits of mantissa, of SAMS_BF16 with both sides from 1024 on to 11.
+ * Between the products, matrices are held to 22 bits of mantissa, of SAMS_BF16 with both sides from 1024 on to 11; numbers far below a
+ * matrix's largest possible singular value to fewer, some 2^-38 of it.  A matrix of zeros stays zero, with eps = 0 too.
  *
  * muon_update is the momentum update of weight matrices that uses it (type SAMS_F32), from the n workers' gradients:
  *     mean = (g[0] + g[1] + ...) / n  (workers in ascending order),   m_out = beta * m + (1 - beta) * mean

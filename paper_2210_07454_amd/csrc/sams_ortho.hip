@@ -10,11 +10,11 @@
 // which p keeps below max |p| over the range before.  So they are held as fixed-point-like words: 16-bit floats (11 bits) after
 // scaling by a power of two that puts the bound near the top of their range: pairs of words (22 bits), or single ones for large bfloat16
 // matrices (bfloat16's own 8 bits cost the same and would add up to several roundings of the result; nothing here needs their
-// range).  G itself is only scaled by a power of two, which loses nothing of a 16-bit G; the rest of 1 / (|G| + eps) goes into the
-// first step's products.
+// range).  G itself is only scaled by the power of two that brings its norm to 2^14 to 2^15, which loses nothing of a 16-bit G's
+// numbers above 2^-29 of the norm and up to 2^-39 of the norm of smaller ones; the rest of 1 / (|G| + eps) goes into the first step's products.
 //
-// Large matrices are bound by the matrix cores: five steps of one 4096 x 8192 in bf16 take 2.38 ms, 1.01 PFLOP/s over everything; 12 of
-// 768 x 768 in 32 bits from 8 workers' gradients 551 us (0.20 PFLOP/s of pairs, each product one or two rounds of tiles), 75 of them
+// Large matrices are bound by the matrix cores: five steps of one 4096 x 8192 in bf16 take 2.36 ms, 1.02 PFLOP/s over everything; 12 of
+// 768 x 768 in 32 bits from 8 workers' gradients 565 us (0.19 PFLOP/s of pairs, each product one or two rounds of tiles), 78 of them
 // for the gradients' bytes.  Small ones are bound by the steps' chain: 50 of 84 x 120 take 52 us.
 #include <math.h>
 #include <new>
@@ -191,7 +191,7 @@ __device__ __forceinline__ void put_symmetric(uint16_t *o, int64_t ld, int64_t s
     if (m0 != n0) eights<S, true>(acc, lds, [&](int dm, int dn, const float (&raw)[8]) { emit(m0 + dm, n0 + dn, raw); });
 }
 
-// A = X X' (X' X where X is tall), times f and, in the first step, sigma^2.  163 us at 4096 x 8192 in single words, 0.84 PFLOP/s of the half
+// A = X X' (X' X where X is tall), times f and, in the first step, sigma^2.  161 us at 4096 x 8192 in single words, 0.85 PFLOP/s of the half
 // that is computed: 253 tiles of 192 fill the chip once, where 136 of 256 would take half of it.
 template <class S, int KIND, bool TALL>
 __global__ void __launch_bounds__(S::THREADS) k_ortho_gram(const uint16_t *x, OrthoDims d, float f, const OrthoScale *scale, uint16_t *gram)
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(256) k_ortho_gram_join(const float *sums, uint
     put8<KIND>(gram + matrix * d.small * ld + row * ld, col, v);
 }
 
-// P = a I + b A + c A A: 102 us at 4096, 0.67 PFLOP/s of the half that is computed, 253 tiles of 192 on 256 CUs.
+// P = a I + b A + c A A: 99 us at 4096, 0.70 PFLOP/s of the half that is computed, 253 tiles of 192 on 256 CUs.
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_ortho_poly(const uint16_t *gram, OrthoDims d, float a, float b, float c, uint16_t *poly)
 {
@@ -312,7 +312,7 @@ struct OrthoOut {
     float keep, rate;
 };
 
-// 239 us at 4096 x 8192 in single words, 1.15 PFLOP/s; 45 us for 12 pairs-of-words 768 x 768, 432 tiles of 128 on 256 CUs.
+// 233 us at 4096 x 8192 in single words, 1.18 PFLOP/s; 48 us for 12 pairs-of-words 768 x 768, 432 tiles of 128 on 256 CUs.
 //
 // X' = P X (X P where X is tall), times f and, in the first step, sigma; LAST: to the caller (T: its type; with parameters f32)
 template <class S, int KIND, bool TALL, bool LAST, int T>

@@ -14,10 +14,10 @@
 // vocabulary is there.  Only where one worker's dz is too large for the scratch does it go by pieces of the vocabulary, with a pass over
 // the logits before them for the sums.
 //
-// All but the smallest are bound by the matrix cores: 8 x 1024 tokens of 768 against 50,257 words in bf16 take 2.4 ms for four products
-// of 632 GFLOP, 1.05 PFLOP/s with everything between them (the library's largest plain product: 1.54); in 32 bits 4 x 511 tokens
+// All but the smallest are bound by the matrix cores: 8 x 1024 tokens of 768 against 50,257 words in bf16 take 2.47 ms for four products
+// of 632 GFLOP, 1.02 PFLOP/s with everything between them (the library's largest plain product: 1.54); in 32 bits 4 x 511 tokens
 // 1.9 ms, of which 0.19 are the words of W made twice, at the rate of a copy.  A handful of tokens (4 x 5 of 256, 4,001 words)
-// takes 47 us, ten launches of 3.4 to 8 us that each wait for the one before.
+// takes 51 us, eleven launches of 2.3 to 9 us that each wait for the one before.
 //
 // Words: tensors of 16 bits are multiplied as they are; those of 32 bits as pairs of 16-bit floats (22 bits), scaled by the power of two
 // that takes the tensor's largest finite number to 2^14.  dz is kept without grad_w / count_w (which the products' results are
@@ -181,7 +181,7 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b)
 template <int KIND> constexpr bool kStatsInTurn = KIND != SPLIT;
 
 // Bound by the matrix cores, and by the exponentials while these wait: 8192 tokens of 768 and 50,257
-// words 618 us, 1.02 PFLOP/s in bf16; pairs 0.35.
+// words 611 us, 1.03 PFLOP/s in bf16; pairs 0.34.
 //
 // Per token and tile of the vocabulary: the largest logit, in units of log 2, and the sum of 2^(logit - largest) over the words but the
 // label.  A lane holds numbers of one token (32 of a tile's 64), so that the maximum and the sum run over its registers.  The label's
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(256) k_xent_loss(const float *token, const int
     loss[blockIdx.x] = count ? (sums[0] + sums[1] + sums[2] + sums[3]) / (float)count : 0.f;
 }
 
-// dz of one piece of the vocabulary (W: the piece), a row of words per token.  705 us at 8192 x 50,257 x 768 in bf16, 0.90 PFLOP/s: beside
+// dz over the vocabulary or one piece of it (W: the piece), a row of words per token.  703 us at 8192 x 50,257 x 768 in bf16, 0.90 PFLOP/s: beside
 // the product an exponential each, and 823 MB written, a wavefront's rows through LDS so that they leave in whole lines.
 //
 // rest == NULL: dz at the label is p - 1 for now, and `sums` [tiles_v][rows] gets each token's sum over the tile of the others; else `rest` is
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(256) k_xent_rest(const float2 *part, int tiles
 }
 
 // dW of one worker and piece.  ADD: to what is there, as 32-bit numbers.  Both operands lie with their k's, the tokens, as rows; a worker's
-// products are its own, so that there are tiles enough without a split of k.  690 us at 8 x 1024 x 50,257 x 768 in bf16, 0.92 PFLOP/s,
+// products are its own, so that there are tiles enough without a split of k.  682 us at 8 x 1024 x 50,257 x 768 in bf16, 0.93 PFLOP/s,
 // with 617 MB written.
 template <class S, int KIND, int T, bool ADD>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int64_t piece, const uint16_t *h, int64_t dim, int64_t t, Launch launch, uint32_t tiles_d, uint32_t tiles_v,
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(S::THREADS) k_xent_dw(const uint16_t *dz, int6
 
 // dh over one piece, its vocabulary cut into parts; a part's sums are added to those of the pieces before.  part: [parts][rows][pitch]
 // The result has few tiles (96 of 256 x 256 for 8192 tokens of 768) and k is the vocabulary: the parts make them enough for the chip.
-// 586 us at 8192 x 50,257 x 768 in bf16, 1.08 PFLOP/s, and 23 us to join the parts.
+// 578 us at 8192 x 50,257 x 768 in bf16, 1.09 PFLOP/s, and 24 us to join the parts.
 template <class S, int KIND>
 __global__ void __launch_bounds__(S::THREADS) k_xent_dh(const uint16_t *dz, int64_t piece, Operand W, int64_t rows, Launch launch, uint32_t tiles_d, uint32_t tiles_t, int first, float *part,
                                                         int64_t pitch, uint32_t parts)

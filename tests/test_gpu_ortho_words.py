@@ -34,3 +34,14 @@ def test_pairs_of_words(sams, kind, shape, steps, coef):
         rounding = 1.1 * rounding if want[i].numel() >= 1000 else HALF_ULP[kind] * float(torch.linalg.matrix_norm(want[i]))
         off = float(torch.linalg.matrix_norm(got[i] - want[i]))
         assert off <= 16 * 2.0 ** -22 * bounds[i] + rounding, (i, off, rounding, bounds[i])
+
+
+@pytest.mark.parametrize("kind", [torch.float32, *HALF_ULP], ids=str)
+@pytest.mark.parametrize("rows,cols", [(30, 40), (300, 200), (1024, 1030)])
+def test_zeros_stay_zero_whatever_eps(sams, kind, rows, cols):
+    g = torch.zeros((2, rows, cols), device="cuda", dtype=kind)
+    g[1] = torch.randn((rows, cols), device="cuda").to(kind)
+    out = torch.full_like(g, float("nan"))
+    with sams.Orthogonalizer(2, rows, cols, kind) as op:
+        op.orthogonalize(g, out, eps=0.0)
+    assert (out[0] == 0).all() and torch.isfinite(out[1]).all() and (out[1] != 0).any()
