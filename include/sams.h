@@ -364,10 +364,15 @@ int amsgrad_ef_update_pa(sams_ctx *ctx, const float *g_next, float *m, float *e_
 #define SAMS_MAX_VOCAB 16777216
 #define SAMS_MAX_BATCH 65535
 #define SAMS_MAX_ORTHO_STEPS 100
+#define SAMS_MAX_HEADS 1024
+#define SAMS_MAX_HEAD_DIM 128
+#define SAMS_MAX_BUCKETS 512
 
 typedef struct sams_norm sams_norm;
 typedef struct sams_xent sams_xent;
 typedef struct sams_ortho sams_ortho;
+typedef struct sams_dropout sams_dropout;
+typedef struct sams_attn sams_attn;
 
 /*
  * Layer norm over the last axis:
@@ -444,6 +449,67 @@ int muon_update(sams_ortho *ctx, int32_t n, int64_t batch, const float *g, int64
                 int64_t m_mat, const float *x, int64_t x_mat, float *m_out, int64_t m_out_mat, float *x_out,
                 int64_t x_out_mat, float beta, int32_t nesterov, float lr, float scale, float weight_decay, int32_t steps,
                 const float *coef_host, float eps);
+
+/*
+ * Dropout.  Which elements are dropped is a function of a seed, a step and the element's place, made anew in every pass, so that no mask
+ * is stored.  rng [2] int64, on the device: the seed, and the step, of which the lower 32 bits count.  They are read when the call runs, so a
+ * captured graph that raises the step drops other elements at every replay; a backward pass needs them as its forward pass had them.
+ * Calls with equal seed and step drop the same places: give every layer a seed of its own.
+ * p (0 <= p < 1) is rounded to a multiple of 2^-16, and may not round to 1; with 0 rng may be NULL.
+ * Philox 4x32 with 7 rounds, the seed's lower and upper half as key and the step as its last counter word, gives eight 16-bit numbers (the lower
+ * half of its first word, the upper half, ...); an element is kept where its number is at least 65536 p.  Its counter and number:
+ *     dropout    (column / 8, row t, worker, step), number column % 8
+ *     attention  (2 (key / 16) + key / 4 % 2, query, (worker * seqs + sequence) * heads + head, step), number 4 (key / 8 % 2) + key % 4
+ *
+ *     y = residual + x / (1 - p) where kept, residual elsewhere      dx = dy / (1 - p) where kept, 0 elsewhere   (residual's gradient is dy)
+ *   x, residual (or NULL), y, dy, dx [n][t][dim] of `type`; y may be x or residual, dx may be dy (same distances).
+ * Ranges as for layer norm.
+ */
+int sams_dropout_create(sams_dropout **out, int32_t n, int64_t t_max, int64_t dim, int32_t type, void *hip_stream);
+int sams_dropout_destroy(sams_dropout *ctx);
+int64_t sams_dropout_scratch_bytes(const sams_dropout *ctx);
+int dropout_forward(sams_dropout *ctx, int64_t t, const void *x, int64_t x_worker, int64_t x_row, const void *residual,
+                    int64_t residual_worker, int64_t residual_row, const int64_t *rng, double p, void *y, int64_t y_worker, int64_t y_row);
+int dropout_backward(sams_dropout *ctx, int64_t t, const void *dy, int64_t dy_worker, int64_t dy_row, const int64_t *rng, double p, void *dx,
+                     int64_t dx_worker, int64_t dx_row);
+
+/*
+ * Self-attention with a learned bias by buckets of the relative position, and dropout of its probabilities.  A worker's t tokens are `seqs`
+ * sequences of t / seqs each, one after the other; for every head and sequence, with query i and key j inside it,
+ *     s_ij = scale q_i . k_j + bias[head][bucket(j - i)],   P = softmax over the keys j (j <= i with causal != 0) of a row,
+ *     o_i = sum over the keys kept of P_ij v_j / (1 - p)
+ *   q, o [n][t][heads * dim], k, v [n][t][kv_heads * dim] of `type`: head h reads the keys and values of head h / (heads / kv_heads)
+ *   lengths [n][seqs] int32 or NULL: a sequence's first lengths[.] tokens (between 0 and t / seqs; values outside are taken to the nearer end)
+ *     are its own, the rest is padding: it may hold anything (NaN included), changes nothing, and its rows of o and of all gradients are 0
+ *   bias [heads][buckets] fp32; given exactly if the context has buckets.  Bucket b is the distances j - i from starts_host[b] to
+ *     starts_host[b + 1] - 1; what lies before starts_host[1] belongs to bucket 0, whose start is not looked at.  A bias of minus infinity bans the bucket's keys;
+ *     a row without any key left has o = 0 and gradients 0.
+ *   rng, p as for dropout
+ *   row_max, row_sum [n][heads][t] fp32 out, contiguous: a row's largest logit (in units of ln 2) and its sum of exponentials, for the backward pass
+ * Backward, from o, row_max and row_sum of the forward pass with the same other arguments: of sum(dout * o), dq [n][t][heads * dim], dk, dv
+ * [n][t][kv_heads * dim], and, per worker, dbias [n][heads][buckets] fp32 with the distance from worker to worker (or NULL); accumulate != 0 adds to
+ * what dbias holds.  No output may overlap an input.
+ *   starts_host  HOST pointer to `buckets` ascending numbers, copied; NULL with buckets == 0
+ * 16-bit tensors are multiplied as they are, with P and its gradient rounded to their type between the products (f16: scaled by powers of two,
+ * so that small ones keep their digits); 32-bit ones in 32 bits.  Sums and the softmax are held in 32 bits.
+ * Ranges: 1 <= heads <= SAMS_MAX_HEADS, kv_heads divides heads, 1 <= dim <= SAMS_MAX_HEAD_DIM, 0 <= buckets <= SAMS_MAX_BUCKETS, n * t_max <=
+ * SAMS_MAX_TOKENS, seqs divides t, n * heads * seqs * (t / seqs / 128, rounded up) < 2^31.
+ * Scratch with train != 0: 4 * n * heads * (t_max + buckets * (t_max / 64 + 64)) bytes; a backward pass needs it (SAMS_EINVAL otherwise).
+ */
+int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim, int32_t buckets,
+                     const int32_t *starts_host, int32_t type, int32_t train, void *hip_stream);
+int sams_attn_destroy(sams_attn *ctx);
+int64_t sams_attn_scratch_bytes(const sams_attn *ctx);
+int attention_forward(sams_attn *ctx, int64_t t, int64_t seqs, const int32_t *lengths, const void *q, int64_t q_worker, int64_t q_row,
+                      const void *k, int64_t k_worker, int64_t k_row, const void *v, int64_t v_worker, int64_t v_row, const float *bias,
+                      float scale, int32_t causal, const int64_t *rng, double p, void *o, int64_t o_worker, int64_t o_row, float *row_max,
+                      float *row_sum);
+int attention_backward(sams_attn *ctx, int64_t t, int64_t seqs, const int32_t *lengths, const void *dout, int64_t dout_worker,
+                       int64_t dout_row, const void *q, int64_t q_worker, int64_t q_row, const void *k, int64_t k_worker, int64_t k_row,
+                       const void *v, int64_t v_worker, int64_t v_row, const float *bias, float scale, int32_t causal,
+                       const int64_t *rng, double p, const void *o, int64_t o_worker, int64_t o_row, const float *row_max,
+                       const float *row_sum, void *dq, int64_t dq_worker, int64_t dq_row, void *dk, int64_t dk_worker, int64_t dk_row,
+                       void *dv, int64_t dv_worker, int64_t dv_row, float *dbias, int64_t dbias_worker, int32_t accumulate);
 
 #ifdef __cplusplus
 }

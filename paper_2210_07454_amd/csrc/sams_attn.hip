@@ -1,0 +1,335 @@
+// Self-attention with a learned bias by buckets of the relative position and dropout of the probabilities, forward pass:
+//
+//   s_ij = scale q_i . k_j + bias[bucket(j - i)],   P = softmax over the keys j of a row,   o_i = sum_j m_ij / (1 - p) P_ij v_j
+//
+// one pass over the keys with a running maximum and sum of every row.
+#include <new>
+
+#include "sams_attn.h"
+
+namespace sams {
+namespace attn {
+
+// A workgroup has 128 queries of a head, a wavefront 32 of them, a lane (and the lane 32 from it) one: the products are made as
+// S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
+// Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.
+template <int T, int D, bool DROP>
+__global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch launch)
+{
+    typedef Tile<T, D> Ti;
+    typedef typename TypeOf<T>::type E;
+    constexpr int BN = Ti::ROWS, NB = BN / 32;
+    constexpr float SHIFT = T == SAMS_F16 ? 14.f : 0.f;             // 16-bit floats of up to 2^14: small weights keep their digits
+    extern __shared__ __align__(16) char lds[];
+    char *tile_k = lds, *tile_v = lds + 2 * Ti::BYTES;
+    Window *window = (Window *)(lds + 4 * Ti::BYTES);
+    int *starts_lds = (int *)(window + 2);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Place at = place_of(a, launch, a.heads, a.causal);
+    const uint32_t q0 = at.first + wave * 32, query = q0 + (lane & 31);
+    const bool row_there = query < a.len, live = query < at.length;
+    E *out = rows_of<T>(a.out, a.outs, a, at, at.head) + (int64_t)query * a.outs.row;
+    const int64_t stat = stats_of(a, at, at.head) + query;
+
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    float top = -__builtin_inff(), sum = 0.f;
+
+    if (at.first < at.length) {
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) starts_lds[b] = a.starts[b];
+        const Starts starts = {starts_lds, a.buckets};
+        const float *bias = a.bias + (int64_t)at.head * a.buckets;
+        const uint32_t kv = at.head / (a.heads / a.kv_heads);
+        const E *k = rows_of<T>(a.k, a.ks, a, at, kv), *v = rows_of<T>(a.v, a.vs, a, at, kv);
+        const uint32_t end = a.causal && at.first + kRows < at.length ? at.first + kRows : at.length;
+        Seed seed = {};
+        if constexpr (DROP) seed = read_seed(a.rng);
+        const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head;
+
+        typename Ti::Frag qf[D / 16];
+        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
+        Bring<T, D> bk, bv;
+        bk.load(k, a.ks.row, 0, at.length, a.dim);
+        bv.load(v, a.vs.row, 0, at.length, a.dim);
+        __syncthreads();
+        bk.store(tile_k);
+        bv.store(tile_v);
+        const int lo = -(int)(at.first + kRows - 1);
+        Band band = band_of(starts, bias, lo, BN + kRows - 1, window[0]);
+        __syncthreads();
+        int turn = 0;
+        for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
+            const bool more = key0 + BN < end;
+            if (more) {
+                bk.load(k, a.ks.row, key0 + BN, at.length, a.dim);
+                bv.load(v, a.vs.row, key0 + BN, at.length, a.dim);
+            }
+            const bool needed = q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(band.one && band.value == -__builtin_inff());
+            if (needed) {
+                const char *tk = tile_k + turn * Ti::BYTES, *tv = tile_v + turn * Ti::BYTES;
+                f32x16 s[NB];
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) s[j] = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s[j]);
+                }
+                if (band.one) {
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], a.scale2, band.value);
+                } else {
+                    const float *by = window[turn].value + (kRows - 1 - (int)(query - at.first));
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], a.scale2, by[32 * j + row_of(i, lane)]);
+                }
+                if (key0 + BN > at.length || (a.causal && key0 + BN - 1 > q0)) {
+                    const int limit = (int)(a.causal && query < at.length ? query + 1 : at.length) - (int)key0;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[j][i] = 32 * j + row_of(i, lane) < limit ? s[j][i] : -__builtin_inff();
+                }
+                float most = s[0][0];
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) most = fmaxf(most, s[j][i]);
+                most = fmaxf(fmaxf(most, other_half(most)), top);
+                if (__any(most > top)) {
+                    const float less = most == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - most);
+                    sum *= less;
+#pragma unroll
+                    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[d][i] *= less;
+                    top = most;
+                }
+                const float base = top == -__builtin_inff() ? 0.f : top - SHIFT;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[j][i] = __builtin_amdgcn_exp2f(s[j][i] - base);
+                        sum += s[j][i];
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        if constexpr (DROP) {
+                            uint32_t numbers[4];
+                            philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) s[j][8 * half + e] = kept(numbers, e, a.keep.least) ? s[j][8 * half + e] : 0.f;
+                        }
+                        const typename Ti::Frag w = words_of<T>(s[j], half);
+#pragma unroll
+                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tv, 32 * j + 16 * half, 32 * d, lane), w, acc[d]);
+                    }
+                }
+            }
+            if (more) {
+                bk.store(tile_k + (turn ^ 1) * Ti::BYTES);
+                bv.store(tile_v + (turn ^ 1) * Ti::BYTES);
+                band = band_of(starts, bias, lo + (int)(key0 + BN), BN + kRows - 1, window[turn ^ 1]);
+            }
+            __syncthreads();
+        }
+    }
+    sum += other_half(sum);
+    const float by = live && sum != 0.f ? a.keep.scale / sum : 0.f;
+    if (!live) {
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    }
+    store_columns<T, D>(out, row_there, a.dim, acc, by, lane);
+    if (row_there && lane < 32) {
+        a.row_max[stat] = live && top != -__builtin_inff() ? top : 0.f;
+        a.row_sum[stat] = live ? sum * (T == SAMS_F16 ? 0x1p-14f : 1.f) : 0.f;
+    }
+}
+
+template <int T, int D>
+static int lds_forward(const Args &a)
+{
+    return 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + ((int)a.buckets * 4 + 15) / 16 * 16;
+}
+
+// a context's kernels may take more LDS than a launch gets unasked
+hipError_t prepare_forward(int type, uint32_t dim)
+{
+    hipError_t e = hipSuccess;
+    SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(dim, D, {
+        e = hipFuncSetAttribute((const void *)k_attn_forward<T, D, true>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        if (e == hipSuccess) e = hipFuncSetAttribute((const void *)k_attn_forward<T, D, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    }));
+    return e;
+}
+
+void launch_forward(const Args &a, int type, hipStream_t stream)
+{
+    const int64_t blocks = (int64_t)a.n * a.seq_count * a.heads * a.tiles;
+    SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
+        const int bytes = lds_forward<T, D>(a);
+        gemm::in_launches(blocks, kThreads, [&](dim3 grid, gemm::Launch l) {
+            if (a.keep.least) hipLaunchKernelGGL((k_attn_forward<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l);
+            else hipLaunchKernelGGL((k_attn_forward<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l);
+        });
+    }));
+}
+
+}  // namespace attn
+}  // namespace sams
+
+struct sams_attn {
+    int32_t n, heads, kv_heads, dim, buckets, type, train;
+    int64_t t_max, parts;
+    hipStream_t stream;
+    sams::Scratch scratch;
+    int64_t starts, delta, part;
+};
+
+using namespace sams;
+
+// what both passes take, checked; false: refused
+static bool arguments(sams_attn *c, int64_t t, int64_t seqs, const int32_t *lengths, const void *q, Rows qs, const void *k, Rows ks, const void *v, Rows vs,
+                      const float *bias, float scale, int32_t causal, const int64_t *rng, double p, attn::Args &a)
+{
+    if (!c || t < 0 || t > c->t_max || seqs < 1 || t % seqs || !__builtin_isfinite(scale) || !keep_of(p, a.keep)) return false;
+    if ((c->buckets > 0) != (bias != nullptr) || !aligned_to(bias, 4) || !aligned_to(lengths, 4) || !aligned_to(rng, 8) || (a.keep.least && !rng)) return false;
+    const int size = type_size(c->type);
+    if (t > 0) {
+        if (!q || !k || !v || !aligned_to(q, size) || !aligned_to(k, size) || !aligned_to(v, size)) return false;
+        if (qs.row < 0 || qs.worker < 0 || ks.row < 0 || ks.worker < 0 || vs.row < 0 || vs.worker < 0) return false;
+    }
+    a.q = q; a.k = k; a.v = v;
+    a.qs = qs; a.ks = ks; a.vs = vs;
+    a.bias = bias;
+    a.starts = c->scratch.at<int32_t>(c->starts);
+    a.lengths = lengths;
+    a.rng = rng;
+    a.t = t;
+    a.n = c->n; a.seqs = (uint32_t)seqs; a.len = (uint32_t)(t / seqs);
+    a.heads = c->heads; a.kv_heads = c->kv_heads; a.dim = c->dim; a.buckets = c->buckets;
+    a.tiles = (a.len + attn::kRows - 1) / attn::kRows;
+    a.seq_first = 0;
+    a.seq_count = a.seqs;
+    a.scale = scale;
+    a.scale2 = scale * attn::kLog2e;
+    a.causal = causal != 0;
+    a.delta = c->scratch.at<float>(c->delta);
+    a.part = c->scratch.at<float>(c->part);
+    return (int64_t)c->n * seqs * c->heads * a.tiles < (int64_t)1 << 31;
+}
+
+extern "C" {
+
+int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim, int32_t buckets, const int32_t *starts_host,
+                     int32_t type, int32_t train, void *hip_stream)
+{
+    if (!out) return SAMS_EINVAL;
+    *out = nullptr;
+    if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || heads < 1 || heads > SAMS_MAX_HEADS || kv_heads < 1 || heads % kv_heads || dim < 1 ||
+        dim > SAMS_MAX_HEAD_DIM || buckets < 0 || buckets > SAMS_MAX_BUCKETS || (buckets > 0 && !starts_host) || !type_ok(type)) return SAMS_EINVAL;
+    for (int b = 1; b < buckets; ++b)
+        if (starts_host[b] <= starts_host[b - 1]) return SAMS_EINVAL;
+    sams_attn *c = new (std::nothrow) sams_attn();
+    if (!c) return SAMS_ENOMEM;
+    c->n = n; c->t_max = t_max; c->heads = heads; c->kv_heads = kv_heads; c->dim = dim; c->buckets = buckets; c->type = type; c->train = train != 0;
+    c->stream = (hipStream_t)hip_stream;
+    c->parts = (t_max + 63) / 64 + 64;
+    c->starts = c->scratch.reserve((int64_t)buckets * 4);
+    if (train) {
+        c->delta = c->scratch.reserve((int64_t)n * heads * t_max * 4);
+        c->part = c->scratch.reserve((int64_t)n * heads * c->parts * buckets * 4);
+    }
+    int rc = c->scratch.take();
+    if (rc == SAMS_OK) {
+        hipError_t e = attn::prepare_forward(type, (uint32_t)dim);
+        if (e == hipSuccess && train) e = attn::prepare_backward(type, (uint32_t)dim);
+        if (e == hipSuccess && buckets) e = hipMemcpyAsync(c->scratch.base + c->starts, starts_host, (size_t)buckets * 4, hipMemcpyHostToDevice, c->stream);
+        if (e == hipSuccess && buckets) e = hipStreamSynchronize(c->stream);
+        if (e != hipSuccess) {
+            g_last_hip_error = (int)e;
+            (void)hipGetLastError();
+            if (c->scratch.base) (void)hipFree(c->scratch.base);
+            rc = SAMS_EHIP;
+        }
+    }
+    if (rc != SAMS_OK) { delete c; return rc; }
+    *out = c;
+    return SAMS_OK;
+}
+
+int sams_attn_destroy(sams_attn *c)
+{
+    if (!c) return SAMS_OK;
+    hipError_t e = hipStreamSynchronize(c->stream);
+    if (c->scratch.base) (void)hipFree(c->scratch.base);
+    delete c;
+    if (e != hipSuccess) { g_last_hip_error = (int)e; return SAMS_EHIP; }
+    return SAMS_OK;
+}
+
+int64_t sams_attn_scratch_bytes(const sams_attn *c) { return c ? c->scratch.bytes : 0; }
+
+int attention_forward(sams_attn *c, int64_t t, int64_t seqs, const int32_t *lengths, const void *q, int64_t q_worker, int64_t q_row, const void *k,
+                      int64_t k_worker, int64_t k_row, const void *v, int64_t v_worker, int64_t v_row, const float *bias, float scale,
+                      int32_t causal, const int64_t *rng, double p, void *o, int64_t o_worker, int64_t o_row, float *row_max, float *row_sum)
+{
+    attn::Args a = {};
+    if (!arguments(c, t, seqs, lengths, q, Rows{q_worker, q_row}, k, Rows{k_worker, k_row}, v, Rows{v_worker, v_row}, bias, scale, causal, rng, p, a)) return SAMS_EINVAL;
+    if (t == 0) return SAMS_OK;
+    const int64_t wide = (int64_t)c->heads * c->dim;
+    if (!o || !aligned_to(o, type_size(c->type)) || !row_max || !row_sum || !aligned_to(row_max, 4) || !aligned_to(row_sum, 4)) return SAMS_EINVAL;
+    if ((t > 1 && o_row < wide) || (c->n > 1 && o_worker < wide)) return SAMS_EINVAL;
+    a.out = o;
+    a.outs = Rows{o_worker, o_row};
+    a.row_max = row_max;
+    a.row_sum = row_sum;
+    attn::launch_forward(a, c->type, c->stream);
+    SAMS_HIP(hipGetLastError());
+    return SAMS_OK;
+}
+
+int attention_backward(sams_attn *c, int64_t t, int64_t seqs, const int32_t *lengths, const void *dout, int64_t dout_worker, int64_t dout_row, const void *q,
+                       int64_t q_worker, int64_t q_row, const void *k, int64_t k_worker, int64_t k_row, const void *v, int64_t v_worker, int64_t v_row,
+                       const float *bias, float scale, int32_t causal, const int64_t *rng, double p, const void *o, int64_t o_worker, int64_t o_row,
+                       const float *row_max, const float *row_sum, void *dq, int64_t dq_worker, int64_t dq_row, void *dk, int64_t dk_worker,
+                       int64_t dk_row, void *dv, int64_t dv_worker, int64_t dv_row, float *dbias, int64_t dbias_worker, int32_t accumulate)
+{
+    attn::Args a = {};
+    if (!arguments(c, t, seqs, lengths, q, Rows{q_worker, q_row}, k, Rows{k_worker, k_row}, v, Rows{v_worker, v_row}, bias, scale, causal, rng, p, a)) return SAMS_EINVAL;
+    if (!c->train || (dbias && (!c->buckets || !aligned_to(dbias, 4)))) return SAMS_EINVAL;
+    const int64_t wide = (int64_t)c->heads * c->dim, narrow = (int64_t)c->kv_heads * c->dim;
+    const int size = type_size(c->type);
+    if (dbias && c->n > 1 && dbias_worker < (int64_t)c->heads * c->buckets) return SAMS_EINVAL;
+    if (t > 0) {
+        if (!dout || !o || !row_max || !row_sum || !dq || !dk || !dv) return SAMS_EINVAL;
+        if (!aligned_to(dout, size) || !aligned_to(o, size) || !aligned_to(dq, size) || !aligned_to(dk, size) || !aligned_to(dv, size) || !aligned_to(row_max, 4) || !aligned_to(row_sum, 4)) return SAMS_EINVAL;
+        if (dout_row < 0 || dout_worker < 0 || o_row < 0 || o_worker < 0) return SAMS_EINVAL;
+        if (t > 1 && (dq_row < wide || dk_row < narrow || dv_row < narrow)) return SAMS_EINVAL;
+        if (c->n > 1 && (dq_worker < wide || dk_worker < narrow || dv_worker < narrow)) return SAMS_EINVAL;
+    }
+    a.dout = dout; a.douts = Rows{dout_worker, dout_row};
+    a.o = o; a.os = Rows{o_worker, o_row};
+    a.row_max = (float *)row_max;
+    a.row_sum = (float *)row_sum;
+    a.dq = dq; a.dqs = Rows{dq_worker, dq_row};
+    a.dk = dk; a.dks = Rows{dk_worker, dk_row};
+    a.dv = dv; a.dvs = Rows{dv_worker, dv_row};
+    attn::launch_backward(a, c->type, c->parts, dbias, dbias_worker, accumulate, c->stream);
+    SAMS_HIP(hipGetLastError());
+    return SAMS_OK;
+}
+
+}  // extern "C"

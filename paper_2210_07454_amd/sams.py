@@ -26,7 +26,9 @@ EXPORTS = ["sams_create", "sams_destroy", "sams_scratch_bytes", "sams_preconditi
            "amsgrad_ef_update", "amsgrad_ef_update_pa", "topk_refine_static", "topk_refine_static_max_candidates",
            "sams_norm_create", "sams_norm_destroy", "sams_norm_scratch_bytes", "layer_norm_forward", "layer_norm_backward",
            "sams_xent_create", "sams_xent_destroy", "sams_xent_scratch_bytes", "linear_xent_forward", "linear_xent_backward",
-           "sams_ortho_create", "sams_ortho_destroy", "sams_ortho_scratch_bytes", "orthogonalize", "muon_update"]
+           "sams_ortho_create", "sams_ortho_destroy", "sams_ortho_scratch_bytes", "orthogonalize", "muon_update",
+           "sams_dropout_create", "sams_dropout_destroy", "sams_dropout_scratch_bytes", "dropout_forward", "dropout_backward",
+           "sams_attn_create", "sams_attn_destroy", "sams_attn_scratch_bytes", "attention_forward", "attention_backward"]
 
 _lib = None
 _F32, _I32 = torch.float32, torch.int32
@@ -89,13 +91,20 @@ def load() -> ctypes.CDLL:
     lib.sams_ortho_create.argtypes = [ctypes.POINTER(vp), i64, i64, i64, i32, vp]
     lib.orthogonalize.argtypes = [vp, i64, vp, i64, i64, i32, vp, f32, vp, i64, i64]
     lib.muon_update.argtypes = [vp, i32, i64, vp, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, f32, i32, f32, f32, f32, i32, vp, f32]
-    for name in ("sams_norm", "sams_xent", "sams_ortho"):
+    f64, row = ctypes.c_double, [vp, i64, i64]
+    lib.sams_dropout_create.argtypes = [ctypes.POINTER(vp), i32, i64, i64, i32, vp]
+    lib.dropout_forward.argtypes = [vp, i64, *row, *row, vp, f64, *row]
+    lib.dropout_backward.argtypes = [vp, i64, *row, vp, f64, *row]
+    lib.sams_attn_create.argtypes = [ctypes.POINTER(vp), i32, i64, i32, i32, i32, i32, vp, i32, i32, vp]
+    lib.attention_forward.argtypes = [vp, i64, i64, vp, *row, *row, *row, vp, f32, i32, vp, f64, *row, vp, vp]
+    lib.attention_backward.argtypes = [vp, i64, i64, vp, *row, *row, *row, *row, vp, f32, i32, vp, f64, *row, vp, vp, *row, *row, *row, vp, i64, i32]
+    for name in ("sams_norm", "sams_xent", "sams_ortho", "sams_dropout", "sams_attn"):
         getattr(lib, name + "_destroy").argtypes = getattr(lib, name + "_scratch_bytes").argtypes = [vp]
         getattr(lib, name + "_scratch_bytes").restype = i64
     for name in EXPORTS:
         if name not in ("sams_scratch_bytes", "sams_profile_name", "sams_precondition_device_memory",
                         "topk_refine_static_max_candidates", "sams_record_rows", "sams_norm_scratch_bytes",
-                        "sams_xent_scratch_bytes", "sams_ortho_scratch_bytes"):
+                        "sams_xent_scratch_bytes", "sams_ortho_scratch_bytes", "sams_dropout_scratch_bytes", "sams_attn_scratch_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     lib.sams_profile_name.restype = ctypes.c_char_p
     _lib = lib
@@ -490,3 +499,103 @@ class Orthogonalizer(_TrainContext):
         self._call("muon_update", n, batch, *_strided(g, _F32, (n, *full), 2, "g"), *_strided(m, _F32, full, 2, "m"),
                    *_strided(x, _F32, full, 2, "x"), *_strided(m_out, _F32, full, 2, "m_out"), *_strided(x_out, _F32, full, 2, "x_out"),
                    beta, int(bool(nesterov)), lr, scale, weight_decay, steps, _coefficients(coef), eps)
+
+
+class Dropout(_TrainContext):
+    """Dropout of [n][t][dim] tensors, t up to ``t_max``, by a seed and a step that lie on the device; see sams.h."""
+
+    _name = "sams_dropout"
+
+    def __init__(self, n: int, t_max: int, dim: int, dtype=torch.float32, stream=None):
+        self.n, self.t_max, self.dim = n, t_max, dim
+        super().__init__(dtype, stream, n, t_max, dim, TYPES.get(dtype, -1))
+
+    def dropout_forward(self, x, residual, rng, p, y):
+        t = _leading(x, 3, "x")[1]
+        full = (self.n, t, self.dim)
+        self._call("dropout_forward", t, *_strided(x, self.dtype, full, 1, "x"),
+                   *(_strided(residual, self.dtype, full, 1, "residual") if residual is not None else (None, 0, 0)), _ptr(rng, torch.int64, (2,), "rng"),
+                   p, *_strided(y, self.dtype, full, 1, "y"))
+
+    def dropout_backward(self, dy, rng, p, dx):
+        t = _leading(dy, 3, "dy")[1]
+        full = (self.n, t, self.dim)
+        self._call("dropout_backward", t, *_strided(dy, self.dtype, full, 1, "dy"), _ptr(rng, torch.int64, (2,), "rng"), p,
+                   *_strided(dx, self.dtype, full, 1, "dx"))
+
+
+def relative_buckets(buckets: int, max_distance: int, causal: bool = True):
+    """First distances (key minus query) of ``buckets`` buckets, for ``Attention``: one by one near the query, then stretches whose lengths grow
+    by a constant factor up to ``max_distance``, from which on all distances share a bucket.  causal: keys up to the query; otherwise one bucket
+    for the query itself, and the others shared out to both sides."""
+    if buckets < 1 or max_distance < 1:
+        raise ValueError("relative_buckets: buckets and max_distance have to be at least 1")
+
+    def reach(count):
+        """The least distance to one side of each of `count` buckets, from 1 on: exact up to half of them, then near * (max / near) ** (i / far)."""
+        near = (count + 1) // 2
+        far, out = count - near, list(range(1, near + 1))
+        for i in range(1, far + 1):
+            low = out[-1] + 1
+            # the least whole number d with d ** far * near ** (i - far) >= max_distance ** i
+            d = low
+            top = max(low, max_distance)
+            while d < top:
+                mid = (d + top) // 2
+                if mid ** far >= max_distance ** i * max(near, 1) ** (far - i):
+                    top = mid
+                else:
+                    d = mid + 1
+            out.append(d)
+        return out
+
+    left = buckets - 1 if causal else (buckets - 1 + 1) // 2
+    right = buckets - 1 - left
+    # a bucket on the left that begins at distance a and ends before b is the distances -(b - 1) .. -a
+    least = reach(left)
+    ends = [b - 1 for b in least[1:]] + [2 ** 30]
+    return [-e for e in reversed(ends[:left])] + [0] + reach(right)
+
+
+class Attention(_TrainContext):
+    """Self-attention of [n][t][heads * dim] queries with a bias by buckets of the relative position, t up to ``t_max``; see sams.h.
+    ``starts``: the buckets' first distances (``relative_buckets`` makes some), or None for no bias."""
+
+    _name = "sams_attn"
+
+    def __init__(self, n: int, t_max: int, heads: int, dim: int, kv_heads=None, starts=None, dtype=torch.float32, train=True, stream=None):
+        self.n, self.t_max, self.heads, self.dim = n, t_max, heads, dim
+        self.kv_heads = heads if kv_heads is None else kv_heads
+        starts = () if starts is None else tuple(int(v) for v in starts)
+        if any(not -2 ** 31 <= v < 2 ** 31 for v in starts):
+            raise ValueError("starts: expected 32-bit numbers")
+        self.buckets = len(starts)
+        super().__init__(dtype, stream, n, t_max, heads, self.kv_heads, dim, self.buckets, (ctypes.c_int32 * self.buckets)(*starts) if starts else None,
+                         TYPES.get(dtype, -1), int(bool(train)))
+
+    def _inputs(self, t, q, k, v):
+        narrow = (self.n, t, self.kv_heads * self.dim)
+        return (*_strided(q, self.dtype, (self.n, t, self.heads * self.dim), 1, "q"), *_strided(k, self.dtype, narrow, 1, "k"), *_strided(v, self.dtype, narrow, 1, "v"))
+
+    def _how(self, bias, causal, scale, rng, p):
+        return (_ptr(bias, _F32, (self.heads, self.buckets), "bias"), self.dim ** -0.5 if scale is None else scale, int(bool(causal)),
+                _ptr(rng, torch.int64, (2,), "rng"), p)
+
+    def attention_forward(self, q, k, v, bias, o, row_max, row_sum, seqs=1, lengths=None, causal=True, scale=None, rng=None, p=0.0):
+        t = _leading(q, 3, "q")[1]
+        stats = (self.n, self.heads, t)
+        self._call("attention_forward", t, seqs, _ptr(lengths, _I32, (self.n, seqs), "lengths"), *self._inputs(t, q, k, v),
+                   *self._how(bias, causal, scale, rng, p), *_strided(o, self.dtype, (self.n, t, self.heads * self.dim), 1, "o"),
+                   _ptr(row_max, _F32, stats, "row_max"), _ptr(row_sum, _F32, stats, "row_sum"))
+
+    def attention_backward(self, do, q, k, v, bias, o, row_max, row_sum, dq, dk, dv, dbias=None, seqs=1, lengths=None, causal=True, scale=None,
+                           rng=None, p=0.0, accumulate=False):
+        t = _leading(q, 3, "q")[1]
+        wide, narrow, stats = (self.n, t, self.heads * self.dim), (self.n, t, self.kv_heads * self.dim), (self.n, self.heads, t)
+        into = (None, 0)
+        if dbias is not None:
+            into = _strided(dbias, _F32, (self.n, self.heads, self.buckets), 2, "dbias")
+        self._call("attention_backward", t, seqs, _ptr(lengths, _I32, (self.n, seqs), "lengths"), *_strided(do, self.dtype, wide, 1, "do"),
+                   *self._inputs(t, q, k, v), *self._how(bias, causal, scale, rng, p), *_strided(o, self.dtype, wide, 1, "o"),
+                   _ptr(row_max, _F32, stats, "row_max"), _ptr(row_sum, _F32, stats, "row_sum"), *_strided(dq, self.dtype, wide, 1, "dq"),
+                   *_strided(dk, self.dtype, narrow, 1, "dk"), *_strided(dv, self.dtype, narrow, 1, "dv"), *into, int(bool(accumulate)))
