@@ -4,8 +4,8 @@
 //   dv_j = sum_i m_ij / (1 - p) P_ij do_i,   dq_i = scale sum_j dS_ij k_j,   dk_j = scale sum_i dS_ij q_i
 //   dbias[bucket] = sum of dS over the pairs whose distance lies in the bucket
 //
-// in two kernels, each of which makes S and dP again: one has the queries in registers and goes over the keys (delta, dq, dbias), one has
-// the keys and goes over the queries of every head that shares them (dk, dv).  So every sum has one place and a fixed order, without
+// in two kernels, each of which makes S and dP again: one has the queries in registers and goes over the keys (delta, dq), one has
+// the keys and goes over the queries of every head that shares them (dk, dv, dbias).  So every sum has one place and a fixed order, without
 // atomics; seven products of a pair where one kernel would take five.
 #include "sams_attn.h"
 
@@ -59,8 +59,10 @@ struct BucketSums {
             flush(lane);
             bucket = b;
         }
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) own += ds[i];
+        for (int i = 0; i < 8; ++i) v[i] = ds[i] + ds[i + 8];
+        own += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
     // by[x]: the bucket of the distance x - 32 from that of the block's corner, x = 1 .. 63
     __device__ __forceinline__ void many(const uint16_t *by, const f32x16 &ds, int lane)
@@ -70,8 +72,8 @@ struct BucketSums {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = row_of(i, lane);
-            const float v = __shfl(ds[i], ((r - lane) & 31) | half);
-            if ((lane & 31) <= r) up += v;
+            const float v = __shfl(ds[i], ((r + lane) & 31) | half);
+            if ((lane & 31) + r < 32) up += v;
             else down += v;
         }
         up += other_half(up);
@@ -90,18 +92,20 @@ struct BucketSums {
     }
 };
 
-// dq, delta and dbias; laid out as the forward pass.
+// dq and delta; laid out as the forward pass.  o has been rounded to 16 bits: what do . o is off by is small beside dP, but not beside the
+// 32 bits that dbias is held to.  So delta is also added up as it is defined, sum P dP, for the other kernel, and dq, which needs it before that
+// sum is done, is put right at the end: dq = scale (sum P (dP - d) k + (d - delta) sum P k), with d = do . o.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launch, int64_t parts)
+__global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
     constexpr int BN = Ti::ROWS, NB = BN / 32;
+    constexpr float SHIFT = T == SAMS_F16 ? 0x1p14f : 1.f;          // P in 16-bit floats
     extern __shared__ __align__(16) char lds[];
     char *tile_k = lds, *tile_v = lds + 2 * Ti::BYTES;
     Window *window = (Window *)(lds + 4 * Ti::BYTES);
     int *starts_lds = (int *)(window + 2);
-    float *sums_lds = (float *)(starts_lds + a.buckets);            // [kWaves][buckets]
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Place at = place_of(a, launch, a.heads, a.causal);
@@ -109,20 +113,17 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
     const bool row_there = query < a.len, live = query < at.length;
     const int64_t stat = stats_of(a, at, at.head) + query;
 
-    f32x16 acc[D / 32];
+    constexpr bool ROUNDED = T != SAMS_F32;
+    f32x16 acc[D / 32], pk[ROUNDED ? D / 32 : 1];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
-    for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
-        starts_lds[b] = a.starts[b];
-        for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
-    }
-    BucketSums sums = {sums_lds + wave * a.buckets, 0.f, 0};
+        for (int i = 0; i < 16; ++i) acc[d][i] = pk[ROUNDED ? d : 0][i] = 0.f;
     ColumnScale<T, D> fit;
     fit.start();
 
     if (at.first < at.length) {
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) starts_lds[b] = a.starts[b];
         const Starts starts = {starts_lds, a.buckets};
         const float *bias = a.bias + (int64_t)at.head * a.buckets;
         const uint32_t kv = at.head / (a.heads / a.kv_heads);
@@ -154,9 +155,9 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
             }
             delta += other_half(delta);
         }
-        if (live && lane < 32) a.delta[stat] = delta;
         const float top = live ? a.row_max[stat] : 0.f, total = live ? a.row_sum[stat] : 0.f;
-        const float over = total == 0.f ? 0.f : 1.f / total;
+        const float over = total == 0.f ? 0.f : SHIFT / total;
+        float exact = 0.f;
 
         Bring<T, D> bk, bv;
         bk.load(k, a.ks.row, 0, at.length, a.dim);
@@ -207,22 +208,33 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
                             for (int e = 0; e < 8; ++e) dp[8 * half + e] = kept(numbers, e, a.keep.least) ? dp[8 * half + e] * a.keep.scale : 0.f;
                         }
                     }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
                     if (edge) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = 32 * j + row_of(i, lane) < limit ? s[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) {
+                            const bool allowed = 32 * j + row_of(i, lane) < limit;
+                            s[i] = allowed ? s[i] : 0.f;
+                            dp[i] = allowed ? dp[i] : 0.f;
+                        }
                     }
-                    if (a.buckets) {
-                        if (band.one) sums.one(band.bucket, s, lane);
-                        else sums.many(window[turn].bucket + (kRows - 1 - wave * 32 + 32 * j) - 32, s, lane);
+                    typename Ti::Frag wp[2];
+                    if constexpr (ROUNDED) {
+                        wp[0] = words_of<T>(s, 0);
+                        wp[1] = words_of<T>(s, 1);
                     }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) exact = __builtin_fmaf(s[i], dp[i], exact);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
                     fit.fit(s, acc);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const typename Ti::Frag w = words_of<T>(s, half);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tk, 32 * j + 16 * half, 32 * d, lane), w, acc[d]);
+                        for (int d = 0; d < D / 32; ++d) {
+                            const typename Ti::Frag columns = Ti::across(tk, 32 * j + 16 * half, 32 * d, lane);
+                            acc[d] = product<T>(columns, w, acc[d]);
+                            if constexpr (ROUNDED) pk[d] = product<T>(columns, wp[half], pk[d]);
+                        }
                     }
                 }
             }
@@ -233,20 +245,22 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
             }
             __syncthreads();
         }
-        if (a.buckets) sums.flush(lane);
+        exact = (exact + other_half(exact)) * (1.f / SHIFT);
+        if (live && lane < 32) a.delta[stat] = exact;
+        if constexpr (ROUNDED) {
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] = __builtin_fmaf(acc[d][i], 1.f / fit.by, (delta - exact) * pk[d][i]);
+        }
     }
-    store_columns<T, D>(rows_of<T>(a.dq, a.dqs, a, at, at.head) + (int64_t)query * a.dqs.row, row_there, a.dim, acc, a.scale / fit.by, lane);
-    if (a.buckets == 0) return;
-    __syncthreads();
-    float *part = a.part + ((((int64_t)at.worker * a.heads + at.head) * parts) + (int64_t)(at.seq - a.seq_first) * a.tiles + at.first / kRows) * a.buckets;
-    for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads)
-        part[b] = (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]);
+    store_columns<T, D>(rows_of<T>(a.dq, a.dqs, a, at, at.head) + (int64_t)query * a.dqs.row, row_there, a.dim, acc, a.scale / SHIFT, lane);
 }
 
-// dk and dv.  A workgroup has 128 keys, a lane (and the lane 32 from it) one; queries and the output's gradients come by tiles.  The
+// dk, dv and dbias.  A workgroup has 128 keys, a lane (and the lane 32 from it) one; queries and the output's gradients come by tiles.  The
 // products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch launch)
+__global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
 {
     typedef Tile<T, D> Ti;
     constexpr int BQ = Ti::ROWS, NB = BQ / 32;
@@ -258,6 +272,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
     float *stats = (float *)(window + 2);                           // [2][3][BQ]
     char *numbers_lds = (char *)(stats + 2 * 3 * BQ);               // [kWaves][32] queries' numbers
     int *starts_lds = (int *)(numbers_lds + (DROP ? kWaves * 32 * NUMBERS : 0));
+    float *sums_lds = (float *)(starts_lds + a.buckets);            // [kWaves][buckets]
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Place at = place_of(a, launch, a.kv_heads, false);
@@ -272,12 +287,27 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
     ColumnScale<T, D> fit;
     fit.start();
 
-    if (at.first < at.length) {
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) starts_lds[b] = a.starts[b];
+    const uint32_t group = a.heads / a.kv_heads;
+    BucketSums sums = {sums_lds + wave * a.buckets, 0.f, 0};
+    const bool summed = a.part != nullptr;
+    // a head's sums of the workgroup; between barriers
+    auto leave = [&](uint32_t head, bool some) {
+        float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + (int64_t)(at.seq - a.seq_first) * a.tiles + at.first / kRows) * a.buckets;
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
+            part[b] = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
+            for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
+        }
+    };
+    if (at.first >= at.length) {
+        for (uint32_t h = 0; summed && h < group; ++h) leave(at.head * group + h, false);
+    } else {
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
+            starts_lds[b] = a.starts[b];
+            for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
+        }
         const Starts starts = {starts_lds, a.buckets};
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
-        const uint32_t group = a.heads / a.kv_heads;
         const uint32_t begin = a.causal ? at.first / BQ * BQ : 0;   // 128 is a multiple of BQ: the first key's tile
         typename Ti::Frag kf[D / 16], vf[D / 16];
         row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head) + (int64_t)key * a.ks.row, live, a.dim, lane, kf);
@@ -387,6 +417,10 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = allowed(i) ? s[i] : 0.f;
                     }
+                    if (summed) {
+                        if (band.one) sums.one(band.bucket, s, lane);
+                        else sums.many(window[turn].bucket + (wave * 32 + BQ - 1 - 32 * j) - 32, s, lane);
+                    }
                     fit.fit(s, dk);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -397,6 +431,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
                         for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(Ti::across(tq, 32 * j + 16 * half, 32 * d, lane), ws, dk[d]);
                     }
                 }
+            }
+            if (next_head != head && summed) {
+                sums.flush(lane);
+                __syncthreads();
+                leave(head, true);
             }
             if (!more) break;
             store(turn ^ 1);
@@ -417,7 +456,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
 }
 
 // dbias of a worker's head: its parts added up, four threads a bucket, each its quarter of the parts in order
-__global__ void __launch_bounds__(256) k_attn_dbias(const float *part, int64_t parts, uint32_t count, uint32_t heads, uint32_t buckets, float *dbias, int64_t dbias_worker, int accumulate)
+__global__ void __launch_bounds__(256) k_attn_dbias(const float *part, int64_t parts, uint32_t count, uint32_t heads, uint32_t buckets, float scale, float *dbias, int64_t dbias_worker, int accumulate)
 {
     __shared__ float sums[4][64];
     const uint32_t lane = threadIdx.x & 63, q = threadIdx.x >> 6, b = blockIdx.y * 64 + lane;
@@ -430,7 +469,7 @@ __global__ void __launch_bounds__(256) k_attn_dbias(const float *part, int64_t p
     sums[q][lane] = v;
     __syncthreads();
     if (q || b >= buckets) return;
-    v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    v = ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])) * scale;
     float *o = dbias + blockIdx.x / heads * dbias_worker + (int64_t)(blockIdx.x % heads) * buckets + b;
     *o = accumulate ? *o + v : v;
 }
@@ -448,36 +487,35 @@ hipError_t prepare_backward(int type, uint32_t dim)
 void launch_backward(const Args &all, int type, int64_t parts, float *dbias, int64_t dbias_worker, int accumulate, hipStream_t stream)
 {
     Args a = all;
-    const bool some = a.len > 0;
-    if (some) {
-        // as many sequences at a time as there is room for their parts of the bias's gradient
-        const uint32_t step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / a.tiles)) : a.seqs;
-        for (uint32_t first = 0; first < all.seqs; first += step) {
-            a.seq_first = first;
-            a.seq_count = std::min(step, all.seqs - first);
-            SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-                const int bytes = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + (int)a.buckets * 4 * (1 + kWaves);
-                gemm::in_launches((int64_t)a.n * a.seq_count * a.heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
-                    if (a.keep.least) hipLaunchKernelGGL((k_attn_dq<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l, parts);
-                    else hipLaunchKernelGGL((k_attn_dq<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l, parts);
-                });
-            }));
-            if (dbias)
-                hipLaunchKernelGGL(k_attn_dbias, dim3(a.n * a.heads, (a.buckets + 63) / 64), dim3(256), 0, stream, a.part, parts, a.seq_count * a.tiles, a.heads, a.buckets, dbias, dbias_worker,
-                                   accumulate || first > 0);
-        }
-        a.seq_first = 0;
-        a.seq_count = a.seqs;
+    if (!dbias) a.part = nullptr;
+    const float scale = type == SAMS_F16 ? 0x1p-14f : 1.f;          // of the parts: P was held larger
+    auto join = [&](uint32_t count, bool add) {
+        hipLaunchKernelGGL(k_attn_dbias, dim3(a.n * a.heads, (a.buckets + 63) / 64), dim3(256), 0, stream, a.part, parts, count, a.heads, a.buckets, scale, dbias, dbias_worker, add);
+    };
+    if (a.len == 0) {
+        if (dbias) join(0, accumulate);
+        return;
+    }
+    SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
+        const int bytes = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + (int)a.buckets * 4;
+        gemm::in_launches((int64_t)a.n * a.seqs * a.heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+            if (a.keep.least) hipLaunchKernelGGL((k_attn_dq<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l);
+            else hipLaunchKernelGGL((k_attn_dq<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l);
+        });
+    }));
+    // as many sequences at a time as there is room for their parts of the bias's gradient
+    const uint32_t step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / a.tiles)) : a.seqs;
+    for (uint32_t first = 0; first < all.seqs; first += step) {
+        a.seq_first = first;
+        a.seq_count = std::min(step, all.seqs - first);
         SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-            constexpr int fixed = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + 2 * 3 * Tile<T, D>::ROWS * 4;
-            gemm::in_launches((int64_t)a.n * a.seqs * a.kv_heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
-                const int starts = (int)a.buckets * 4;
-                if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true>), grid, dim3(kThreads), fixed + kWaves * 32 * 80 + starts, stream, a, l);
-                else hipLaunchKernelGGL((k_attn_dkv<T, D, false>), grid, dim3(kThreads), fixed + starts, stream, a, l);
+            const int bytes = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + 2 * 3 * Tile<T, D>::ROWS * 4 + (int)a.buckets * 4 * (1 + kWaves);
+            gemm::in_launches((int64_t)a.n * a.seq_count * a.kv_heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+                if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true>), grid, dim3(kThreads), bytes + kWaves * 32 * 80, stream, a, l, parts);
+                else hipLaunchKernelGGL((k_attn_dkv<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l, parts);
             });
         }));
-    } else if (dbias) {
-        hipLaunchKernelGGL(k_attn_dbias, dim3(a.n * a.heads, (a.buckets + 63) / 64), dim3(256), 0, stream, a.part, parts, 0, a.heads, a.buckets, dbias, dbias_worker, accumulate);
+        if (dbias) join(a.seq_count * a.tiles, accumulate || first > 0);
     }
 }
 

@@ -7,7 +7,7 @@ A sum of m numbers made in 32 bits is off by at most m u times the sum of magnit
   P     by the share ep = es + max es of the row + (len + 24) u               (exp2's own rounding, the sum's, its reciprocal, rescaling)
   o     by sum_j P' |v| (ep + W + (len + 24) u),  P' = m P / (1 - p)
   dP    by edp = (dim + 4) u m / (1 - p) |do|.|v|
-  delta by ed = |do|.(what o may be off by, rounded to its type) + (dim + 4) u |do|.|o|
+  delta by ed = sum_j P (edp + |dP| (ep + (len + 4) u))                         (it is added up as sum_j P dP)
   dS    by eds = P (edp + ed) + |dS| (ep + 4 u)
   dq, dk by scale sum (eds + |dS| (W + (len + 24) u)) |k| or |q|; dv by sum P' (ep + W + (len + 24) u) |do|; dbias by sum eds + |dS| N u, N terms
 and every output by its own rounding.  A word of a 16-bit float that was scaled is off by 2^-38 of its column's largest, where it is subnormal."""
@@ -85,11 +85,13 @@ def formulas(q, k, v, bias, starts, do=None, seqs=1, lengths=None, causal=True, 
                 delta = (dO * o).sum(1, keepdim=True)
                 dS = P * (dP - delta)
                 edp = (dim + 4) * U * m * (dO.abs() @ V.abs().t())
-                ed = (dO.abs() * rounded(o, eo, kind)).sum(1, keepdim=True) + (dim + 4) * U * (dO.abs() * o.abs()).sum(1, keepdim=True)
+                ed = (P * (edp + dP.abs() * (ep + (l + 4) * U))).sum(1, keepdim=True)
                 eds = P * (edp + ed) + dS.abs() * (ep + 4 * U)
+                # dq is made with do . o for delta, of which o's rounding is taken back at the end by sum P k, whose P's are words
                 ew = eds + dS.abs() * more
+                eo_k = more * (dO.abs() * rounded(o, eo, kind)).sum(1, keepdim=True) * (P @ K.abs())
                 out["dq"][i, s, :l, h] = scale * (dS @ K)
-                tol["dq"][i, s, :l, h] = abs(scale) * ((ew + tiny * dS.abs().amax(1, keepdim=True)) @ K.abs())
+                tol["dq"][i, s, :l, h] = abs(scale) * (eo_k + (ew + more * P * (dO.abs() * rounded(o, eo, kind)).sum(1, keepdim=True) + tiny * dS.abs().amax(1, keepdim=True)) @ K.abs())
                 out["dk"][i, s, :l, h // group] += scale * (dS.t() @ Q)
                 tol["dk"][i, s, :l, h // group] += abs(scale) * ((ew + tiny * dS.abs().amax(0, keepdim=True)).t() @ Q.abs())
                 out["dv"][i, s, :l, h // group] += PD.t() @ dO
