@@ -28,6 +28,11 @@ struct Args {
     int64_t t;
     uint32_t n, seqs, len, heads, kv_heads, dim, buckets, tiles;
     uint32_t seq_first, seq_count;  // sequences that a launch deals with, of every worker
+    int32_t edge_lo, edge_hi;       // the second bucket's start, and the last one's
+    int32_t table_first;            // distances that are looked up in a table: the first one, and how many; 0: none are
+    uint32_t table_count;
+    uint32_t head_pieces, query_pieces;     // that the rows of a key's sums are cut into, of a group's heads and of a head's queries
+    float *dk_parts, *dv_parts;     // [pieces][n][t][kv_heads * dim], if there are several
     float scale, scale2;            // the logits' factor, and the same times log2 e
     Keep keep;
     int32_t causal;
@@ -119,12 +124,21 @@ struct Bring {
     __device__ __forceinline__ void load(const E *p, int64_t row, uint32_t first, uint32_t limit, uint32_t dim)
     {
         p += (int64_t)first * row;
+        if (first + Ti::ROWS <= limit && dim == D) {
 #pragma unroll
-        for (int i = 0; i < Ti::N; ++i) {
-            const uint32_t r = (i * kThreads + threadIdx.x) / Ti::PIECES, at = (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>;
+            for (int i = 0; i < Ti::N; ++i) {
+                const uint32_t r = (i * kThreads + threadIdx.x) / Ti::PIECES, at = (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>;
+                const piece_t v = *(const piece_t *)(p + r * row + at);
+                raw[i][0] = v[0]; raw[i][1] = v[1]; raw[i][2] = v[2]; raw[i][3] = v[3];
+            }
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) raw[i][e] = 0;
-            if (first + r < limit && at < dim) load_piece<T>(p + r * row, at, dim, raw[i]);
+            for (int i = 0; i < Ti::N; ++i) {
+                const uint32_t r = (i * kThreads + threadIdx.x) / Ti::PIECES, at = (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[i][e] = 0;
+                if (first + r < limit && at < dim) load_piece<T>(p + r * row, at, dim, raw[i]);
+            }
         }
     }
     __device__ __forceinline__ void store(char *tile) const
@@ -157,8 +171,26 @@ __device__ __forceinline__ void row_fragments(const typename TypeOf<T>::type *p,
     }
 }
 
-// what the other half of the wavefront has for the same column
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// what both halves of the wavefront have for a column, added up, and the larger of both
+__device__ __forceinline__ void halves(float v, float &a, float &b)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    a = __builtin_bit_cast(float, (uint32_t)r[0]);
+    b = __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ __forceinline__ float sum_halves(float v)
+{
+    float a, b;
+    halves(v, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float max_halves(float v)
+{
+    float a, b;
+    halves(v, a, b);
+    return fmaxf(a, b);
+}
 
 // ---- a wavefront's 32 columns of D numbers, of which a lane has four next to each other at a time, stored as rows ----
 template <int T, int D>
@@ -187,74 +219,120 @@ __device__ __forceinline__ void store_columns(typename TypeOf<T>::type *row, boo
 }
 
 // ---- the bias ----
-// Bucket b is the distances (key minus query) from starts[b] on to starts[b + 1] - 1; what lies before starts[1] is bucket 0.  A workgroup
-// has the starts in LDS; a tile whose distances all lie in one bucket adds one number, any other one looks its numbers up by distance in a
-// window that the workgroup has filled for it.
+// Bucket b is the distances (key minus query) from starts[b] on to starts[b + 1] - 1; what lies before starts[1] is bucket 0.  A wavefront's
+// tile whose distances all lie before starts[1], or all from the last start on, adds one number.  For others the workgroup has the biases
+// of the distances in between by distance in LDS, and kReach more on both sides, so that such a tile's all are there; where
+// these are too many ("wide"), a tile is looked at for a start within its distances, and where there is one, each number is searched for.
+constexpr int kReach = 96, kMaxTable = 4096;
+
 __device__ __forceinline__ float bias_of(float v)
 {
     // numbers stay numbers, however large: rows of nothing but the type's lowest value have equal weights
     return __builtin_isfinite(v) ? fminf(fmaxf(v * kLog2e, -1.7e38f), 1.7e38f) : v;
 }
 
-struct Starts {
-    const int *at;          // [buckets] in LDS
-    uint32_t buckets;
+struct Bias {
+    const int *starts;      // [buckets] in LDS
+    float *table;           // [table_count] in LDS
+    const float *row;       // [buckets], the head's
+    float before, behind;   // the first and the last bucket's
 
-    // of a tile's distances from lo to hi: the bucket of lo, and whether it is that of hi too.  Every wavefront finds out for itself.
-    __device__ __forceinline__ bool one_bucket(int lo, int hi, uint32_t &bucket) const
+    // where they lie in LDS, and how much they take
+    __device__ __forceinline__ void place(const Args &a, char *lds)
     {
-        uint32_t below = 0, above = 0;
-        for (uint32_t b = 0; b < buckets; b += 64) {
-            const uint32_t i = b + (threadIdx.x & 63);
-            const bool there = i > 0 && i < buckets;
-            const int start = there ? at[i] : 0;
-            below += __builtin_popcountll(__ballot(there && start <= lo));
-            above += __builtin_popcountll(__ballot(there && start <= hi));
-        }
-        bucket = below;
-        return below == above;
+        starts = (const int *)lds;
+        table = (float *)(lds + a.buckets * 4);
     }
-    __device__ __forceinline__ uint32_t of(int distance) const
+    static int bytes(const Args &a) { return (int)(a.buckets + a.table_count) * 4; }
+    // the workgroup's starts, before a barrier
+    __device__ __forceinline__ void bring_starts(const Args &a) const
     {
-        uint32_t lo = 0, n = buckets;               // the answer is one of lo .. lo + n - 1
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) ((int *)starts)[b] = a.starts[b];
+    }
+    // a head's biases, behind a barrier and before another
+    __device__ __forceinline__ void bring(const Args &a, uint32_t head)
+    {
+        before = behind = 0.f;
+        if (a.buckets == 0) return;
+        row = a.bias + (int64_t)head * a.buckets;
+        before = bias_of(row[0]);
+        behind = bias_of(row[a.buckets - 1]);
+        for (uint32_t i = threadIdx.x; i < a.table_count; i += kThreads) table[i] = bias_of(row[bucket(a, a.table_first + (int)i)]);
+    }
+    __device__ __forceinline__ uint32_t bucket(const Args &a, int distance) const
+    {
+        uint32_t lo = 0, n = a.buckets;             // the answer is one of lo .. lo + n - 1
         while (n > 1) {
             const uint32_t half = n >> 1;
-            const bool up = at[lo + half] <= distance;
+            const bool up = starts[lo + half] <= distance;
             lo = up ? lo + half : lo;
             n = up ? n - half : half;
         }
         return lo;
     }
-};
+    __device__ __forceinline__ float searched(const Args &a, int distance) const { return bias_of(row[bucket(a, distance)]); }
 
-// What a tile of `cols` streamed rows against a workgroup's kRows needs to know of its distances, in LDS, two of them in turn.
-struct Window {
-    float value[64 + kRows];
-    uint16_t bucket[64 + kRows];
-};
-// the same in registers: one bucket, or the window
-struct Band {
-    bool one;
-    uint32_t bucket;
-    float value;
-};
-__device__ __forceinline__ Band band_of(const Starts &starts, const float *bias, int lo, int count, Window &w)
-{
-    Band b = {true, 0, 0.f};
-    if (starts.buckets == 0) return b;
-    b.one = starts.one_bucket(lo, lo + count - 1, b.bucket);
-    if (b.one) {
-        b.value = bias_of(bias[b.bucket]);
-    } else if ((int)threadIdx.x < count) {
-        const uint32_t k = starts.of(lo + (int)threadIdx.x);
-        w.value[threadIdx.x] = bias_of(bias[k]);
-        w.bucket[threadIdx.x] = (uint16_t)k;
+    // whether the distances from lo to hi (kReach apart at most) share a bucket, which one, and its bias
+    __device__ __forceinline__ bool one(const Args &a, int lo, int hi, uint32_t &bucket, float &value) const
+    {
+        bucket = 0;
+        value = before;
+        if (a.buckets < 2 || hi < a.edge_lo) return true;
+        bucket = a.buckets - 1;
+        value = behind;
+        if (lo >= a.edge_hi) return true;
+        if (a.table_count) return false;
+        uint32_t below = 0, above = 0;
+        for (uint32_t b = 0; b < a.buckets; b += 64) {
+            const uint32_t i = b + (threadIdx.x & 63);
+            const bool there = i > 0 && i < a.buckets;
+            const int start = there ? starts[i] : 0;
+            below += __builtin_popcountll(__ballot(there && start <= lo));
+            above += __builtin_popcountll(__ballot(there && start <= hi));
+        }
+        bucket = below;
+        value = bias_of(row[below]);
+        return below == above;
     }
-    return b;
-}
+};
 
 // 4 (i / 4) + ... : row i of a lane in an accumulator
 __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
+
+__device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// wavefronts that a SIMD holds: what is more takes accumulators through moves
+template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= 96 ? 2 : 1;
+
+template <int T, int D>
+__device__ __forceinline__ void flip(typename Fragment<T>::type (&f)[D / 16])
+{
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+        if constexpr (T == SAMS_F32) f[s] = -f[s];
+        else f[s] ^= 0x80008000u;
+    }
+}
+
+// s = times s + bias of every pair, of a lane's query and the keys of its accumulators; distance: the first key's less the query
+template <int T, int NB>
+__device__ __forceinline__ void add_bias(const Args &a, const Bias &bias, bool one, float by, int distance, float times, int lane, f32x16 (&s)[NB])
+{
+    const float *from = bias.table + (distance - a.table_first);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        if (one) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by);
+        } else if (a.table_count) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, from[32 * j + row_of(i, lane)]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, bias.searched(a, distance + 32 * j + row_of(i, lane)));
+        }
+    }
+}
 
 // A tile's place: worker, sequence, head, and its first row
 struct Place {
@@ -307,7 +385,9 @@ constexpr int kLdsBytes = 160 * 1024;
 hipError_t prepare_forward(int type, uint32_t dim);
 hipError_t prepare_backward(int type, uint32_t dim);
 void launch_forward(const Args &a, int type, hipStream_t stream);
-void launch_backward(const Args &a, int type, int64_t parts, float *dbias, int64_t dbias_worker, int accumulate, hipStream_t stream);
+// numbers that the scratch holds of dk's parts, and of dv's
+int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim);
+void launch_backward(const Args &a, int type, int64_t parts, int64_t sums, float *dbias, int64_t dbias_worker, int accumulate, hipStream_t stream);
 
 }  // namespace attn
 }  // namespace sams

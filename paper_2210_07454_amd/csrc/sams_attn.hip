@@ -14,7 +14,7 @@ namespace attn {
 // S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
 // Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch launch)
+__global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forward(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
@@ -22,10 +22,10 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
     constexpr float SHIFT = T == SAMS_F16 ? 14.f : 0.f;             // 16-bit floats of up to 2^14: small weights keep their digits
     extern __shared__ __align__(16) char lds[];
     char *tile_k = lds, *tile_v = lds + 2 * Ti::BYTES;
-    Window *window = (Window *)(lds + 4 * Ti::BYTES);
-    int *starts_lds = (int *)(window + 2);
+    Bias bias;
+    bias.place(a, lds + 4 * Ti::BYTES);
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uniform_wave();
     const Place at = place_of(a, launch, a.heads, a.causal);
     const uint32_t q0 = at.first + wave * 32, query = q0 + (lane & 31);
     const bool row_there = query < a.len, live = query < at.length;
@@ -40,26 +40,26 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
     float top = -__builtin_inff(), sum = 0.f;
 
     if (at.first < at.length) {
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) starts_lds[b] = a.starts[b];
-        const Starts starts = {starts_lds, a.buckets};
-        const float *bias = a.bias + (int64_t)at.head * a.buckets;
         const uint32_t kv = at.head / (a.heads / a.kv_heads);
         const E *k = rows_of<T>(a.k, a.ks, a, at, kv), *v = rows_of<T>(a.v, a.vs, a, at, kv);
         const uint32_t end = a.causal && at.first + kRows < at.length ? at.first + kRows : at.length;
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
-        const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head;
+        const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head, less = (a.keep.least - 1) * 0x10001u;
 
-        typename Ti::Frag qf[D / 16];
-        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
         Bring<T, D> bk, bv;
         bk.load(k, a.ks.row, 0, at.length, a.dim);
         bv.load(v, a.vs.row, 0, at.length, a.dim);
+        typename Ti::Frag qf[D / 16];
+        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
+        // the scale's sign goes into q, so that the largest product is the largest logit
+        const float scale = fabsf(a.scale2);
+        if (a.scale2 < 0.f) flip<T, D>(qf);
+        bias.bring_starts(a);
         __syncthreads();
+        bias.bring(a, at.head);
         bk.store(tile_k);
         bv.store(tile_v);
-        const int lo = -(int)(at.first + kRows - 1);
-        Band band = band_of(starts, bias, lo, BN + kRows - 1, window[0]);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -68,8 +68,11 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
                 bk.load(k, a.ks.row, key0 + BN, at.length, a.dim);
                 bv.load(v, a.vs.row, key0 + BN, at.length, a.dim);
             }
-            const bool needed = q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(band.one && band.value == -__builtin_inff());
-            if (needed) {
+            const int lo = (int)key0 - (int)(q0 + 31);
+            uint32_t bucket;
+            float by;
+            const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
+            if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 const char *tk = tile_k + turn * Ti::BYTES, *tv = tile_v + turn * Ti::BYTES;
                 f32x16 s[NB];
 #pragma unroll
@@ -79,31 +82,29 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) s[j] = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s[j]);
                 }
-                if (band.one) {
+                // logits are times * s + by.  Within a tile of one bucket without a border nothing is done to s for that: the largest one is
+                // found, and the exponents are made, from it.  (A large bias, as a mask has, is added first, so that it swallows the rest as it
+                // does in any other tile and in the backward pass.)
+                float times = scale;
+                const bool edge = key0 + BN > at.length || (a.causal && key0 + BN - 1 > q0);
+                if (edge || !one || !(fabsf(by) < 1e6f)) {
+                    add_bias<T, NB>(a, bias, one, by, lo + 31 - (lane & 31), scale, lane, s);
+                    times = 1.f;
+                    by = 0.f;
+                    if (edge) {
+                        const int limit = (int)(a.causal && query < at.length ? query + 1 : at.length) - (int)key0;
 #pragma unroll
-                    for (int j = 0; j < NB; ++j)
+                        for (int j = 0; j < NB; ++j)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], a.scale2, band.value);
-                } else {
-                    const float *by = window[turn].value + (kRows - 1 - (int)(query - at.first));
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], a.scale2, by[32 * j + row_of(i, lane)]);
-                }
-                if (key0 + BN > at.length || (a.causal && key0 + BN - 1 > q0)) {
-                    const int limit = (int)(a.causal && query < at.length ? query + 1 : at.length) - (int)key0;
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[j][i] = 32 * j + row_of(i, lane) < limit ? s[j][i] : -__builtin_inff();
+                            for (int i = 0; i < 16; ++i) s[j][i] = 32 * j + row_of(i, lane) < limit ? s[j][i] : -__builtin_inff();
+                    }
                 }
                 float most = s[0][0];
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) most = fmaxf(most, s[j][i]);
-                most = fmaxf(fmaxf(most, other_half(most)), top);
+                most = fmaxf(__builtin_fmaf(max_halves(most), times, by), top);
                 if (__any(most > top)) {
                     const float less = most == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - most);
                     sum *= less;
@@ -113,37 +114,46 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
                         for (int i = 0; i < 16; ++i) acc[d][i] *= less;
                     top = most;
                 }
-                const float base = top == -__builtin_inff() ? 0.f : top - SHIFT;
+                const float from = by - (top == -__builtin_inff() ? 0.f : top - SHIFT);
 #pragma unroll
-                for (int j = 0; j < NB; ++j) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[j][i] = __builtin_amdgcn_exp2f(s[j][i] - base);
-                        sum += s[j][i];
-                    }
+                for (int j = 0; j < NB; ++j)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
+                        float part[4];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][8 * half + e], times, from));
+                            s[j][8 * half + e] = x;
+                            part[e & 3] = e < 4 ? x : part[e & 3] + x;
+                        }
+                        sum += (part[0] + part[1]) + (part[2] + part[3]);
+                        typename Ti::Frag w;
                         if constexpr (DROP) {
                             uint32_t numbers[4];
                             philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
+                            w = words_of<T>(s[j], half);
+                            if constexpr (T == SAMS_F32) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) s[j][8 * half + e] = kept(numbers, e, a.keep.least) ? s[j][8 * half + e] : 0.f;
+                                for (int e = 0; e < 8; ++e) w[e] = kept(numbers, e, a.keep.least) ? w[e] : 0.f;
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) w[e] = keep_words(w[e], numbers[e], less);
+                            }
+                        } else {
+                            w = words_of<T>(s[j], half);
                         }
-                        const typename Ti::Frag w = words_of<T>(s[j], half);
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tv, 32 * j + 16 * half, 32 * d, lane), w, acc[d]);
                     }
-                }
             }
             if (more) {
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES);
-                band = band_of(starts, bias, lo + (int)(key0 + BN), BN + kRows - 1, window[turn ^ 1]);
             }
             __syncthreads();
         }
     }
-    sum += other_half(sum);
+    sum = sum_halves(sum);
     const float by = live && sum != 0.f ? a.keep.scale / sum : 0.f;
     if (!live) {
 #pragma unroll
@@ -161,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) k_attn_forward(Args a, gemm::Launch 
 template <int T, int D>
 static int lds_forward(const Args &a)
 {
-    return 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + ((int)a.buckets * 4 + 15) / 16 * 16;
+    return 4 * Tile<T, D>::BYTES + Bias::bytes(a);
 }
 
 // a context's kernels may take more LDS than a launch gets unasked
@@ -192,10 +202,11 @@ void launch_forward(const Args &a, int type, hipStream_t stream)
 
 struct sams_attn {
     int32_t n, heads, kv_heads, dim, buckets, type, train;
-    int64_t t_max, parts;
+    int64_t t_max, parts, sums;
+    int32_t edge_lo, edge_hi, table_first, table_count;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t starts, delta, part;
+    int64_t starts, delta, part, dk_parts, dv_parts;
 };
 
 using namespace sams;
@@ -223,6 +234,9 @@ static bool arguments(sams_attn *c, int64_t t, int64_t seqs, const int32_t *leng
     a.tiles = (a.len + attn::kRows - 1) / attn::kRows;
     a.seq_first = 0;
     a.seq_count = a.seqs;
+    a.edge_lo = c->edge_lo; a.edge_hi = c->edge_hi;
+    a.table_first = c->table_first; a.table_count = (uint32_t)c->table_count;
+    a.head_pieces = a.query_pieces = 1;
     a.scale = scale;
     a.scale2 = scale * attn::kLog2e;
     a.causal = causal != 0;
@@ -248,7 +262,19 @@ int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, i
     c->stream = (hipStream_t)hip_stream;
     c->parts = (t_max + 63) / 64 + 64;
     c->starts = c->scratch.reserve((int64_t)buckets * 4);
+    if (buckets > 1) {
+        c->edge_lo = starts_host[1];
+        c->edge_hi = starts_host[buckets - 1];
+        const int64_t count = (int64_t)c->edge_hi - c->edge_lo + 2 * attn::kReach + 1;
+        if (count <= attn::kMaxTable && c->edge_lo > INT32_MIN + attn::kReach) {
+            c->table_first = c->edge_lo - attn::kReach;
+            c->table_count = (int32_t)count;
+        }
+    }
     if (train) {
+        c->sums = attn::sums_room(n, t_max, heads, kv_heads, dim);
+        c->dk_parts = c->scratch.reserve(c->sums * 4);
+        c->dv_parts = c->scratch.reserve(c->sums * 4);
         c->delta = c->scratch.reserve((int64_t)n * heads * t_max * 4);
         c->part = c->scratch.reserve((int64_t)n * heads * c->parts * buckets * 4);
     }
@@ -327,7 +353,9 @@ int attention_backward(sams_attn *c, int64_t t, int64_t seqs, const int32_t *len
     a.dq = dq; a.dqs = Rows{dq_worker, dq_row};
     a.dk = dk; a.dks = Rows{dk_worker, dk_row};
     a.dv = dv; a.dvs = Rows{dv_worker, dv_row};
-    attn::launch_backward(a, c->type, c->parts, dbias, dbias_worker, accumulate, c->stream);
+    a.dk_parts = c->scratch.at<float>(c->dk_parts);
+    a.dv_parts = c->scratch.at<float>(c->dv_parts);
+    attn::launch_backward(a, c->type, c->parts, c->sums, dbias, dbias_worker, accumulate, c->stream);
     SAMS_HIP(hipGetLastError());
     return SAMS_OK;
 }

@@ -23,7 +23,7 @@ template <int T, int D> struct ColumnScale {
             float most = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(v[i]));
-            most = fmaxf(most, other_half(most));
+            most = max_halves(most);
             if (__any(most * by > 32768.f)) {
                 const uint32_t power = __builtin_bit_cast(uint32_t, most) >> 23;            // 127 + its exponent
                 const float next = most * by > 32768.f ? __builtin_bit_cast(float, (127 + 14 + 127 - power) << 23) : by;
@@ -64,8 +64,8 @@ struct BucketSums {
         for (int i = 0; i < 8; ++i) v[i] = ds[i] + ds[i + 8];
         own += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
-    // by[x]: the bucket of the distance x - 32 from that of the block's corner, x = 1 .. 63
-    __device__ __forceinline__ void many(const uint16_t *by, const f32x16 &ds, int lane)
+    // corner: the distance of the block's first key and query
+    __device__ __forceinline__ void many(const Args &a, const Bias &bias, int corner, const f32x16 &ds, int lane)
     {
         float up = 0.f, down = 0.f;             // distances lane % 32 and lane % 32 - 32
         const int half = lane & 32;
@@ -76,10 +76,10 @@ struct BucketSums {
             if ((lane & 31) + r < 32) up += v;
             else down += v;
         }
-        up += other_half(up);
-        down += other_half(down);
+        up = sum_halves(up);
+        down = sum_halves(down);
         float v = half ? up : down;             // the distance lane - 32
-        const int mine = by[lane ? lane : 1];
+        const int mine = (int)bias.bucket(a, corner + (lane ? lane : 1) - 32);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {      // sums over the lanes of a bucket, which follow each other
             const float below = __shfl_up(v, o);
@@ -96,36 +96,32 @@ struct BucketSums {
 // 32 bits that dbias is held to.  So delta is also added up as it is defined, sum P dP, for the other kernel, and dq, which needs it before that
 // sum is done, is put right at the end: dq = scale (sum P (dP - d) k + (d - delta) sum P k), with d = do . o.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launch)
+__global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
     constexpr int BN = Ti::ROWS, NB = BN / 32;
-    constexpr float SHIFT = T == SAMS_F16 ? 0x1p14f : 1.f;          // P in 16-bit floats
+    constexpr float SHIFT = T == SAMS_F16 ? 14.f : 0.f;             // P in 16-bit floats: times 2^14
+    constexpr bool ROUNDED = T != SAMS_F32;
     extern __shared__ __align__(16) char lds[];
     char *tile_k = lds, *tile_v = lds + 2 * Ti::BYTES;
-    Window *window = (Window *)(lds + 4 * Ti::BYTES);
-    int *starts_lds = (int *)(window + 2);
+    Bias bias;
+    bias.place(a, lds + 4 * Ti::BYTES);
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uniform_wave();
     const Place at = place_of(a, launch, a.heads, a.causal);
     const uint32_t q0 = at.first + wave * 32, query = q0 + (lane & 31);
     const bool row_there = query < a.len, live = query < at.length;
     const int64_t stat = stats_of(a, at, at.head) + query;
 
-    constexpr bool ROUNDED = T != SAMS_F32;
     f32x16 acc[D / 32], pk[ROUNDED ? D / 32 : 1];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = pk[ROUNDED ? d : 0][i] = 0.f;
-    ColumnScale<T, D> fit;
-    fit.start();
+    float over = 0.f;
 
     if (at.first < at.length) {
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) starts_lds[b] = a.starts[b];
-        const Starts starts = {starts_lds, a.buckets};
-        const float *bias = a.bias + (int64_t)at.head * a.buckets;
         const uint32_t kv = at.head / (a.heads / a.kv_heads);
         const E *k = rows_of<T>(a.k, a.ks, a, at, kv), *v = rows_of<T>(a.v, a.vs, a, at, kv);
         const uint32_t end = a.causal && at.first + kRows < at.length ? at.first + kRows : at.length;
@@ -133,40 +129,39 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
         if constexpr (DROP) seed = read_seed(a.rng);
         const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head;
 
+        Bring<T, D> bk, bv;
+        bk.load(k, a.ks.row, 0, at.length, a.dim);
+        bv.load(v, a.vs.row, 0, at.length, a.dim);
         typename Ti::Frag qf[D / 16], df[D / 16];
         row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
         row_fragments<T, D>(rows_of<T>(a.dout, a.douts, a, at, at.head) + (int64_t)query * a.douts.row, live, a.dim, lane, df);
-        float delta = 0.f;
+        // do . o, less the factor 1 / (1 - p) that dP is made without
+        float d = 0.f, exact = 0.f;
         {
             const E *o = rows_of<T>(a.o, a.os, a, at, at.head) + (int64_t)query * a.os.row;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                float x[8], y[8];
-                const uint32_t from = 16 * s + 8 * (lane >> 5);
+                float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = 0.f;
-                if (live) load8<T>(o, from, a.dim, x);
-                typename TypeOf<T>::type e[8];
+                if (live) load8<T>(o, 16 * s + 8 * (lane >> 5), a.dim, x);
+                E e[8];
                 __builtin_memcpy(e, &df[s], sizeof(e));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = (float)e[i];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(x[i], y[i], delta);
+                for (int i = 0; i < 8; ++i) d = __builtin_fmaf(x[i], (float)e[i], d);
             }
-            delta += other_half(delta);
+            d = sum_halves(d) / a.keep.scale;
         }
         const float top = live ? a.row_max[stat] : 0.f, total = live ? a.row_sum[stat] : 0.f;
-        const float over = total == 0.f ? 0.f : SHIFT / total;
-        float exact = 0.f;
+        over = total == 0.f ? 0.f : 1.f / total;
+        ColumnScale<T, D> fit;
+        fit.start();
 
-        Bring<T, D> bk, bv;
-        bk.load(k, a.ks.row, 0, at.length, a.dim);
-        bv.load(v, a.vs.row, 0, at.length, a.dim);
+        bias.bring_starts(a);
         __syncthreads();
+        bias.bring(a, at.head);
         bk.store(tile_k);
         bv.store(tile_v);
-        const int lo = -(int)(at.first + kRows - 1);
-        Band band = band_of(starts, bias, lo, BN + kRows - 1, window[0]);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -175,60 +170,67 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
                 bk.load(k, a.ks.row, key0 + BN, at.length, a.dim);
                 bv.load(v, a.vs.row, key0 + BN, at.length, a.dim);
             }
-            const bool needed = q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(band.one && band.value == -__builtin_inff());
-            if (needed) {
+            const int lo = (int)key0 - (int)(q0 + 31);
+            uint32_t bucket;
+            float by;
+            const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
+            if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 const char *tk = tile_k + turn * Ti::BYTES, *tv = tile_v + turn * Ti::BYTES;
                 const bool edge = key0 + BN > at.length || q0 + 32 > at.length || (a.causal && key0 + BN - 1 > q0);
+                const bool plain = one && fabsf(by) < 1e6f;         // as in the forward pass
                 const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)key0;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    f32x16 s, dp;
+                    f32x16 s[1], dp;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+                    for (int i = 0; i < 16; ++i) s[0][i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s);
+                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s[0]);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(tv, 32 * j, c, lane), df[c], dp);
-                    if (band.one) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, band.value);
-                    } else {
-                        const float *by = window[turn].value + (kRows - 1 - (int)(query - at.first)) + 32 * j;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by[row_of(i, lane)]);
+                    float times = a.scale2, from = by - top + SHIFT;
+                    if (!plain) {
+                        add_bias<T, 1>(a, bias, one, by, lo + 31 - (lane & 31) + 32 * j, a.scale2, lane, s);
+                        times = 1.f;
+                        from = SHIFT - top;
                     }
+                    // P, times the row's sum: that is divided out of the row's results at the end
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] - top) * over;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        if constexpr (DROP) {
-                            uint32_t numbers[4];
-                            philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) dp[8 * half + e] = kept(numbers, e, a.keep.least) ? dp[8 * half + e] * a.keep.scale : 0.f;
-                        }
-                    }
+                    for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i], times, from));
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const bool allowed = 32 * j + row_of(i, lane) < limit;
-                            s[i] = allowed ? s[i] : 0.f;
+                            s[0][i] = allowed ? s[0][i] : 0.f;
                             dp[i] = allowed ? dp[i] : 0.f;
                         }
                     }
                     typename Ti::Frag wp[2];
                     if constexpr (ROUNDED) {
-                        wp[0] = words_of<T>(s, 0);
-                        wp[1] = words_of<T>(s, 1);
+                        wp[0] = words_of<T>(s[0], 0);
+                        wp[1] = words_of<T>(s[0], 1);
                     }
+                    // dS = m P dP - P d
+                    if constexpr (DROP) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) exact = __builtin_fmaf(s[i], dp[i], exact);
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t numbers[4];
+                            philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
-                    fit.fit(s, acc);
+                            for (int e = 0; e < 8; ++e) dp[8 * half + e] = kept(numbers, e, a.keep.least) ? dp[8 * half + e] : 0.f;
+                        }
+                    }
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        part[i & 3] = __builtin_fmaf(s[0][i], dp[i], part[i & 3]);
+                        s[0][i] *= dp[i] - d;
+                    }
+                    exact += (part[0] + part[1]) + (part[2] + part[3]);
+                    fit.fit(s[0], acc);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const typename Ti::Frag w = words_of<T>(s, half);
+                        const typename Ti::Frag w = words_of<T>(s[0], half);
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) {
                             const typename Ti::Frag columns = Ti::across(tk, 32 * j + 16 * half, 32 * d, lane);
@@ -241,26 +243,27 @@ __global__ void __launch_bounds__(kThreads) k_attn_dq(Args a, gemm::Launch launc
             if (more) {
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES);
-                band = band_of(starts, bias, lo + (int)(key0 + BN), BN + kRows - 1, window[turn ^ 1]);
             }
             __syncthreads();
         }
-        exact = (exact + other_half(exact)) * (1.f / SHIFT);
+        over *= T == SAMS_F16 ? 0x1p-14f : 1.f;
+        exact = sum_halves(exact) * over;
         if (live && lane < 32) a.delta[stat] = exact;
         if constexpr (ROUNDED) {
 #pragma unroll
-            for (int d = 0; d < D / 32; ++d)
+            for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[d][i] = __builtin_fmaf(acc[d][i], 1.f / fit.by, (delta - exact) * pk[d][i]);
+                for (int e = 0; e < 16; ++e) acc[i][e] = __builtin_fmaf(acc[i][e], 1.f / fit.by, (d - exact) * pk[i][e]);
         }
     }
-    store_columns<T, D>(rows_of<T>(a.dq, a.dqs, a, at, at.head) + (int64_t)query * a.dqs.row, row_there, a.dim, acc, a.scale / SHIFT, lane);
+    store_columns<T, D>(rows_of<T>(a.dq, a.dqs, a, at, at.head) + (int64_t)query * a.dqs.row, row_there, a.dim, acc, a.scale * a.keep.scale * over, lane);
 }
 
 // dk, dv and dbias.  A workgroup has 128 keys, a lane (and the lane 32 from it) one; queries and the output's gradients come by tiles.  The
-// products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.
+// products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.  Where there are few keys
+// and heads of keys, a group's heads and a head's queries are shared out to several workgroups, whose sums another kernel joins.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
+__global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
 {
     typedef Tile<T, D> Ti;
     constexpr int BQ = Ti::ROWS, NB = BQ / 32;
@@ -268,14 +271,17 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
     constexpr int NUMBERS = 80;                                     // bytes of a query's numbers: 32 of 16 bits, and 16 that put the queries on different banks
     extern __shared__ __align__(16) char lds[];
     char *tile_q = lds, *tile_d = lds + 2 * Ti::BYTES;
-    Window *window = (Window *)(lds + 4 * Ti::BYTES);
-    float *stats = (float *)(window + 2);                           // [2][3][BQ]
+    float *stats = (float *)(lds + 4 * Ti::BYTES);                  // [2][3][BQ]
     char *numbers_lds = (char *)(stats + 2 * 3 * BQ);               // [kWaves][32] queries' numbers
-    int *starts_lds = (int *)(numbers_lds + (DROP ? kWaves * 32 * NUMBERS : 0));
-    float *sums_lds = (float *)(starts_lds + a.buckets);            // [kWaves][buckets]
+    float *sums_lds = (float *)(numbers_lds + (DROP ? kWaves * 32 * NUMBERS : 0));      // [kWaves][buckets]
+    Bias bias;
+    bias.place(a, (char *)(sums_lds + kWaves * a.buckets));
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Place at = place_of(a, launch, a.kv_heads, false);
+    const int lane = threadIdx.x & 63, wave = uniform_wave();
+    const uint32_t pieces = a.head_pieces * a.query_pieces;
+    Place at = place_of(a, launch, a.kv_heads * pieces, false);
+    const uint32_t piece = at.head % pieces, head_piece = piece / a.query_pieces, query_piece = piece % a.query_pieces;
+    at.head /= pieces;
     const uint32_t k0 = at.first + wave * 32, key = k0 + (lane & 31);
     const bool row_there = key < a.len, live = key < at.length;
 
@@ -286,33 +292,32 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.f;
     ColumnScale<T, D> fit;
     fit.start();
-
-    const uint32_t group = a.heads / a.kv_heads;
+    const uint32_t group = a.heads / a.kv_heads / a.head_pieces, head0 = at.head * (a.heads / a.kv_heads) + head_piece * group;
+    // this piece's tiles of queries; 128 is a multiple of BQ, so that the first key's tile is the first one where earlier queries see none
+    const uint32_t tile0 = a.causal ? at.first / BQ : 0, tiles = (at.length + BQ - 1) / BQ;
+    uint32_t begin = 0, end = 0;
+    if (at.first < at.length) {
+        begin = (tile0 + (tiles - tile0) * query_piece / a.query_pieces) * BQ;
+        end = (tile0 + (tiles - tile0) * (query_piece + 1) / a.query_pieces) * BQ;
+    }
     BucketSums sums = {sums_lds + wave * a.buckets, 0.f, 0};
     const bool summed = a.part != nullptr;
     // a head's sums of the workgroup; between barriers
     auto leave = [&](uint32_t head, bool some) {
-        float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + (int64_t)(at.seq - a.seq_first) * a.tiles + at.first / kRows) * a.buckets;
+        float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + ((int64_t)(at.seq - a.seq_first) * a.tiles + at.first / kRows) * a.query_pieces + query_piece) * a.buckets;
         for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
             part[b] = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
             for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
         }
     };
-    if (at.first >= at.length) {
-        for (uint32_t h = 0; summed && h < group; ++h) leave(at.head * group + h, false);
+    if (begin >= end) {
+        for (uint32_t h = 0; summed && h < group; ++h) leave(head0 + h, false);
     } else {
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
-            starts_lds[b] = a.starts[b];
+        bias.bring_starts(a);
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads)
             for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
-        }
-        const Starts starts = {starts_lds, a.buckets};
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
-        const uint32_t begin = a.causal ? at.first / BQ * BQ : 0;   // 128 is a multiple of BQ: the first key's tile
-        typename Ti::Frag kf[D / 16], vf[D / 16];
-        row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head) + (int64_t)key * a.ks.row, live, a.dim, lane, kf);
-        row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head) + (int64_t)key * a.vs.row, live, a.dim, lane, vf);
-
         Bring<T, D> bq, bd;
         float stat[3] = {0.f, 0.f, 0.f};
         auto load = [&](uint32_t head, uint32_t query0) {
@@ -335,27 +340,30 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
 #pragma unroll
                 for (int i = 0; i < 3; ++i) stats[(turn * 3 + i) * BQ + threadIdx.x] = stat[i];
         };
-        // distances of a tile: from at.first - (query0 + BQ - 1) on
-        auto band_at = [&](uint32_t head, uint32_t query0, int turn) {
-            return band_of(starts, a.bias + (int64_t)head * a.buckets, (int)at.first - (int)(query0 + BQ - 1), BQ + kRows - 1, window[turn]);
-        };
-        uint32_t head = at.head * group, query0 = begin;
+        uint32_t head = head0, query0 = begin;
         const uint32_t last = head + group - 1;
         load(head, query0);
+        typename Ti::Frag kf[D / 16], vf[D / 16];
+        row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head) + (int64_t)key * a.ks.row, live, a.dim, lane, kf);
+        row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head) + (int64_t)key * a.vs.row, live, a.dim, lane, vf);
         __syncthreads();
+        bias.bring(a, head);
         store(0);
-        Band band = band_at(head, query0, 0);
         __syncthreads();
         for (int turn = 0;; turn ^= 1) {
             uint32_t next_head = head, next_query0 = query0 + BQ;
-            if (next_query0 >= at.length) { ++next_head; next_query0 = begin; }
+            if (next_query0 >= end) { ++next_head; next_query0 = begin; }
             const bool more = next_head <= last;
             if (more) load(next_head, next_query0);
-            const bool needed = k0 < at.length && (!a.causal || query0 + BQ - 1 >= k0) && !(band.one && band.value == -__builtin_inff());
-            if (needed) {
+            const int lo = (int)k0 - (int)(query0 + BQ - 1);
+            uint32_t bucket;
+            float by;
+            const bool one = bias.one(a, lo, lo + BQ - 1 + 31, bucket, by);
+            if (k0 < at.length && (!a.causal || query0 + BQ - 1 >= k0) && !(one && by == -__builtin_inff())) {
                 const char *tq = tile_q + turn * Ti::BYTES, *td = tile_d + turn * Ti::BYTES;
                 const float *st = stats + turn * 3 * BQ;
                 const bool edge = query0 + BQ > at.length || k0 + 32 > at.length || (a.causal && query0 < k0 + 31);
+                const bool plain = one && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
@@ -366,26 +374,33 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
                     for (int c = 0; c < D / 16; ++c) s = product<T>(Ti::along(tq, 32 * j, c, lane), kf[c], s);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(td, 32 * j, c, lane), vf[c], dp);
-                    if (band.one) {
+                    const int distance = (int)key - (int)(query0 + 32 * j);             // to the block's first query
+                    if (one) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, band.value);
+                        for (int i = 0; i < 16; ++i) {
+                            const float top = st[32 * j + row_of(i, lane)];
+                            s[i] = plain ? __builtin_fmaf(s[i], a.scale2, by - top) : __builtin_fmaf(s[i], a.scale2, by) - top;
+                        }
                     } else {
-                        const float *by = window[turn].value + (int)(key - at.first) + BQ - 1 - 32 * j;
+                        const float *from = bias.table + (distance - a.table_first);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by[-row_of(i, lane)]);
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = row_of(i, lane);
+                            s[i] = __builtin_fmaf(s[i], a.scale2, a.table_count ? from[-r] : bias.searched(a, distance - r)) - st[32 * j + r];
+                        }
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int r = 32 * j + row_of(i, lane);
-                        s[i] = __builtin_amdgcn_exp2f(s[i] - st[r]) * st[BQ + r];
-                    }
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * st[BQ + 32 * j + row_of(i, lane)];
                     auto allowed = [&](int i) {
                         const uint32_t query = query0 + 32 * j + row_of(i, lane);
                         return live && query < at.length && (!a.causal || query >= key);
                     };
                     if (edge) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = allowed(i) ? s[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) {
+                            s[i] = allowed(i) ? s[i] : 0.f;
+                            dp[i] = allowed(i) ? dp[i] : 0.f;
+                        }
                     }
                     f32x16 pd = s;
                     if constexpr (DROP) {
@@ -404,22 +419,18 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
                         const int c = lane & 31;
                         const char *from = mine + ((c >> 4) * 2 + ((c >> 2) & 1)) * 16 + (((c >> 3) & 1) * 4 + (c & 3)) * 2;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const bool keep = *(const uint16_t *)(from + row_of(i, lane) * NUMBERS) >= a.keep.least;
-                            pd[i] = keep ? s[i] : 0.f;
-                            dp[i] = keep ? dp[i] * a.keep.scale : 0.f;
-                        }
+                        for (int i = 0; i < 16; ++i) pd[i] = *(const uint16_t *)(from + row_of(i, lane) * NUMBERS) >= a.keep.least ? s[i] : 0.f;
                         __builtin_amdgcn_wave_barrier();
                     }
+                    // dS = m P dP - P delta, without the factor 1 / (1 - p), which delta has not either
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] *= dp[i] - st[2 * BQ + 32 * j + row_of(i, lane)];
-                    if (edge) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = allowed(i) ? s[i] : 0.f;
+                    for (int i = 0; i < 16; ++i) {
+                        const float delta = st[2 * BQ + 32 * j + row_of(i, lane)];
+                        s[i] = DROP ? __builtin_fmaf(pd[i], dp[i], -(s[i] * delta)) : s[i] * (dp[i] - delta);
                     }
                     if (summed) {
-                        if (band.one) sums.one(band.bucket, s, lane);
-                        else sums.many(window[turn].bucket + (wave * 32 + BQ - 1 - 32 * j) - 32, s, lane);
+                        if (one) sums.one(bucket, s, lane);
+                        else sums.many(a, bias, (int)k0 - (int)(query0 + 32 * j), s, lane);
                     }
                     fit.fit(s, dk);
 #pragma unroll
@@ -432,14 +443,14 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
                     }
                 }
             }
-            if (next_head != head && summed) {
-                sums.flush(lane);
+            if (next_head != head && a.buckets) {
+                if (summed) sums.flush(lane);
                 __syncthreads();
-                leave(head, true);
+                if (summed) leave(head, true);
+                if (more) bias.bring(a, next_head);
             }
             if (!more) break;
             store(turn ^ 1);
-            band = band_at(next_head, next_query0, turn ^ 1);
             __syncthreads();
             head = next_head;
             query0 = next_query0;
@@ -451,8 +462,45 @@ __global__ void __launch_bounds__(kThreads) k_attn_dkv(Args a, gemm::Launch laun
 #pragma unroll
             for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.f;
     }
-    store_columns<T, D>(rows_of<T>(a.dk, a.dks, a, at, at.head) + (int64_t)key * a.dks.row, row_there, a.dim, dk, a.scale / (fit.by * SHIFT), lane);
-    store_columns<T, D>(rows_of<T>(a.dv, a.dvs, a, at, at.head) + (int64_t)key * a.dvs.row, row_there, a.dim, dv, a.keep.scale / SHIFT, lane);
+    const float by_k = a.scale * a.keep.scale / (fit.by * SHIFT), by_v = a.keep.scale / SHIFT;
+    if (pieces == 1) {
+        store_columns<T, D>(rows_of<T>(a.dk, a.dks, a, at, at.head) + (int64_t)key * a.dks.row, row_there, a.dim, dk, by_k, lane);
+        store_columns<T, D>(rows_of<T>(a.dv, a.dvs, a, at, at.head) + (int64_t)key * a.dvs.row, row_there, a.dim, dv, by_v, lane);
+    } else {
+        const int64_t narrow = (int64_t)a.kv_heads * a.dim;
+        const int64_t from = (((int64_t)piece * a.n + at.worker) * a.t + (int64_t)at.seq * a.len + key) * narrow + (int64_t)at.head * a.dim;
+        store_columns<SAMS_F32, D>(a.dk_parts + from, row_there, a.dim, dk, by_k, lane);
+        store_columns<SAMS_F32, D>(a.dv_parts + from, row_there, a.dim, dv, by_v, lane);
+    }
+}
+
+// dk and dv from the workgroups' parts, which are added up in order
+template <int T>
+__global__ void __launch_bounds__(256) k_attn_join(Args a, uint32_t pieces, uint32_t first)
+{
+    typedef typename TypeOf<T>::type E;
+    const uint32_t narrow = a.kv_heads * a.dim, fours = (narrow + 3) / 4;
+    const uint64_t id = (uint64_t)(first + blockIdx.x) * 256 + threadIdx.x, row = id / fours;
+    if (row >= a.n * (uint64_t)a.t) return;
+    const uint32_t at = (uint32_t)(id - row * fours) * 4;
+    const uint64_t worker = row / (uint64_t)a.t, token = row - worker * (uint64_t)a.t;
+    const int64_t apart = (int64_t)a.n * a.t * narrow;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        const float *p = (which ? a.dv_parts : a.dk_parts) + row * narrow;
+        const Rows r = which ? a.dvs : a.dks;
+        E *to = (E *)(which ? a.dv : a.dk) + worker * r.worker + token * r.row;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t i = 0; i < pieces; ++i) {
+            uint32_t raw[4] = {0, 0, 0, 0};
+            load_piece<SAMS_F32>(p + i * apart, at, narrow, raw);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += __builtin_bit_cast(float, raw[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (at + e < narrow) to[at + e] = (E)v[e];
+    }
 }
 
 // dbias of a worker's head: its parts added up, four threads a bucket, each its quarter of the parts in order
@@ -484,11 +532,35 @@ hipError_t prepare_backward(int type, uint32_t dim)
     return e;
 }
 
-void launch_backward(const Args &all, int type, int64_t parts, float *dbias, int64_t dbias_worker, int accumulate, hipStream_t stream)
+// Workgroups that the keys' kernel is given at least, where cutting its sums into pieces gets it there: four for every CU
+constexpr int64_t kKeyBlocks = 1024;
+constexpr int kMostPieces = 16;
+
+int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim)
+{
+    const int64_t blocks = std::max<int64_t>(1, (int64_t)n * kv_heads * ((t_max + kRows - 1) / kRows));
+    const int64_t pieces = std::min<int64_t>(kMostPieces, (kKeyBlocks + blocks - 1) / blocks);
+    return pieces > 1 ? pieces * n * t_max * kv_heads * dim : 0;
+}
+
+// how a group's heads and a head's queries are cut: heads first, whose pieces need nothing more; a piece of queries has 8 tiles at least
+static void cut(Args &a, int rows, int64_t parts, int64_t sums)
+{
+    const int64_t blocks = (int64_t)a.n * a.seqs * a.kv_heads * a.tiles, each = (int64_t)a.n * a.t * a.kv_heads * a.dim;
+    const int64_t most = std::min<int64_t>({kMostPieces, (kKeyBlocks + blocks - 1) / blocks, sums / each});
+    const uint32_t group = a.heads / a.kv_heads;
+    a.head_pieces = 1;
+    for (uint32_t p = 2; p <= group && p <= most; ++p)
+        if (group % p == 0) a.head_pieces = p;
+    const int64_t some = std::min<int64_t>({most / a.head_pieces, (a.len + rows - 1) / rows / 8, parts / a.tiles});
+    a.query_pieces = (uint32_t)std::max<int64_t>(1, some);
+}
+
+void launch_backward(const Args &all, int type, int64_t parts, int64_t sums, float *dbias, int64_t dbias_worker, int accumulate, hipStream_t stream)
 {
     Args a = all;
     if (!dbias) a.part = nullptr;
-    const float scale = type == SAMS_F16 ? 0x1p-14f : 1.f;          // of the parts: P was held larger
+    const float scale = a.keep.scale * (type == SAMS_F16 ? 0x1p-14f : 1.f);         // what the parts of dbias were made without
     auto join = [&](uint32_t count, bool add) {
         hipLaunchKernelGGL(k_attn_dbias, dim3(a.n * a.heads, (a.buckets + 63) / 64), dim3(256), 0, stream, a.part, parts, count, a.heads, a.buckets, scale, dbias, dbias_worker, add);
     };
@@ -497,25 +569,33 @@ void launch_backward(const Args &all, int type, int64_t parts, float *dbias, int
         return;
     }
     SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-        const int bytes = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + (int)a.buckets * 4;
+        const int bytes = 4 * Tile<T, D>::BYTES + Bias::bytes(a);
         gemm::in_launches((int64_t)a.n * a.seqs * a.heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
             if (a.keep.least) hipLaunchKernelGGL((k_attn_dq<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l);
             else hipLaunchKernelGGL((k_attn_dq<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l);
         });
     }));
+    cut(a, type == SAMS_F32 ? 32 : 64, parts, sums);
+    const uint32_t pieces = a.head_pieces * a.query_pieces, own = a.tiles * a.query_pieces;
     // as many sequences at a time as there is room for their parts of the bias's gradient
-    const uint32_t step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / a.tiles)) : a.seqs;
+    const uint32_t step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / own)) : a.seqs;
     for (uint32_t first = 0; first < all.seqs; first += step) {
         a.seq_first = first;
         a.seq_count = std::min(step, all.seqs - first);
         SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-            const int bytes = 4 * Tile<T, D>::BYTES + 2 * (int)sizeof(Window) + 2 * 3 * Tile<T, D>::ROWS * 4 + (int)a.buckets * 4 * (1 + kWaves);
-            gemm::in_launches((int64_t)a.n * a.seq_count * a.kv_heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+            const int bytes = 4 * Tile<T, D>::BYTES + 2 * 3 * Tile<T, D>::ROWS * 4 + (int)a.buckets * 4 * kWaves + Bias::bytes(a);
+            gemm::in_launches((int64_t)a.n * a.seq_count * a.kv_heads * pieces * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
                 if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true>), grid, dim3(kThreads), bytes + kWaves * 32 * 80, stream, a, l, parts);
                 else hipLaunchKernelGGL((k_attn_dkv<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l, parts);
             });
         }));
-        if (dbias) join(a.seq_count * a.tiles, accumulate || first > 0);
+        if (dbias) join(a.seq_count * own, accumulate || first > 0);
+    }
+    if (pieces > 1) {
+        const int64_t blocks = ((int64_t)a.n * a.t * ((a.kv_heads * a.dim + 3) / 4) + 255) / 256;
+        SAMS_BY_TYPE(type, T, gemm::in_launches(blocks, 256, [&](dim3 grid, gemm::Launch l) {
+                         hipLaunchKernelGGL(k_attn_join<T>, grid, dim3(256), 0, stream, a, pieces, l.first);
+                     }));
     }
 }
 

@@ -29,6 +29,8 @@ __device__ __forceinline__ Seed read_seed(const int64_t *rng)
     return Seed{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)(uint64_t)rng[1]};
 }
 
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
 // Eight 16-bit numbers, two to a word, the first in its lower half: 14 products of 32 x 32 bits, which take a quarter of the rate of
 // other instructions and most of the time; one call serves eight elements.
 __device__ __forceinline__ void philox(const Seed &s, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t (&out)[4])
@@ -37,9 +39,9 @@ __device__ __forceinline__ void philox(const Seed &s, uint32_t c0, uint32_t c1, 
 #pragma unroll
     for (int round = 0; round < 7; ++round) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = xor3((uint32_t)(b >> 32), c1, k0);
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = xor3((uint32_t)(a >> 32), c3, k1);
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -51,6 +53,17 @@ __device__ __forceinline__ void philox(const Seed &s, uint32_t c0, uint32_t c1, 
 __device__ __forceinline__ bool kept(const uint32_t (&numbers)[4], int e, uint32_t least)
 {
     return ((e & 1) ? numbers[e >> 1] >> 16 : numbers[e >> 1] & 0xffffu) >= least;
+}
+
+// Two 16-bit words, of which those are zero whose numbers are below least; less: least - 1 twice (least > 0).  The difference, which stops
+// at 0, taken to 0 or 1, times the word: three instructions for two words, where comparing and selecting each takes four and what parts
+// and joins them.  (Written out: the compiler would turn it into the latter.)
+__device__ __forceinline__ uint32_t keep_words(uint32_t words, uint32_t numbers, uint32_t less)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    uint32_t one;
+    asm("v_pk_sub_u16 %0, %1, %2 clamp\n\tv_pk_min_u16 %0, %0, 1 op_sel_hi:[1,0]" : "=v"(one) : "v"(numbers), "s"(less));
+    return __builtin_bit_cast(uint32_t, (u16x2)(__builtin_bit_cast(u16x2, words) * __builtin_bit_cast(u16x2, one)));
 }
 
 }  // namespace sams
