@@ -492,7 +492,7 @@ int dropout_backward(sams_dropout *ctx, int64_t t, const void *dy, int64_t dy_wo
  *   starts_host  HOST pointer to `buckets` ascending numbers, copied; NULL with buckets == 0
  * 16-bit tensors are multiplied as they are, with P and its gradient rounded to their type between the products (f16: scaled by powers of two,
  * so that small ones keep their digits); 32-bit ones in 32 bits.  Sums and the softmax are held in 32 bits.
- * Ranges: 1 <= heads <= SAMS_MAX_HEADS, kv_heads divides heads, 1 <= dim <= SAMS_MAX_HEAD_DIM, 0 <= buckets <= SAMS_MAX_BUCKETS, n * t_max <=
+ * Ranges: 1 <= heads <= SAMS_MAX_HEADS, kv_heads divides heads, 8 <= dim <= SAMS_MAX_HEAD_DIM, 0 <= buckets <= SAMS_MAX_BUCKETS, n * t_max <=
  * SAMS_MAX_TOKENS, seqs divides t, n * heads * seqs * (t / seqs / 128, rounded up) < 2^31.
  * Scratch with train != 0: 4 * n * heads * (t_max + buckets * (t_max / 64 + 64)) bytes; a backward pass needs it (SAMS_EINVAL otherwise).
  */

@@ -72,47 +72,116 @@ __device__ __forceinline__ typename Fragment<T>::type words_of(const f32x16 &v, 
     return f;
 }
 
-// ---- tiles in LDS: rows of D numbers, and some bytes that put the rows on different banks ----
+// ---- tiles in LDS ----
+// Rows of D numbers in pieces of 16 bytes, as many as a power of two; piece c of row r lies at c ^ turn(r).  So the pieces that sixteen lanes
+// read at a time lie on different banks, whether they are one piece of sixteen rows, or four of each of four rows.  The turn of a row is that of
+// its bits one by one: a lane's part of an address is made once, and what the instruction adds to it comes by exclusive or.
+template <int PIECES>
+__host__ __device__ constexpr uint32_t turn(uint32_t r)
+{
+    return PIECES == 4 ? (r >> 2) & 3 : PIECES == 8 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3);
+}
+constexpr int power_of_two(int n) { return n <= 4 ? 4 : 2 * power_of_two((n + 1) / 2); }
+
+typedef __attribute__((address_space(3))) char *lds_at;
+__device__ __forceinline__ lds_at lds(uint32_t at) { return (lds_at)(uintptr_t)at; }
+__device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_at)p; }
+
 template <int T, int D> struct Tile {
     typedef typename TypeOf<T>::type E;
     typedef typename Fragment<T>::type Frag;
+    static constexpr int SIZE = sizeof(E);
     static constexpr int ROWS = T == SAMS_F32 ? 32 : 64;                        // that a workgroup takes at a time
-    static constexpr int LD = D * (int)sizeof(E) + (T != SAMS_F32 && D == 128 ? 80 : 16);     // bytes from row to row
-    static constexpr int BYTES = ROWS * LD;
-    static constexpr int PIECES = D * (int)sizeof(E) / 16, N = ROWS * PIECES / kThreads;      // of 16 bytes: a row's, a thread's
+    static constexpr int PIECES = D * SIZE / 16, ROOM = power_of_two(PIECES);   // a row's, and what it has room for
+    static constexpr int LD = ROOM * 16, BYTES = ROWS * LD;
+    static constexpr int N = ROWS * PIECES / kThreads;                          // pieces that a thread brings
     static_assert(ROWS * PIECES % kThreads == 0, "every thread brings as many");
 
-    // numbers 16 s + 8 (lane / 32) .. + 7 of row row0 + lane % 32
-    __device__ __forceinline__ static Frag along(const char *tile, int row0, int s, int lane)
+    // numbers 16 s + 8 (lane / 32) .. + 7 of row row0 + lane % 32; from: along_lane of the tile
+    __device__ __forceinline__ static uint32_t along_lane(uint32_t tile, int lane)
     {
-        const char *at = tile + (row0 + (lane & 31)) * LD + (16 * s + 8 * (lane >> 5)) * (int)sizeof(E);
+        const uint32_t r = lane & 31, c = (lane >> 5) * (SIZE / 2);
+        return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4);
+    }
+    __device__ __forceinline__ static Frag along(uint32_t from, int row0, int s)
+    {
+        const uint32_t at = (from ^ (s * 16 * SIZE)) + row0 * LD;
         if constexpr (T == SAMS_F32) {
             typedef float f4 __attribute__((ext_vector_type(4)));
-            const f4 a = *(const f4 *)at, b = *(const f4 *)(at + 16);
+            typedef __attribute__((address_space(3))) const f4 *f4_at;
+            const f4 a = *(f4_at)lds(at), b = *(f4_at)lds((from ^ (s * 64 + 16)) + row0 * LD);
             return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         } else {
-            return *(const u32x4 *)at;
+            return *(__attribute__((address_space(3))) const u32x4 *)lds(at);
         }
     }
     // column col0 + lane % 32 of the rows row0 + 4 (lane / 32) + {0 .. 3, 8 .. 11}.  16-bit words through the transposing load: of every
     // 16 lanes four give the address of one row's 16 columns, and each gets one column's four rows.
-    __device__ __forceinline__ static Frag across(const char *tile, int row0, int col0, int lane)
+    __device__ __forceinline__ static uint32_t across_lane(uint32_t tile, int lane)
+    {
+        if constexpr (T == SAMS_F32) {
+            const uint32_t r = 4 * (lane >> 5), c = (lane & 31) >> 2;
+            return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (lane & 3) * 4;
+        } else {
+            const uint32_t g = lane >> 4, q = lane & 15, r = 4 * (g >> 1) + (q >> 2), c = (g & 1) * 2 + ((q & 3) >> 1);
+            return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (q & 1) * 8;
+        }
+    }
+    __device__ __forceinline__ static Frag across(uint32_t from, int row0, int col0)
     {
         if constexpr (T == SAMS_F32) {
             Frag f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = *(const float *)(tile + (row0 + 4 * (lane >> 5) + (i & 3) + 8 * (i >> 2)) * LD + (col0 + (lane & 31)) * 4);
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t r = (i & 3) + 8 * (i >> 2);
+                f[i] = *(__attribute__((address_space(3))) const float *)lds((from ^ ((turn<ROOM>(r) << 4) ^ (col0 * 4))) + (row0 + r) * LD);
+            }
             return f;
         } else {
-            const int g = lane >> 4, q = lane & 15;
-            const char *at = tile + (row0 + 4 * (g >> 1) + (q >> 2)) * LD + (col0 + (g & 1) * 16 + (q & 3) * 4) * 2;
-            typedef __attribute__((address_space(3))) gemm::short4v *lds_ptr;
-            const gemm::words2 a = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at)));
-            const gemm::words2 b = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * LD)));
+            typedef __attribute__((address_space(3))) gemm::short4v *words_at;
+            const uint32_t at = from ^ (col0 * 2), further = from ^ ((turn<ROOM>(8) << 4) ^ (col0 * 2));
+            const gemm::words2 a = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)lds(at + row0 * LD)));
+            const gemm::words2 b = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)lds(further + (row0 + 8) * LD)));
             return Frag{a[0], a[1], b[0], b[1]};
         }
     }
 };
+
+// ---- rows in memory ----
+// A piece of 16 bytes of a row of dim numbers is read where all of it exists: one that reaches past the row's end, or starts there, in its place
+// the row's last 16 bytes, of which `ended` makes what was meant.  (dim >= 8; rows start anywhere.)
+template <int T> __device__ __forceinline__ uint32_t piece_start(uint32_t at, uint32_t dim) { return at + kPiece<T> <= dim ? at : dim - kPiece<T>; }
+
+template <int T>
+__device__ __forceinline__ void read_piece(const char *p, uint32_t (&raw)[4])
+{
+    const piece_t v = *(const piece_t *)p;
+    raw[0] = v[0]; raw[1] = v[1]; raw[2] = v[2]; raw[3] = v[3];
+}
+template <int T>
+__device__ __forceinline__ void ended(uint32_t (&raw)[4], bool there, uint32_t at, uint32_t dim)
+{
+    constexpr uint32_t N = kPiece<T>;
+    if (const uint32_t rest = dim % N) {                            // the same for all threads
+        uint64_t lo = raw[0] | (uint64_t)raw[1] << 32, hi = raw[2] | (uint64_t)raw[3] << 32;
+        const uint32_t bits = (N - rest) * (128 / N);               // that lie before the piece
+        if (bits < 64) {
+            lo = lo >> bits | hi << (64 - bits);
+            hi >>= bits;
+        } else {
+            lo = hi >> (bits - 64);
+            hi = 0;
+        }
+        const bool part = at + N > dim;
+        raw[0] = part ? (uint32_t)lo : raw[0];
+        raw[1] = part ? (uint32_t)(lo >> 32) : raw[1];
+        raw[2] = part ? (uint32_t)hi : raw[2];
+        raw[3] = part ? (uint32_t)(hi >> 32) : raw[3];
+    }
+    there = there && at < dim;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) raw[e] = there ? raw[e] : 0;
+}
 
 // A tile on its way to LDS: rows from `first` on, those from `limit` on and columns from dim on as zeros.
 template <int T, int D>
@@ -121,54 +190,56 @@ struct Bring {
     typedef typename TypeOf<T>::type E;
     uint32_t raw[Ti::N][4];
 
+    __device__ __forceinline__ static uint32_t row_of(int i) { return (i * kThreads + threadIdx.x) / Ti::PIECES; }
+    __device__ __forceinline__ static uint32_t column_of(int i) { return (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>; }
+
+    // limit > first
     __device__ __forceinline__ void load(const E *p, int64_t row, uint32_t first, uint32_t limit, uint32_t dim)
     {
-        p += (int64_t)first * row;
-        if (first + Ti::ROWS <= limit && dim == D) {
-#pragma unroll
-            for (int i = 0; i < Ti::N; ++i) {
-                const uint32_t r = (i * kThreads + threadIdx.x) / Ti::PIECES, at = (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>;
-                const piece_t v = *(const piece_t *)(p + r * row + at);
-                raw[i][0] = v[0]; raw[i][1] = v[1]; raw[i][2] = v[2]; raw[i][3] = v[3];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < Ti::N; ++i) {
-                const uint32_t r = (i * kThreads + threadIdx.x) / Ti::PIECES, at = (i * kThreads + threadIdx.x) % Ti::PIECES * kPiece<T>;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) raw[i][e] = 0;
-                if (first + r < limit && at < dim) load_piece<T>(p + r * row, at, dim, raw[i]);
-            }
-        }
-    }
-    __device__ __forceinline__ void store(char *tile) const
-    {
+        const char *base = (const char *)(p + (int64_t)first * row);
+        const int64_t bytes = row * Ti::SIZE;
+        const uint32_t last = limit - first - 1;
 #pragma unroll
         for (int i = 0; i < Ti::N; ++i) {
-            const int r = (i * kThreads + threadIdx.x) / Ti::PIECES, c = (i * kThreads + threadIdx.x) % Ti::PIECES;
-            *(u32x4 *)(tile + r * Ti::LD + c * 16) = u32x4{raw[i][0], raw[i][1], raw[i][2], raw[i][3]};
+            const uint32_t r = row_of(i) < last ? row_of(i) : last;
+            read_piece<T>(base + r * bytes + piece_start<T>(column_of(i), dim) * Ti::SIZE, raw[i]);
+        }
+    }
+    // first, limit, dim: as they were loaded
+    __device__ __forceinline__ void store(char *tile, uint32_t first, uint32_t limit, uint32_t dim)
+    {
+        if (first + Ti::ROWS > limit || dim != D) {
+#pragma unroll
+            for (int i = 0; i < Ti::N; ++i) ended<T>(raw[i], first + row_of(i) < limit, column_of(i), dim);
+        }
+#pragma unroll
+        for (int i = 0; i < Ti::N; ++i) {
+            const uint32_t r = row_of(i), c = (i * kThreads + threadIdx.x) % Ti::PIECES;
+            *(u32x4 *)(tile + r * Ti::LD + ((c ^ turn<Ti::ROOM>(r)) << 4)) = u32x4{raw[i][0], raw[i][1], raw[i][2], raw[i][3]};
         }
     }
 };
 
-// a lane's fragments of a row that stays in registers: all zeros where it does not exist
+// A lane's fragments of row `row` of those from p on, which stay in registers: all zeros from row `limit` on (limit > 0).
 template <int T, int D>
-__device__ __forceinline__ void row_fragments(const typename TypeOf<T>::type *p, bool there, uint32_t dim, int lane, typename Fragment<T>::type (&f)[D / 16])
+__device__ __forceinline__ void row_fragments(const typename TypeOf<T>::type *p, int64_t stride, uint32_t row, uint32_t limit, uint32_t dim, int lane,
+                                              typename Fragment<T>::type (&f)[D / 16])
 {
+    p += (int64_t)(row < limit ? row : limit - 1) * stride;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-        const uint32_t at = 16 * s + 8 * (lane >> 5);
+    for (int s = 0; s < D / 16; ++s)
 #pragma unroll
         for (int h = 0; h < 8; h += kPiece<T>) {
-            uint32_t raw[4] = {0, 0, 0, 0};
-            if (there && at + h < dim) load_piece<T>(p, at + h, dim, raw);
+            const uint32_t at = 16 * s + 8 * (lane >> 5) + h;
+            uint32_t raw[4];
+            read_piece<T>((const char *)(p + piece_start<T>(at, dim)), raw);
+            ended<T>(raw, row < limit, at, dim);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if constexpr (T == SAMS_F32) f[s][h + e] = __builtin_bit_cast(float, raw[e]);
                 else f[s][e] = raw[e];
             }
         }
-    }
 }
 
 // what both halves of the wavefront have for a column, added up, and the larger of both
@@ -206,10 +277,9 @@ __device__ __forceinline__ void store_columns(typename TypeOf<T>::type *row, boo
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = acc[d][4 * a + i] * scale;
-            if (at + 4 <= dim) {
-                const auto w = gemm::pack_numbers<E>(v);
+            if (dim % 4 == 0) {                                     // the same for all threads
                 typedef uint32_t anywhere __attribute__((ext_vector_type(sizeof(E)), aligned(2)));
-                *(anywhere *)(row + at) = __builtin_bit_cast(anywhere, w);
+                if (at < dim) *(anywhere *)(row + at) = __builtin_bit_cast(anywhere, gemm::pack_numbers<E>(v));
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -222,7 +292,8 @@ __device__ __forceinline__ void store_columns(typename TypeOf<T>::type *row, boo
 // Bucket b is the distances (key minus query) from starts[b] on to starts[b + 1] - 1; what lies before starts[1] is bucket 0.  A wavefront's
 // tile whose distances all lie before starts[1], or all from the last start on, adds one number.  For others the workgroup has the biases
 // of the distances in between by distance in LDS, and kReach more on both sides, so that such a tile's all are there; where
-// these are too many ("wide"), a tile is looked at for a start within its distances, and where there is one, each number is searched for.
+// these are too many ("wide"), a tile is looked at for a start within its distances, and where there is one, the wavefront makes a table
+// of its own for it.
 constexpr int kReach = 96, kMaxTable = 4096;
 
 __device__ __forceinline__ float bias_of(float v)
@@ -233,7 +304,7 @@ __device__ __forceinline__ float bias_of(float v)
 
 struct Bias {
     const int *starts;      // [buckets] in LDS
-    float *table;           // [table_count] in LDS
+    float *table;           // in LDS: [table_count], or, where that is 0, [kWaves][kReach] of the wavefronts' present tiles
     const float *row;       // [buckets], the head's
     float before, behind;   // the first and the last bucket's
 
@@ -243,7 +314,7 @@ struct Bias {
         starts = (const int *)lds;
         table = (float *)(lds + a.buckets * 4);
     }
-    static int bytes(const Args &a) { return (int)(a.buckets + a.table_count) * 4; }
+    static int bytes(const Args &a) { return (int)(a.buckets + (a.table_count ? a.table_count : kWaves * kReach)) * 4; }
     // the workgroup's starts, before a barrier
     __device__ __forceinline__ void bring_starts(const Args &a) const
     {
@@ -270,8 +341,6 @@ struct Bias {
         }
         return lo;
     }
-    __device__ __forceinline__ float searched(const Args &a, int distance) const { return bias_of(row[bucket(a, distance)]); }
-
     // whether the distances from lo to hi (kReach apart at most) share a bucket, which one, and its bias
     __device__ __forceinline__ bool one(const Args &a, int lo, int hi, uint32_t &bucket, float &value) const
     {
@@ -294,6 +363,19 @@ struct Bias {
         value = bias_of(row[below]);
         return below == above;
     }
+    // where the bias of `distance`, one of those from lo to lo + kReach - 1, lies, and of those around it
+    __device__ __forceinline__ const float *at(const Args &a, int wave, int lo, int distance) const
+    {
+        if (a.table_count) return table + (distance - a.table_first);
+        float *mine = table + wave * kReach;
+        const int lane = threadIdx.x & 63;
+        __builtin_amdgcn_wave_barrier();
+        for (int i = lane; i < kReach; i += 64) mine[i] = bias_of(row[bucket(a, lo + i)]);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        return mine + (distance - lo);
+    }
 };
 
 // 4 (i / 4) + ... : row i of a lane in an accumulator
@@ -303,6 +385,9 @@ __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirs
 
 // wavefronts that a SIMD holds: what is more takes accumulators through moves
 template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= 96 ? 2 : 1;
+#ifndef FWD_WAVES
+#define FWD_WAVES (T == SAMS_F32 ? kWavesPerSimd<T, D> : 2)
+#endif
 
 template <int T, int D>
 __device__ __forceinline__ void flip(typename Fragment<T>::type (&f)[D / 16])
@@ -314,22 +399,19 @@ __device__ __forceinline__ void flip(typename Fragment<T>::type (&f)[D / 16])
     }
 }
 
-// s = times s + bias of every pair, of a lane's query and the keys of its accumulators; distance: the first key's less the query
-template <int T, int NB>
-__device__ __forceinline__ void add_bias(const Args &a, const Bias &bias, bool one, float by, int distance, float times, int lane, f32x16 (&s)[NB])
+// s = times s + bias of every pair, of a lane's query and the keys of its accumulators; from: where the bias of the first key lies, where
+// they differ
+template <int NB>
+__device__ __forceinline__ void add_bias(const float *from, bool one, float by, float times, int lane, f32x16 (&s)[NB])
 {
-    const float *from = bias.table + (distance - a.table_first);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         if (one) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by);
-        } else if (a.table_count) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, from[32 * j + row_of(i, lane)]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, bias.searched(a, distance + 32 * j + row_of(i, lane)));
+            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, from[32 * j + row_of(i, lane)]);
         }
     }
 }

@@ -14,7 +14,7 @@ namespace attn {
 // S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
 // Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.
 template <int T, int D, bool DROP>
-__global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forward(Args a, gemm::Launch launch)
+__global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
@@ -51,15 +51,16 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forwar
         bk.load(k, a.ks.row, 0, at.length, a.dim);
         bv.load(v, a.vs.row, 0, at.length, a.dim);
         typename Ti::Frag qf[D / 16];
-        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
+        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head), a.qs.row, query, at.length, a.dim, lane, qf);
         // the scale's sign goes into q, so that the largest product is the largest logit
         const float scale = fabsf(a.scale2);
         if (a.scale2 < 0.f) flip<T, D>(qf);
         bias.bring_starts(a);
         __syncthreads();
         bias.bring(a, at.head);
-        bk.store(tile_k);
-        bv.store(tile_v);
+        bk.store(tile_k, 0, at.length, a.dim);
+        bv.store(tile_v, 0, at.length, a.dim);
+        const uint32_t lane_k = Ti::along_lane(lds_address(tile_k), lane), lane_v = Ti::across_lane(lds_address(tile_v), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -73,14 +74,14 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forwar
             float by;
             const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
             if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
-                const char *tk = tile_k + turn * Ti::BYTES, *tv = tile_v + turn * Ti::BYTES;
+                const uint32_t tk = lane_k + turn * Ti::BYTES, tv = lane_v + turn * Ti::BYTES;
                 f32x16 s[NB];
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s[j] = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s[j]);
+                    for (int c = 0; c < D / 16; ++c) s[j] = product<T>(Ti::along(tk, 32 * j, c), qf[c], s[j]);
                 }
                 // logits are times * s + by.  Within a tile of one bucket without a border nothing is done to s for that: the largest one is
                 // found, and the exponents are made, from it.  (A large bias, as a mask has, is added first, so that it swallows the rest as it
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forwar
                 float times = scale;
                 const bool edge = key0 + BN > at.length || (a.causal && key0 + BN - 1 > q0);
                 if (edge || !one || !(fabsf(by) < 1e6f)) {
-                    add_bias<T, NB>(a, bias, one, by, lo + 31 - (lane & 31), scale, lane, s);
+                    add_bias<NB>(one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31)), one, by, scale, lane, s);
                     times = 1.f;
                     by = 0.f;
                     if (edge) {
@@ -143,12 +144,12 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_forwar
                             w = words_of<T>(s[j], half);
                         }
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tv, 32 * j + 16 * half, 32 * d, lane), w, acc[d]);
+                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tv, 32 * j + 16 * half, 32 * d), w, acc[d]);
                     }
             }
             if (more) {
-                bk.store(tile_k + (turn ^ 1) * Ti::BYTES);
-                bv.store(tile_v + (turn ^ 1) * Ti::BYTES);
+                bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
+                bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
             __syncthreads();
         }
@@ -252,7 +253,7 @@ int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, i
 {
     if (!out) return SAMS_EINVAL;
     *out = nullptr;
-    if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || heads < 1 || heads > SAMS_MAX_HEADS || kv_heads < 1 || heads % kv_heads || dim < 1 ||
+    if (n < 1 || n > kMaxWorkers || t_max < 0 || t_max > SAMS_MAX_TOKENS / n || heads < 1 || heads > SAMS_MAX_HEADS || kv_heads < 1 || heads % kv_heads || dim < 8 ||
         dim > SAMS_MAX_HEAD_DIM || buckets < 0 || buckets > SAMS_MAX_BUCKETS || (buckets > 0 && !starts_host) || !type_ok(type)) return SAMS_EINVAL;
     for (int b = 1; b < buckets; ++b)
         if (starts_host[b] <= starts_host[b - 1]) return SAMS_EINVAL;

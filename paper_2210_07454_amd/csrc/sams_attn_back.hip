@@ -9,6 +9,12 @@
 // atomics; seven products of a pair where one kernel would take five.
 #include "sams_attn.h"
 
+#ifndef KEY_BLOCKS
+#define KEY_BLOCKS 512
+#endif
+#ifndef BLOCKS_AT_ONCE
+#define BLOCKS_AT_ONCE 1
+#endif
 namespace sams {
 namespace attn {
 
@@ -133,22 +139,20 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         bk.load(k, a.ks.row, 0, at.length, a.dim);
         bv.load(v, a.vs.row, 0, at.length, a.dim);
         typename Ti::Frag qf[D / 16], df[D / 16];
-        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head) + (int64_t)query * a.qs.row, live, a.dim, lane, qf);
-        row_fragments<T, D>(rows_of<T>(a.dout, a.douts, a, at, at.head) + (int64_t)query * a.douts.row, live, a.dim, lane, df);
+        row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head), a.qs.row, query, at.length, a.dim, lane, qf);
+        row_fragments<T, D>(rows_of<T>(a.dout, a.douts, a, at, at.head), a.douts.row, query, at.length, a.dim, lane, df);
         // do . o, less the factor 1 / (1 - p) that dP is made without
         float d = 0.f, exact = 0.f;
         {
-            const E *o = rows_of<T>(a.o, a.os, a, at, at.head) + (int64_t)query * a.os.row;
+            typename Ti::Frag of[D / 16];
+            row_fragments<T, D>(rows_of<T>(a.o, a.os, a, at, at.head), a.os.row, query, at.length, a.dim, lane, of);
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                float x[8];
+                E x[8], y[8];
+                __builtin_memcpy(x, &of[s], sizeof(x));
+                __builtin_memcpy(y, &df[s], sizeof(y));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = 0.f;
-                if (live) load8<T>(o, 16 * s + 8 * (lane >> 5), a.dim, x);
-                E e[8];
-                __builtin_memcpy(e, &df[s], sizeof(e));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d = __builtin_fmaf(x[i], (float)e[i], d);
+                for (int i = 0; i < 8; ++i) d = __builtin_fmaf((float)x[i], (float)y[i], d);
             }
             d = sum_halves(d) / a.keep.scale;
         }
@@ -160,8 +164,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         bias.bring_starts(a);
         __syncthreads();
         bias.bring(a, at.head);
-        bk.store(tile_k);
-        bv.store(tile_v);
+        bk.store(tile_k, 0, at.length, a.dim);
+        bv.store(tile_v, 0, at.length, a.dim);
+        const uint32_t lane_k = Ti::along_lane(lds_address(tile_k), lane), lane_v = Ti::along_lane(lds_address(tile_v), lane), lane_kt = Ti::across_lane(lds_address(tile_k), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -175,22 +180,23 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             float by;
             const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
             if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
-                const char *tk = tile_k + turn * Ti::BYTES, *tv = tile_v + turn * Ti::BYTES;
+                const uint32_t tk = lane_k + turn * Ti::BYTES, tv = lane_v + turn * Ti::BYTES, tkt = lane_kt + turn * Ti::BYTES;
                 const bool edge = key0 + BN > at.length || q0 + 32 > at.length || (a.causal && key0 + BN - 1 > q0);
                 const bool plain = one && fabsf(by) < 1e6f;         // as in the forward pass
+                const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
                 const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)key0;
-#pragma unroll
+#pragma unroll BLOCKS_AT_ONCE
                 for (int j = 0; j < NB; ++j) {
                     f32x16 s[1], dp;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[0][i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(Ti::along(tk, 32 * j, c, lane), qf[c], s[0]);
+                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(Ti::along(tk, 32 * j, c), qf[c], s[0]);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(tv, 32 * j, c, lane), df[c], dp);
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(tv, 32 * j, c), df[c], dp);
                     float times = a.scale2, from = by - top + SHIFT;
                     if (!plain) {
-                        add_bias<T, 1>(a, bias, one, by, lo + 31 - (lane & 31) + 32 * j, a.scale2, lane, s);
+                        add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
                         times = 1.f;
                         from = SHIFT - top;
                     }
@@ -233,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                         const typename Ti::Frag w = words_of<T>(s[0], half);
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) {
-                            const typename Ti::Frag columns = Ti::across(tk, 32 * j + 16 * half, 32 * d, lane);
+                            const typename Ti::Frag columns = Ti::across(tkt, 32 * j + 16 * half, 32 * d);
                             acc[d] = product<T>(columns, w, acc[d]);
                             if constexpr (ROUNDED) pk[d] = product<T>(columns, wp[half], pk[d]);
                         }
@@ -241,8 +247,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                 }
             }
             if (more) {
-                bk.store(tile_k + (turn ^ 1) * Ti::BYTES);
-                bv.store(tile_v + (turn ^ 1) * Ti::BYTES);
+                bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
+                bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
             __syncthreads();
         }
@@ -333,9 +339,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 stat[2] = there ? a.delta[from] : 0.f;
             }
         };
-        auto store = [&](int turn) {
-            bq.store(tile_q + turn * Ti::BYTES);
-            bd.store(tile_d + turn * Ti::BYTES);
+        auto store = [&](uint32_t query0, int turn) {
+            bq.store(tile_q + turn * Ti::BYTES, query0, at.length, a.dim);
+            bd.store(tile_d + turn * Ti::BYTES, query0, at.length, a.dim);
             if (threadIdx.x < BQ)
 #pragma unroll
                 for (int i = 0; i < 3; ++i) stats[(turn * 3 + i) * BQ + threadIdx.x] = stat[i];
@@ -344,11 +350,13 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         const uint32_t last = head + group - 1;
         load(head, query0);
         typename Ti::Frag kf[D / 16], vf[D / 16];
-        row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head) + (int64_t)key * a.ks.row, live, a.dim, lane, kf);
-        row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head) + (int64_t)key * a.vs.row, live, a.dim, lane, vf);
+        row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head), a.ks.row, key, at.length, a.dim, lane, kf);
+        row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head), a.vs.row, key, at.length, a.dim, lane, vf);
         __syncthreads();
         bias.bring(a, head);
-        store(0);
+        store(query0, 0);
+        const uint32_t lane_q = Ti::along_lane(lds_address(tile_q), lane), lane_d = Ti::along_lane(lds_address(tile_d), lane);
+        const uint32_t lane_qt = Ti::across_lane(lds_address(tile_q), lane), lane_dt = Ti::across_lane(lds_address(tile_d), lane);
         __syncthreads();
         for (int turn = 0;; turn ^= 1) {
             uint32_t next_head = head, next_query0 = query0 + BQ;
@@ -360,21 +368,21 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             float by;
             const bool one = bias.one(a, lo, lo + BQ - 1 + 31, bucket, by);
             if (k0 < at.length && (!a.causal || query0 + BQ - 1 >= k0) && !(one && by == -__builtin_inff())) {
-                const char *tq = tile_q + turn * Ti::BYTES, *td = tile_d + turn * Ti::BYTES;
+                const uint32_t tq = lane_q + turn * Ti::BYTES, td = lane_d + turn * Ti::BYTES, tqt = lane_qt + turn * Ti::BYTES, tdt = lane_dt + turn * Ti::BYTES;
                 const float *st = stats + turn * 3 * BQ;
                 const bool edge = query0 + BQ > at.length || k0 + 32 > at.length || (a.causal && query0 < k0 + 31);
                 const bool plain = one && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
-#pragma unroll
+                const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)query0);        // of the first query
+#pragma unroll BLOCKS_AT_ONCE
                 for (int j = 0; j < NB; ++j) {
                     f32x16 s, dp;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s = product<T>(Ti::along(tq, 32 * j, c, lane), kf[c], s);
+                    for (int c = 0; c < D / 16; ++c) s = product<T>(Ti::along(tq, 32 * j, c), kf[c], s);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(td, 32 * j, c, lane), vf[c], dp);
-                    const int distance = (int)key - (int)(query0 + 32 * j);             // to the block's first query
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(td, 32 * j, c), vf[c], dp);
                     if (one) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -382,11 +390,10 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                             s[i] = plain ? __builtin_fmaf(s[i], a.scale2, by - top) : __builtin_fmaf(s[i], a.scale2, by) - top;
                         }
                     } else {
-                        const float *from = bias.table + (distance - a.table_first);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int r = row_of(i, lane);
-                            s[i] = __builtin_fmaf(s[i], a.scale2, a.table_count ? from[-r] : bias.searched(a, distance - r)) - st[32 * j + r];
+                            const int r = 32 * j + row_of(i, lane);
+                            s[i] = __builtin_fmaf(s[i], a.scale2, biases[-r]) - st[r];
                         }
                     }
 #pragma unroll
@@ -437,9 +444,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     for (int half = 0; half < 2; ++half) {
                         const typename Ti::Frag wp = words_of<T>(pd, half), ws = words_of<T>(s, half);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(Ti::across(td, 32 * j + 16 * half, 32 * d, lane), wp, dv[d]);
+                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(Ti::across(tdt, 32 * j + 16 * half, 32 * d), wp, dv[d]);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(Ti::across(tq, 32 * j + 16 * half, 32 * d, lane), ws, dk[d]);
+                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(Ti::across(tqt, 32 * j + 16 * half, 32 * d), ws, dk[d]);
                     }
                 }
             }
@@ -450,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 if (more) bias.bring(a, next_head);
             }
             if (!more) break;
-            store(turn ^ 1);
+            store(next_query0, turn ^ 1);
             __syncthreads();
             head = next_head;
             query0 = next_query0;
@@ -533,7 +540,7 @@ hipError_t prepare_backward(int type, uint32_t dim)
 }
 
 // Workgroups that the keys' kernel is given at least, where cutting its sums into pieces gets it there: four for every CU
-constexpr int64_t kKeyBlocks = 1024;
+constexpr int64_t kKeyBlocks = KEY_BLOCKS;
 constexpr int kMostPieces = 16;
 
 int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim)

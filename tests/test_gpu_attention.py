@@ -57,7 +57,7 @@ def compare(run, x, starts, heads, kv_heads, **how):
 
 
 # n, seqs, len, heads, kv_heads, dim, buckets, causal, p
-SHAPES = [(1, 1, 1, 1, 1, 1, 1, True, 0.0), (1, 1, 1, 2, 1, 64, 32, True, 0.5), (2, 1, 5, 4, 4, 64, 32, True, 0.1), (1, 3, 31, 2, 2, 32, 8, False, 0.0),
+SHAPES = [(1, 1, 1, 1, 1, 8, 1, True, 0.0), (1, 1, 1, 2, 1, 64, 32, True, 0.5), (2, 1, 5, 4, 4, 64, 32, True, 0.1), (1, 3, 31, 2, 2, 32, 8, False, 0.0),
           (2, 2, 33, 2, 1, 40, 9, True, 0.3), (1, 1, 64, 1, 1, 64, 0, False, 0.0), (1, 1, 65, 3, 3, 16, 5, False, 0.1), (1, 2, 127, 2, 2, 72, 32, True, 0.0),
           (1, 1, 128, 2, 1, 96, 17, False, 0.2), (1, 1, 129, 4, 2, 128, 32, True, 0.1), (3, 1, 200, 1, 1, 17, 64, False, 0.0), (1, 1, 333, 6, 2, 80, 33, True, 0.2),
           (1, 1, 515, 2, 2, 64, 32, True, 0.0), (1, 1, 700, 1, 1, 128, 12, False, 0.05), (1, 1, 260, 2, 2, 33, 300, False, 0.0)]
