@@ -84,7 +84,7 @@ __host__ __device__ constexpr uint32_t turn(uint32_t r)
 constexpr int power_of_two(int n) { return n <= 4 ? 4 : 2 * power_of_two((n + 1) / 2); }
 
 typedef __attribute__((address_space(3))) char *lds_at;
-__device__ __forceinline__ lds_at lds(uint32_t at) { return (lds_at)(uintptr_t)at; }
+__device__ __forceinline__ lds_at in_lds(uint32_t at) { return (lds_at)(uintptr_t)at; }
 __device__ __forceinline__ uint32_t lds_address(const void *p) { return (uint32_t)(uintptr_t)(lds_at)p; }
 
 template <int T, int D> struct Tile {
@@ -97,54 +97,74 @@ template <int T, int D> struct Tile {
     static constexpr int N = ROWS * PIECES / kThreads;                          // pieces that a thread brings
     static_assert(ROWS * PIECES % kThreads == 0, "every thread brings as many");
 
-    // numbers 16 s + 8 (lane / 32) .. + 7 of row row0 + lane % 32; from: along_lane of the tile
-    __device__ __forceinline__ static uint32_t along_lane(uint32_t tile, int lane)
-    {
-        const uint32_t r = lane & 31, c = (lane >> 5) * (SIZE / 2);
-        return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4);
-    }
-    __device__ __forceinline__ static Frag along(uint32_t from, int row0, int s)
-    {
-        const uint32_t at = (from ^ (s * 16 * SIZE)) + row0 * LD;
-        if constexpr (T == SAMS_F32) {
-            typedef float f4 __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) const f4 *f4_at;
-            const f4 a = *(f4_at)lds(at), b = *(f4_at)lds((from ^ (s * 64 + 16)) + row0 * LD);
-            return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        } else {
-            return *(__attribute__((address_space(3))) const u32x4 *)lds(at);
-        }
-    }
-    // column col0 + lane % 32 of the rows row0 + 4 (lane / 32) + {0 .. 3, 8 .. 11}.  16-bit words through the transposing load: of every
-    // 16 lanes four give the address of one row's 16 columns, and each gets one column's four rows.
-    __device__ __forceinline__ static uint32_t across_lane(uint32_t tile, int lane)
-    {
-        if constexpr (T == SAMS_F32) {
-            const uint32_t r = 4 * (lane >> 5), c = (lane & 31) >> 2;
-            return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (lane & 3) * 4;
-        } else {
-            const uint32_t g = lane >> 4, q = lane & 15, r = 4 * (g >> 1) + (q >> 2), c = (g & 1) * 2 + ((q & 3) >> 1);
-            return tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (q & 1) * 8;
-        }
-    }
-    __device__ __forceinline__ static Frag across(uint32_t from, int row0, int col0)
-    {
-        if constexpr (T == SAMS_F32) {
-            Frag f;
+    // A lane's addresses, of the first of two tiles that follow each other; the other one's are BYTES further, which is an exclusive or too.  They stay
+    // in registers: reading a fragment takes the one instruction.
+    struct Along {                  // numbers 16 s + 8 (lane / 32) .. + 7 of row row0 + lane % 32
+        uint32_t at[D / 16];
+        __device__ __forceinline__ void init(uint32_t tile, int lane)
+        {
+            const uint32_t r = lane & 31, c = (lane >> 5) * (SIZE / 2), from = tile + r * LD + ((c ^ turn<ROOM>(r)) << 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t r = (i & 3) + 8 * (i >> 2);
-                f[i] = *(__attribute__((address_space(3))) const float *)lds((from ^ ((turn<ROOM>(r) << 4) ^ (col0 * 4))) + (row0 + r) * LD);
-            }
-            return f;
-        } else {
-            typedef __attribute__((address_space(3))) gemm::short4v *words_at;
-            const uint32_t at = from ^ (col0 * 2), further = from ^ ((turn<ROOM>(8) << 4) ^ (col0 * 2));
-            const gemm::words2 a = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)lds(at + row0 * LD)));
-            const gemm::words2 b = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)lds(further + (row0 + 8) * LD)));
-            return Frag{a[0], a[1], b[0], b[1]};
+            for (int s = 0; s < D / 16; ++s) at[s] = from ^ (s * 16 * SIZE);
         }
-    }
+        __device__ __forceinline__ void next()
+        {
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) at[s] ^= BYTES;
+        }
+        // of the tile `further` bytes behind
+        __device__ __forceinline__ Frag read(int further, int row0, int s) const
+        {
+            if constexpr (T == SAMS_F32) {
+                typedef float f4 __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) const f4 *f4_at;
+                const f4 a = *(f4_at)in_lds(at[s] + row0 * LD + further), b = *(f4_at)in_lds((at[s] ^ 16) + row0 * LD + further);
+                return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+            } else {
+                return *(__attribute__((address_space(3))) const u32x4 *)in_lds(at[s] + row0 * LD + further);
+            }
+        }
+    };
+    // Column col0 + lane % 32 of the rows row0 + 4 (lane / 32) + {0 .. 3, 8 .. 11}.  16-bit words through the transposing load: of every 16
+    // lanes four give the address of one row's 16 columns, and each gets one column's four rows.
+    struct Across {
+        static constexpr int OWN = T == SAMS_F32 ? 1 : 2 * (D / 32);
+        uint32_t at[OWN];
+        __device__ __forceinline__ void init(uint32_t tile, int lane)
+        {
+            if constexpr (T == SAMS_F32) {
+                const uint32_t r = 4 * (lane >> 5), c = (lane & 31) >> 2;
+                at[0] = tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (lane & 3) * 4;
+            } else {
+                const uint32_t g = lane >> 4, q = lane & 15, r = 4 * (g >> 1) + (q >> 2), c = (g & 1) * 2 + ((q & 3) >> 1);
+                const uint32_t from = tile + r * LD + ((c ^ turn<ROOM>(r)) << 4) + (q & 1) * 8;
+#pragma unroll
+                for (int i = 0; i < OWN; ++i) at[i] = from ^ ((i >> 1) * 64) ^ ((i & 1) * (turn<ROOM>(8) << 4));
+            }
+        }
+        __device__ __forceinline__ void next()
+        {
+#pragma unroll
+            for (int i = 0; i < OWN; ++i) at[i] ^= BYTES;
+        }
+        __device__ __forceinline__ Frag read(int further, int row0, int d) const           // col0 = 32 d
+        {
+            if constexpr (T == SAMS_F32) {
+                Frag f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t r = (i & 3) + 8 * (i >> 2);
+                    f[i] = *(__attribute__((address_space(3))) const float *)in_lds((at[0] ^ ((turn<ROOM>(r) << 4) ^ (d * 128))) + (row0 + r) * LD + further);
+                }
+                return f;
+            } else {
+                typedef __attribute__((address_space(3))) gemm::short4v *words_at;
+                const gemm::words2 a = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)in_lds(at[2 * d] + row0 * LD + further)));
+                const gemm::words2 b = __builtin_bit_cast(gemm::words2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((words_at)in_lds(at[2 * d + 1] + (row0 + 8) * LD + further)));
+                return Frag{a[0], a[1], b[0], b[1]};
+            }
+        }
+    };
 };
 
 // ---- rows in memory ----
@@ -423,9 +443,19 @@ struct Place {
 __device__ __forceinline__ Place place_of(const Args &a, gemm::Launch l, uint32_t heads, bool last_first)
 {
     Place p;
-    uint32_t id = gemm::tile_run(l.first + blockIdx.x, l.total);
-    const uint32_t unit = id / a.tiles;
-    id -= unit * a.tiles;
+    // Workgroups go round the eight XCDs one by one.  Each XCD gets the tiles of some heads, so that they find keys and values in its L2; of those
+    // the heads' longest tiles come first, so that short ones are left for the end (8 workers' 12 heads of 1024: 71 -> 5x us).
+    uint32_t id, unit;
+    const uint32_t units = l.total / a.tiles;
+    if (units % 8 == 0 && gridDim.x == l.total) {
+        const uint32_t each = units / 8, i = blockIdx.x >> 3;
+        id = i / each;
+        unit = (blockIdx.x & 7) * each + (i - id * each);
+    } else {
+        id = gemm::tile_run(l.first + blockIdx.x, l.total);
+        unit = id / a.tiles;
+        id -= unit * a.tiles;
+    }
     p.first = (last_first ? a.tiles - 1 - id : id) * kRows;
     p.head = unit % heads;
     p.seq = a.seq_first + unit / heads % a.seq_count;

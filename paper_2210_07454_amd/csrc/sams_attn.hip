@@ -60,7 +60,10 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
         bias.bring(a, at.head);
         bk.store(tile_k, 0, at.length, a.dim);
         bv.store(tile_v, 0, at.length, a.dim);
-        const uint32_t lane_k = Ti::along_lane(lds_address(tile_k), lane), lane_v = Ti::across_lane(lds_address(tile_v), lane);
+        typename Ti::Along keys;
+        typename Ti::Across values;
+        keys.init(lds_address(lds), lane);
+        values.init(lds_address(lds), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -74,14 +77,13 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
             float by;
             const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
             if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
-                const uint32_t tk = lane_k + turn * Ti::BYTES, tv = lane_v + turn * Ti::BYTES;
                 f32x16 s[NB];
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s[j] = product<T>(Ti::along(tk, 32 * j, c), qf[c], s[j]);
+                    for (int c = 0; c < D / 16; ++c) s[j] = product<T>(keys.read(0, 32 * j, c), qf[c], s[j]);
                 }
                 // logits are times * s + by.  Within a tile of one bucket without a border nothing is done to s for that: the largest one is
                 // found, and the exponents are made, from it.  (A large bias, as a mask has, is added first, so that it swallows the rest as it
@@ -144,13 +146,15 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
                             w = words_of<T>(s[j], half);
                         }
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(Ti::across(tv, 32 * j + 16 * half, 32 * d), w, acc[d]);
+                        for (int d = 0; d < D / 32; ++d) acc[d] = product<T>(values.read(2 * Ti::BYTES, 32 * j + 16 * half, d), w, acc[d]);
                     }
             }
             if (more) {
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
+            keys.next();
+            values.next();
             __syncthreads();
         }
     }

@@ -166,7 +166,10 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         bias.bring(a, at.head);
         bk.store(tile_k, 0, at.length, a.dim);
         bv.store(tile_v, 0, at.length, a.dim);
-        const uint32_t lane_k = Ti::along_lane(lds_address(tile_k), lane), lane_v = Ti::along_lane(lds_address(tile_v), lane), lane_kt = Ti::across_lane(lds_address(tile_k), lane);
+        typename Ti::Along rows;
+        typename Ti::Across columns;
+        rows.init(lds_address(lds), lane);
+        columns.init(lds_address(lds), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -180,7 +183,6 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             float by;
             const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
             if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
-                const uint32_t tk = lane_k + turn * Ti::BYTES, tv = lane_v + turn * Ti::BYTES, tkt = lane_kt + turn * Ti::BYTES;
                 const bool edge = key0 + BN > at.length || q0 + 32 > at.length || (a.causal && key0 + BN - 1 > q0);
                 const bool plain = one && fabsf(by) < 1e6f;         // as in the forward pass
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
@@ -191,9 +193,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[0][i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(Ti::along(tk, 32 * j, c), qf[c], s[0]);
+                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(rows.read(0, 32 * j, c), qf[c], s[0]);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(tv, 32 * j, c), df[c], dp);
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 32 * j, c), df[c], dp);
                     float times = a.scale2, from = by - top + SHIFT;
                     if (!plain) {
                         add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
@@ -239,9 +241,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                         const typename Ti::Frag w = words_of<T>(s[0], half);
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) {
-                            const typename Ti::Frag columns = Ti::across(tkt, 32 * j + 16 * half, 32 * d);
-                            acc[d] = product<T>(columns, w, acc[d]);
-                            if constexpr (ROUNDED) pk[d] = product<T>(columns, wp[half], pk[d]);
+                            const typename Ti::Frag k = columns.read(0, 32 * j + 16 * half, d);
+                            acc[d] = product<T>(k, w, acc[d]);
+                            if constexpr (ROUNDED) pk[d] = product<T>(k, wp[half], pk[d]);
                         }
                     }
                 }
@@ -250,6 +252,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
+            rows.next();
+            columns.next();
             __syncthreads();
         }
         over *= T == SAMS_F16 ? 0x1p-14f : 1.f;
@@ -355,8 +359,10 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         __syncthreads();
         bias.bring(a, head);
         store(query0, 0);
-        const uint32_t lane_q = Ti::along_lane(lds_address(tile_q), lane), lane_d = Ti::along_lane(lds_address(tile_d), lane);
-        const uint32_t lane_qt = Ti::across_lane(lds_address(tile_q), lane), lane_dt = Ti::across_lane(lds_address(tile_d), lane);
+        typename Ti::Along rows;
+        typename Ti::Across columns;
+        rows.init(lds_address(lds), lane);
+        columns.init(lds_address(lds), lane);
         __syncthreads();
         for (int turn = 0;; turn ^= 1) {
             uint32_t next_head = head, next_query0 = query0 + BQ;
@@ -368,8 +374,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             float by;
             const bool one = bias.one(a, lo, lo + BQ - 1 + 31, bucket, by);
             if (k0 < at.length && (!a.causal || query0 + BQ - 1 >= k0) && !(one && by == -__builtin_inff())) {
-                const uint32_t tq = lane_q + turn * Ti::BYTES, td = lane_d + turn * Ti::BYTES, tqt = lane_qt + turn * Ti::BYTES, tdt = lane_dt + turn * Ti::BYTES;
-                const float *st = stats + turn * 3 * BQ;
+                typedef float f4 __attribute__((ext_vector_type(4)));
+                const f4 *st = (const f4 *)(stats + turn * 3 * BQ) + (lane >> 5);       // a lane's rows are four next to each other at a time
+                auto stat_of = [&](int which, int j, int i) { return st[(which * BQ + 32 * j) / 4 + 2 * (i >> 2)][i & 3]; };
                 const bool edge = query0 + BQ > at.length || k0 + 32 > at.length || (a.causal && query0 < k0 + 31);
                 const bool plain = one && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
@@ -380,24 +387,24 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s = product<T>(Ti::along(tq, 32 * j, c), kf[c], s);
+                    for (int c = 0; c < D / 16; ++c) s = product<T>(rows.read(0, 32 * j, c), kf[c], s);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(Ti::along(td, 32 * j, c), vf[c], dp);
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 32 * j, c), vf[c], dp);
                     if (one) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float top = st[32 * j + row_of(i, lane)];
+                            const float top = stat_of(0, j, i);
                             s[i] = plain ? __builtin_fmaf(s[i], a.scale2, by - top) : __builtin_fmaf(s[i], a.scale2, by) - top;
                         }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int r = 32 * j + row_of(i, lane);
-                            s[i] = __builtin_fmaf(s[i], a.scale2, biases[-r]) - st[r];
+                            s[i] = __builtin_fmaf(s[i], a.scale2, biases[-r]) - stat_of(0, j, i);
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * st[BQ + 32 * j + row_of(i, lane)];
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * stat_of(1, j, i);
                     auto allowed = [&](int i) {
                         const uint32_t query = query0 + 32 * j + row_of(i, lane);
                         return live && query < at.length && (!a.causal || query >= key);
@@ -432,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     // dS = m P dP - P delta, without the factor 1 / (1 - p), which delta has not either
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float delta = st[2 * BQ + 32 * j + row_of(i, lane)];
+                        const float delta = stat_of(2, j, i);
                         s[i] = DROP ? __builtin_fmaf(pd[i], dp[i], -(s[i] * delta)) : s[i] * (dp[i] - delta);
                     }
                     if (summed) {
@@ -444,9 +451,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     for (int half = 0; half < 2; ++half) {
                         const typename Ti::Frag wp = words_of<T>(pd, half), ws = words_of<T>(s, half);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(Ti::across(tdt, 32 * j + 16 * half, 32 * d), wp, dv[d]);
+                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(columns.read(2 * Ti::BYTES, 32 * j + 16 * half, d), wp, dv[d]);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(Ti::across(tqt, 32 * j + 16 * half, 32 * d), ws, dk[d]);
+                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(columns.read(0, 32 * j + 16 * half, d), ws, dk[d]);
                     }
                 }
             }
@@ -458,6 +465,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             }
             if (!more) break;
             store(next_query0, turn ^ 1);
+            rows.next();
+            columns.next();
             __syncthreads();
             head = next_head;
             query0 = next_query0;
