@@ -10,7 +10,10 @@ namespace attn {
 using gemm::f32x16;
 using gemm::u32x4;
 
-constexpr int kThreads = 256, kWaves = 4, kRows = 128;      // a workgroup's rows: 32 for each wavefront, which keeps them in registers
+// A workgroup's rows: 32 for each wavefront, which keeps them in registers; or, with SPLIT 2, for each two of them, which take half of the
+// rows that are streamed each and add up their results at the end.
+constexpr int kThreads = 256, kWaves = 4, kRows = 128;
+template <int SPLIT> constexpr int kOwn = kRows / SPLIT;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Args {
@@ -91,7 +94,7 @@ template <int T, int D> struct Tile {
     typedef typename TypeOf<T>::type E;
     typedef typename Fragment<T>::type Frag;
     static constexpr int SIZE = sizeof(E);
-    static constexpr int ROWS = T == SAMS_F32 ? 32 : 64;                        // that a workgroup takes at a time
+    static constexpr int ROWS = T == SAMS_F32 && D > 64 ? 32 : 64;              // that a workgroup takes at a time
     static constexpr int PIECES = D * SIZE / 16, ROOM = power_of_two(PIECES);   // a row's, and what it has room for
     static constexpr int LD = ROOM * 16, BYTES = ROWS * LD;
     static constexpr int N = ROWS * PIECES / kThreads;                          // pieces that a thread brings
@@ -107,10 +110,10 @@ template <int T, int D> struct Tile {
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) at[s] = from ^ (s * 16 * SIZE);
         }
-        __device__ __forceinline__ void next()
+        __device__ __forceinline__ void move(uint32_t bits)        // to the other tile (BYTES), or to its other 32 rows (32 LD)
         {
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s) at[s] ^= BYTES;
+            for (int s = 0; s < D / 16; ++s) at[s] ^= bits;
         }
         // of the tile `further` bytes behind
         __device__ __forceinline__ Frag read(int further, int row0, int s) const
@@ -142,10 +145,10 @@ template <int T, int D> struct Tile {
                 for (int i = 0; i < OWN; ++i) at[i] = from ^ ((i >> 1) * 64) ^ ((i & 1) * (turn<ROOM>(8) << 4));
             }
         }
-        __device__ __forceinline__ void next()
+        __device__ __forceinline__ void move(uint32_t bits)
         {
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) at[i] ^= BYTES;
+            for (int i = 0; i < OWN; ++i) at[i] ^= bits;
         }
         __device__ __forceinline__ Frag read(int further, int row0, int d) const           // col0 = 32 d
         {
@@ -166,6 +169,20 @@ template <int T, int D> struct Tile {
         }
     };
 };
+
+// The order of READS reads of LDS and MFMAS matrix instructions that stand before it: AHEAD reads are under way when the first matrix instruction
+// begins, and behind each come some more.  (Left to itself, the compiler reads a fragment, waits for it and uses it.)
+template <int READS, int MFMAS, int AHEAD>
+__device__ __forceinline__ void in_order()
+{
+    constexpr int EACH = (READS + MFMAS - 1) / MFMAS;
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < MFMAS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (AHEAD + i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    }
+}
 
 // ---- rows in memory ----
 // A piece of 16 bytes of a row of dim numbers is read where all of it exists: one that reaches past the row's end, or starts there, in its place
@@ -404,9 +421,12 @@ __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4
 __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // wavefronts that a SIMD holds: what is more takes accumulators through moves
-template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= 96 ? 2 : 1;
+#ifndef WIDE2
+#define WIDE2 96
+#endif
+template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= WIDE2 ? 2 : 1;
 #ifndef FWD_WAVES
-#define FWD_WAVES (T == SAMS_F32 ? kWavesPerSimd<T, D> : 2)
+#define FWD_WAVES (T == SAMS_F32 ? kWavesPerSimd<T, D> : D <= 64 ? 3 : 2)
 #endif
 
 template <int T, int D>
@@ -440,6 +460,7 @@ __device__ __forceinline__ void add_bias(const float *from, bool one, float by, 
 struct Place {
     uint32_t worker, seq, head, first, length;
 };
+template <int OWN>
 __device__ __forceinline__ Place place_of(const Args &a, gemm::Launch l, uint32_t heads, bool last_first)
 {
     Place p;
@@ -456,7 +477,7 @@ __device__ __forceinline__ Place place_of(const Args &a, gemm::Launch l, uint32_
         unit = id / a.tiles;
         id -= unit * a.tiles;
     }
-    p.first = (last_first ? a.tiles - 1 - id : id) * kRows;
+    p.first = (last_first ? a.tiles - 1 - id : id) * OWN;
     p.head = unit % heads;
     p.seq = a.seq_first + unit / heads % a.seq_count;
     p.worker = unit / heads / a.seq_count;
@@ -494,6 +515,32 @@ __device__ __forceinline__ int64_t stats_of(const Args &a, const Place &at, uint
     } while (0)
 
 constexpr int kLdsBytes = 160 * 1024;
+
+// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make less than two for every CU (4 workers' 12 heads of 511
+// in 32 bits, forward: 59 -> xx us; where there are enough it costs: 8 workers' 12 heads of 1024 46 -> xx).
+#ifndef FEW
+#define FEW 400
+#endif
+constexpr int64_t kFewBlocks = FEW;
+static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
+template <int SPLIT> static inline uint32_t tiles_of(uint32_t len) { return (len + kOwn<SPLIT> - 1) / kOwn<SPLIT>; }
+// f(SPLIT), as a compile-time constant; tiles of 32 streamed rows are not split
+template <int ROWS, typename F>
+static void by_split(bool halves, F f)
+{
+    if constexpr (ROWS == 64) {
+        if (halves) return f(std::integral_constant<int, 2>());
+    }
+    f(std::integral_constant<int, 1>());
+}
+
+// One wavefront's 64 numbers of every lane for another one of the same rows, through LDS
+template <int N>
+__device__ __forceinline__ void give(float *lds, const float (&v)[N], int lane)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[i * 64 + lane] = v[i];
+}
 hipError_t prepare_forward(int type, uint32_t dim);
 hipError_t prepare_backward(int type, uint32_t dim);
 void launch_forward(const Args &a, int type, hipStream_t stream);

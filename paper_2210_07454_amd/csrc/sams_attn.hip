@@ -13,12 +13,12 @@ namespace attn {
 // A workgroup has 128 queries of a head, a wavefront 32 of them, a lane (and the lane 32 from it) one: the products are made as
 // S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
 // Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.
-template <int T, int D, bool DROP>
+template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
-    constexpr int BN = Ti::ROWS, NB = BN / 32;
+    constexpr int BN = Ti::ROWS, NB = BN / 32 / SPLIT, OWN = kOwn<SPLIT>;
     constexpr float SHIFT = T == SAMS_F16 ? 14.f : 0.f;             // 16-bit floats of up to 2^14: small weights keep their digits
     extern __shared__ __align__(16) char lds[];
     char *tile_k = lds, *tile_v = lds + 2 * Ti::BYTES;
@@ -26,8 +26,9 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
     bias.place(a, lds + 4 * Ti::BYTES);
 
     const int lane = threadIdx.x & 63, wave = uniform_wave();
-    const Place at = place_of(a, launch, a.heads, a.causal);
-    const uint32_t q0 = at.first + wave * 32, query = q0 + (lane & 31);
+    const int part = wave % SPLIT;                                 // which of a tile's keys
+    const Place at = place_of<OWN>(a, launch, a.heads, a.causal);
+    const uint32_t q0 = at.first + wave / SPLIT * 32, query = q0 + (lane & 31);
     const bool row_there = query < a.len, live = query < at.length;
     E *out = rows_of<T>(a.out, a.outs, a, at, at.head) + (int64_t)query * a.outs.row;
     const int64_t stat = stats_of(a, at, at.head) + query;
@@ -42,7 +43,7 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
     if (at.first < at.length) {
         const uint32_t kv = at.head / (a.heads / a.kv_heads);
         const E *k = rows_of<T>(a.k, a.ks, a, at, kv), *v = rows_of<T>(a.v, a.vs, a, at, kv);
-        const uint32_t end = a.causal && at.first + kRows < at.length ? at.first + kRows : at.length;
+        const uint32_t end = a.causal && at.first + OWN < at.length ? at.first + OWN : at.length;
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
         const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head, less = (a.keep.least - 1) * 0x10001u;
@@ -62,8 +63,8 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
         bv.store(tile_v, 0, at.length, a.dim);
         typename Ti::Along keys;
         typename Ti::Across values;
-        keys.init(lds_address(lds), lane);
-        values.init(lds_address(lds), lane);
+        keys.init(lds_address(lds) + part * (32 * Ti::LD), lane);
+        values.init(lds_address(lds) + part * (32 * Ti::LD), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -72,11 +73,12 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
                 bk.load(k, a.ks.row, key0 + BN, at.length, a.dim);
                 bv.load(v, a.vs.row, key0 + BN, at.length, a.dim);
             }
-            const int lo = (int)key0 - (int)(q0 + 31);
+            const uint32_t mine = key0 + part * 32;                 // the wavefront's first key
+            const int lo = (int)mine - (int)(q0 + 31);
             uint32_t bucket;
             float by;
-            const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
-            if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
+            const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
+            if (q0 < at.length && mine < at.length && (!a.causal || mine <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 f32x16 s[NB];
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
@@ -89,13 +91,13 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
                 // found, and the exponents are made, from it.  (A large bias, as a mask has, is added first, so that it swallows the rest as it
                 // does in any other tile and in the backward pass.)
                 float times = scale;
-                const bool edge = key0 + BN > at.length || (a.causal && key0 + BN - 1 > q0);
+                const bool edge = mine + NB * 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
                 if (edge || !one || !(fabsf(by) < 1e6f)) {
                     add_bias<NB>(one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31)), one, by, scale, lane, s);
                     times = 1.f;
                     by = 0.f;
                     if (edge) {
-                        const int limit = (int)(a.causal && query < at.length ? query + 1 : at.length) - (int)key0;
+                        const int limit = (int)(a.causal && query < at.length ? query + 1 : at.length) - (int)mine;
 #pragma unroll
                         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -133,7 +135,7 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
                         typename Ti::Frag w;
                         if constexpr (DROP) {
                             uint32_t numbers[4];
-                            philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
+                            philox(seed, ((mine + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
                             w = words_of<T>(s[j], half);
                             if constexpr (T == SAMS_F32) {
 #pragma unroll
@@ -153,12 +155,33 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
-            keys.next();
-            values.next();
+            keys.move(Ti::BYTES);
+            values.move(Ti::BYTES);
             __syncthreads();
         }
     }
     sum = sum_halves(sum);
+    if constexpr (SPLIT == 2) {
+        // the odd wavefronts' results, which their neighbours add to their own; tiles are done with
+        constexpr int N = D / 2 + 2;
+        float *there = (float *)lds + wave / 2 * (N * 64);
+        if (part) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < D / 2; ++i) v[i] = acc[i / 16][i % 16];
+            v[N - 2] = top;
+            v[N - 1] = sum;
+            give<N>(there, v, lane);
+        }
+        __syncthreads();
+        if (part) return;
+        const float other = there[(N - 2) * 64 + lane], most = fmaxf(top, other);
+        const float mine = most == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - most), theirs = most == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(other - most);
+        sum = __builtin_fmaf(sum, mine, there[(N - 1) * 64 + lane] * theirs);
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i) acc[i / 16][i % 16] = __builtin_fmaf(acc[i / 16][i % 16], mine, there[i * 64 + lane] * theirs);
+        top = most;
+    }
     const float by = live && sum != 0.f ? a.keep.scale / sum : 0.f;
     if (!live) {
 #pragma unroll
@@ -176,30 +199,40 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
 template <int T, int D>
 static int lds_forward(const Args &a)
 {
-    return 4 * Tile<T, D>::BYTES + Bias::bytes(a);
+    return std::max(4 * Tile<T, D>::BYTES + Bias::bytes(a), 2 * (D / 2 + 2) * 256);
 }
 
 // a context's kernels may take more LDS than a launch gets unasked
 hipError_t prepare_forward(int type, uint32_t dim)
 {
     hipError_t e = hipSuccess;
+    auto allow = [&](const void *f) {
+        if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    };
     SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(dim, D, {
-        e = hipFuncSetAttribute((const void *)k_attn_forward<T, D, true>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
-        if (e == hipSuccess) e = hipFuncSetAttribute((const void *)k_attn_forward<T, D, false>, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        for (bool halves : {false, true})
+            by_split<Tile<T, D>::ROWS>(halves, [&](auto split) {
+                constexpr int SPLIT = decltype(split)::value;
+                allow((const void *)k_attn_forward<T, D, true, SPLIT>);
+                allow((const void *)k_attn_forward<T, D, false, SPLIT>);
+            });
     }));
     return e;
 }
 
-void launch_forward(const Args &a, int type, hipStream_t stream)
+void launch_forward(const Args &all, int type, hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)a.n * a.seq_count * a.heads * a.tiles;
-    SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
+    const int64_t heads = (int64_t)all.n * all.seqs * all.heads;
+    SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(all.dim, D, by_split<Tile<T, D>::ROWS>(in_halves(heads, all.len), [&](auto split) {
+        constexpr int SPLIT = decltype(split)::value;
+        Args a = all;
+        a.tiles = tiles_of<SPLIT>(a.len);
         const int bytes = lds_forward<T, D>(a);
-        gemm::in_launches(blocks, kThreads, [&](dim3 grid, gemm::Launch l) {
-            if (a.keep.least) hipLaunchKernelGGL((k_attn_forward<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l);
-            else hipLaunchKernelGGL((k_attn_forward<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l);
+        gemm::in_launches(heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+            if (a.keep.least) hipLaunchKernelGGL((k_attn_forward<T, D, true, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l);
+            else hipLaunchKernelGGL((k_attn_forward<T, D, false, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l);
         });
-    }));
+    })));
 }
 
 }  // namespace attn
@@ -236,7 +269,6 @@ static bool arguments(sams_attn *c, int64_t t, int64_t seqs, const int32_t *leng
     a.t = t;
     a.n = c->n; a.seqs = (uint32_t)seqs; a.len = (uint32_t)(t / seqs);
     a.heads = c->heads; a.kv_heads = c->kv_heads; a.dim = c->dim; a.buckets = c->buckets;
-    a.tiles = (a.len + attn::kRows - 1) / attn::kRows;
     a.seq_first = 0;
     a.seq_count = a.seqs;
     a.edge_lo = c->edge_lo; a.edge_hi = c->edge_hi;
@@ -247,7 +279,7 @@ static bool arguments(sams_attn *c, int64_t t, int64_t seqs, const int32_t *leng
     a.causal = causal != 0;
     a.delta = c->scratch.at<float>(c->delta);
     a.part = c->scratch.at<float>(c->part);
-    return (int64_t)c->n * seqs * c->heads * a.tiles < (int64_t)1 << 31;
+    return (int64_t)c->n * seqs * c->heads * attn::tiles_of<1>(a.len) < (int64_t)1 << 31;
 }
 
 extern "C" {
@@ -265,7 +297,7 @@ int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, i
     if (!c) return SAMS_ENOMEM;
     c->n = n; c->t_max = t_max; c->heads = heads; c->kv_heads = kv_heads; c->dim = dim; c->buckets = buckets; c->type = type; c->train = train != 0;
     c->stream = (hipStream_t)hip_stream;
-    c->parts = (t_max + 63) / 64 + 64;
+    c->parts = (t_max + 31) / 32 + 64;
     c->starts = c->scratch.reserve((int64_t)buckets * 4);
     if (buckets > 1) {
         c->edge_lo = starts_host[1];

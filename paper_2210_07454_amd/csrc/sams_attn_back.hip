@@ -12,8 +12,8 @@
 #ifndef KEY_BLOCKS
 #define KEY_BLOCKS 512
 #endif
-#ifndef BLOCKS_AT_ONCE
-#define BLOCKS_AT_ONCE 1
+#ifndef BACK_AHEAD
+#define BACK_AHEAD 4
 #endif
 namespace sams {
 namespace attn {
@@ -101,12 +101,12 @@ struct BucketSums {
 // dq and delta; laid out as the forward pass.  o has been rounded to 16 bits: what do . o is off by is small beside dP, but not beside the
 // 32 bits that dbias is held to.  So delta is also added up as it is defined, sum P dP, for the other kernel, and dq, which needs it before that
 // sum is done, is put right at the end: dq = scale (sum P (dP - d) k + (d - delta) sum P k), with d = do . o.
-template <int T, int D, bool DROP>
+template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;
-    constexpr int BN = Ti::ROWS, NB = BN / 32;
+    constexpr int BN = Ti::ROWS, NB = BN / 32 / SPLIT, OWN = kOwn<SPLIT>;
     constexpr float SHIFT = T == SAMS_F16 ? 14.f : 0.f;             // P in 16-bit floats: times 2^14
     constexpr bool ROUNDED = T != SAMS_F32;
     extern __shared__ __align__(16) char lds[];
@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
     bias.place(a, lds + 4 * Ti::BYTES);
 
     const int lane = threadIdx.x & 63, wave = uniform_wave();
-    const Place at = place_of(a, launch, a.heads, a.causal);
-    const uint32_t q0 = at.first + wave * 32, query = q0 + (lane & 31);
+    const int half_of = wave % SPLIT;                              // which of a tile's keys
+    const Place at = place_of<OWN>(a, launch, a.heads, a.causal);
+    const uint32_t q0 = at.first + wave / SPLIT * 32, query = q0 + (lane & 31);
     const bool row_there = query < a.len, live = query < at.length;
     const int64_t stat = stats_of(a, at, at.head) + query;
 
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
     if (at.first < at.length) {
         const uint32_t kv = at.head / (a.heads / a.kv_heads);
         const E *k = rows_of<T>(a.k, a.ks, a, at, kv), *v = rows_of<T>(a.v, a.vs, a, at, kv);
-        const uint32_t end = a.causal && at.first + kRows < at.length ? at.first + kRows : at.length;
+        const uint32_t end = a.causal && at.first + OWN < at.length ? at.first + OWN : at.length;
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
         const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + at.head;
@@ -168,8 +169,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         bv.store(tile_v, 0, at.length, a.dim);
         typename Ti::Along rows;
         typename Ti::Across columns;
-        rows.init(lds_address(lds), lane);
-        columns.init(lds_address(lds), lane);
+        rows.init(lds_address(lds) + half_of * (32 * Ti::LD), lane);
+        columns.init(lds_address(lds) + half_of * (32 * Ti::LD), lane);
         __syncthreads();
         int turn = 0;
         for (uint32_t key0 = 0; key0 < end; key0 += BN, turn ^= 1) {
@@ -178,24 +179,26 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                 bk.load(k, a.ks.row, key0 + BN, at.length, a.dim);
                 bv.load(v, a.vs.row, key0 + BN, at.length, a.dim);
             }
-            const int lo = (int)key0 - (int)(q0 + 31);
+            const uint32_t mine = key0 + half_of * 32;              // the wavefront's first key
+            const int lo = (int)mine - (int)(q0 + 31);
             uint32_t bucket;
             float by;
-            const bool one = bias.one(a, lo, lo + BN - 1 + 31, bucket, by);
-            if (q0 < at.length && (!a.causal || key0 <= q0 + 31) && !(one && by == -__builtin_inff())) {
-                const bool edge = key0 + BN > at.length || q0 + 32 > at.length || (a.causal && key0 + BN - 1 > q0);
+            const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
+            if (q0 < at.length && mine < at.length && (!a.causal || mine <= q0 + 31) && !(one && by == -__builtin_inff())) {
+                const bool edge = mine + NB * 32 > at.length || q0 + 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
                 const bool plain = one && fabsf(by) < 1e6f;         // as in the forward pass
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
-                const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)key0;
-#pragma unroll BLOCKS_AT_ONCE
+                const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)mine;
+#pragma unroll 1
                 for (int j = 0; j < NB; ++j) {
                     f32x16 s[1], dp;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[0][i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(rows.read(0, 32 * j, c), qf[c], s[0]);
+                    for (int c = 0; c < D / 16; ++c) s[0] = product<T>(rows.read(0, 0, c), qf[c], s[0]);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 32 * j, c), df[c], dp);
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), df[c], dp);
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
                     float times = a.scale2, from = by - top + SHIFT;
                     if (!plain) {
                         add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
@@ -223,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             uint32_t numbers[4];
-                            philox(seed, ((key0 + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
+                            philox(seed, ((mine + 32 * j + 16 * half) >> 4) * 2 + (lane >> 5), query, stream, numbers);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) dp[8 * half + e] = kept(numbers, e, a.keep.least) ? dp[8 * half + e] : 0.f;
                         }
@@ -241,10 +244,15 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                         const typename Ti::Frag w = words_of<T>(s[0], half);
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) {
-                            const typename Ti::Frag k = columns.read(0, 32 * j + 16 * half, d);
+                            const typename Ti::Frag k = columns.read(0, 16 * half, d);
                             acc[d] = product<T>(k, w, acc[d]);
                             if constexpr (ROUNDED) pk[d] = product<T>(k, wp[half], pk[d]);
                         }
+                    }
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
+                    if constexpr (NB == 2) {
+                        rows.move(32 * Ti::LD);
+                        columns.move(32 * Ti::LD);
                     }
                 }
             }
@@ -252,12 +260,36 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                 bk.store(tile_k + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
                 bv.store(tile_v + (turn ^ 1) * Ti::BYTES, key0 + BN, at.length, a.dim);
             }
-            rows.next();
-            columns.next();
+            rows.move(Ti::BYTES);
+            columns.move(Ti::BYTES);
             __syncthreads();
         }
         over *= T == SAMS_F16 ? 0x1p-14f : 1.f;
         exact = sum_halves(exact) * over;
+        if constexpr (SPLIT == 2) {
+            // the odd wavefronts' results, which their neighbours add to their own; tiles are done with
+            constexpr int N = (ROUNDED ? D : D / 2) + 1;
+            float *there = (float *)lds + wave / 2 * (N * 64);
+            if (half_of) {
+                float v[N];
+#pragma unroll
+                for (int i = 0; i < D / 2; ++i) v[i] = acc[i / 16][i % 16] * (1.f / fit.by);
+                if constexpr (ROUNDED)
+#pragma unroll
+                    for (int i = 0; i < D / 2; ++i) v[D / 2 + i] = pk[i / 16][i % 16];
+                v[N - 1] = exact;
+                give<N>(there, v, lane);
+            }
+            __syncthreads();
+            if (half_of) return;
+#pragma unroll
+            for (int i = 0; i < D / 2; ++i) acc[i / 16][i % 16] = __builtin_fmaf(acc[i / 16][i % 16], 1.f / fit.by, there[i * 64 + lane]);
+            if constexpr (ROUNDED)
+#pragma unroll
+                for (int i = 0; i < D / 2; ++i) pk[i / 16][i % 16] += there[(D / 2 + i) * 64 + lane];
+            exact += there[(N - 1) * 64 + lane];
+            fit.by = 1.f;
+        }
         if (live && lane < 32) a.delta[stat] = exact;
         if constexpr (ROUNDED) {
 #pragma unroll
@@ -266,17 +298,18 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                 for (int e = 0; e < 16; ++e) acc[i][e] = __builtin_fmaf(acc[i][e], 1.f / fit.by, (d - exact) * pk[i][e]);
         }
     }
+    if (SPLIT == 2 && half_of) return;
     store_columns<T, D>(rows_of<T>(a.dq, a.dqs, a, at, at.head) + (int64_t)query * a.dqs.row, row_there, a.dim, acc, a.scale * a.keep.scale * over, lane);
 }
 
 // dk, dv and dbias.  A workgroup has 128 keys, a lane (and the lane 32 from it) one; queries and the output's gradients come by tiles.  The
 // products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.  Where there are few keys
 // and heads of keys, a group's heads and a head's queries are shared out to several workgroups, whose sums another kernel joins.
-template <int T, int D, bool DROP>
+template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
 {
     typedef Tile<T, D> Ti;
-    constexpr int BQ = Ti::ROWS, NB = BQ / 32;
+    constexpr int BQ = Ti::ROWS, NB = BQ / 32 / SPLIT, OWN = kOwn<SPLIT>;
     constexpr float SHIFT = T == SAMS_F16 ? 0x1p14f : 1.f;          // P in 16-bit floats
     constexpr int NUMBERS = 80;                                     // bytes of a query's numbers: 32 of 16 bits, and 16 that put the queries on different banks
     extern __shared__ __align__(16) char lds[];
@@ -289,10 +322,11 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 
     const int lane = threadIdx.x & 63, wave = uniform_wave();
     const uint32_t pieces = a.head_pieces * a.query_pieces;
-    Place at = place_of(a, launch, a.kv_heads * pieces, false);
+    const int half_of = wave % SPLIT;                              // which of a tile's queries
+    Place at = place_of<OWN>(a, launch, a.kv_heads * pieces, false);
     const uint32_t piece = at.head % pieces, head_piece = piece / a.query_pieces, query_piece = piece % a.query_pieces;
     at.head /= pieces;
-    const uint32_t k0 = at.first + wave * 32, key = k0 + (lane & 31);
+    const uint32_t k0 = at.first + wave / SPLIT * 32, key = k0 + (lane & 31);
     const bool row_there = key < a.len, live = key < at.length;
 
     f32x16 dk[D / 32], dv[D / 32];
@@ -303,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
     ColumnScale<T, D> fit;
     fit.start();
     const uint32_t group = a.heads / a.kv_heads / a.head_pieces, head0 = at.head * (a.heads / a.kv_heads) + head_piece * group;
-    // this piece's tiles of queries; 128 is a multiple of BQ, so that the first key's tile is the first one where earlier queries see none
+    // this piece's tiles of queries; OWN is a multiple of BQ, so that the first key's tile is the first one where earlier queries see none
     const uint32_t tile0 = a.causal ? at.first / BQ : 0, tiles = (at.length + BQ - 1) / BQ;
     uint32_t begin = 0, end = 0;
     if (at.first < at.length) {
@@ -314,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
     const bool summed = a.part != nullptr;
     // a head's sums of the workgroup; between barriers
     auto leave = [&](uint32_t head, bool some) {
-        float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + ((int64_t)(at.seq - a.seq_first) * a.tiles + at.first / kRows) * a.query_pieces + query_piece) * a.buckets;
+        float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + ((int64_t)(at.seq - a.seq_first) * a.tiles + at.first / OWN) * a.query_pieces + query_piece) * a.buckets;
         for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
             part[b] = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
             for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
@@ -361,41 +395,43 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         store(query0, 0);
         typename Ti::Along rows;
         typename Ti::Across columns;
-        rows.init(lds_address(lds), lane);
-        columns.init(lds_address(lds), lane);
+        rows.init(lds_address(lds) + half_of * (32 * Ti::LD), lane);
+        columns.init(lds_address(lds) + half_of * (32 * Ti::LD), lane);
         __syncthreads();
         for (int turn = 0;; turn ^= 1) {
             uint32_t next_head = head, next_query0 = query0 + BQ;
             if (next_query0 >= end) { ++next_head; next_query0 = begin; }
             const bool more = next_head <= last;
             if (more) load(next_head, next_query0);
-            const int lo = (int)k0 - (int)(query0 + BQ - 1);
+            const uint32_t mine0 = query0 + half_of * 32;           // the wavefront's first query
+            const int lo = (int)k0 - (int)(mine0 + NB * 32 - 1);
             uint32_t bucket;
             float by;
-            const bool one = bias.one(a, lo, lo + BQ - 1 + 31, bucket, by);
-            if (k0 < at.length && (!a.causal || query0 + BQ - 1 >= k0) && !(one && by == -__builtin_inff())) {
+            const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
+            if (k0 < at.length && mine0 < at.length && (!a.causal || mine0 + NB * 32 - 1 >= k0) && !(one && by == -__builtin_inff())) {
                 typedef float f4 __attribute__((ext_vector_type(4)));
-                const f4 *st = (const f4 *)(stats + turn * 3 * BQ) + (lane >> 5);       // a lane's rows are four next to each other at a time
+                const f4 *st = (const f4 *)(stats + turn * 3 * BQ + half_of * 32) + (lane >> 5);       // a lane's rows are four next to each other at a time
                 auto stat_of = [&](int which, int j, int i) { return st[(which * BQ + 32 * j) / 4 + 2 * (i >> 2)][i & 3]; };
-                const bool edge = query0 + BQ > at.length || k0 + 32 > at.length || (a.causal && query0 < k0 + 31);
+                const bool edge = mine0 + NB * 32 > at.length || k0 + 32 > at.length || (a.causal && mine0 < k0 + 31);
                 const bool plain = one && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
-                const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)query0);        // of the first query
-#pragma unroll BLOCKS_AT_ONCE
+                const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)mine0);        // of the first query
+#pragma unroll 1
                 for (int j = 0; j < NB; ++j) {
                     f32x16 s, dp;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) s = product<T>(rows.read(0, 32 * j, c), kf[c], s);
+                    for (int c = 0; c < D / 16; ++c) s = product<T>(rows.read(0, 0, c), kf[c], s);
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 32 * j, c), vf[c], dp);
-                    if (one) {
+                    for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), vf[c], dp);
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
+                    if (plain) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float top = stat_of(0, j, i);
-                            s[i] = plain ? __builtin_fmaf(s[i], a.scale2, by - top) : __builtin_fmaf(s[i], a.scale2, by) - top;
-                        }
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by - stat_of(0, j, i));
+                    } else if (one) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, j, i);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -406,7 +442,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * stat_of(1, j, i);
                     auto allowed = [&](int i) {
-                        const uint32_t query = query0 + 32 * j + row_of(i, lane);
+                        const uint32_t query = mine0 + 32 * j + row_of(i, lane);
                         return live && query < at.length && (!a.causal || query >= key);
                     };
                     if (edge) {
@@ -424,7 +460,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
                             uint32_t numbers[4];
-                            philox(seed, ((k0 + 16 * half) >> 4) * 2 + (lane >> 5), query0 + 32 * j + (lane & 31), stream, numbers);
+                            philox(seed, ((k0 + 16 * half) >> 4) * 2 + (lane >> 5), mine0 + 32 * j + (lane & 31), stream, numbers);
                             *(u32x4 *)(mine + (lane & 31) * NUMBERS + (half * 2 + (lane >> 5)) * 16) = u32x4{numbers[0], numbers[1], numbers[2], numbers[3]};
                         }
                         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -444,16 +480,21 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     }
                     if (summed) {
                         if (one) sums.one(bucket, s, lane);
-                        else sums.many(a, bias, (int)k0 - (int)(query0 + 32 * j), s, lane);
+                        else sums.many(a, bias, (int)k0 - (int)(mine0 + 32 * j), s, lane);
                     }
                     fit.fit(s, dk);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const typename Ti::Frag wp = words_of<T>(pd, half), ws = words_of<T>(s, half);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(columns.read(2 * Ti::BYTES, 32 * j + 16 * half, d), wp, dv[d]);
+                        for (int d = 0; d < D / 32; ++d) dv[d] = product<T>(columns.read(2 * Ti::BYTES, 16 * half, d), wp, dv[d]);
 #pragma unroll
-                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(columns.read(0, 32 * j + 16 * half, d), ws, dk[d]);
+                        for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(columns.read(0, 16 * half, d), ws, dk[d]);
+                    }
+                    if constexpr (T != SAMS_F32) in_order<D / 4, D / 8, 2 * BACK_AHEAD>();
+                    if constexpr (NB == 2) {
+                        rows.move(32 * Ti::LD);
+                        columns.move(32 * Ti::LD);
                     }
                 }
             }
@@ -465,12 +506,31 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             }
             if (!more) break;
             store(next_query0, turn ^ 1);
-            rows.next();
-            columns.next();
+            rows.move(Ti::BYTES);
+            columns.move(Ti::BYTES);
             __syncthreads();
             head = next_head;
             query0 = next_query0;
         }
+    }
+    if constexpr (SPLIT == 2) {
+        // the odd wavefronts' results, which their neighbours add to their own; tiles are done with
+        float *there = (float *)lds + wave / 2 * (D * 64);
+        __syncthreads();
+        if (half_of) {
+            float v[D];
+#pragma unroll
+            for (int i = 0; i < D / 2; ++i) { v[i] = dk[i / 16][i % 16] * (1.f / fit.by); v[D / 2 + i] = dv[i / 16][i % 16]; }
+            give<D>(there, v, lane);
+        }
+        __syncthreads();
+        if (half_of) return;
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i) {
+            dk[i / 16][i % 16] = __builtin_fmaf(dk[i / 16][i % 16], 1.f / fit.by, there[i * 64 + lane]);
+            dv[i / 16][i % 16] += there[(D / 2 + i) * 64 + lane];
+        }
+        fit.by = 1.f;
     }
     if (!live) {
 #pragma unroll
@@ -541,9 +601,18 @@ __global__ void __launch_bounds__(256) k_attn_dbias(const float *part, int64_t p
 hipError_t prepare_backward(int type, uint32_t dim)
 {
     hipError_t e = hipSuccess;
+    auto allow = [&](const void *f) {
+        if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+    };
     SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(dim, D, {
-        for (const void *f : {(const void *)k_attn_dq<T, D, true>, (const void *)k_attn_dq<T, D, false>, (const void *)k_attn_dkv<T, D, true>, (const void *)k_attn_dkv<T, D, false>})
-            if (e == hipSuccess) e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kLdsBytes);
+        for (bool halves : {false, true})
+            by_split<Tile<T, D>::ROWS>(halves, [&](auto split) {
+                constexpr int SPLIT = decltype(split)::value;
+                allow((const void *)k_attn_dq<T, D, true, SPLIT>);
+                allow((const void *)k_attn_dq<T, D, false, SPLIT>);
+                allow((const void *)k_attn_dkv<T, D, true, SPLIT>);
+                allow((const void *)k_attn_dkv<T, D, false, SPLIT>);
+            });
     }));
     return e;
 }
@@ -555,7 +624,7 @@ constexpr int kMostPieces = 16;
 int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim)
 {
     const int64_t blocks = std::max<int64_t>(1, (int64_t)n * kv_heads * ((t_max + kRows - 1) / kRows));
-    const int64_t pieces = std::min<int64_t>(kMostPieces, (kKeyBlocks + blocks - 1) / blocks);
+    const int64_t pieces = std::min<int64_t>(kMostPieces, 2 * ((kKeyBlocks + blocks - 1) / blocks) - 1);       // more than are wanted: heads are cut evenly
     return pieces > 1 ? pieces * n * t_max * kv_heads * dim : 0;
 }
 
@@ -563,12 +632,12 @@ int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int
 static void cut(Args &a, int rows, int64_t parts, int64_t sums)
 {
     const int64_t blocks = (int64_t)a.n * a.seqs * a.kv_heads * a.tiles, each = (int64_t)a.n * a.t * a.kv_heads * a.dim;
-    const int64_t most = std::min<int64_t>({kMostPieces, (kKeyBlocks + blocks - 1) / blocks, sums / each});
+    const int64_t want = (kKeyBlocks + blocks - 1) / blocks, most = std::min<int64_t>(kMostPieces, sums / each);
     const uint32_t group = a.heads / a.kv_heads;
     a.head_pieces = 1;
-    for (uint32_t p = 2; p <= group && p <= most; ++p)
+    for (uint32_t p = 2; p <= group && p <= most && a.head_pieces < want; ++p)
         if (group % p == 0) a.head_pieces = p;
-    const int64_t some = std::min<int64_t>({most / a.head_pieces, (a.len + rows - 1) / rows / 8, parts / a.tiles});
+    const int64_t some = std::min<int64_t>({want / a.head_pieces, most / a.head_pieces, (a.len + rows - 1) / rows / 8, parts / a.tiles});
     a.query_pieces = (uint32_t)std::max<int64_t>(1, some);
 }
 
@@ -584,29 +653,38 @@ void launch_backward(const Args &all, int type, int64_t parts, int64_t sums, flo
         if (dbias) join(0, accumulate);
         return;
     }
+    uint32_t pieces = 1;
     SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-        const int bytes = 4 * Tile<T, D>::BYTES + Bias::bytes(a);
-        gemm::in_launches((int64_t)a.n * a.seqs * a.heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
-            if (a.keep.least) hipLaunchKernelGGL((k_attn_dq<T, D, true>), grid, dim3(kThreads), bytes, stream, a, l);
-            else hipLaunchKernelGGL((k_attn_dq<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l);
+        constexpr int ROWS = Tile<T, D>::ROWS;
+        constexpr int TILES = 4 * Tile<T, D>::BYTES;
+        by_split<ROWS>(in_halves((int64_t)a.n * a.seqs * a.heads, a.len), [&](auto split) {
+            constexpr int SPLIT = decltype(split)::value;
+            a.tiles = tiles_of<SPLIT>(a.len);
+            const int bytes = std::max(TILES + Bias::bytes(a), 2 * (D + 1) * 256);
+            gemm::in_launches((int64_t)a.n * a.seqs * a.heads * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+                if (a.keep.least) hipLaunchKernelGGL((k_attn_dq<T, D, true, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l);
+                else hipLaunchKernelGGL((k_attn_dq<T, D, false, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l);
+            });
+        });
+        by_split<ROWS>(in_halves((int64_t)a.n * a.seqs * a.heads, a.len), [&](auto split) {
+            constexpr int SPLIT = decltype(split)::value;
+            a.tiles = tiles_of<SPLIT>(a.len);
+            cut(a, ROWS, parts, sums);
+            pieces = a.head_pieces * a.query_pieces;
+            // as many sequences at a time as there is room for their parts of the bias's gradient
+            const uint32_t own = a.tiles * a.query_pieces, step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / own)) : a.seqs;
+            const int bytes = std::max(TILES + 2 * 3 * ROWS * 4 + (int)a.buckets * 4 * kWaves + Bias::bytes(a) + (a.keep.least ? kWaves * 32 * 80 : 0), 2 * D * 256);
+            for (uint32_t first = 0; first < all.seqs; first += step) {
+                a.seq_first = first;
+                a.seq_count = std::min(step, all.seqs - first);
+                gemm::in_launches((int64_t)a.n * a.seq_count * a.kv_heads * pieces * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
+                    if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l, parts);
+                    else hipLaunchKernelGGL((k_attn_dkv<T, D, false, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l, parts);
+                });
+                if (dbias) join(a.seq_count * own, accumulate || first > 0);
+            }
         });
     }));
-    cut(a, type == SAMS_F32 ? 32 : 64, parts, sums);
-    const uint32_t pieces = a.head_pieces * a.query_pieces, own = a.tiles * a.query_pieces;
-    // as many sequences at a time as there is room for their parts of the bias's gradient
-    const uint32_t step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / own)) : a.seqs;
-    for (uint32_t first = 0; first < all.seqs; first += step) {
-        a.seq_first = first;
-        a.seq_count = std::min(step, all.seqs - first);
-        SAMS_BY_TYPE(type, T, SAMS_BY_WIDTH(a.dim, D, {
-            const int bytes = 4 * Tile<T, D>::BYTES + 2 * 3 * Tile<T, D>::ROWS * 4 + (int)a.buckets * 4 * kWaves + Bias::bytes(a);
-            gemm::in_launches((int64_t)a.n * a.seq_count * a.kv_heads * pieces * a.tiles, kThreads, [&](dim3 grid, gemm::Launch l) {
-                if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true>), grid, dim3(kThreads), bytes + kWaves * 32 * 80, stream, a, l, parts);
-                else hipLaunchKernelGGL((k_attn_dkv<T, D, false>), grid, dim3(kThreads), bytes, stream, a, l, parts);
-            });
-        }));
-        if (dbias) join(a.seq_count * own, accumulate || first > 0);
-    }
     if (pieces > 1) {
         const int64_t blocks = ((int64_t)a.n * a.t * ((a.kv_heads * a.dim + 3) / 4) + 255) / 256;
         SAMS_BY_TYPE(type, T, gemm::in_launches(blocks, 256, [&](dim3 grid, gemm::Launch l) {
