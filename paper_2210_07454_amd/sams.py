@@ -501,6 +501,13 @@ class Orthogonalizer(_TrainContext):
                    beta, int(bool(nesterov)), lr, scale, weight_decay, steps, _coefficients(coef), eps)
 
 
+def _on(device, **tensors):
+    """Every tensor given lies on the context's device."""
+    for name, t in tensors.items():
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != device:
+            raise ValueError(f"{name}: expected a tensor on cuda:{device}, got {t.device}")
+
+
 class Dropout(_TrainContext):
     """Dropout of [n][t][dim] tensors, t up to ``t_max``, by a seed and a step that lie on the device; see sams.h."""
 
@@ -512,6 +519,7 @@ class Dropout(_TrainContext):
 
     def dropout_forward(self, x, residual, rng, p, y):
         t = _leading(x, 3, "x")[1]
+        _on(self._device, x=x, residual=residual, rng=rng, y=y)
         full = (self.n, t, self.dim)
         self._call("dropout_forward", t, *_strided(x, self.dtype, full, 1, "x"),
                    *(_strided(residual, self.dtype, full, 1, "residual") if residual is not None else (None, 0, 0)), _ptr(rng, torch.int64, (2,), "rng"),
@@ -519,6 +527,7 @@ class Dropout(_TrainContext):
 
     def dropout_backward(self, dy, rng, p, dx):
         t = _leading(dy, 3, "dy")[1]
+        _on(self._device, dy=dy, rng=rng, dx=dx)
         full = (self.n, t, self.dim)
         self._call("dropout_backward", t, *_strided(dy, self.dtype, full, 1, "dy"), _ptr(rng, torch.int64, (2,), "rng"), p,
                    *_strided(dx, self.dtype, full, 1, "dx"))
@@ -583,6 +592,7 @@ class Attention(_TrainContext):
 
     def attention_forward(self, q, k, v, bias, o, row_max, row_sum, seqs=1, lengths=None, causal=True, scale=None, rng=None, p=0.0):
         t = _leading(q, 3, "q")[1]
+        _on(self._device, q=q, k=k, v=v, bias=bias, o=o, row_max=row_max, row_sum=row_sum, lengths=lengths, rng=rng)
         stats = (self.n, self.heads, t)
         self._call("attention_forward", t, seqs, _ptr(lengths, _I32, (self.n, seqs), "lengths"), *self._inputs(t, q, k, v),
                    *self._how(bias, causal, scale, rng, p), *_strided(o, self.dtype, (self.n, t, self.heads * self.dim), 1, "o"),
@@ -591,6 +601,7 @@ class Attention(_TrainContext):
     def attention_backward(self, do, q, k, v, bias, o, row_max, row_sum, dq, dk, dv, dbias=None, seqs=1, lengths=None, causal=True, scale=None,
                            rng=None, p=0.0, accumulate=False):
         t = _leading(q, 3, "q")[1]
+        _on(self._device, do=do, q=q, k=k, v=v, bias=bias, o=o, row_max=row_max, row_sum=row_sum, dq=dq, dk=dk, dv=dv, dbias=dbias, lengths=lengths, rng=rng)
         wide, narrow, stats = (self.n, t, self.heads * self.dim), (self.n, t, self.kv_heads * self.dim), (self.n, self.heads, t)
         into = (None, 0)
         if dbias is not None:

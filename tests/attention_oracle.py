@@ -31,9 +31,9 @@ def rounded(value, tol, kind):
     return tol + HALF_ULP[kind] * (value.abs() + tol) + TINY[kind]
 
 
-def formulas(q, k, v, bias, starts, do=None, seqs=1, lengths=None, causal=True, scale=None, rng=None, p=0.0, heads=1, kv_heads=1):
+def formulas(q, k, v, bias, starts, do=None, seqs=1, lengths=None, causal=True, scale=None, rng=None, p=0.0, heads=1, kv_heads=1, kind=None):
     """Outputs and gradients, and what each may be off by (with its rounding).  Tensors on the CPU, [n][t][heads * dim]."""
-    kind, (n, t, wide) = q.dtype, q.shape
+    kind, (n, t, wide) = kind or q.dtype, q.shape
     dim, length, group = wide // heads, t // seqs, heads // kv_heads
     scale = float(np.float32(dim ** -0.5 if scale is None else scale))
     word = 0.0 if kind == torch.float32 else HALF_ULP[kind]
