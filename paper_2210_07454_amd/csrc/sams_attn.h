@@ -34,6 +34,7 @@ struct Args {
     int32_t edge_lo, edge_hi;       // the second bucket's start, and the last one's
     int32_t table_first;            // distances that are looked up in a table: the first one, and how many; 0: none are
     uint32_t table_count;
+    const uint16_t *table_buckets;  // [table_count]
     uint32_t head_pieces, query_pieces;     // that the rows of a key's sums are cut into, of a group's heads and of a head's queries
     float *dk_parts, *dv_parts;     // [pieces][n][t][kv_heads * dim], if there are several
     float scale, scale2;            // the logits' factor, and the same times log2 e
@@ -340,24 +341,34 @@ __device__ __forceinline__ float bias_of(float v)
 }
 
 struct Bias {
-    const int *starts;      // [buckets] in LDS
     float *table;           // in LDS: [table_count], or, where that is 0, [kWaves][kReach] of the wavefronts' present tiles
+    uint16_t *which;        // in LDS: [table_count] the buckets that the table's biases are of, for who wants them
+    const int *starts;      // in LDS: [buckets], where there is no table
     const float *row;       // [buckets], the head's
     float before, behind;   // the first and the last bucket's
 
     // where they lie in LDS, and how much they take
     __device__ __forceinline__ void place(const Args &a, char *lds)
     {
-        starts = (const int *)lds;
-        table = (float *)(lds + a.buckets * 4);
+        table = (float *)lds;
+        which = (uint16_t *)(table + a.table_count);
+        starts = (const int *)(table + kWaves * kReach);
     }
-    static int bytes(const Args &a) { return (int)(a.buckets + (a.table_count ? a.table_count : kWaves * kReach)) * 4; }
-    // the workgroup's starts, before a barrier
-    __device__ __forceinline__ void bring_starts(const Args &a) const
+    static int bytes(const Args &a, bool buckets_too = false)
     {
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) ((int *)starts)[b] = a.starts[b];
+        return a.table_count ? (int)a.table_count * (buckets_too ? 6 : 4) : (kWaves * kReach + (int)a.buckets) * 4;
     }
-    // a head's biases, behind a barrier and before another
+    // the workgroup's starts, or the table's buckets; a barrier follows
+    __device__ __forceinline__ void bring_starts(const Args &a, bool buckets_too = false) const
+    {
+        if (a.table_count) {
+            if (buckets_too)
+                for (uint32_t i = threadIdx.x; i < a.table_count; i += kThreads) which[i] = a.table_buckets[i];
+        } else {
+            for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) ((int *)starts)[b] = a.starts[b];
+        }
+    }
+    // a head's biases; a barrier follows
     __device__ __forceinline__ void bring(const Args &a, uint32_t head)
     {
         before = behind = 0.f;
@@ -365,10 +376,11 @@ struct Bias {
         row = a.bias + (int64_t)head * a.buckets;
         before = bias_of(row[0]);
         behind = bias_of(row[a.buckets - 1]);
-        for (uint32_t i = threadIdx.x; i < a.table_count; i += kThreads) table[i] = bias_of(row[bucket(a, a.table_first + (int)i)]);
+        for (uint32_t i = threadIdx.x; i < a.table_count; i += kThreads) table[i] = bias_of(row[a.table_buckets[i]]);
     }
     __device__ __forceinline__ uint32_t bucket(const Args &a, int distance) const
     {
+        if (a.table_count) return which[distance - a.table_first];
         uint32_t lo = 0, n = a.buckets;             // the answer is one of lo .. lo + n - 1
         while (n > 1) {
             const uint32_t half = n >> 1;

@@ -57,7 +57,6 @@ __global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, 
         const float scale = fabsf(a.scale2);
         if (a.scale2 < 0.f) flip<T, D>(qf);
         bias.bring_starts(a);
-        __syncthreads();
         bias.bring(a, at.head);
         bk.store(tile_k, 0, at.length, a.dim);
         bv.store(tile_v, 0, at.length, a.dim);
@@ -244,7 +243,7 @@ struct sams_attn {
     int32_t edge_lo, edge_hi, table_first, table_count;
     hipStream_t stream;
     sams::Scratch scratch;
-    int64_t starts, delta, part, dk_parts, dv_parts;
+    int64_t starts, table, delta, part, dk_parts, dv_parts;
 };
 
 using namespace sams;
@@ -273,6 +272,7 @@ static bool arguments(sams_attn *c, int64_t t, int64_t seqs, const int32_t *leng
     a.seq_count = a.seqs;
     a.edge_lo = c->edge_lo; a.edge_hi = c->edge_hi;
     a.table_first = c->table_first; a.table_count = (uint32_t)c->table_count;
+    a.table_buckets = c->scratch.at<uint16_t>(c->table);
     a.head_pieces = a.query_pieces = 1;
     a.scale = scale;
     a.scale2 = scale * attn::kLog2e;
@@ -308,6 +308,7 @@ int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, i
             c->table_count = (int32_t)count;
         }
     }
+    c->table = c->scratch.reserve((int64_t)c->table_count * 2);
     if (train) {
         c->sums = attn::sums_room(n, t_max, heads, kv_heads, dim);
         c->dk_parts = c->scratch.reserve(c->sums * 4);
@@ -320,6 +321,12 @@ int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, i
         hipError_t e = attn::prepare_forward(type, (uint32_t)dim);
         if (e == hipSuccess && train) e = attn::prepare_backward(type, (uint32_t)dim);
         if (e == hipSuccess && buckets) e = hipMemcpyAsync(c->scratch.base + c->starts, starts_host, (size_t)buckets * 4, hipMemcpyHostToDevice, c->stream);
+        uint16_t table[attn::kMaxTable];                            // the distances' buckets, one after the other
+        for (int32_t i = 0, b = 0; i < c->table_count; ++i) {
+            while (b + 1 < buckets && starts_host[b + 1] <= c->table_first + i) ++b;
+            table[i] = (uint16_t)b;
+        }
+        if (e == hipSuccess && c->table_count) e = hipMemcpyAsync(c->scratch.base + c->table, table, (size_t)c->table_count * 2, hipMemcpyHostToDevice, c->stream);
         if (e == hipSuccess && buckets) e = hipStreamSynchronize(c->stream);
         if (e != hipSuccess) {
             g_last_hip_error = (int)e;

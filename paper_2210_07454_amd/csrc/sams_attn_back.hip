@@ -46,8 +46,9 @@ template <int T, int D> struct ColumnScale {
     }
 };
 
-// Sums of dS by bucket.  A tile of one bucket adds to a lane's own number, which is joined when the bucket changes; in other tiles the 32 x 32 numbers
-// of a wavefront are first added up along their diagonals: rotated by their row, a lane's numbers all belong to one of two distances.
+// Sums of dS by bucket, of a wavefront.  A tile of one bucket adds to a lane's own number, which is joined when the bucket changes.  In others the 32 x 32 numbers
+// of a block are first added up along their diagonals: rotated by their row, a lane's numbers all belong to one of two distances, and those of a bucket follow
+// each other.  (Adding each number to its bucket's in LDS takes twice the kernel's time: LDS adds 32-bit floats at a third of one a cycle.)
 struct BucketSums {
     float *to;              // [buckets] in LDS, of this wavefront alone
     float own;
@@ -70,7 +71,7 @@ struct BucketSums {
         for (int i = 0; i < 8; ++i) v[i] = ds[i] + ds[i + 8];
         own += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
     }
-    // corner: the distance of the block's first key and query
+    // corner: the block's first key less its first query
     __device__ __forceinline__ void many(const Args &a, const Bias &bias, int corner, const f32x16 &ds, int lane)
     {
         float up = 0.f, down = 0.f;             // distances lane % 32 and lane % 32 - 32
@@ -163,7 +164,6 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         fit.start();
 
         bias.bring_starts(a);
-        __syncthreads();
         bias.bring(a, at.head);
         bk.store(tile_k, 0, at.length, a.dim);
         bv.store(tile_v, 0, at.length, a.dim);
@@ -349,17 +349,17 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
     // a head's sums of the workgroup; between barriers
     auto leave = [&](uint32_t head, bool some) {
         float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + ((int64_t)(at.seq - a.seq_first) * a.tiles + at.first / OWN) * a.query_pieces + query_piece) * a.buckets;
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads)
             part[b] = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
-            for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
-        }
+    };
+    auto clear = [&]() {
+        for (uint32_t i = threadIdx.x; i < kWaves * a.buckets; i += kThreads) sums_lds[i] = 0.f;
     };
     if (begin >= end) {
         for (uint32_t h = 0; summed && h < group; ++h) leave(head0 + h, false);
     } else {
-        bias.bring_starts(a);
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads)
-            for (int w = 0; w < kWaves; ++w) sums_lds[w * a.buckets + b] = 0.f;
+        bias.bring_starts(a, summed);
+        clear();
         Seed seed = {};
         if constexpr (DROP) seed = read_seed(a.rng);
         Bring<T, D> bq, bd;
@@ -390,7 +390,6 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         typename Ti::Frag kf[D / 16], vf[D / 16];
         row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head), a.ks.row, key, at.length, a.dim, lane, kf);
         row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head), a.vs.row, key, at.length, a.dim, lane, vf);
-        __syncthreads();
         bias.bring(a, head);
         store(query0, 0);
         typename Ti::Along rows;
@@ -502,7 +501,13 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 if (summed) sums.flush(lane);
                 __syncthreads();
                 if (summed) leave(head, true);
-                if (more) bias.bring(a, next_head);
+                if (more) {
+                    bias.bring(a, next_head);
+                    if (summed) {
+                        __syncthreads();
+                        clear();
+                    }
+                }
             }
             if (!more) break;
             store(next_query0, turn ^ 1);
@@ -673,7 +678,7 @@ void launch_backward(const Args &all, int type, int64_t parts, int64_t sums, flo
             pieces = a.head_pieces * a.query_pieces;
             // as many sequences at a time as there is room for their parts of the bias's gradient
             const uint32_t own = a.tiles * a.query_pieces, step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / own)) : a.seqs;
-            const int bytes = std::max(TILES + 2 * 3 * ROWS * 4 + (int)a.buckets * 4 * kWaves + Bias::bytes(a) + (a.keep.least ? kWaves * 32 * 80 : 0), 2 * D * 256);
+            const int bytes = std::max(TILES + 2 * 3 * ROWS * 4 + Bias::bytes(a, true) + (a.keep.least ? kWaves * 32 * 80 : 0) + (int)a.buckets * kWaves * 4, 2 * D * 256);
             for (uint32_t first = 0; first < all.seqs; first += step) {
                 a.seq_first = first;
                 a.seq_count = std::min(step, all.seqs - first);
