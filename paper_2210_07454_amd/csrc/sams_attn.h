@@ -433,13 +433,7 @@ __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4
 __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // wavefronts that a SIMD holds: what is more takes accumulators through moves
-#ifndef WIDE2
-#define WIDE2 96
-#endif
-template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= WIDE2 ? 2 : 1;
-#ifndef FWD_WAVES
-#define FWD_WAVES (T == SAMS_F32 ? kWavesPerSimd<T, D> : D <= 64 ? 3 : 2)
-#endif
+template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= 96 ? 2 : 1;
 
 template <int T, int D>
 __device__ __forceinline__ void flip(typename Fragment<T>::type (&f)[D / 16])
@@ -530,10 +524,7 @@ constexpr int kLdsBytes = 160 * 1024;
 
 // Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make less than two for every CU (4 workers' 12 heads of 511
 // in 32 bits, forward: 59 -> xx us; where there are enough it costs: 8 workers' 12 heads of 1024 46 -> xx).
-#ifndef FEW
-#define FEW 400
-#endif
-constexpr int64_t kFewBlocks = FEW;
+constexpr int64_t kFewBlocks = 400;
 static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
 template <int SPLIT> static inline uint32_t tiles_of(uint32_t len) { return (len + kOwn<SPLIT> - 1) / kOwn<SPLIT>; }
 // f(SPLIT), as a compile-time constant; tiles of 32 streamed rows are not split

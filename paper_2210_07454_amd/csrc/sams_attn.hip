@@ -14,7 +14,7 @@ namespace attn {
 // S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
 // Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.
 template <int T, int D, bool DROP, int SPLIT>
-__global__ void __launch_bounds__(kThreads, (FWD_WAVES)) k_attn_forward(Args a, gemm::Launch launch)
+__global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D> : D <= 64 ? 3 : 2)) k_attn_forward(Args a, gemm::Launch launch)
 {
     typedef Tile<T, D> Ti;
     typedef typename TypeOf<T>::type E;

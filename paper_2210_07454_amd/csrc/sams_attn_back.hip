@@ -9,14 +9,10 @@
 // atomics; seven products of a pair where one kernel would take five.
 #include "sams_attn.h"
 
-#ifndef KEY_BLOCKS
-#define KEY_BLOCKS 512
-#endif
-#ifndef BACK_AHEAD
-#define BACK_AHEAD 4
-#endif
 namespace sams {
 namespace attn {
+
+constexpr int kAhead = 4;       // fragments under way before the matrix instructions begin (8: 1 % either way)
 
 // 16-bit floats have few digits below 2^-14, and dS may be all below that: a column of dS (a lane's, and that of the lane 32 from it) is
 // multiplied by a power of two that brings its largest number so far to 2^14, and the column's sums with it.
@@ -186,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
             if (q0 < at.length && mine < at.length && (!a.causal || mine <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 const bool edge = mine + NB * 32 > at.length || q0 + 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
-                const bool plain = one && fabsf(by) < 1e6f;         // as in the forward pass
+                const bool plain = one && !edge && fabsf(by) < 1e6f;        // as in the forward pass
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
                 const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)mine;
 #pragma unroll 1
@@ -198,24 +194,20 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                     for (int c = 0; c < D / 16; ++c) s[0] = product<T>(rows.read(0, 0, c), qf[c], s[0]);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), df[c], dp);
-                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, kAhead>();
                     float times = a.scale2, from = by - top + SHIFT;
                     if (!plain) {
                         add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
                         times = 1.f;
                         from = SHIFT - top;
+                        if (edge) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[0][i] = 32 * j + row_of(i, lane) < limit ? s[0][i] : -__builtin_inff();
+                        }
                     }
                     // P, times the row's sum: that is divided out of the row's results at the end
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[0][i], times, from));
-                    if (edge) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const bool allowed = 32 * j + row_of(i, lane) < limit;
-                            s[0][i] = allowed ? s[0][i] : 0.f;
-                            dp[i] = allowed ? dp[i] : 0.f;
-                        }
-                    }
                     typename Ti::Frag wp[2];
                     if constexpr (ROUNDED) {
                         wp[0] = words_of<T>(s[0], 0);
@@ -249,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                             if constexpr (ROUNDED) pk[d] = product<T>(k, wp[half], pk[d]);
                         }
                     }
-                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, kAhead>();
                     if constexpr (NB == 2) {
                         rows.move(32 * Ti::LD);
                         columns.move(32 * Ti::LD);
@@ -412,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 const f4 *st = (const f4 *)(stats + turn * 3 * BQ + half_of * 32) + (lane >> 5);       // a lane's rows are four next to each other at a time
                 auto stat_of = [&](int which, int j, int i) { return st[(which * BQ + 32 * j) / 4 + 2 * (i >> 2)][i & 3]; };
                 const bool edge = mine0 + NB * 32 > at.length || k0 + 32 > at.length || (a.causal && mine0 < k0 + 31);
-                const bool plain = one && fabsf(by) < 1e6f;
+                const bool plain = one && !edge && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)mine0);        // of the first query
 #pragma unroll 1
@@ -424,33 +416,28 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     for (int c = 0; c < D / 16; ++c) s = product<T>(rows.read(0, 0, c), kf[c], s);
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), vf[c], dp);
-                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, BACK_AHEAD>();
+                    if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, kAhead>();
                     if (plain) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by - stat_of(0, j, i));
-                    } else if (one) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, j, i);
                     } else {
+                        if (one) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = 32 * j + row_of(i, lane);
-                            s[i] = __builtin_fmaf(s[i], a.scale2, biases[-r]) - stat_of(0, j, i);
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, j, i);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, biases[-(32 * j + row_of(i, lane))]) - stat_of(0, j, i);
+                        }
+                        if (edge) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const uint32_t query = mine0 + 32 * j + row_of(i, lane);
+                                s[i] = live && query < at.length && (!a.causal || query >= key) ? s[i] : -__builtin_inff();
+                            }
                         }
                     }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * stat_of(1, j, i);
-                    auto allowed = [&](int i) {
-                        const uint32_t query = mine0 + 32 * j + row_of(i, lane);
-                        return live && query < at.length && (!a.causal || query >= key);
-                    };
-                    if (edge) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            s[i] = allowed(i) ? s[i] : 0.f;
-                            dp[i] = allowed(i) ? dp[i] : 0.f;
-                        }
-                    }
                     f32x16 pd = s;
                     if constexpr (DROP) {
                         // A generator's call is for one query and eight keys: every lane makes two of the 128 calls for its query, and takes what
@@ -477,10 +464,13 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                         const float delta = stat_of(2, j, i);
                         s[i] = DROP ? __builtin_fmaf(pd[i], dp[i], -(s[i] * delta)) : s[i] * (dp[i] - delta);
                     }
-                    if (summed) {
-                        if (one) sums.one(bucket, s, lane);
-                        else sums.many(a, bias, (int)k0 - (int)(mine0 + 32 * j), s, lane);
-                    }
+                    auto add_up = [&]() {
+                        if (summed) {
+                            if (one) sums.one(bucket, s, lane);
+                            else sums.many(a, bias, (int)k0 - (int)(mine0 + 32 * j), s, lane);
+                        }
+                    };
+                    if constexpr (T == SAMS_F16) add_up();          // before they are scaled
                     fit.fit(s, dk);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -490,7 +480,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 #pragma unroll
                         for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(columns.read(0, 16 * half, d), ws, dk[d]);
                     }
-                    if constexpr (T != SAMS_F32) in_order<D / 4, D / 8, 2 * BACK_AHEAD>();
+                    if constexpr (T != SAMS_F32) in_order<D / 4, D / 8, 2 * kAhead>();
+                    if constexpr (T != SAMS_F16) add_up();          // while the matrix cores are at it
                     if constexpr (NB == 2) {
                         rows.move(32 * Ti::LD);
                         columns.move(32 * Ti::LD);
@@ -623,7 +614,7 @@ hipError_t prepare_backward(int type, uint32_t dim)
 }
 
 // Workgroups that the keys' kernel is given at least, where cutting its sums into pieces gets it there: four for every CU
-constexpr int64_t kKeyBlocks = KEY_BLOCKS;
+constexpr int64_t kKeyBlocks = 512;
 constexpr int kMostPieces = 16;
 
 int64_t sums_room(int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim)
