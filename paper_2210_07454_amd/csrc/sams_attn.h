@@ -27,7 +27,11 @@ struct Args {
     const int64_t *rng;
     float *row_max, *row_sum;       // [n][heads][t]: a row's largest logit (times log2 e) and its sum of exponentials
     float *delta;                   // [n][heads][t]: sums of dP P
-    float *part;                    // [n][heads][seqs * tiles][buckets]: the bias's gradient
+    float *part;                    // [n][heads][seqs * tiles][buckets]: the bias's gradient, in parts
+    float *dbias;                   // [n][heads][buckets], where there is one part
+    int64_t dbias_worker;
+    float dbias_scale;
+    int32_t accumulate;
     int64_t t;
     uint32_t n, seqs, len, heads, kv_heads, dim, buckets, tiles;
     uint32_t seq_first, seq_count;  // sequences that a launch deals with, of every worker

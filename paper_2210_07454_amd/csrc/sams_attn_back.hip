@@ -337,12 +337,16 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         end = (tile0 + (tiles - tile0) * (query_piece + 1) / a.query_pieces) * BQ;
     }
     BucketSums sums = {sums_lds + wave * a.buckets, 0.f, 0};
-    const bool summed = a.part != nullptr;
+    const bool summed = a.part || a.dbias;
     // a head's sums of the workgroup; between barriers
     auto leave = [&](uint32_t head, bool some) {
         float *part = a.part + (((int64_t)at.worker * a.heads + head) * parts + ((int64_t)(at.seq - a.seq_first) * a.tiles + at.first / OWN) * a.query_pieces + query_piece) * a.buckets;
-        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads)
-            part[b] = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
+        float *all = a.dbias + at.worker * a.dbias_worker + (int64_t)head * a.buckets;
+        for (uint32_t b = threadIdx.x; b < a.buckets; b += kThreads) {
+            const float v = some ? (sums_lds[b] + sums_lds[a.buckets + b]) + (sums_lds[2 * a.buckets + b] + sums_lds[3 * a.buckets + b]) : 0.f;
+            if (a.dbias) all[b] = a.accumulate ? __builtin_fmaf(v, a.dbias_scale, all[b]) : v * a.dbias_scale;
+            else part[b] = v;
+        }
     };
     auto clear = [&]() {
         for (uint32_t i = threadIdx.x; i < kWaves * a.buckets; i += kThreads) sums_lds[i] = 0.f;
@@ -670,6 +674,10 @@ void launch_backward(const Args &all, int type, int64_t parts, int64_t sums, flo
             // as many sequences at a time as there is room for their parts of the bias's gradient
             const uint32_t own = a.tiles * a.query_pieces, step = a.buckets ? (uint32_t)std::min<int64_t>(a.seqs, std::max<int64_t>(1, parts / own)) : a.seqs;
             const int bytes = std::max(TILES + 2 * 3 * ROWS * 4 + Bias::bytes(a, true) + (a.keep.least ? kWaves * 32 * 80 : 0) + (int)a.buckets * kWaves * 4, 2 * D * 256);
+            if (dbias && a.seqs * own == 1) {                       // nothing to join
+                a.part = nullptr;
+                a.dbias = dbias; a.dbias_worker = dbias_worker; a.dbias_scale = scale; a.accumulate = accumulate;
+            }
             for (uint32_t first = 0; first < all.seqs; first += step) {
                 a.seq_first = first;
                 a.seq_count = std::min(step, all.seqs - first);
@@ -677,7 +685,7 @@ void launch_backward(const Args &all, int type, int64_t parts, int64_t sums, flo
                     if (a.keep.least) hipLaunchKernelGGL((k_attn_dkv<T, D, true, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l, parts);
                     else hipLaunchKernelGGL((k_attn_dkv<T, D, false, SPLIT>), grid, dim3(kThreads), bytes, stream, a, l, parts);
                 });
-                if (dbias) join(a.seq_count * own, accumulate || first > 0);
+                if (a.part) join(a.seq_count * own, accumulate || first > 0);
             }
         });
     }));

@@ -501,11 +501,11 @@ class Orthogonalizer(_TrainContext):
                    beta, int(bool(nesterov)), lr, scale, weight_decay, steps, _coefficients(coef), eps)
 
 
-def _on(device, **tensors):
-    """Every tensor given lies on the context's device."""
-    for name, t in tensors.items():
-        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != device:
-            raise ValueError(f"{name}: expected a tensor on cuda:{device}, got {t.device}")
+def _on(device, *tensors):
+    """Every tensor given lies on the context's device (those that are none, or on the host, are refused by name later)."""
+    for t in tensors:
+        if t is not None and isinstance(t, torch.Tensor) and t.get_device() not in (device, -1):
+            raise ValueError(f"expected tensors on cuda:{device}, got one on {t.device}")
 
 
 class Dropout(_TrainContext):
@@ -519,7 +519,7 @@ class Dropout(_TrainContext):
 
     def dropout_forward(self, x, residual, rng, p, y):
         t = _leading(x, 3, "x")[1]
-        _on(self._device, x=x, residual=residual, rng=rng, y=y)
+        _on(self._device, x, residual, rng, y)
         full = (self.n, t, self.dim)
         self._call("dropout_forward", t, *_strided(x, self.dtype, full, 1, "x"),
                    *(_strided(residual, self.dtype, full, 1, "residual") if residual is not None else (None, 0, 0)), _ptr(rng, torch.int64, (2,), "rng"),
@@ -527,7 +527,7 @@ class Dropout(_TrainContext):
 
     def dropout_backward(self, dy, rng, p, dx):
         t = _leading(dy, 3, "dy")[1]
-        _on(self._device, dy=dy, rng=rng, dx=dx)
+        _on(self._device, dy, rng, dx)
         full = (self.n, t, self.dim)
         self._call("dropout_backward", t, *_strided(dy, self.dtype, full, 1, "dy"), _ptr(rng, torch.int64, (2,), "rng"), p,
                    *_strided(dx, self.dtype, full, 1, "dx"))
@@ -592,7 +592,7 @@ class Attention(_TrainContext):
 
     def attention_forward(self, q, k, v, bias, o, row_max, row_sum, seqs=1, lengths=None, causal=True, scale=None, rng=None, p=0.0):
         t = _leading(q, 3, "q")[1]
-        _on(self._device, q=q, k=k, v=v, bias=bias, o=o, row_max=row_max, row_sum=row_sum, lengths=lengths, rng=rng)
+        _on(self._device, q, k, v, bias, o, row_max, row_sum, lengths, rng)
         stats = (self.n, self.heads, t)
         self._call("attention_forward", t, seqs, _ptr(lengths, _I32, (self.n, seqs), "lengths"), *self._inputs(t, q, k, v),
                    *self._how(bias, causal, scale, rng, p), *_strided(o, self.dtype, (self.n, t, self.heads * self.dim), 1, "o"),
@@ -601,7 +601,7 @@ class Attention(_TrainContext):
     def attention_backward(self, do, q, k, v, bias, o, row_max, row_sum, dq, dk, dv, dbias=None, seqs=1, lengths=None, causal=True, scale=None,
                            rng=None, p=0.0, accumulate=False):
         t = _leading(q, 3, "q")[1]
-        _on(self._device, do=do, q=q, k=k, v=v, bias=bias, o=o, row_max=row_max, row_sum=row_sum, dq=dq, dk=dk, dv=dv, dbias=dbias, lengths=lengths, rng=rng)
+        _on(self._device, do, q, k, v, bias, o, row_max, row_sum, dq, dk, dv, dbias, lengths, rng)
         wide, narrow, stats = (self.n, t, self.heads * self.dim), (self.n, t, self.kv_heads * self.dim), (self.n, self.heads, t)
         into = (None, 0)
         if dbias is not None:
