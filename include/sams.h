@@ -490,11 +490,13 @@ int dropout_backward(sams_dropout *ctx, int64_t t, const void *dy, int64_t dy_wo
  * [n][t][kv_heads * dim], and, per worker, dbias [n][heads][buckets] fp32 with the distance from worker to worker (or NULL); accumulate != 0 adds to
  * what dbias holds.  No output may overlap an input.
  *   starts_host  HOST pointer to `buckets` ascending numbers, copied; NULL with buckets == 0
- * 16-bit tensors are multiplied as they are, with P and its gradient rounded to their type between the products (f16: scaled by powers of two,
+ * Equal inputs give equal results, bit for bit.  16-bit tensors are multiplied as they are, with P and its gradient rounded to their type between the products (f16: scaled by powers of two,
  * so that small ones keep their digits); 32-bit ones in 32 bits.  Sums and the softmax are held in 32 bits.
  * Ranges: 1 <= heads <= SAMS_MAX_HEADS, kv_heads divides heads, 8 <= dim <= SAMS_MAX_HEAD_DIM, 0 <= buckets <= SAMS_MAX_BUCKETS, n * t_max <=
  * SAMS_MAX_TOKENS, seqs divides t, n * heads * seqs * (t / seqs / 128, rounded up) < 2^31.
- * Scratch with train != 0: 4 * n * heads * (t_max + buckets * (t_max / 64 + 64)) bytes; a backward pass needs it (SAMS_EINVAL otherwise).
+ * Scratch: 2 bytes for every distance between the second and the last bucket's start, up to 4096; with train != 0, which a backward pass needs (SAMS_EINVAL
+ * otherwise), 4 * n * heads * (t_max + buckets * (t_max / 32 + 64)) bytes, and, where n * kv_heads * t_max / 128 < 512, up to 16 times
+ * 8 * n * t_max * kv_heads * dim.
  */
 int sams_attn_create(sams_attn **out, int32_t n, int64_t t_max, int32_t heads, int32_t kv_heads, int32_t dim, int32_t buckets,
                      const int32_t *starts_host, int32_t type, int32_t train, void *hip_stream);

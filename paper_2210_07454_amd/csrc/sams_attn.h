@@ -81,7 +81,7 @@ __device__ __forceinline__ typename Fragment<T>::type words_of(const f32x16 &v, 
 }
 
 // ---- tiles in LDS ----
-// Rows of D numbers in pieces of 16 bytes, as many as a power of two; piece c of row r lies at c ^ turn(r).  So the pieces that sixteen lanes
+// Rows of D numbers in pieces of 16 bytes, as many as a power of two; piece c of row r lies at c ^ turn(r), without bank conflicts that way.  So the pieces that sixteen lanes
 // read at a time lie on different banks, whether they are one piece of sixteen rows, or four of each of four rows.  The turn of a row is that of
 // its bits one by one: a lane's part of an address is made once, and what the instruction adds to it comes by exclusive or.
 template <int PIECES>
@@ -176,7 +176,8 @@ template <int T, int D> struct Tile {
 };
 
 // The order of READS reads of LDS and MFMAS matrix instructions that stand before it: AHEAD reads are under way when the first matrix instruction
-// begins, and behind each come some more.  (Left to itself, the compiler reads a fragment, waits for it and uses it.)
+// begins, and behind each come some more.  (Left to itself, the compiler reads a fragment, waits for it and uses it: dk and dv of 8,192 tokens of 128 columns
+// 1.36 ms instead of 1.13, where a SIMD has one wavefront.)
 template <int READS, int MFMAS, int AHEAD>
 __device__ __forceinline__ void in_order()
 {
@@ -336,7 +337,7 @@ __device__ __forceinline__ void store_columns(typename TypeOf<T>::type *row, boo
 // of the distances in between by distance in LDS, and kReach more on both sides, so that such a tile's all are there; where
 // these are too many ("wide"), a tile is looked at for a start within its distances, and where there is one, the wavefront makes a table
 // of its own for it.
-constexpr int kReach = 96, kMaxTable = 4096;
+constexpr int kReach = 96, kMaxTable = 4096;     // 16 KB of LDS
 
 __device__ __forceinline__ float bias_of(float v)
 {
@@ -436,7 +437,9 @@ __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4
 
 __device__ __forceinline__ int uniform_wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-// wavefronts that a SIMD holds: what is more takes accumulators through moves
+// Wavefronts that a SIMD is to hold, as registers for them go: 256 for each of two, which cover each other's waits.  What the 96 columns' kernels keep in
+// memory for that costs less than one wavefront does (14 padded sequences' 10 heads of 72: dk and dv 85 us, alone 107; dq 40 and 52); at 128 columns it
+// costs more (8,192 tokens: dk and dv 1.12 ms alone, 2.4 as two).
 template <int T, int D> constexpr int kWavesPerSimd = (T == SAMS_F32 ? 2 : 1) * D <= 96 ? 2 : 1;
 
 template <int T, int D>
@@ -475,7 +478,8 @@ __device__ __forceinline__ Place place_of(const Args &a, gemm::Launch l, uint32_
 {
     Place p;
     // Workgroups go round the eight XCDs one by one.  Each XCD gets the tiles of some heads, so that they find keys and values in its L2; of those
-    // the heads' longest tiles come first, so that short ones are left for the end (8 workers' 12 heads of 1024: 71 -> 5x us).
+    // the heads' longest tiles come first, so that short ones are left for the end (8 workers' 12 heads of 1024: 71 -> 51 us forward, 89 -> 67 for dq,
+    // 176 -> 128 for dk and dv).
     uint32_t id, unit;
     const uint32_t units = l.total / a.tiles;
     if (units % 8 == 0 && gridDim.x == l.total) {
@@ -526,8 +530,9 @@ __device__ __forceinline__ int64_t stats_of(const Args &a, const Place &at, uint
 
 constexpr int kLdsBytes = 160 * 1024;
 
-// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make less than two for every CU (4 workers' 12 heads of 511
-// in 32 bits, forward: 59 -> xx us; where there are enough it costs: 8 workers' 12 heads of 1024 46 -> xx).
+// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them.  4 workers' 12 heads of 511 in 32 bits (192 workgroups):
+// forward 54 -> 41 us, dq 73 -> 50, dk and dv 119 -> 79; 48 heads of 1024 (384): forward 27 -> 23; but 14 padded sequences' 10 heads of 333 (420) 25 -> 31,
+// and 8 workers' 12 heads of 1024 (768) 46 -> 48.
 constexpr int64_t kFewBlocks = 400;
 static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
 template <int SPLIT> static inline uint32_t tiles_of(uint32_t len) { return (len + kOwn<SPLIT> - 1) / kOwn<SPLIT>; }
