@@ -530,11 +530,11 @@ __device__ __forceinline__ int64_t stats_of(const Args &a, const Place &at, uint
 
 constexpr int kLdsBytes = 160 * 1024;
 
-// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them.  4 workers' 12 heads of 511 in 32 bits (192 workgroups):
+// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them, or half of a workgroup's wavefronts had none.  4 workers' 12 heads of 511 in 32 bits (192 workgroups):
 // forward 54 -> 41 us, dq 73 -> 50, dk and dv 119 -> 79; 48 heads of 1024 (384): forward 27 -> 23; but 14 padded sequences' 10 heads of 333 (420) 25 -> 31,
-// and 8 workers' 12 heads of 1024 (768) 46 -> 48.
+// and 8 workers' 12 heads of 1024 (768) 46 -> 48.  64 sequences of 50, 16 heads of 64 over 4: forward 15 -> 13.5, backward 55 -> 48; of 40 in 32 bits, 12 heads: 30 -> 20, 104 -> 83.
 constexpr int64_t kFewBlocks = 400;
-static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
+static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return len <= kRows / 2 || heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
 template <int SPLIT> static inline uint32_t tiles_of(uint32_t len) { return (len + kOwn<SPLIT> - 1) / kOwn<SPLIT>; }
 // f(SPLIT), as a compile-time constant; tiles of 32 streamed rows are not split
 template <int ROWS, typename F>
