@@ -190,6 +190,10 @@ __device__ __forceinline__ void in_order()
     }
 }
 
+// What was read before this is under way before any of it is used.  (The compiler would wait for each number in turn: dk and dv of 14 padded sequences'
+// 10 heads of 72 79 us instead of 63, of 8 workers' 12 heads of 1024 107 instead of 100.)
+__device__ __forceinline__ void all_under_way() { __builtin_amdgcn_sched_barrier(0); }
+
 // ---- rows in memory ----
 // A piece of 16 bytes of a row of dim numbers is read where all of it exists: one that reaches past the row's end, or starts there, in its place
 // the row's last 16 bytes, of which `ended` makes what was meant.  (dim >= 8; rows start anywhere.)
@@ -463,8 +467,12 @@ __device__ __forceinline__ void add_bias(const float *from, bool one, float by, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by);
         } else {
+            float b[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, from[32 * j + row_of(i, lane)]);
+            for (int i = 0; i < 16; ++i) b[i] = from[32 * j + row_of(i, lane)];
+            all_under_way();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, b[i]);
         }
     }
 }
@@ -530,8 +538,8 @@ __device__ __forceinline__ int64_t stats_of(const Args &a, const Place &at, uint
 
 constexpr int kLdsBytes = 160 * 1024;
 
-// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them, or half of a workgroup's wavefronts had none.  4 workers' 12 heads of 511 in 32 bits (192 workgroups):
-// forward 54 -> 41 us, dq 73 -> 50, dk and dv 119 -> 79; 48 heads of 1024 (384): forward 27 -> 23; but 14 padded sequences' 10 heads of 333 (420) 25 -> 31,
+// Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them, or half of a workgroup's wavefronts had
+// none.  4 workers' 12 heads of 511 in 32 bits (192 workgroups): forward 54 -> 41 us, dq 73 -> 50, dk and dv 119 -> 79; 48 heads of 1024 (384): forward 27 -> 23; but 14 padded sequences' 10 heads of 333 (420) 25 -> 31,
 // and 8 workers' 12 heads of 1024 (768) 46 -> 48.  64 sequences of 50, 16 heads of 64 over 4: forward 15 -> 13.5, backward 55 -> 48; of 40 in 32 bits, 12 heads: 30 -> 20, 104 -> 83.
 constexpr int64_t kFewBlocks = 400;
 static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return len <= kRows / 2 || heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
@@ -546,7 +554,7 @@ static void by_split(bool halves, F f)
     f(std::integral_constant<int, 1>());
 }
 
-// One wavefront's 64 numbers of every lane for another one of the same rows, through LDS
+// N numbers of every lane of a wavefront for another one of the same rows, through LDS
 template <int N>
 __device__ __forceinline__ void give(float *lds, const float (&v)[N], int lane)
 {

@@ -72,17 +72,19 @@ struct BucketSums {
     {
         float up = 0.f, down = 0.f;             // distances lane % 32 and lane % 32 - 32
         const int half = lane & 32;
+        const int mine = (int)bias.bucket(a, corner + (lane ? lane : 1) - 32);
+        float rotated[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) rotated[i] = __shfl(ds[i], ((row_of(i, lane) + lane) & 31) | half);
+        all_under_way();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int r = row_of(i, lane);
-            const float v = __shfl(ds[i], ((r + lane) & 31) | half);
-            if ((lane & 31) + r < 32) up += v;
-            else down += v;
+            if ((lane & 31) + row_of(i, lane) < 32) up += rotated[i];
+            else down += rotated[i];
         }
         up = sum_halves(up);
         down = sum_halves(down);
         float v = half ? up : down;             // the distance lane - 32
-        const int mine = (int)bias.bucket(a, corner + (lane ? lane : 1) - 32);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {      // sums over the lanes of a bucket, which follow each other
             const float below = __shfl_up(v, o);
@@ -299,8 +301,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
 // dk, dv and dbias.  A workgroup has 128 keys, a lane (and the lane 32 from it) one; queries and the output's gradients come by tiles.  The
 // products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.  Where there are few keys
 // and heads of keys, a group's heads and a head's queries are shared out to several workgroups, whose sums another kernel joins.  The most of the three
-// kernels' work for every pair: four products, two of them with both sides through LDS, and what the bias's gradient takes (25 of 174 us of a backward pass of 8 workers' 12 heads of 1024
-// with 32 buckets).  107 us there, 480 TFLOP/s; 8,192 tokens' 16 heads of 128 columns, two heads of keys, 1.11 ms, 500 TFLOP/s.
+// kernels' work for every pair: four products, two of them with both sides through LDS, and what the bias's gradient takes (16 of 148 us of a backward pass of 8 workers' 12 heads of 1024
+// with 32 buckets).  100 us there, 260 TFLOP/s; 8,192 tokens' 16 heads of 128 columns, two heads of keys, 1.0 ms, 550 TFLOP/s, one wavefront a SIMD.
 template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
 {
@@ -410,7 +412,6 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             if (k0 < at.length && mine0 < at.length && (!a.causal || mine0 + NB * 32 - 1 >= k0) && !(one && by == -__builtin_inff())) {
                 typedef float f4 __attribute__((ext_vector_type(4)));
                 const f4 *st = (const f4 *)(stats + turn * 3 * BQ + half_of * 32) + (lane >> 5);       // a lane's rows are four next to each other at a time
-                auto stat_of = [&](int which, int j, int i) { return st[(which * BQ + 32 * j) / 4 + 2 * (i >> 2)][i & 3]; };
                 const bool edge = mine0 + NB * 32 > at.length || k0 + 32 > at.length || (a.causal && mine0 < k0 + 31);
                 const bool plain = one && !edge && fabsf(by) < 1e6f;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
@@ -425,16 +426,36 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), vf[c], dp);
                     if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, kAhead>();
+                    // the queries' statistics, read here where there are registers for them (8,192 tokens of 128 columns: 1.10 -> 0.99 ms; where two wavefronts share
+                    // a SIMD, 100 -> 106 us with 64 columns, 63 -> 84 with 72)
+                    constexpr bool EARLY = T != SAMS_F32 && kWavesPerSimd<T, D> == 1;
+                    auto four_of = [&](int which, int i) { return st[(which * BQ + 32 * j) / 4 + 2 * (i >> 2)]; };
+                    f4 early[EARLY ? 3 : 1][4];
+                    if constexpr (EARLY) {
+#pragma unroll
+                        for (int w = 0; w < 3; ++w)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) early[w][i] = four_of(w, 4 * i);
+                        all_under_way();
+                    }
+                    auto stat_of = [&](int which, int i) {
+                        if constexpr (EARLY) return early[which][i >> 2][i & 3];
+                        else return four_of(which, i)[i & 3];
+                    };
                     if (plain) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by - stat_of(0, j, i));
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by - stat_of(0, i));
                     } else {
                         if (one) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, j, i);
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, i);
                         } else {
+                            float b[16];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, biases[-(32 * j + row_of(i, lane))]) - stat_of(0, j, i);
+                            for (int i = 0; i < 16; ++i) b[i] = biases[-(32 * j + row_of(i, lane))];
+                            all_under_way();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, b[i]) - stat_of(0, i);
                         }
                         if (edge) {
 #pragma unroll
@@ -445,7 +466,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                         }
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * stat_of(1, j, i);
+                    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i]) * stat_of(1, i);
                     f32x16 pd = s;
                     if constexpr (DROP) {
                         // A generator's call is for one query and eight keys: every lane makes two of the 128 calls for its query, and takes what
@@ -462,14 +483,18 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
                         const int c = lane & 31;
                         const char *from = mine + ((c >> 4) * 2 + ((c >> 2) & 1)) * 16 + (((c >> 3) & 1) * 4 + (c & 3)) * 2;
+                        uint32_t number[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) pd[i] = *(const uint16_t *)(from + row_of(i, lane) * NUMBERS) >= a.keep.least ? s[i] : 0.f;
+                        for (int i = 0; i < 16; ++i) number[i] = *(const uint16_t *)(from + row_of(i, lane) * NUMBERS);
+                        all_under_way();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) pd[i] = number[i] >= a.keep.least ? s[i] : 0.f;
                         __builtin_amdgcn_wave_barrier();
                     }
                     // dS = m P dP - P delta, without the factor 1 / (1 - p), which delta has not either
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float delta = stat_of(2, j, i);
+                        const float delta = stat_of(2, i);
                         s[i] = DROP ? __builtin_fmaf(pd[i], dp[i], -(s[i] * delta)) : s[i] * (dp[i] - delta);
                     }
                     auto add_up = [&]() {
