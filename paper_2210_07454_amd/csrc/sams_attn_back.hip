@@ -503,7 +503,10 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                             else sums.many(a, bias, (int)k0 - (int)(mine0 + 32 * j), s, lane);
                         }
                     };
-                    if constexpr (T == SAMS_F16) add_up();          // before they are scaled
+                    // 16-bit floats: before they are scaled. 32-bit ones: behind the products stood a branch, and where it was
+                    // taken the compiler read the last product's last register after 13 of the 18 wait states that a
+                    // 32x32x2 product needs (dk wrong in that register's columns); in front, every such read has its 18.
+                    if constexpr (T != SAMS_BF16) add_up();
                     fit.fit(s, dk);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                         for (int d = 0; d < D / 32; ++d) dk[d] = product<T>(columns.read(0, 16 * half, d), ws, dk[d]);
                     }
                     if constexpr (T != SAMS_F32) in_order<D / 4, D / 8, 2 * kAhead>();
-                    if constexpr (T != SAMS_F16) add_up();          // while the matrix cores are at it
+                    if constexpr (T == SAMS_BF16) add_up();         // while the matrix cores are at it
                     if constexpr (NB == 2) {
                         rows.move(32 * Ti::LD);
                         columns.move(32 * Ti::LD);
