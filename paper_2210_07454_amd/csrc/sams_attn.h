@@ -15,6 +15,9 @@ using gemm::u32x4;
 constexpr int kThreads = 256, kWaves = 4, kRows = 128;
 template <int SPLIT> constexpr int kOwn = kRows / SPLIT;
 constexpr float kLog2e = 1.44269504088896340736f;
+// A bias, or a row's largest logit, of this size or more leaves less than three bits behind the point for the rest of a logit (in units of ln 2): what is added to one
+// later, or taken from it in another order, moves P by more than words of 16 bits show, and from 2^25 on by powers of two.
+constexpr float kLarge = 1e6f;
 
 struct Args {
     const void *q, *k, *v, *o, *dout;

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D>
                 // does in any other tile and in the backward pass.)
                 float times = scale;
                 const bool edge = mine + NB * 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
-                if (edge || !one || !(fabsf(by) < 1e6f)) {
+                if (edge || !one || !(fabsf(by) < kLarge)) {
                     add_bias<NB>(one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31)), one, by, scale, lane, s);
                     times = 1.f;
                     by = 0.f;
@@ -124,7 +124,20 @@ __global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D>
                         for (int i = 0; i < 16; ++i) acc[d][i] *= less;
                     top = most;
                 }
-                const float from = by - (top == -__builtin_inff() ? 0.f : top - SHIFT);
+                const float least = top == -__builtin_inff() ? 0.f : top;
+                float from = by - (least - SHIFT);
+                // A large logit loses the shift's digits: the largest one is taken from all first.  (Without, biases of -5e7 to -1e8 in all of a row
+                // made infinite words, and from -1e9 on its sum was 2^14 too small.)
+                if constexpr (T == SAMS_F16) {
+                    if (__any(fabsf(least) >= kLarge)) {
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by) - least;
+                        times = 1.f;
+                        from = SHIFT;
+                    }
+                }
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
 #pragma unroll

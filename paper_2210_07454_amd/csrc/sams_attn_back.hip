@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             d = sum_halves(d) / a.keep.scale;
         }
         const float top = live ? a.row_max[stat] : 0.f, total = live ? a.row_sum[stat] : 0.f;
+        const bool large = __any(fabsf(top) >= kLarge);
         over = total == 0.f ? 0.f : 1.f / total;
         ColumnScale<T, D> fit;
         fit.start();
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
             if (q0 < at.length && mine < at.length && (!a.causal || mine <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 const bool edge = mine + NB * 32 > at.length || q0 + 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
-                const bool plain = one && !edge && fabsf(by) < 1e6f;        // as in the forward pass
+                const bool plain = one && !edge && fabsf(by) < kLarge;        // as in the forward pass
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
                 const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)mine;
 #pragma unroll 1
@@ -204,6 +205,11 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
                         add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
                         times = 1.f;
                         from = SHIFT - top;
+                        if (T == SAMS_F16 && large) {               // as in the forward pass
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) s[0][i] -= top;
+                            from = SHIFT;
+                        }
                         if (edge) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) s[0][i] = 32 * j + row_of(i, lane) < limit ? s[0][i] : -__builtin_inff();
@@ -413,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 typedef float f4 __attribute__((ext_vector_type(4)));
                 const f4 *st = (const f4 *)(stats + turn * 3 * BQ + half_of * 32) + (lane >> 5);       // a lane's rows are four next to each other at a time
                 const bool edge = mine0 + NB * 32 > at.length || k0 + 32 > at.length || (a.causal && mine0 < k0 + 31);
-                const bool plain = one && !edge && fabsf(by) < 1e6f;
+                const bool plain = one && !edge && fabsf(by) < kLarge;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)mine0);        // of the first query
 #pragma unroll 1

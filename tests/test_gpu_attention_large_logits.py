@@ -1,0 +1,140 @@
+"""Attention where logits are so large that 32 bits of one have no place left for the products beside a bias, or a mask's lowest value is all that a
+row has: the output, the row statistics and the gradients of every type.
+
+A bias of 1e7 or more takes the rest of its logit in (products here are below 1.3, less than half of what a logit of 3e7 moves by), so that a row's weights go
+by its largest bias: equal ones for the keys that have it where it is that large, the softmax of the others' logits where it is a usual
+number.  Tolerances are those of tests/attention_oracle.py with an error of logits, es, only for keys that have a weight: 0 where it is a row's largest
+bias alone, which all its keys have in the same 32 bits."""
+import pytest
+import torch
+
+from tests import philox
+from tests.attention_oracle import HALF_ULP, U, bucket_of, check, rounded
+from tests.test_gpu_attention import TYPES, Run, make, sams  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+LARGE = 1e7
+LOWEST = torch.finfo(torch.float32).min
+
+
+def expected(x, starts, heads, kv_heads, causal=True, lengths=None, p=0.0, rng=None, scale=None):
+    """Outputs, gradients and sums of exponentials of one sequence a worker, what each may be off by, and the magnitudes that it is summed up from."""
+    kind, (n, t, wide) = x["q"].dtype, x["q"].shape
+    dim, group = wide // heads, heads // kv_heads
+    scale = dim ** -0.5 if scale is None else scale
+    word, tiny = (0.0 if kind == torch.float32 else HALF_ULP[kind]), 2.0 ** -38 if kind == torch.float16 else 0.0
+    split = lambda v, h: v.double().unflatten(2, (h, dim)).transpose(1, 2)                  # [n][heads][t][dim]
+    q, do = split(x["q"], heads), split(x["do"], heads)
+    k, v = (split(x[name], kv_heads).repeat_interleave(group, 1).contiguous() for name in ("k", "v"))
+    across = lambda m: m.transpose(-1, -2).contiguous()
+    length = torch.full((n,), t) if lengths is None else lengths[:, 0].long().clamp(0, t)
+    inside = torch.arange(t)[None, :] < length[:, None]
+    allowed = inside[:, None, :, None] & inside[:, None, None, :]
+    if causal:
+        allowed = allowed & torch.ones(t, t, dtype=torch.bool).tril()
+    products = scale * (q @ across(k))
+    b = x["bias"].double()[:, bucket_of(starts, t)][None] if starts else torch.zeros(1, heads, t, t, dtype=torch.float64)
+    most = torch.where(allowed, b, -torch.inf).amax(3, keepdim=True)
+    ruled = most.abs() >= LARGE                                                             # rows that one bias rules
+    near = b.abs() < LARGE
+    assert not starts or float(products.abs().max()) < 1.3
+    live = allowed & torch.where(ruled, b == most, near)
+    logits = torch.where(live, torch.where(ruled, 0.0, products + b), -torch.inf)
+    top = logits.amax(3, keepdim=True)
+    E = torch.where(live, torch.exp(logits - torch.where(torch.isfinite(top), top, 0.0)), 0.0)
+    sums = E.sum(3, keepdim=True)
+    P = E / sums.clamp(min=1e-300)
+    usual = live & ~ruled
+    es = torch.where(usual, (dim + 4) * U * abs(scale) * (q.abs() @ across(k.abs())) + 4 * U * (torch.where(usual, logits.abs() + b.abs(), 0.0) + torch.where(usual, top.abs(), 0.0)), 0.0)
+    ep = es + es.amax(3, keepdim=True) + (t + 24) * U
+    more = word + (t + 24) * U
+    m = torch.ones(n, heads, t, t, dtype=torch.float64)
+    if p:
+        m = torch.from_numpy(philox.keep_pairs(rng, torch.arange(n * heads).numpy(), t, p)).double().reshape(n, heads, t, t) / (1 - philox.least(p) / 65536)
+    share = 1 - philox.least(p) / 65536
+    PD = P * m
+    o = PD @ v
+    some = live.any(3, keepdim=True)
+    eo = (PD * (ep + more)) @ v.abs() + torch.where(some, tiny * v.abs().sum(2, keepdim=True) / share, 0.0)
+    ro = rounded(o, eo, kind)
+    dP = (do @ across(v)) * m
+    delta = (P * dP).sum(3, keepdim=True)
+    dS = P * (dP - delta)
+    edp = (dim + 4) * U * m * (do.abs() @ across(v.abs()))
+    ed = (P * (edp + dP.abs() * (ep + (t + 4) * U))).sum(3, keepdim=True)
+    eds = P * (edp + ed) + dS.abs() * (ep + 4 * U)
+    ew = eds + dS.abs() * more
+    # the rounding of do . o is taken back at the end by sum P k, whose P's are words
+    back = more * (do.abs() * ro).sum(3, keepdim=True)
+    joined = lambda w: w.unflatten(1, (kv_heads, group)).sum(2)
+    rows = lambda w: w.transpose(1, 2).reshape(n, t, -1)
+    want, tol = {"o": rows(o), "dq": rows(scale * (dS @ k)), "dk": rows(joined(scale * (across(dS) @ q))), "dv": rows(joined(across(PD) @ do))}, {"o": rows(ro)}
+    tol["dq"] = rows(abs(scale) * (back * (P @ k.abs()) + (ew + back * P + tiny * dS.abs().amax(3, keepdim=True)) @ k.abs()))
+    tol["dk"] = rows(joined(abs(scale) * (across(ew + tiny * dS.abs().amax(2, keepdim=True)) @ q.abs()))) * (1 + group * U)
+    tol["dv"] = rows(joined(across(PD * (ep + more)) @ do.abs() + tiny * do.abs().sum(2, keepdim=True) / share)) * (1 + group * U)
+    for name in ("dq", "dk", "dv"):
+        tol[name] = rounded(want[name], tol[name], kind)
+    if starts:
+        which = torch.nn.functional.one_hot(bucket_of(starts, t), len(starts)).double()
+        want["dbias"] = torch.tensordot(dS, which, 2)
+        count = which.sum((0, 1))
+        tol["dbias"] = rounded(want["dbias"], torch.tensordot(eds, which, 2) + torch.tensordot(dS.abs(), which, 2) * (count + 72) * U, torch.float32)
+    want["row_sum"], tol["row_sum"] = sums[..., 0], sums[..., 0] * (ep.amax(3) + (t + 24) * U)
+    sd = P * (dP.abs() + delta.abs())
+    size = {"o": rows(PD @ v.abs()), "dq": rows(abs(scale) * (sd @ k.abs())), "dk": rows(joined(abs(scale) * (across(sd) @ q.abs()))), "dv": rows(joined(across(PD) @ do.abs())),
+            "row_sum": want["row_sum"]}
+    if starts:
+        size["dbias"] = torch.tensordot(sd, which, 2)
+    return want, tol, size
+
+
+def compare(got, want, tol, size, name):
+    """The tolerance is one that only right numbers keep to: 1 % of the magnitudes that a number is summed up from at most."""
+    assert float(tol[name].max()) <= 0.01 * float(size[name].max()), name
+    check(got, want[name], tol[name], name)
+
+
+# n, t, heads, kv_heads, dim: two wavefronts for 32 rows, and one (enough workgroups for that)
+SIZES = [(1, 130, 2, 1, 64), (1, 50, 2, 2, 40), (2, 130, 104, 52, 16)]
+# The bias's large buckets, of distances up to -9, from -8 on to -1, 0 and above: a first row, or the first rows, without another key, tiles of mixed buckets
+# and of one, every row
+WHERE = {"own": [2], "near": [1, 2], "far": [0], "all": [0, 1, 2, 3]}
+
+
+def inputs(kind, size, buckets, low):
+    n, t, heads, kv_heads, dim = size
+    x = make(n, t, heads, kv_heads, dim, 4, kind, seed=5)
+    x["q"] = (x["q"].clamp(-3, 3) * 0.125).to(kind)
+    x["k"] = x["k"].clamp(-2, 2)
+    x["bias"][:, buckets] = low
+    return x, [-(2 ** 31), -8, 0, 1]
+
+
+@pytest.mark.parametrize("low", [-3e7, -5e7, -1e8, -1e9, LOWEST, 3e7, 1e9], ids=str)
+@pytest.mark.parametrize("where", WHERE)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+def test_output_beside_large_biases(sams, kind, size, where, low):
+    x, starts = inputs(kind, size, WHERE[where], low)
+    n, t, heads, kv_heads, dim = size
+    for causal in (True, False):
+        run = Run(sams, x, starts, heads, kv_heads, train=False, causal=causal)
+        right = expected(x, starts, heads, kv_heads, causal)
+        for name, got in (("row_sum", run.row_sum), ("o", run.o)):
+            compare(got, *right, name)
+
+
+@pytest.mark.parametrize("low", [-3e7, -1e8, -1e9, LOWEST, 3e7], ids=str)
+@pytest.mark.parametrize("where", WHERE)
+@pytest.mark.parametrize("size", SIZES, ids=str)
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+def test_gradients_beside_large_biases(sams, kind, size, where, low):
+    x, starts = inputs(kind, size, WHERE[where], low)
+    n, t, heads, kv_heads, dim = size
+    lengths = torch.full((n, 1), t - 3, dtype=torch.int32)
+    for how in (dict(causal=True), dict(causal=False, p=0.2, rng=torch.tensor([11, 12]), lengths=lengths)):
+        run = Run(sams, x, starts, heads, kv_heads, **how)
+        right = expected(x, starts, heads, kv_heads, **how)
+        for name, got in run.outputs().items():
+            compare(got, *right, name)
