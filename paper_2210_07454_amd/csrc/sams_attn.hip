@@ -126,17 +126,16 @@ __global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D>
                 }
                 const float least = top == -__builtin_inff() ? 0.f : top;
                 float from = by - (least - SHIFT);
-                // A large logit loses the shift's digits: the largest one is taken from all first.  (Without, biases of -5e7 to -1e8 in all of a row
-                // made infinite words, and from -1e9 on its sum was 2^14 too small.)
-                if constexpr (T == SAMS_F16) {
-                    if (__any(fabsf(least) >= kLarge)) {
+                // Beside a large logit the shift's digits are lost, and what is taken off here is not what every product is rounded to: the largest logit is
+                // taken from rounded ones first.  (Without, biases of -5e7 to -1e8 in all of a row made infinite words of 16-bit floats, from -1e9 on its sum
+                // was 2^14 too small, and logits of 2^32 made infinities or zeros of weights of 1 in any type.)
+                if (__any(fabsf(least) >= kLarge)) {
 #pragma unroll
-                        for (int j = 0; j < NB; ++j)
+                    for (int j = 0; j < NB; ++j)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by) - least;
-                        times = 1.f;
-                        from = SHIFT;
-                    }
+                        for (int i = 0; i < 16; ++i) s[j][i] = __builtin_fmaf(s[j][i], times, by) - least;
+                    times = 1.f;
+                    from = SHIFT;
                 }
 #pragma unroll
                 for (int j = 0; j < NB; ++j)

@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
             const bool one = bias.one(a, lo, lo + NB * 32 - 1 + 31, bucket, by);
             if (q0 < at.length && mine < at.length && (!a.causal || mine <= q0 + 31) && !(one && by == -__builtin_inff())) {
                 const bool edge = mine + NB * 32 > at.length || q0 + 32 > at.length || (a.causal && mine + NB * 32 - 1 > q0);
-                const bool plain = one && !edge && fabsf(by) < kLarge;        // as in the forward pass
+                const bool plain = one && !edge && fabsf(by) < kLarge && !large;    // as in the forward pass
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, lo + 31 - (lane & 31));
                 const int limit = (live ? (int)(a.causal ? query + 1 : at.length) : 0) - (int)mine;
 #pragma unroll 1
@@ -411,6 +411,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
             const bool more = next_head <= last;
             if (more) load(next_head, next_query0);
             const uint32_t mine0 = query0 + half_of * 32;           // the wavefront's first query
+            const bool large = __any(fabsf(stats[turn * 3 * BQ + half_of * 32 + (lane & (NB * 32 - 1))]) >= kLarge);
             const int lo = (int)k0 - (int)(mine0 + NB * 32 - 1);
             uint32_t bucket;
             float by;
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                 typedef float f4 __attribute__((ext_vector_type(4)));
                 const f4 *st = (const f4 *)(stats + turn * 3 * BQ + half_of * 32) + (lane >> 5);       // a lane's rows are four next to each other at a time
                 const bool edge = mine0 + NB * 32 > at.length || k0 + 32 > at.length || (a.causal && mine0 < k0 + 31);
-                const bool plain = one && !edge && fabsf(by) < kLarge;
+                const bool plain = one && !edge && fabsf(by) < kLarge && !large;
                 const uint32_t stream = (at.worker * a.seqs + at.seq) * a.heads + head;
                 const float *biases = one ? nullptr : bias.at(a, wave, lo, (int)key - (int)mine0);        // of the first query
 #pragma unroll 1

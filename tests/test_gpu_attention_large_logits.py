@@ -138,3 +138,34 @@ def test_gradients_beside_large_biases(sams, kind, size, where, low):
         right = expected(x, starts, heads, kv_heads, **how)
         for name, got in run.outputs().items():
             compare(got, *right, name)
+
+
+# n, t, heads, dim: tiles of 32 or 64 keys inside the sequence, and such as reach past its end
+@pytest.mark.parametrize("size", [(1, 192, 2, 64), (1, 100, 1, 128), (1, 128, 3, 16), (2, 128, 200, 8)], ids=str)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+def test_large_products(sams, kind, causal, size):
+    """Rows whose own key's logit is 2^28 (16-bit floats) or 2^38, and the other keys' are 2^25 or 2^35 lower at least: all weight on the own key, whatever
+    32 bits make of such a logit.  Products are whole multiples of a power of two that 32 bits hold."""
+    n, t, heads, dim = size
+    gen = torch.Generator().manual_seed(t + dim)
+    # signs of a row, no two alike and, of 8 columns, by a column of the row's number
+    signs = torch.randint(0, 2, (n, t, heads, dim), generator=gen) * 2 - 1
+    if dim < 64:
+        bits = torch.arange(t)[:, None] >> torch.arange(8)[None, :] & 1
+        signs[..., :8] = (bits * 2 - 1)[None, :, None, :]
+    size_of = 2.0 ** 11 if kind == torch.float16 else 2.0 ** 16
+    whole = (signs * size_of).reshape(n, t, heads * dim).to(kind)
+    x = make(n, t, heads, heads, dim, 0, kind, seed=2)
+    x["q"], x["k"] = whole, whole.clone()
+    how = dict(causal=causal, scale=64.0 / dim)
+    run = Run(sams, x, [], heads, heads, **how)
+    assert torch.equal(run.row_sum, torch.ones_like(run.row_sum))
+    assert torch.equal(run.o.cpu(), x["v"])
+    assert torch.equal(run.dv.cpu(), x["do"])
+    # dS is 0 in 64 bits; in 32, what the sums do . v, made twice, are off by from one another, times the row's own key
+    slack = (dim + 4) * U * (x["do"].double() * x["v"].double()).abs().reshape(n, t, heads, dim).sum(-1, keepdim=True)
+    slack = (2 * how["scale"] * size_of * slack).expand(-1, -1, -1, dim).reshape(n, t, -1)
+    word = 0.0 if kind == torch.float32 else HALF_ULP[kind]
+    for got in (run.dq, run.dk):
+        check(got, torch.zeros_like(slack), slack * (1 + 2 * word) + 2.0 ** -25, "a row's own key")
