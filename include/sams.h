@@ -483,13 +483,16 @@ int dropout_backward(sams_dropout *ctx, int64_t t, const void *dy, int64_t dy_wo
  *     are its own, the rest is padding: it may hold anything (NaN included), changes nothing, and its rows of o and of all gradients are 0
  *   bias [heads][buckets] fp32; given exactly if the context has buckets.  Bucket b is the distances j - i from starts_host[b] to
  *     starts_host[b + 1] - 1; what lies before starts_host[1] belongs to bucket 0, whose start is not looked at.  A bias of minus infinity bans the bucket's keys;
- *     a row without any key left has o = 0 and gradients 0.
+ *     a row without any key left has o = 0 and gradients 0.  Finite ones may be as large as they come (beyond 1.17e38 they count as that): logits are held in 32
+ *     bits, so that a row that has only keys with a bias of -1e9, or the type's lowest value, has equal weights for those of the largest.
  *   rng, p as for dropout
  *   row_max, row_sum [n][heads][t] fp32 out, contiguous: a row's largest logit (in units of ln 2) and its sum of exponentials, for the backward pass
  * Backward, from o, row_max and row_sum of the forward pass with the same other arguments: of sum(dout * o), dq [n][t][heads * dim], dk, dv
  * [n][t][kv_heads * dim], and, per worker, dbias [n][heads][buckets] fp32 with the distance from worker to worker (or NULL); accumulate != 0 adds to
  * what dbias holds.  No output may overlap an input.
  *   starts_host  HOST pointer to `buckets` ascending numbers, copied; NULL with buckets == 0
+ * Numbers of a sequence's own tokens have to be finite: an infinity or NaN may reach all rows of its sequence, since a key without weight (a later one with causal, a
+ * banned or a dropped one) enters the products as 0 times its value.
  * Equal inputs give equal results, bit for bit.  16-bit tensors are multiplied as they are, with P and its gradient rounded to their type between the products (f16: scaled by powers of two,
  * so that small ones keep their digits); 32-bit ones in 32 bits.  Sums and the softmax are held in 32 bits.
  * Ranges: 1 <= heads <= SAMS_MAX_HEADS, kv_heads divides heads, 8 <= dim <= SAMS_MAX_HEAD_DIM, 0 <= buckets <= SAMS_MAX_BUCKETS, n * t_max <=

@@ -15,8 +15,9 @@ using gemm::u32x4;
 constexpr int kThreads = 256, kWaves = 4, kRows = 128;
 template <int SPLIT> constexpr int kOwn = kRows / SPLIT;
 constexpr float kLog2e = 1.44269504088896340736f;
-// A bias, or a row's largest logit, of this size or more leaves less than three bits behind the point for the rest of a logit (in units of ln 2): what is added to one
-// later, or taken from it in another order, moves P by more than words of 16 bits show, and from 2^25 on by powers of two.
+// A bias, or a row's largest logit, of this size or more leaves a logit (in units of ln 2) four bits behind the point at most, so that the order in which
+// numbers are added to it moves P by more than a word of 16 bits shows, and from 2^25 on by powers of two.  From here on logits are rounded as sums first, the same in
+// all kernels, before the largest is taken off.
 constexpr float kLarge = 1e6f;
 
 struct Args {
@@ -84,9 +85,9 @@ __device__ __forceinline__ typename Fragment<T>::type words_of(const f32x16 &v, 
 }
 
 // ---- tiles in LDS ----
-// Rows of D numbers in pieces of 16 bytes, as many as a power of two; piece c of row r lies at c ^ turn(r), without bank conflicts that way.  So the pieces that sixteen lanes
-// read at a time lie on different banks, whether they are one piece of sixteen rows, or four of each of four rows.  The turn of a row is that of
-// its bits one by one: a lane's part of an address is made once, and what the instruction adds to it comes by exclusive or.
+// Rows of D numbers have room for a power of two of pieces of 16 bytes; piece c of row r lies at c ^ turn(r).  So the pieces that sixteen lanes read at a time lie on
+// different banks, whether they are one piece of sixteen rows, or four of each of four rows (counters show no bank conflict in any kernel).  The
+// turn of a row is that of its bits one by one: a lane's part of an address is made once, and what the instruction adds to it comes by exclusive or.
 template <int PIECES>
 __host__ __device__ constexpr uint32_t turn(uint32_t r)
 {
@@ -344,7 +345,7 @@ __device__ __forceinline__ void store_columns(typename TypeOf<T>::type *row, boo
 // of the distances in between by distance in LDS, and kReach more on both sides, so that such a tile's all are there; where
 // these are too many ("wide"), a tile is looked at for a start within its distances, and where there is one, the wavefront makes a table
 // of its own for it.
-constexpr int kReach = 96, kMaxTable = 4096;     // 16 KB of LDS
+constexpr int kReach = 96, kMaxTable = 4096;     // 16 KB of LDS, 24 where the bias's gradient is made
 
 __device__ __forceinline__ float bias_of(float v)
 {
@@ -543,7 +544,8 @@ constexpr int kLdsBytes = 160 * 1024;
 
 // Whether workgroups have two wavefronts for every 32 rows: where 128 rows each would make few of them, or half of a workgroup's wavefronts had
 // none.  4 workers' 12 heads of 511 in 32 bits (192 workgroups): forward 54 -> 41 us, dq 73 -> 50, dk and dv 119 -> 79; 48 heads of 1024 (384): forward 27 -> 23; but 14 padded sequences' 10 heads of 333 (420) 25 -> 31,
-// and 8 workers' 12 heads of 1024 (768) 46 -> 48.  64 sequences of 50, 16 heads of 64 over 4: forward 15 -> 13.5, backward 55 -> 48; of 40 in 32 bits, 12 heads: 30 -> 20, 104 -> 83.
+// and 8 workers' 12 heads of 1024 (768) 46 -> 48.  64 sequences of 50, 16 heads of 64 over 4: forward 15 -> 13.5, backward 55 -> 48; of 40 in 32 bits, 12 heads: 30 -> 20, 104 -> 83.  The limit lies between the 384 and 420 measured, of two widths, and is
+// one for all kernels and widths.
 constexpr int64_t kFewBlocks = 400;
 static inline bool in_halves(int64_t heads_in_all, uint32_t len) { return len <= kRows / 2 || heads_in_all * ((len + kRows - 1) / kRows) < kFewBlocks; }
 template <int SPLIT> static inline uint32_t tiles_of(uint32_t len) { return (len + kOwn<SPLIT> - 1) / kOwn<SPLIT>; }

@@ -14,11 +14,12 @@ namespace attn {
 // S' = K Q' and O' = V' P', so that a query's logits are a lane's own accumulators, which become the second product's operand as they are.
 // Keys and values come by tiles through LDS, the next ones on their way in registers meanwhile.  Every wavefront reads all of them from LDS.
 //
-// Bound by what the vector units do beside the products: for every number a scale, a maximum, an exponential (four times an ordinary instruction's time), a sum, half a
-// conversion, and with dropout an eighth of a generator's call; at 64 columns that is three times the products' own time.  8 workers' 12 heads of 1024 x 64 bf16,
-// causal, with bias and dropout: 46 us (36 without both), 280 TFLOP/s; 8,192 tokens' 16 heads of 128 columns: 355 us, 775 TFLOP/s; 4 workers' 12 heads of 511 in
-// 32 bits, whose products take eight instructions of twice the time each: 41 us.  Three wavefronts a SIMD up to 64 columns (51 -> 46 us; four keep
-// registers in memory: 57).
+// Bound by waiting: within a wavefront loads from LDS, products, maximum, exponentials, second product and barrier follow each other, and one to three
+// wavefronts a SIMD do not fill the gaps.  8 workers' 12 heads of 1024 x 64 bf16, causal, with bias and dropout, 46 us (36 without both), 280 TFLOP/s: vector
+// instructions issue in 66 % of a SIMD's time (for every number a scale, a maximum, an exponential, which takes four times as long, a sum, half a
+// conversion, an eighth of a generator's call), its matrix core is busy in 16 %, and a wavefront waits in 42 % of its time.  8,192 tokens' 16 heads of 128
+// columns, 365 us, 750 TFLOP/s: 49, 38 and 40 %.  4 workers' 12 heads of 511 in 32 bits, whose products take eight instructions of twice the
+// time each, 41 us: 24, 41 and 29 %.  Three wavefronts a SIMD up to 64 columns (51 -> 46 us; four keep registers in memory: 57).
 template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D> : D <= 64 ? 3 : 2)) k_attn_forward(Args a, gemm::Launch launch)
 {

@@ -100,8 +100,9 @@ struct BucketSums {
 // dq and delta; laid out as the forward pass.  o has been rounded to 16 bits: what do . o is off by is small beside dP, but not beside the
 // 32 bits that dbias is held to.  So delta is also added up as it is defined, sum P dP, for the other kernel, and dq, which needs it before that
 // sum is done, is put right at the end: dq = scale (sum P (dP - d) k + (d - delta) sum P k), with d = do . o.  (Without: dbias off by 2.6e-3, dq by 2.6e-3
-// instead of 2.4e-3.)  Bound as the forward pass: 8 workers' 12 heads of 1024 x 64 bf16 64 us, of four products 400 TFLOP/s; 8,192 tokens' 16 heads of 128
-// columns 650 us, 845 TFLOP/s, one wavefront a SIMD with 380 registers.
+// instead of 2.4e-3; sum P k takes a quarter of the products.)  Bound as the forward pass: 8 workers' 12 heads of 1024 x 64 bf16 65 us, 400 TFLOP/s with sum P k and
+// 300 without it, vector instructions in 56 % of a SIMD's time, the matrix core in 23 %; 8,192 tokens' 16 heads of 128 columns 677 us, 810 TFLOP/s (610), 35
+// and 36 %, one wavefront a SIMD with 380 registers, which waits in 32 % of its time.
 template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Args a, gemm::Launch launch)
 {
@@ -308,7 +309,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
 // products are S = Q K' and dP = dO V', whose accumulators become the second operands of dV' = dO' P and dK' = Q' dS as they are.  Where there are few keys
 // and heads of keys, a group's heads and a head's queries are shared out to several workgroups, whose sums another kernel joins.  The most of the three
 // kernels' work for every pair: four products, two of them with both sides through LDS, and what the bias's gradient takes (16 of 148 us of a backward pass of 8 workers' 12 heads of 1024
-// with 32 buckets).  100 us there, 260 TFLOP/s; 8,192 tokens' 16 heads of 128 columns, two heads of keys, 1.0 ms, 550 TFLOP/s, one wavefront a SIMD.
+// with 32 buckets).  103 us there, 250 TFLOP/s: vector instructions in 46 % of a SIMD's time, the matrix core busy in 13 %, a wavefront waiting in 48 % of its own; 8,192 tokens' 16
+// heads of 128 columns, two heads of keys, 1.05 ms, 520 TFLOP/s, one wavefront a SIMD: 29, 23 and 43 %.
 template <int T, int D, bool DROP, int SPLIT>
 __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Args a, gemm::Launch launch, int64_t parts)
 {
@@ -512,7 +514,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     };
                     // 16-bit floats: before they are scaled. 32-bit ones: behind the products stood a branch, and where it was
                     // taken the compiler read the last product's last register after 13 of the 18 wait states that a
-                    // 32x32x2 product needs (dk wrong in that register's columns); in front, every such read has its 18.
+                    // 32x32x2 product needs (dk wrong in that register's columns); in front, every such read has its 18
+                    // (tests/test_isa_product_waits.py follows every path of the library's code).
                     if constexpr (T != SAMS_BF16) add_up();
                     fit.fit(s, dk);
 #pragma unroll
