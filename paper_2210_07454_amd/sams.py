@@ -535,8 +535,8 @@ class Dropout(_TrainContext):
 
 def relative_buckets(buckets: int, max_distance: int, causal: bool = True):
     """First distances (key minus query) of ``buckets`` buckets, for ``Attention``: one by one near the query, then stretches whose lengths grow
-    by a constant factor up to ``max_distance``, from which on all distances share a bucket (with more buckets than distances up to it, from where they are used up).  causal: keys up to the query; otherwise one bucket
-    for the query itself, and the others shared out to both sides."""
+    by a constant factor up to ``max_distance``, from which on all distances share a bucket (with more buckets than distances up to it, from where
+    the buckets are used up).  causal: keys up to the query; otherwise one bucket for the query itself, and the others shared out to both sides."""
     if buckets < 1 or max_distance < 1:
         raise ValueError("relative_buckets: buckets and max_distance have to be at least 1")
 
