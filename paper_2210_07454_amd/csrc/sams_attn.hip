@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kThreads, (T == SAMS_F32 ? kWavesPerSimd<T, D>
         bv.load(v, a.vs.row, 0, at.length, a.dim);
         typename Ti::Frag qf[D / 16];
         row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head), a.qs.row, query, at.length, a.dim, lane, qf);
-        // the scale's sign goes into q, so that the largest product is the largest logit
+        // the scale's sign goes into q (and, in dk's kernel, k), so that the largest product is the largest logit
         const float scale = fabsf(a.scale2);
         if (a.scale2 < 0.f) flip<T, D>(qf);
         bias.bring_starts(a);

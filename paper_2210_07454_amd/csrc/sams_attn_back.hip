@@ -143,6 +143,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
         bv.load(v, a.vs.row, 0, at.length, a.dim);
         typename Ti::Frag qf[D / 16], df[D / 16];
         row_fragments<T, D>(rows_of<T>(a.q, a.qs, a, at, at.head), a.qs.row, query, at.length, a.dim, lane, qf);
+        // as in the forward pass: the matrix cores' sums of 16-bit words' products are not always negated with the words (those of 32-bit numbers are)
+        const float scale = ROUNDED ? fabsf(a.scale2) : a.scale2;
+        if (ROUNDED && a.scale2 < 0.f) flip<T, D>(qf);
         row_fragments<T, D>(rows_of<T>(a.dout, a.douts, a, at, at.head), a.douts.row, query, at.length, a.dim, lane, df);
         // do . o, less the factor 1 / (1 - p) that dP is made without
         float d = 0.f, exact = 0.f;
@@ -201,9 +204,9 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dq(Arg
 #pragma unroll
                     for (int c = 0; c < D / 16; ++c) dp = product<T>(rows.read(2 * Ti::BYTES, 0, c), df[c], dp);
                     if constexpr (T != SAMS_F32) in_order<D / 8, D / 8, kAhead>();
-                    float times = a.scale2, from = by - top + SHIFT;
+                    float times = scale, from = by - top + SHIFT;
                     if (!plain) {
-                        add_bias<1>(biases + 32 * j, one, by, a.scale2, lane, s);
+                        add_bias<1>(biases + 32 * j, one, by, scale, lane, s);
                         times = 1.f;
                         from = SHIFT - top;
                         if (T == SAMS_F16 && large) {               // as in the forward pass
@@ -400,6 +403,8 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
         typename Ti::Frag kf[D / 16], vf[D / 16];
         row_fragments<T, D>(rows_of<T>(a.k, a.ks, a, at, at.head), a.ks.row, key, at.length, a.dim, lane, kf);
         row_fragments<T, D>(rows_of<T>(a.v, a.vs, a, at, at.head), a.vs.row, key, at.length, a.dim, lane, vf);
+        const float scale = T == SAMS_F32 ? a.scale2 : fabsf(a.scale2);
+        if (T != SAMS_F32 && a.scale2 < 0.f) flip<T, D>(kf);        // products as the other kernels make them
         bias.bring(a, head);
         store(query0, 0);
         typename Ti::Along rows;
@@ -453,18 +458,18 @@ __global__ void __launch_bounds__(kThreads, (kWavesPerSimd<T, D>)) k_attn_dkv(Ar
                     };
                     if (plain) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by - stat_of(0, i));
+                        for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale, by - stat_of(0, i));
                     } else {
                         if (one) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, by) - stat_of(0, i);
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale, by) - stat_of(0, i);
                         } else {
                             float b[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) b[i] = biases[-(32 * j + row_of(i, lane))];
                             all_under_way();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], a.scale2, b[i]) - stat_of(0, i);
+                            for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], scale, b[i]) - stat_of(0, i);
                         }
                         if (edge) {
 #pragma unroll

@@ -169,3 +169,39 @@ def test_large_products(sams, kind, causal, size):
     word = 0.0 if kind == torch.float32 else HALF_ULP[kind]
     for got in (run.dq, run.dk):
         check(got, torch.zeros_like(slack), slack * (1 + 2 * word) + 2.0 ** -25, "a row's own key")
+
+
+# n, t, heads, dim
+@pytest.mark.parametrize("size", [(1, 137, 3, 64), (1, 300, 2, 96), (1, 70, 4, 113), (2, 130, 104, 16)], ids=str)
+@pytest.mark.parametrize("scale", [1.0, 0.3, -0.5, -1.0])
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+def test_large_products_of_any_number(sams, kind, scale, size):
+    """Logits of 1e7 and more that 32 bits hold to whole numbers or hundreds: which of two near ones is larger is left to rounding, but every kernel has to see it alike.
+    A weight is at most 1 and a row's sum to 1, so that o is at most the largest v, a key's dv the sum of all rows' do, dS of a row P (|dP| + |delta|) with P summing to 1; and
+    where one logit is above all others by more than its roundings, o is that key's v."""
+    n, t, heads, dim = size
+    x = make(n, t, heads, heads, dim, 0, kind, seed=8)
+    for name in ("q", "k"):
+        x[name] = (x[name].clamp(-4, 4) * (4000 if kind == torch.float16 else 1e6)).to(kind)
+    run = Run(sams, x, [], heads, heads, scale=scale, causal=False)
+    q, k, v, do = (x[name].double().unflatten(2, (heads, dim)).transpose(1, 2) for name in ("q", "k", "v", "do"))
+    across = lambda m: m.transpose(-1, -2).contiguous()
+    o, dq, dk, dv = (got.cpu().double().unflatten(2, (heads, dim)).transpose(1, 2) for got in (run.o, run.dq, run.dk, run.dv))
+    assert all(bool(torch.isfinite(got).all()) for got in (o, dq, dk, dv))
+    sums = run.row_sum.cpu()
+    assert (sums >= 1).all() and (sums <= t).all()
+    # a word's rounding of P and of dS each, an output's, and a rounding of 32 bits for each number of a sum
+    word = HALF_ULP[kind] if kind != torch.float32 else U
+    more = 1 + 4 * word + 4 * (t + dim) * U
+    assert (o.abs() <= v.abs().amax(2, keepdim=True) * more).all()
+    assert (dv.abs() <= do.abs().sum(2, keepdim=True) * more).all()
+    most = (do.abs() @ across(v.abs())).amax(3)                                             # of |dP| and |delta| in a row
+    assert (dq.abs() <= abs(scale) * 2 * most[..., None] * k.abs().amax(2, keepdim=True) * more).all()
+    assert (dk.abs() <= abs(scale) * (2 * most[..., None] * q.abs()).sum(2, keepdim=True) * more).all()
+    logits = scale * (q @ across(k))
+    top, which = logits.max(3)
+    below = logits.scatter(3, which[..., None], -torch.inf).amax(3)
+    off = 2 * abs(scale) * ((dim + 8) * U * (q.abs() @ across(k.abs()))).amax(3)             # (dim + 4) roundings of a product and four of the logit, two logits
+    sure = top - below > off + 120                                                          # e^-120 is no number beside 1, in any type
+    assert float(sure.double().mean()) > 0.9
+    assert torch.equal(o[sure], v.gather(2, which[..., None].expand(-1, -1, -1, dim))[sure])
