@@ -140,6 +140,20 @@ def test_gradients_beside_large_biases(sams, kind, size, where, low):
             compare(got, *right, name)
 
 
+def signs(size, kind, by):
+    """Queries and keys of plus or minus `by`, a row's query like its key, no two rows of a head alike."""
+    n, t, heads, dim = size
+    gen = torch.Generator().manual_seed(t + dim)
+    rows = torch.randint(0, 2, (n, t, heads, dim), generator=gen) * 2 - 1
+    if dim < 64:                                                    # by the bits of the row's number
+        bits = torch.arange(t)[:, None] >> torch.arange(8)[None, :] & 1
+        rows[..., :8] = (bits * 2 - 1)[None, :, None, :]
+    x = make(n, t, heads, heads, dim, 0, kind, seed=2)
+    x["q"] = (rows * by).reshape(n, t, heads * dim).to(kind)
+    x["k"] = x["q"].clone()
+    return x
+
+
 # n, t, heads, dim: tiles of 32 or 64 keys inside the sequence, and such as reach past its end
 @pytest.mark.parametrize("size", [(1, 192, 2, 64), (1, 100, 1, 128), (1, 128, 3, 16), (2, 128, 200, 8)], ids=str)
 @pytest.mark.parametrize("causal", [True, False])
@@ -148,16 +162,8 @@ def test_large_products(sams, kind, causal, size):
     """Rows whose own key's logit is 2^28 (16-bit floats) or 2^38, and the other keys' are 2^25 or 2^35 lower at least: all weight on the own key, whatever
     32 bits make of such a logit.  Products are whole multiples of a power of two that 32 bits hold."""
     n, t, heads, dim = size
-    gen = torch.Generator().manual_seed(t + dim)
-    # signs of a row, no two alike and, of 8 columns, by a column of the row's number
-    signs = torch.randint(0, 2, (n, t, heads, dim), generator=gen) * 2 - 1
-    if dim < 64:
-        bits = torch.arange(t)[:, None] >> torch.arange(8)[None, :] & 1
-        signs[..., :8] = (bits * 2 - 1)[None, :, None, :]
     size_of = 2.0 ** 11 if kind == torch.float16 else 2.0 ** 16
-    whole = (signs * size_of).reshape(n, t, heads * dim).to(kind)
-    x = make(n, t, heads, heads, dim, 0, kind, seed=2)
-    x["q"], x["k"] = whole, whole.clone()
+    x = signs(size, kind, size_of)
     how = dict(causal=causal, scale=64.0 / dim)
     run = Run(sams, x, [], heads, heads, **how)
     assert torch.equal(run.row_sum, torch.ones_like(run.row_sum))
@@ -169,6 +175,21 @@ def test_large_products(sams, kind, causal, size):
     word = 0.0 if kind == torch.float32 else HALF_ULP[kind]
     for got in (run.dq, run.dk):
         check(got, torch.zeros_like(slack), slack * (1 + 2 * word) + 2.0 ** -25, "a row's own key")
+
+
+@pytest.mark.parametrize("power", [2, 3, 4, 6, 8])
+@pytest.mark.parametrize("size", [(1, 192, 2, 64), (1, 100, 1, 128), (2, 128, 200, 8)], ids=str)
+@pytest.mark.parametrize("kind", TYPES, ids=str)
+def test_products_that_leave_few_bits(sams, kind, size, power):
+    """Logits from 2^10 to 2^22, the other keys' an eighth lower at least: the forward pass and the backward one agree on the weight, whatever
+    of the largest logit is rounded away.  A word's rounding of P and an output's, and sixteen of 32 bits."""
+    n, t, heads, dim = size
+    x = signs(size, kind, 2.0 ** power)
+    for causal in (True, False):
+        run = Run(sams, x, [], heads, heads, causal=causal, scale=64.0 / dim)
+        for got, name in ((run.o, "v"), (run.dv, "do")):
+            want = x[name].double()
+            check(got, want, want.abs() * (2 * HALF_ULP[kind] + 16 * U) + 2.0 ** -25, (name, causal))
 
 
 # n, t, heads, dim
